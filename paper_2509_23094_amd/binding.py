@@ -60,11 +60,30 @@ class d2c_tunable(C.Structure):
     _fields_ = [("name", C.c_char_p), ("value", C.c_int32)]
 
 
+class d2c_q8_dims(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_heads", "n_kv_heads", "head_dim", "dtype", "max_seq", "max_rows", "max_batch",
+                                          "max_k", "max_n")]
+
+
+class d2c_q8_cache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_codes", "v_codes", "k_scale", "v_scale")]
+
+
+class d2c_q8_seq(C.Structure):
+    _fields_ = [("cache", d2c_q8_cache)] + [(n, C.c_void_p) for n in ("idx", "new_k", "new_v", "q", "out", "attn_avg")] + \
+               [("m", C.c_int32), ("L", C.c_int32)]
+
+
 # include/d2c.h (the method's calls) and include/d2c_tools.h (timing, tunables, planner)
 EXPORTS = ["d2c_init", "d2c_destroy", "d2c_last_error", "d2c_seq_reset", "d2c_select", "d2c_refresh_layer",
            "d2c_attention", "d2c_influence", "d2c_linear", "d2c_step", "d2c_workspace_bytes", "d2c_select_static"]
 TOOL_EXPORTS = ["d2c_profile_begin", "d2c_profile_end", "d2c_init_tuned", "d2c_ctx_set_tunable",
                 "d2c_plan_projection", "d2c_memory_info"]
+# include/d2c_q8.h (the 8-bit operators)
+Q8_EXPORTS = ["d2c_q8_init", "d2c_q8_destroy", "d2c_q8_last_error", "d2c_q8_workspace_bytes", "d2c_q8_cache_size",
+              "d2c_q8_update", "d2c_q8_attention", "d2c_q8_read", "d2c_q8_weight_bytes", "d2c_q8_pack", "d2c_q8_linear",
+              "d2c_q8_weigh", "d2c_q8_evict"]
+Q8_BLOCK = 64
 
 
 def load_library() -> C.CDLL:
@@ -96,8 +115,26 @@ def load_library() -> C.CDLL:
     lib.d2c_ctx_set_tunable.argtypes = [vp, C.c_char_p, i32]
     lib.d2c_memory_info.argtypes = [vp, C.POINTER(C.c_int64)]
     lib.d2c_plan_projection.argtypes = [i32, i32, i32, i32, i32, C.POINTER(i32)]
-    for name in EXPORTS + TOOL_EXPORTS:
-        if name not in ("d2c_last_error", "d2c_workspace_bytes"):
+    i64 = C.c_int64
+    lib.d2c_q8_init.argtypes = [C.POINTER(d2c_q8_dims), C.POINTER(vp)]
+    lib.d2c_q8_destroy.argtypes = [vp]
+    lib.d2c_q8_last_error.argtypes = [vp]
+    lib.d2c_q8_last_error.restype = C.c_char_p
+    lib.d2c_q8_workspace_bytes.argtypes = [vp]
+    lib.d2c_q8_workspace_bytes.restype = i64
+    lib.d2c_q8_cache_size.argtypes = [vp, i64, C.POINTER(i64), C.POINTER(i64)]
+    lib.d2c_q8_update.argtypes = [vp, vp, i32, vp]
+    lib.d2c_q8_attention.argtypes = [vp, vp, i32, vp]
+    lib.d2c_q8_read.argtypes = [vp, vp, i32, vp, i32, vp, vp, vp]
+    lib.d2c_q8_weight_bytes.argtypes = [i32, i32]
+    lib.d2c_q8_weight_bytes.restype = i64
+    lib.d2c_q8_pack.argtypes = [vp, vp, i32, i32, vp, vp, vp]
+    lib.d2c_q8_linear.argtypes = [vp, vp, i32, vp, vp, i32, i32, vp, vp]
+    lib.d2c_q8_weigh.argtypes = [vp, vp, i32, i32, vp, vp]
+    lib.d2c_q8_evict.argtypes = [vp, vp, i32, vp, vp, i32, vp, vp, vp, vp]
+    for name in EXPORTS + TOOL_EXPORTS + Q8_EXPORTS:
+        if name not in ("d2c_last_error", "d2c_workspace_bytes", "d2c_q8_last_error", "d2c_q8_workspace_bytes",
+                        "d2c_q8_weight_bytes"):
             getattr(lib, name).restype = C.c_int
     return lib
 
@@ -342,3 +379,159 @@ class Sequence_:
         self.s_idx[: len(s_idx)] = torch.from_numpy(np.ascontiguousarray(s_idx, np.int32)).cuda()
         self.s_rows[: len(s_rows)] = torch.from_numpy(np.ascontiguousarray(s_rows, np.int32)).cuda()
         self.c.n_s, self.c.n_rows = len(s_idx), len(s_rows)
+
+
+# ---------------------------------------------------------------------- the 8-bit operators (include/d2c_q8.h)
+
+def _checked(t: Optional[torch.Tensor], what: str, dtype: torch.dtype, shape, device: int) -> Optional[int]:
+    """The pointer of a tensor that has to have this type and shape: a call must not read past it."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.get_device() != device:
+        raise D2CError(D2C_EINVAL, "%s: contiguous %s of shape %s on device %d expected, got %s %s on %s"
+                       % (what, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr()
+
+
+class Q8Context:
+    """Owns a d2c_q8 handle on the current device."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, dtype: str, max_seq: int = 0, max_rows: int = 0,
+                 max_batch: int = 1, max_k: int = 0, max_n: int = 0):
+        self.n_heads, self.n_kv_heads, self.head_dim, self.dtype = int(n_heads), int(n_kv_heads), int(head_dim), dtype
+        self.torch_dtype = torch_dtype(dtype)
+        self.d_q, self.d_kv = self.n_heads * self.head_dim, self.n_kv_heads * self.head_dim
+        self.handle = C.c_void_p()
+        self.device = torch.cuda.current_device()
+        d = d2c_q8_dims(n_heads, n_kv_heads, head_dim, D2C_BF16 if dtype == "bf16" else D2C_F32, max_seq, max_rows, max_batch,
+                        max_k, max_n)
+        rc = _lib.d2c_q8_init(C.byref(d), C.byref(self.handle))
+        if rc != D2C_OK:
+            raise D2CError(rc, (_lib.d2c_q8_last_error(None) or b"").decode())
+
+    def _check(self, rc: int) -> None:
+        if rc != D2C_OK:
+            raise D2CError(rc, (_lib.d2c_q8_last_error(self.handle) or b"").decode())
+
+    def close(self) -> None:
+        if self.handle:
+            _lib.d2c_q8_destroy(self.handle)
+            self.handle = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def workspace_bytes(self) -> int:
+        return int(_lib.d2c_q8_workspace_bytes(self.handle))
+
+    # ------------------------------------------------------------------ C ABI calls
+    def d2c_q8_update(self, seqs) -> None:
+        """seqs: a Q8Batch (made once, used again) or a list of Q8Seq."""
+        b = seqs if isinstance(seqs, Q8Batch) else Q8Batch(self, seqs)
+        self._check(_lib.d2c_q8_update(self.handle, b.arr, b.n, _stream()))
+
+    def d2c_q8_attention(self, seqs) -> None:
+        b = seqs if isinstance(seqs, Q8Batch) else Q8Batch(self, seqs)
+        self._check(_lib.d2c_q8_attention(self.handle, b.arr, b.n, _stream()))
+
+    def d2c_q8_read(self, cache: "Q8Cache", L: int, idx: Optional[torch.Tensor], out_k: Optional[torch.Tensor],
+                    out_v: Optional[torch.Tensor]) -> None:
+        """Rows idx (None: 0, 1, ...) as values; as many as the outputs have rows."""
+        n = (out_k if out_k is not None else out_v).shape[0]
+        cache.holds(L)
+        shape = (n, self.d_kv)
+        self._check(_lib.d2c_q8_read(self.handle, cache.ref, L, _checked(idx, "idx", torch.int32, (n,), self.device), n,
+                                     _checked(out_k, "out_k", self.torch_dtype, shape, self.device),
+                                     _checked(out_v, "out_v", self.torch_dtype, shape, self.device), _stream()))
+
+    def d2c_q8_pack(self, w: torch.Tensor) -> "Q8Weights":
+        """w T [N, K] as codes and scales for d2c_q8_linear; w can be dropped afterwards."""
+        N, K = w.shape
+        p = Q8Weights(N, K, torch.empty(int(_lib.d2c_q8_weight_bytes(N, K)), dtype=torch.int8, device=w.device),
+                      torch.empty(N, dtype=torch.float32, device=w.device))
+        self._check(_lib.d2c_q8_pack(self.handle, _checked(w, "w", self.torch_dtype, (N, K), self.device), N, K,
+                                     p.codes.data_ptr(), p.scale.data_ptr(), _stream()))
+        return p
+
+    def d2c_q8_linear(self, a: torch.Tensor, w: "Q8Weights", out: torch.Tensor) -> None:
+        m = a.shape[0]
+        self._check(_lib.d2c_q8_linear(self.handle, _checked(a, "a", self.torch_dtype, (m, w.K), self.device), m, w.codes_ptr,
+                                       w.scale_ptr, w.N, w.K, _checked(out, "out", torch.float32, (m, w.N), self.device),
+                                       _stream()))
+
+    def d2c_q8_weigh(self, attn_avg: torch.Tensor, weight: torch.Tensor) -> None:
+        m, L = attn_avg.shape
+        self._check(_lib.d2c_q8_weigh(self.handle, _checked(attn_avg, "attn_avg", torch.float32, (m, L), self.device), m, L,
+                                      _checked(weight, "weight", torch.int64, (L,), self.device), _stream()))
+
+    def d2c_q8_evict(self, src: "Q8Cache", L: int, weight: torch.Tensor, protect: Optional[torch.Tensor], dst: "Q8Cache",
+                     kept: torch.Tensor, kept_weight: Optional[torch.Tensor] = None) -> None:
+        """Keeps as many rows as kept has places."""
+        n = kept.shape[0]
+        src.holds(L)
+        dst.holds(n)
+        self._check(_lib.d2c_q8_evict(self.handle, src.ref, L, _checked(weight, "weight", torch.int64, (L,), self.device),
+                                      _checked(protect, "protect", torch.uint8, (L,), self.device), n, dst.ref,
+                                      _checked(kept, "kept", torch.int32, (n,), self.device),
+                                      _checked(kept_weight, "kept_weight", torch.int64, (n,), self.device), _stream()))
+
+
+class Q8Weights:
+    """Codes and scales of one weight matrix."""
+
+    def __init__(self, N: int, K: int, codes: torch.Tensor, scale: torch.Tensor):
+        self.N, self.K, self.codes, self.scale = N, K, codes, scale
+        self.codes_ptr, self.scale_ptr = codes.data_ptr(), scale.data_ptr()
+
+
+class Q8Cache:
+    """Codes and scales of one layer's cache of up to `rows` rows (allocated with torch, zero values)."""
+
+    def __init__(self, ctx: Q8Context, rows: int):
+        nb, ns = C.c_int64(), C.c_int64()
+        rc = _lib.d2c_q8_cache_size(ctx.handle, int(rows), C.byref(nb), C.byref(ns))
+        if rc != D2C_OK:
+            raise D2CError(rc, "d2c_q8_cache_size: bad arguments")
+        dev = torch.device("cuda", ctx.device)
+        self.rows = int(rows)
+        self.k_codes, self.v_codes = (torch.full((nb.value,), 128, dtype=torch.uint8, device=dev) for _ in range(2))
+        self.k_scale, self.v_scale = (torch.zeros((ns.value // ctx.n_kv_heads, ctx.n_kv_heads), device=dev) for _ in range(2))
+        self.c = d2c_q8_cache(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr())
+        self.ref = C.byref(self.c)
+
+    def holds(self, L: int) -> None:
+        if L > -(-self.rows // Q8_BLOCK) * Q8_BLOCK:
+            raise D2CError(D2C_ESHAPE, "the cache holds %d rows, %d asked for" % (self.rows, L))
+
+
+class Q8Seq:
+    """One sequence of a d2c_q8_update / d2c_q8_attention call: m rows against the first L rows of a cache."""
+
+    def __init__(self, cache: Q8Cache, L: int, m: int, idx: Optional[torch.Tensor] = None, new_k: Optional[torch.Tensor] = None,
+                 new_v: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                 attn_avg: Optional[torch.Tensor] = None):
+        cache.holds(L)
+        self.cache, self.L, self.m = cache, int(L), int(m)
+        self.idx, self.new_k, self.new_v, self.q, self.out, self.attn_avg = idx, new_k, new_v, q, out, attn_avg
+
+
+class Q8Batch:
+    """The C structs of a call's sequences, checked against the handle's geometry; keeps their tensors alive."""
+
+    def __init__(self, ctx: Q8Context, seqs: Sequence[Q8Seq]):
+        self.n, self.seqs = len(seqs), list(seqs)
+        arr = (d2c_q8_seq * max(1, self.n))()
+        t, dev = ctx.torch_dtype, ctx.device
+        for c, s in zip(arr, self.seqs):
+            c.cache = s.cache.c
+            c.idx = _checked(s.idx, "idx", torch.int32, (s.m,), dev)
+            c.new_k = _checked(s.new_k, "new_k", t, (s.m, ctx.d_kv), dev)
+            c.new_v = _checked(s.new_v, "new_v", t, (s.m, ctx.d_kv), dev)
+            c.q = _checked(s.q, "q", t, (s.m, ctx.d_q), dev)
+            c.out = _checked(s.out, "out", t, (s.m, ctx.d_q), dev)
+            c.attn_avg = _checked(s.attn_avg, "attn_avg", torch.float32, (s.m, s.L), dev)
+            c.m, c.L = s.m, s.L
+        self.arr = arr

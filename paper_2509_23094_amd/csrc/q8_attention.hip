@@ -1,0 +1,417 @@
+// Attention of a few query rows against a whole K/V cache held in 8 bits.
+//
+// A workgroup takes 32 query rows of one kv head (with grouped heads: rows of all its query heads) and a range of the cache's 64-row
+// blocks, four waves one block each at a time.  A wave forms S^T[64 keys x 32 rows] = K Q^T, its softmax terms, and
+// O^T[D x 32 rows] += V^T P^T, all in registers: an accumulator of S^T holds, for one query row, the keys 8a + 4g + j (g = lane / 32),
+// and V's codes lie in the cache as four rows of four dimensions, so that they are the other operand in just that order.
+//   codes -> fp16 exactly: a byte u under the high byte 0x64 is the fp16 number 1024 + u, less 1152 gives code = u - 128 (one byte
+//   permutation and one packed addition for two codes).  q enters as fp16 too, exactly: a row is scaled by a power of two so that its
+//   largest magnitude lies in [2^14, 2^15); bf16 has 8 bits, float takes two pieces of 11.  The product's scale (row, block and
+//   log2(e) / sqrt(D)) is applied to the fp32 score, V's scale when a block's O^T joins the running one.
+//   probabilities times 2^15 are rounded to fp16 (float: two pieces): 11 (22) bits down to 2^-29 of a row's largest, below that to
+//   the nearest 2^-39 of it; the running sum takes them before that rounding.
+// The waves' maxima, sums and O^T are merged through LDS; where the key range is split over workgroups, by a second launch.
+// The head average has a pass of its own over the scores, from the same fp16 q and the final (maximum, sum) of every row.
+#include <algorithm>
+#include <cmath>
+
+#include "q8.h"
+
+namespace d2c {
+namespace {
+
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kTile = 32;                 // query rows per workgroup
+constexpr float kPScale = 32768.f;        // probabilities before their rounding to fp16
+
+struct AttendSeq {
+  Q8CachePtr c;
+  const void* q;
+  void* out;
+  float* avg;
+  int m, L;
+  int splits, per_split;                  // workgroups over the keys, blocks of each
+  int first_wg;                           // of the forward launch
+  int row0;                               // first (row, head) slot in the workspace
+  int avg_tiles, avg_first_wg;            // 32-row tiles of one head; first workgroup of the average's launch
+  size_t q16;                             // this sequence's fp16 rows in the workspace, halves
+};
+struct AttendArgs {
+  AttendSeq s[kQ8Launch];
+  int n, H, Hkv;
+  float* part;                            // [split][slot][D]
+  float2* ml;                             // [split][slot]: maximum (base 2), sum
+  _Float16* q16;
+  float2* row;                            // [slot]: score factor of the row, log2 of its sum of exponentials
+  size_t slots;                           // of the whole launch
+};
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// two codes of a word as fp16: bytes 2i and 2i + 1
+__device__ __forceinline__ h2 codes2(uint32_t w, uint32_t sel) {
+  const uint32_t u = __builtin_amdgcn_perm(0x64646464u, w, sel);
+  return __builtin_bit_cast(h2, u) + h2{(_Float16)-1152.f, (_Float16)-1152.f};
+}
+__device__ __forceinline__ h8 codes8(uint32_t a, uint32_t b) {
+  const h2 x = codes2(a, 0x04010400u), y = codes2(a, 0x04030402u), z = codes2(b, 0x04010400u), w = codes2(b, 0x04030402u);
+  return h8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
+}
+
+__device__ __forceinline__ f32x16 mfma(const h8& a, const h8& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// the power of two that brings amax into [2^14, 2^15); 1 for 0 and what is not finite
+__device__ __forceinline__ float pow2_for(float amax) {
+  if (!(amax > 0.f) || !(amax <= 3.402823466e38f)) return 1.f;
+  return ldexpf(1.f, max(-126, min(126, 14 - ilogbf(amax))));
+}
+
+// D / 16 operands of one query row half (16 dimensions of each 32), scaled; returns the scale
+template <typename T, int D, int QP>
+__device__ __forceinline__ float load_q(const T* q, bool valid, h8 (&f)[QP][D / 16]) {
+  float x[D / 2], amax = 0.f;
+  const int g = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) {
+    if (valid) {
+      q8_load8(q + 32 * c + 16 * g, &x[16 * c]);
+      q8_load8(q + 32 * c + 16 * g + 8, &x[16 * c + 8]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) x[16 * c + j] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < D / 2; ++j) amax = fmaxf(amax, fabsf(x[j]));
+  amax = fmaxf(amax, __shfl_xor(amax, 32, 64));
+  const float p2 = pow2_for(amax);
+#pragma unroll
+  for (int j = 0; j < D / 2; ++j) {
+    const float v = x[j] * p2;
+    const _Float16 hi = (_Float16)v;
+    f[0][j / 8][j % 8] = hi;
+    if constexpr (QP > 1) f[1][j / 8][j % 8] = (_Float16)(v - (float)hi);
+  }
+  return p2;
+}
+
+// S^T of 32 keys of a block: raw[c] = 16 dimensions of this lane's key in chunk 2c + g
+template <int D, int QP>
+__device__ __forceinline__ f32x16 scores(const u32x4 (&raw)[D / 32], const h8 (&q)[QP][D / 16]) {
+  f32x16 acc = {};
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) {
+    const h8 lo = codes8(raw[c][0], raw[c][1]), hi = codes8(raw[c][2], raw[c][3]);
+#pragma unroll
+    for (int p = 0; p < QP; ++p) {
+      acc = mfma(lo, q[p][2 * c], acc);
+      acc = mfma(hi, q[p][2 * c + 1], acc);
+    }
+  }
+  return acc;
+}
+template <int D>
+__device__ __forceinline__ void load_k(const uint8_t* k, int key, u32x4 (&raw)[D / 32]) {
+  const int g = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) raw[c] = ld16(k + (2 * c + g) * 1024 + key * 16);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void q8_attend_kernel(AttendArgs args) {
+  constexpr int QP = sizeof(T) == 2 ? 1 : 2;      // fp16 pieces of q and of a probability
+  constexpr int DT = D / 32;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, r32 = lane & 31;
+  int si = 0;
+  while (si + 1 < args.n && (int)blockIdx.x >= args.s[si + 1].first_wg) ++si;
+  const AttendSeq& s = args.s[si];
+  // (kv head, split) runs fastest: the row tiles that read the same keys are 8 k workgroups apart, on one XCD
+  const int local = blockIdx.x - s.first_wg, groups = args.Hkv * s.splits;
+  const int hk = local % groups % args.Hkv, split = local % groups / args.Hkv, tile = local / groups;
+  const int G = args.H / args.Hkv, R = s.m * G, n_blocks = (s.L + kQ8Rows - 1) / kQ8Rows;
+  const int b0 = split * s.per_split, b1 = min(n_blocks, b0 + s.per_split);
+  const int r = tile * kTile + r32;
+  const bool valid = r < R;
+  const int row = valid ? r / G : 0, head = hk * G + (valid ? r % G : 0);
+
+  h8 q[QP][D / 16];
+  const float p2 = load_q<T, D, QP>((const T*)s.q + ((size_t)row * args.H + head) * D, valid, q);
+  const float factor = 1.4426950408889634f / (sqrtf((float)D) * p2);
+  if (s.avg && split == 0 && wave == 0 && valid) {
+    _Float16* to = args.q16 + s.q16 + (((size_t)head * s.avg_tiles + row / kTile) * (QP * D / 16) * 64 + g * 32 + row % kTile) * 8;
+#pragma unroll
+    for (int p = 0; p < QP; ++p)
+#pragma unroll
+      for (int f = 0; f < D / 16; ++f) *reinterpret_cast<h8*>(to + (size_t)(p * (D / 16) + f) * 512) = q[p][f];
+  }
+
+  f32x16 o[DT] = {};
+  float mx = -INFINITY, l = 0.f;
+  for (int b = b0 + wave; b < b1; b += 4) {
+    const size_t blk = (size_t)b * args.Hkv + hk;
+    const uint8_t *k = s.c.k + blk * kQ8Rows * D, *v = s.c.v + blk * kQ8Rows * D;
+    u32x4 kr[2][D / 32];
+    load_k<D>(k, r32, kr[0]);
+    load_k<D>(k, 32 + r32, kr[1]);
+    u32x4 vr[8];                           // D = 64: eight bytes of each
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint8_t* at = v + (2 * i + g) * 4 * D + r32 * (D / 8);
+      if constexpr (D == 128) vr[i] = ld16(at);
+      else { const u32x2 w = ld8(at); vr[i][0] = w[0]; vr[i][1] = w[1]; }
+    }
+    const float ks = s.c.ks[blk] * factor, vs = s.c.vs[blk];
+    f32x16 x[2];
+    x[0] = scores<D, QP>(kr[0], q);
+    x[1] = scores<D, QP>(kr[1], q);
+    float bm = -INFINITY;
+    const int left = s.L - b * kQ8Rows;    // keys of this block that exist
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float y = x[t][i] * ks;
+        if (left < kQ8Rows && 32 * t + 8 * (i / 4) + 4 * g + i % 4 >= left) y = -INFINITY;
+        x[t][i] = y;
+        bm = fmaxf(bm, y);
+      }
+    bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
+    const float m_new = fmaxf(mx, bm), ref = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = exp2_hw(mx - ref);
+    mx = m_new;
+    h8 p[QP][4];
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float e = exp2_hw(x[t][i] - ref) * kPScale;
+        sum += e;
+        const _Float16 hi = (_Float16)e;
+        p[0][2 * t + i / 8][i % 8] = hi;
+        if constexpr (QP > 1) p[1][2 * t + i / 8][i % 8] = (_Float16)(e - (float)hi);
+      }
+    l = l * alpha + sum;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      f32x16 acc = {};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const h8 a = codes8(vr[2 * i][dt], vr[2 * i + 1][dt]);
+#pragma unroll
+        for (int pp = 0; pp < QP; ++pp) acc = mfma(a, p[pp][i], acc);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[dt][i] = o[dt][i] * alpha + vs * acc[i];
+    }
+  }
+  l += __shfl_xor(l, 32, 64);
+
+  // merge the waves: each adds up a quarter of every accumulator, 16 neighbouring dimensions of a row (D = 64: 8)
+  __shared__ float lds[4][DT * 16][64];
+  __shared__ float wm[4][kTile], wl[4][kTile];
+  if (g == 0) { wm[wave][r32] = mx; wl[wave][r32] = l; }
+  __syncthreads();
+  const float M = fmaxf(fmaxf(wm[0][r32], wm[1][r32]), fmaxf(wm[2][r32], wm[3][r32]));
+  const float ref = M == -INFINITY ? 0.f : M;
+  const float own = exp2_hw(mx - ref);
+  float sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) sum += wl[w][r32] * exp2_hw(wm[w][r32] - ref);
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) lds[wave][dt * 16 + i][lane] = o[dt][i] * own;
+  __syncthreads();
+  if (!valid) return;
+  float y[4 * DT];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const int e = dt * 16 + 4 * wave + j;
+      y[j * DT + dt] = (lds[0][e][lane] + lds[1][e][lane]) + (lds[2][e][lane] + lds[3][e][lane]);
+    }
+  const int d0 = (8 * wave + 4 * g) * DT;        // row 8 w + 4 g + j of tile dt is dimension DT * (that) + dt
+  const size_t slot = (size_t)s.row0 + (size_t)row * args.H + head;
+  if (s.splits > 1) {
+    float* to = args.part + ((size_t)split * args.slots + slot) * D + d0;
+#pragma unroll
+    for (int j = 0; j < DT; ++j) q8_store4(to + 4 * j, y + 4 * j);
+    if (wave == 0 && g == 0) args.ml[(size_t)split * args.slots + slot] = make_float2(M, sum);
+  } else {
+    const float inv = 1.f / sum;
+#pragma unroll
+    for (int j = 0; j < 4 * DT; ++j) y[j] *= inv;
+    T* to = (T*)s.out + ((size_t)row * args.H + head) * D + d0;
+#pragma unroll
+    for (int j = 0; j < DT; ++j) q8_store4(to + 4 * j, y + 4 * j);
+  }
+  if (s.avg && wave == 0 && g == 0 && (s.splits == 1 || split == 0))
+    args.row[slot] = make_float2(factor, ref + log2f(sum / kPScale));       // (the sum of a split row: the merge puts it right)
+}
+
+// Splits of a row joined in order.  A workgroup per 256 / (D / 4) rows.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void q8_join_kernel(AttendArgs args) {
+  const int t = threadIdx.x % (D / 4) * 4;
+  const size_t slot = (size_t)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
+  if (slot >= args.slots) return;
+  int si = 0;
+  while (si + 1 < args.n && slot >= (size_t)args.s[si + 1].row0) ++si;
+  const AttendSeq& s = args.s[si];
+  if (s.splits <= 1) return;
+  float M = -INFINITY, sum = 0.f;
+  for (int i = 0; i < s.splits; ++i) M = fmaxf(M, args.ml[(size_t)i * args.slots + slot].x);
+  const float ref = M == -INFINITY ? 0.f : M;
+  f32x4 y = {};
+  for (int i = 0; i < s.splits; ++i) {
+    const float2 ml = args.ml[(size_t)i * args.slots + slot];
+    const float w = exp2_hw(ml.x - ref);
+    sum += ml.y * w;
+    y += w * *reinterpret_cast<const f32x4*>(args.part + ((size_t)i * args.slots + slot) * D + t);
+  }
+  y *= 1.f / sum;
+  float z[4] = {y[0], y[1], y[2], y[3]};
+  q8_store4((T*)s.out + (slot - s.row0) * D + t, z);
+  if (s.avg && t == 0) args.row[slot].y = ref + log2f(sum / kPScale);
+}
+
+// attn_avg of 32 rows x one block of keys: the four waves take the heads in turn and are added up at the end.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void q8_average_kernel(AttendArgs args) {
+  constexpr int QP = sizeof(T) == 2 ? 1 : 2;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, r32 = lane & 31;
+  int si = 0;
+  while (si + 1 < args.n && (int)blockIdx.x >= args.s[si + 1].avg_first_wg) ++si;
+  const AttendSeq& s = args.s[si];
+  const int n_blocks = (s.L + kQ8Rows - 1) / kQ8Rows, local = blockIdx.x - s.avg_first_wg;
+  const int b = local % n_blocks, tile = local / n_blocks, row = tile * kTile + r32, G = args.H / args.Hkv;
+  const int per = (args.H + 3) / 4, h0 = wave * per, h1 = min(args.H, h0 + per);
+  f32x16 acc[2] = {};
+  for (int h = h0; h < h1; ++h) {
+    const size_t blk = (size_t)b * args.Hkv + h / G;
+    const uint8_t* k = s.c.k + blk * kQ8Rows * D;
+    u32x4 kr[2][D / 32];
+    load_k<D>(k, r32, kr[0]);
+    load_k<D>(k, 32 + r32, kr[1]);
+    h8 q[QP][D / 16];
+    const _Float16* from = args.q16 + s.q16 + (((size_t)h * s.avg_tiles + tile) * (QP * D / 16) * 64 + lane) * 8;
+#pragma unroll
+    for (int p = 0; p < QP; ++p)
+#pragma unroll
+      for (int f = 0; f < D / 16; ++f) q[p][f] = __builtin_bit_cast(h8, ld16(from + (size_t)(p * (D / 16) + f) * 512));
+    const float2 rw = row < s.m ? args.row[(size_t)s.row0 + (size_t)row * args.H + h] : make_float2(0.f, 0.f);
+    const float ks = s.c.ks[blk] * rw.x;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const f32x16 x = scores<D, QP>(kr[t], q);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[t][i] += exp2_hw(x[i] * ks - rw.y);
+    }
+  }
+  __shared__ float lds[4][kTile][kQ8Rows + 1];
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) lds[wave][r32][32 * t + 8 * (i / 4) + 4 * g + i % 4] = acc[t][i];
+  __syncthreads();
+  const int key = b * kQ8Rows + lane;
+  if (key >= s.L) return;
+  const float inv = 1.f / args.H;
+#pragma unroll
+  for (int i = 0; i < kTile / 4; ++i) {
+    const int rr = 4 * i + wave, at = tile * kTile + rr;
+    if (at < s.m) s.avg[(size_t)at * s.L + key] = ((lds[0][rr][lane] + lds[1][rr][lane]) + (lds[2][rr][lane] + lds[3][rr][lane])) * inv;
+  }
+}
+
+// Workgroups over the keys: enough to fill the chip about twice, each with a block for each of its waves.
+constexpr int kTargetWgs = 512;
+int plan_splits(int workgroups, int n_blocks) {
+  return std::max(1, std::min(kTargetWgs / workgroups, n_blocks / 4));
+}
+int row_tiles(const Q8Shape& s, int m) { return (m * (s.H / s.Hkv) + kTile - 1) / kTile; }
+
+// Workspace: partial sums of split rows -- splits x rows is at most kTargetWgs tiles, as rows are at most 32 per unsplit
+// workgroup -- and, for the average, (factor, log-sum) and fp16 rows of every query row and head.
+struct Layout { size_t ml, row, q16, total; };
+Layout layout(const Q8Shape& s, size_t max_rows, size_t max_batch) {
+  const size_t split_rows = (size_t)kTargetWgs * kTile, pieces = s.dtype == kBF16 ? 1 : 2;
+  const size_t q_rows = max_rows + (kTile - 1) * std::min<size_t>(max_batch, kQ8Launch);
+  auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  Layout l;
+  l.ml = up(split_rows * s.D * 4);
+  l.row = l.ml + up(split_rows * 8);
+  l.q16 = l.row + up(max_rows * s.H * 8);
+  l.total = l.q16 + up(q_rows * s.H * pieces * s.D * 2);
+  return l;
+}
+
+template <typename T, int D>
+hipError_t run(const AttendArgs& a, int wgs, int avg_wgs, bool join, hipStream_t st) {
+  q8_attend_kernel<T, D><<<wgs, 256, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && join) {
+    q8_join_kernel<T, D><<<(unsigned)((a.slots + 1024 / D - 1) / (1024 / D)), 256, 0, st>>>(a);
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && avg_wgs) {
+    q8_average_kernel<T, D><<<avg_wgs, 256, 0, st>>>(a);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace
+
+size_t q8_attention_bytes(const Q8Shape& s, int max_rows, int max_batch) { return layout(s, max_rows, max_batch).total; }
+
+hipError_t launch_q8_attention(const Q8Shape& s, const Q8Attend* calls, int n, int max_rows, int max_batch, void* ws, hipStream_t st) {
+  const Layout l = layout(s, max_rows, max_batch);
+  const int pieces = s.dtype == kBF16 ? 1 : 2;
+  for (int c0 = 0; c0 < n; c0 += kQ8Launch) {
+    AttendArgs a{};
+    a.n = std::min(kQ8Launch, n - c0);
+    a.H = s.H;
+    a.Hkv = s.Hkv;
+    a.part = (float*)ws;
+    a.ml = (float2*)((char*)ws + l.ml);
+    a.row = (float2*)((char*)ws + l.row);
+    a.q16 = (_Float16*)((char*)ws + l.q16);
+    int base = 0, wgs = 0, avg_wgs = 0;
+    size_t rows = 0;
+    bool join = false;
+    for (int i = 0; i < a.n; ++i) base += row_tiles(s, calls[c0 + i].m) * s.Hkv;
+    for (int i = 0; i < a.n; ++i) {
+      const Q8Attend& c = calls[c0 + i];
+      AttendSeq& q = a.s[i];
+      const int nb = q8_blocks(c.L);
+      q.c = c.cache; q.q = c.q; q.out = c.out; q.avg = c.avg; q.m = c.m; q.L = c.L;
+      q.splits = plan_splits(base, nb);
+      q.per_split = (nb + q.splits - 1) / q.splits;
+      q.splits = (nb + q.per_split - 1) / q.per_split;      // none empty
+      q.first_wg = wgs;
+      wgs += row_tiles(s, c.m) * s.Hkv * q.splits;
+      q.row0 = (int)a.slots;
+      a.slots += (size_t)c.m * s.H;
+      q.avg_tiles = (c.m + kTile - 1) / kTile;
+      q.avg_first_wg = avg_wgs;
+      if (c.avg) avg_wgs += q.avg_tiles * nb;
+      q.q16 = rows * s.H * pieces * s.D;
+      rows += (size_t)q.avg_tiles * kTile;
+      join = join || q.splits > 1;
+    }
+    const hipError_t e = s.dtype == kBF16 ? (s.D == 128 ? run<bf16, 128>(a, wgs, avg_wgs, join, st) : run<bf16, 64>(a, wgs, avg_wgs, join, st))
+                                          : (s.D == 128 ? run<float, 128>(a, wgs, avg_wgs, join, st) : run<float, 64>(a, wgs, avg_wgs, join, st));
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace d2c

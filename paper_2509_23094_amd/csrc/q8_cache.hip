@@ -1,0 +1,507 @@
+// The 8-bit K/V cache apart from its attention: refreshed rows in, rows out as values, attention weight summed, rows kept and
+// the cache compacted.  All of it moves bytes: one pass over the codes and rows concerned, 16 bytes per access.
+#include <algorithm>
+
+#include "q8.h"
+
+namespace d2c {
+namespace {
+
+// One block of one kv head: 64 * D codes.  K pieces of 16 bytes: 16 dimensions of a row; V pieces: four dimensions of four rows.
+template <int D> struct Pieces {
+  static constexpr int kCount = kQ8Rows * D / 16;
+  static constexpr int kPerThread = kCount / 256;
+  // K: consecutive threads take the pieces of one row (256 bytes of bf16), then the next row
+  __device__ static int k_row(int p) { return p / (D / 16); }
+  __device__ static int k_dim(int p) { return p % (D / 16) * 16; }
+  __device__ static int k_at(int p) { return k_dim(p) * kQ8Rows + k_row(p) * 16; }
+  // V: consecutive threads take neighbouring dimensions of the same four rows: addresses are consecutive
+  __device__ static int v_row(int p) { return p / (D / 4) * 4; }
+  __device__ static int v_dim(int p) { return p % (D / 4) * 4; }
+  __device__ static int v_at(int p) { return p * 16; }
+};
+
+struct UpdateArgs {
+  Q8Update c[kQ8Launch];
+};
+
+// Number of idx entries below `limit`, by all 256 threads together (idx ascending; in bounds whatever it holds).
+__device__ int lower_bound_wide(const int32_t* idx, int m, int limit) {
+  const int step = (m + 255) / 256, t = threadIdx.x;
+  const int c = __syncthreads_count((int64_t)t * step < m && idx[(int64_t)t * step] < limit);
+  int lo = max(0, c - 1) * step, n = 0;
+  for (int i = 0; i < step; i += 256) {
+    const int at = lo + i + t;
+    n += __syncthreads_count(i + t < step && at < m && idx[at] < limit);
+  }
+  return lo + n;
+}
+
+// A workgroup per (block, kv head, K or V, sequence).  Its refreshed rows are found first: blocks are counted from the first refreshed
+// one where the rows are consecutive or many; few scattered rows get a workgroup each, of which the first of a block's does the block.
+// Rows and, where the scale moves, the old codes are then read once and the codes written once.
+// What bounds it: bytes for a whole prompt, the chain index -> rows -> maximum -> codes for a decode step.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void q8_update_kernel(UpdateArgs args, int Hkv) {
+  using P = Pieces<D>;
+  const Q8Update c = args.c[blockIdx.z];
+  const int h = blockIdx.y >> 1, is_v = blockIdx.y & 1, tid = threadIdx.x, slot = blockIdx.x;
+  const int n_blocks = (c.L + kQ8Rows - 1) / kQ8Rows;
+  __shared__ int row_of[kQ8Rows];
+  __shared__ float wave_amax[4];
+  int b;
+  if (tid < kQ8Rows) row_of[tid] = -1;
+  if (!c.idx) {
+    const int first = c.L - c.m;
+    b = first / kQ8Rows + slot;
+    if (b >= n_blocks) return;
+    __syncthreads();
+    const int pos = b * kQ8Rows + tid;
+    if (tid < kQ8Rows && pos >= first && pos < c.L) row_of[tid] = pos - first;
+  } else {
+    int lo = slot;
+    if (c.m < n_blocks) {                       // a slot is a row
+      if (slot >= c.m) return;
+      const int pos = c.idx[slot];
+      if (pos < 0 || pos >= c.L) return;
+      b = pos / kQ8Rows;
+      if (slot > 0 && (c.idx[slot - 1] >> 6) == b) return;
+      __syncthreads();
+    } else {                                    // a slot is a block
+      b = slot;
+      if (b >= n_blocks) return;
+      lo = lower_bound_wide(c.idx, c.m, b * kQ8Rows);
+    }
+    if (tid < kQ8Rows && lo + tid < c.m) {
+      const int pos = c.idx[lo + tid];
+      if (pos >= 0 && pos < c.L && pos / kQ8Rows == b) atomicMax(&row_of[pos % kQ8Rows], lo + tid);
+    }
+  }
+  __syncthreads();
+  const uint64_t fresh = __ballot(row_of[tid & 63] >= 0);
+  if (fresh == 0) return;
+  const int valid = min(kQ8Rows, c.L - b * kQ8Rows);
+  const bool whole = __popcll(fresh) == valid;
+
+  const T* rows = (const T*)(is_v ? c.new_v : c.new_k) + (size_t)h * D;
+  const size_t pitch = (size_t)Hkv * D;
+  const size_t base = ((size_t)b * Hkv + h) * kQ8Rows * D;
+  uint8_t* codes = (is_v ? c.cache.v : c.cache.k) + base;
+  float* scale = (is_v ? c.cache.vs : c.cache.ks) + (size_t)b * Hkv + h;
+  const float s_old = *scale;
+
+  float x[P::kPerThread][16];
+  float amax = 0.f;
+#pragma unroll
+  for (int i = 0; i < P::kPerThread; ++i) {
+    const int p = tid + 256 * i;
+    if (is_v) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int r = row_of[P::v_row(p) + j];
+        if (r >= 0) q8_load4(rows + r * pitch + P::v_dim(p), &x[i][4 * j]);
+        else x[i][4 * j] = x[i][4 * j + 1] = x[i][4 * j + 2] = x[i][4 * j + 3] = 0.f;
+      }
+    } else {
+      const int r = row_of[P::k_row(p)];
+      if (r >= 0) {
+        q8_load8(rows + r * pitch + P::k_dim(p), &x[i][0]);
+        q8_load8(rows + r * pitch + P::k_dim(p) + 8, &x[i][8]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[i][j] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const float a = fabsf(x[i][j]);
+      if (a <= 3.402823466e38f) amax = fmaxf(amax, a);
+    }
+  }
+  amax = wave_max(amax);
+  if ((tid & 63) == 0) wave_amax[tid >> 6] = amax;
+  __syncthreads();
+  amax = fmaxf(fmaxf(wave_amax[0], wave_amax[1]), fmaxf(wave_amax[2], wave_amax[3]));
+  const float want = q8_scale(amax);
+  const float s = whole ? want : want > s_old ? fmaxf(want, s_old * 1.25f) : s_old;
+  const bool moved = !whole && s != s_old;
+  const float inv = q8_inverse(s);
+#pragma unroll
+  for (int i = 0; i < P::kPerThread; ++i) {
+    const int p = tid + 256 * i;
+    if (is_v) {
+      const int t = P::v_row(p);
+      const uint32_t f4 = (uint32_t)(fresh >> t) & 15u;
+      if (f4 == 0 && !moved) continue;
+      u32x4 w = {0, 0, 0, 0};
+      u32x4* at = reinterpret_cast<u32x4*>(codes + P::v_at(p));
+      if (f4 != 15u) w = *at;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        uint32_t word = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int old = q8_code_of(w[d], j);
+          const int code = (f4 >> j & 1u) ? q8_code(x[i][4 * j + d], s, inv) : moved ? q8_recode(old, s_old, s, inv) : old;
+          word |= q8_byte(code) << (8 * j);
+        }
+        w[d] = word;
+      }
+      *at = w;
+    } else {
+      const bool is_new = fresh >> P::k_row(p) & 1;
+      if (!is_new && !moved) continue;
+      u32x4 w = {0, 0, 0, 0};
+      u32x4* at = reinterpret_cast<u32x4*>(codes + P::k_at(p));
+      if (!is_new) w = *at;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        uint32_t word = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int code = is_new ? q8_code(x[i][4 * d + j], s, inv) : q8_recode(q8_code_of(w[d], j), s_old, s, inv);
+          word |= q8_byte(code) << (8 * j);
+        }
+        w[d] = word;
+      }
+      *at = w;
+    }
+  }
+  if (tid == 0 && s != s_old) *scale = s;      // every thread has read the old one before the barrier above
+}
+
+// A thread per (row, four dimensions of a kv head).  A workgroup's rows are neighbours, so that the four rows of a V piece, and the
+// pieces of K in one line, come from the L1.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void q8_read_kernel(Q8CachePtr c, int L, const int32_t* idx, int n, int Hkv, T* out_k, T* out_v) {
+  const int r = blockIdx.x * (1024 / D) + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4, h = blockIdx.y;
+  if (r >= n) return;
+  const int pos = idx ? idx[r] : r;
+  float k[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (pos >= 0 && pos < L) {
+    const int t = pos % kQ8Rows;
+    const size_t g = (size_t)(pos / kQ8Rows) * Hkv + h, base = g * kQ8Rows * D;
+    if (out_k) {
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(c.k + base + d / 16 * 1024 + t * 16 + d % 16);
+      const float s = c.ks[g];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) k[j] = (float)q8_code_of(w, j) * s;
+    }
+    if (out_v) {
+      const u32x4 w = ld16(c.v + base + t / 4 * 4 * D + d * 4);
+      const float s = c.vs[g];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = (float)q8_code_of(w[j], t % 4) * s;
+    }
+  }
+  const size_t at = ((size_t)r * Hkv + h) * D + d;
+  if (out_k) q8_store4(out_k + at, k);
+  if (out_v) q8_store4(out_v + at, v);
+}
+
+// Column sums of [m, L] in fixed point.  A workgroup takes 64 columns, its four waves every fourth of its rows.  Where several
+// workgroups share columns they add with integer atomics: any order gives the same sum.
+__global__ __launch_bounds__(256) void q8_weigh_kernel(const float* avg, int m, int L, int rows_per_wg, unsigned long long* weight) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = blockIdx.x * 64 + lane;
+  const int r0 = blockIdx.y * rows_per_wg, r1 = min(m, r0 + rows_per_wg);
+  __shared__ unsigned long long part[3][64];
+  unsigned long long sum = 0;
+  if (j < L) {
+#pragma unroll 8
+    for (int r = r0 + wave; r < r1; r += 4) {
+      const float c = fminf(fmaxf(avg[(size_t)r * L + j], 0.f), 1.f);
+      sum += c >= 1.f ? 1ull << 32 : (unsigned long long)(uint32_t)(c * 4294967296.f);
+    }
+  }
+  if (wave) part[wave - 1][lane] = sum;
+  __syncthreads();
+  if (wave || j >= L) return;
+  sum += part[0][lane] + part[1][lane] + part[2][lane];
+  if (gridDim.y == 1) weight[j] += sum;
+  else if (sum) atomicAdd(&weight[j], sum);
+}
+
+// ---- the rows to keep: one workgroup of 16 waves
+constexpr int kKeepThreads = 1024;
+constexpr int kKeepChunk = 64 * kKeepThreads;      // positions numbered at once: 64 per thread
+
+// exclusive sum over the workgroup's threads of v, and the total; scratch: 16 values
+__device__ __forceinline__ unsigned long long wg_scan(unsigned long long v, unsigned long long* scratch, unsigned long long* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  unsigned long long s = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const unsigned long long t = __shfl_up(s, o, 64);
+    if (lane >= o) s += t;
+  }
+  __syncthreads();
+  if (lane == 63) scratch[wave] = s;
+  __syncthreads();
+  unsigned long long before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kKeepThreads / 64; ++w) {
+    if (w < wave) before += scratch[w];
+    all += scratch[w];
+  }
+  *total = all;
+  return before + s - v;
+}
+
+// Thread t holds positions t + 1024 i, in registers where there are at most PER of them (PER = 0: read again for each pass).  The
+// protected rows fill up first: if they are more than n_keep the choice is among them, else all of them stay and it is among the others.
+// The chosen class's n-th largest weight is found digit by digit (11 bits, from the highest bit in which its weights differ), with a
+// histogram in LDS and an early end when a digit's rows all stay.  Then the kept positions are numbered in order.
+// What bounds it: a chain of barriers and LDS atomics per digit; the other compute units idle.
+template <int PER>
+__global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* weight, const uint8_t* protect, int L, int n_keep,
+                                                              int32_t* kept, int64_t* kept_weight) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ uint32_t hist[2048];
+  __shared__ unsigned long long scratch[16], red[2][16], counts[1024];
+  __shared__ int found_bin;
+  __shared__ uint32_t found_above, found_in;
+  unsigned long long reg[PER ? PER : 1];                // weight, top bit: protected
+  auto load = [&](int i) -> unsigned long long {
+    const int64_t w = weight[i];
+    return (w < 0 ? 0ull : (unsigned long long)w) | (protect && protect[i] ? 1ull << 63 : 0ull);
+  };
+  if constexpr (PER > 0) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) reg[i] = tid + 1024 * i < L ? load(tid + 1024 * i) : 0ull;
+  }
+  auto each = [&](auto f) {                             // f(key) for this thread's positions
+    if constexpr (PER > 0) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (tid + 1024 * i < L) f(reg[i]);
+    } else {
+      for (int i = tid; i < L; i += kKeepThreads) f(load(i));
+    }
+  };
+  constexpr unsigned long long kTop = 1ull << 63;
+  unsigned long long n_prot = 0, total;
+  if (protect) {
+    each([&](unsigned long long k) { n_prot += k >> 63; });
+    wg_scan(n_prot, scratch, &total);
+    n_prot = total;
+  }
+  const bool among_protected = n_prot >= (unsigned long long)n_keep;
+  const unsigned long long cls = among_protected ? kTop : 0ull;                        // n_keep > 0
+  uint32_t need = among_protected ? (uint32_t)n_keep : (uint32_t)(n_keep - (int)n_prot);   // of the class `cls`
+  const uint32_t size = cls ? (uint32_t)n_prot : (uint32_t)(L - (int)n_prot);
+  // threshold: keys of the class above `thr` stay, of those equal to it (under the mask of the digits looked at) the first `need`
+  unsigned long long thr = cls, mask = kTop;
+  if (need < size) {
+    unsigned long long all_or = 0, all_and = ~0ull;
+    each([&](unsigned long long k) { if ((k & kTop) == cls) { all_or |= k; all_and &= k; } });
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      all_or |= __shfl_xor(all_or, o, 64);
+      all_and &= __shfl_xor(all_and, o, 64);
+    }
+    if (lane == 0) { red[0][wave] = all_or; red[1][wave] = all_and; }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 16; ++w) { all_or |= red[0][w]; all_and &= red[1][w]; }
+    const unsigned long long differ = all_or & ~all_and;
+    int hi = differ ? 64 - __clzll((long long)differ) : 0;     // bits hi .. 63 are common
+    mask = hi >= 64 ? 0ull : ~0ull << hi;
+    thr = all_and & mask;
+    while (hi > 0) {
+      const int lo = max(0, hi - 11), bins = 1 << (hi - lo);
+      for (int b = tid; b < 2048; b += kKeepThreads) hist[b] = 0;
+      __syncthreads();
+      each([&](unsigned long long k) { if ((k & mask) == thr) atomicAdd(&hist[(uint32_t)(k >> lo) & (bins - 1)], 1u); });
+      __syncthreads();
+      // thread t holds bins 2047 - 2t and below: prefix sums run from the largest digit down
+      const uint32_t a = hist[2047 - 2 * tid], c = hist[2046 - 2 * tid];
+      const uint32_t before = (uint32_t)wg_scan((unsigned long long)a + c, scratch, &total);
+      if (before < need && before + a >= need) { found_bin = 2047 - 2 * tid; found_above = before; found_in = a; }
+      else if (before + a < need && before + a + c >= need) { found_bin = 2046 - 2 * tid; found_above = before + a; found_in = c; }
+      __syncthreads();
+      need -= found_above;
+      thr |= (unsigned long long)found_bin << lo;
+      mask = lo ? ~0ull << lo : ~0ull;
+      const bool done = need == found_in;
+      hi = lo;
+      __syncthreads();
+      if (done) break;
+    }
+  }
+  // above: stays; equal under the mask: the first `need` stay
+  const uint32_t ties = need;
+  unsigned long long base = 0;                            // kept above in the low half, equal ones in the high half
+  for (int c0 = 0; c0 < L; c0 += kKeepChunk) {
+    const int n_j = min(64, (L - c0 + kKeepThreads - 1) / kKeepThreads);
+    auto key_at = [&](int j, int i) -> unsigned long long {
+      if constexpr (PER > 0) { (void)i; return reg[j]; } else { (void)j; return i < L ? load(i) : 0ull; }
+    };
+    auto pass = [&](auto f) {
+      if constexpr (PER > 0) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+          if (j < n_j) f(j);
+      } else {
+        for (int j = 0; j < n_j; ++j) f(j);
+      }
+    };
+    __syncthreads();
+    counts[tid] = 0;
+    __syncthreads();
+    pass([&](int j) {
+      const int i = c0 + j * kKeepThreads + tid;
+      const unsigned long long k = key_at(j, i) & mask;
+      const uint64_t up = __ballot(i < L && k > thr), eq = __ballot(i < L && k == thr);
+      if (lane == 0) counts[j * 16 + wave] = (unsigned long long)__popcll(up) | (unsigned long long)__popcll(eq) << 32;
+    });
+    __syncthreads();
+    const unsigned long long own = counts[tid], pre = wg_scan(own, scratch, &total) + base;
+    __syncthreads();
+    counts[tid] = pre;
+    __syncthreads();
+    pass([&](int j) {
+      const int i = c0 + j * kKeepThreads + tid;
+      const unsigned long long key = key_at(j, i), k = key & mask;
+      const bool is_up = i < L && k > thr, is_eq = i < L && k == thr;
+      const uint64_t up = __ballot(is_up), eq = __ballot(is_eq), below = (1ull << lane) - 1;
+      const unsigned long long p = counts[j * 16 + wave];
+      const uint32_t up_before = (uint32_t)p + (uint32_t)__popcll(up & below), eq_before = (uint32_t)(p >> 32) + (uint32_t)__popcll(eq & below);
+      if (is_up || (is_eq && eq_before < ties)) {
+        const uint32_t at = up_before + min(eq_before, ties);
+        kept[at] = i;
+        if (kept_weight) kept_weight[at] = weight[i];
+      }
+    });
+    base += total;
+  }
+}
+
+// Row i of dst is row kept[i] of src.  A workgroup per (block of dst, kv head, K or V): 16 KB read (V: more, its pieces hold four rows
+// of which some go), 8 KB written.
+template <int D>
+__global__ __launch_bounds__(256) void q8_compact_kernel(Q8CachePtr src, const int32_t* kept, int n, Q8CachePtr dst, int Hkv) {
+  using P = Pieces<D>;
+  const int b = blockIdx.x, h = blockIdx.y >> 1, is_v = blockIdx.y & 1, tid = threadIdx.x;
+  __shared__ int from[kQ8Rows];
+  __shared__ float scale_of[kQ8Rows];
+  const uint8_t* codes = is_v ? src.v : src.k;
+  if (tid < kQ8Rows) {
+    const int i = b * kQ8Rows + tid, pos = i < n ? kept[i] : -1;
+    from[tid] = pos;
+    scale_of[tid] = pos >= 0 ? (is_v ? src.vs : src.ks)[(size_t)(pos / kQ8Rows) * Hkv + h] : 0.f;
+  }
+  __syncthreads();
+  const float s = wave_max(scale_of[tid & 63]), inv = q8_inverse(s);
+  uint8_t* out = (is_v ? dst.v : dst.k) + ((size_t)b * Hkv + h) * kQ8Rows * D;
+#pragma unroll
+  for (int i = 0; i < P::kPerThread; ++i) {
+    const int p = tid + 256 * i;
+    if (is_v) {
+      u32x4 w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int pos = from[P::v_row(p) + j];
+        w[j] = u32x4{0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
+        if (pos >= 0)
+          w[j] = ld16(codes + ((size_t)(pos / kQ8Rows) * Hkv + h) * kQ8Rows * D + pos % kQ8Rows / 4 * 4 * D + P::v_dim(p) * 4);
+      }
+      u32x4 r = {0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int t = P::v_row(p) + j, byte = from[t] & 3;
+        const float old = scale_of[t];
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          int code = q8_code_of(w[j][d], byte);
+          if (old != s) code = q8_recode(code, old, s, inv);
+          r[d] |= q8_byte(code) << (8 * j);
+        }
+      }
+      *reinterpret_cast<u32x4*>(out + P::v_at(p)) = r;
+    } else {
+      const int t = P::k_row(p), pos = from[t];
+      u32x4 w = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
+      if (pos >= 0)
+        w = ld16(codes + ((size_t)(pos / kQ8Rows) * Hkv + h) * kQ8Rows * D + P::k_dim(p) * kQ8Rows + pos % kQ8Rows * 16);
+      const float old = scale_of[t];
+      if (old != s) {
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          uint32_t word = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) word |= q8_byte(q8_recode(q8_code_of(w[d], j), old, s, inv)) << (8 * j);
+          w[d] = word;
+        }
+      }
+      *reinterpret_cast<u32x4*>(out + P::k_at(p)) = w;
+    }
+  }
+  if (tid == 0) (is_v ? dst.vs : dst.ks)[(size_t)b * Hkv + h] = s;
+}
+
+template <typename T>
+hipError_t update_t(const Q8Shape& s, const UpdateArgs& a, dim3 grid, hipStream_t st) {
+  if (s.D == 128) q8_update_kernel<T, 128><<<grid, 256, 0, st>>>(a, s.Hkv);
+  else q8_update_kernel<T, 64><<<grid, 256, 0, st>>>(a, s.Hkv);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t read_t(const Q8Shape& s, const Q8CachePtr& c, int L, const int32_t* idx, int n, void* k, void* v, hipStream_t st) {
+  const int rows = 1024 / s.D;
+  const dim3 grid((n + rows - 1) / rows, s.Hkv);
+  if (s.D == 128) q8_read_kernel<T, 128><<<grid, 256, 0, st>>>(c, L, idx, n, s.Hkv, (T*)k, (T*)v);
+  else q8_read_kernel<T, 64><<<grid, 256, 0, st>>>(c, L, idx, n, s.Hkv, (T*)k, (T*)v);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_q8_update(const Q8Shape& s, const Q8Update* calls, int n, hipStream_t st) {
+  for (int c0 = 0; c0 < n; c0 += kQ8Launch) {
+    UpdateArgs a{};
+    const int nc = std::min(kQ8Launch, n - c0);
+    int slots = 0;
+    for (int i = 0; i < nc; ++i) {
+      a.c[i] = calls[c0 + i];
+      const int nb = q8_blocks(a.c[i].L), first = (a.c[i].L - a.c[i].m) / kQ8Rows;
+      slots = std::max(slots, a.c[i].idx ? std::min(a.c[i].m, nb) : nb - first);
+    }
+    const dim3 grid(slots, 2 * s.Hkv, nc);
+    const hipError_t e = s.dtype == kBF16 ? update_t<bf16>(s, a, grid, st) : update_t<float>(s, a, grid, st);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_q8_read(const Q8Shape& s, const Q8CachePtr& c, int L, const int32_t* idx, int n, void* k, void* v, hipStream_t st) {
+  return s.dtype == kBF16 ? read_t<bf16>(s, c, L, idx, n, k, v, st) : read_t<float>(s, c, L, idx, n, k, v, st);
+}
+
+hipError_t launch_q8_weigh(const float* avg, int m, int L, int64_t* weight, hipStream_t st) {
+  const int cols = (L + 63) / 64;
+  const int parts = std::max(1, std::min((m + 15) / 16, 1024 / cols));
+  const int per = (m + parts - 1) / parts;
+  q8_weigh_kernel<<<dim3(cols, (m + per - 1) / per), 256, 0, st>>>(avg, m, L, per, (unsigned long long*)weight);
+  return hipGetLastError();
+}
+
+hipError_t launch_q8_keep(const int64_t* weight, const uint8_t* protect, int L, int n_keep, int32_t* kept, int64_t* kept_weight,
+                          hipStream_t st) {
+  const int per = (L + kKeepThreads - 1) / kKeepThreads;
+  if (per <= 4) q8_keep_kernel<4><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
+  else if (per <= 8) q8_keep_kernel<8><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
+  else if (per <= 20) q8_keep_kernel<20><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
+  else q8_keep_kernel<0><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
+  return hipGetLastError();
+}
+
+hipError_t launch_q8_compact(const Q8Shape& s, const Q8CachePtr& src, const int32_t* kept, int n, const Q8CachePtr& dst,
+                             hipStream_t st) {
+  const dim3 grid(q8_blocks(n), 2 * s.Hkv);
+  if (s.D == 128) q8_compact_kernel<128><<<grid, 256, 0, st>>>(src, kept, n, dst, s.Hkv);
+  else q8_compact_kernel<64><<<grid, 256, 0, st>>>(src, kept, n, dst, s.Hkv);
+  return hipGetLastError();
+}
+
+}  // namespace d2c

@@ -1,0 +1,601 @@
+"""The 8-bit operators on the GPU, through the C ABI, against the plain 64-bit forms of q8_reference: codes, scales, sums, weights and kept
+sets bit for bit, attention within bounds that count its roundings."""
+import numpy as np
+import pytest
+import torch
+
+import q8_reference as R
+from gpu_util import say
+
+pytestmark = pytest.mark.gpu
+
+HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}          # rounding to T
+P_HALF = {"bf16": 2.0 ** -12, "f32": 2.0 ** -22}       # rounding of a probability: fp16 (11 bits), two pieces of it
+GEOS = {"mha": (4, 4, 64), "gqa": (8, 2, 64), "dream": (28, 4, 128), "odd": (5, 1, 128), "llada": (32, 32, 128)}
+
+
+def B():
+    from paper_2509_23094_amd import binding
+    return binding
+
+
+def dev(a, dtype):
+    t = torch.from_numpy(np.ascontiguousarray(a, np.float32))
+    return t.to(torch.bfloat16 if dtype == "bf16" else torch.float32).cuda().contiguous()
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def rows(rng, m, heads, dim, loud=0.3):
+    return rng.standard_normal((m, heads, dim)) * np.exp(loud * rng.standard_normal((m, 1, 1)))
+
+
+class Case:
+    """A handle, a cache with garbage where nothing is written, and the plain cache beside it."""
+
+    def __init__(self, geo, dtype, L, seed=0, max_rows=256, max_batch=1, capacity=None, ctx=None):
+        self.H, self.Hkv, self.D = GEOS[geo] if isinstance(geo, str) else geo
+        self.dtype, self.L, self.rng = dtype, L, np.random.default_rng([seed, L])
+        cap = capacity or L
+        self.ctx = ctx or B().Q8Context(self.H, self.Hkv, self.D, dtype, max_seq=max(cap, L), max_rows=max_rows, max_batch=max_batch)
+        self.cache = B().Q8Cache(self.ctx, cap)
+        for t in (self.cache.k_codes, self.cache.v_codes):
+            t.copy_(torch.randint(0, 256, t.shape, dtype=torch.uint8))
+        self.ref = R.Cache8(cap, self.Hkv, self.D)
+
+    def new(self, m, factor=1.0):
+        """(device tensor, its values) of m rows of K or V."""
+        t = dev(rows(self.rng, m, self.Hkv, self.D) * factor, self.dtype).reshape(m, self.Hkv * self.D)
+        return t, f64(t).reshape(m, self.Hkv, self.D)
+
+    def update(self, idx, m=None, L=None, factor=1.0, new=None):
+        L = self.L if L is None else L
+        m = len(idx) if idx is not None else m
+        (dk, nk), (dv, nv) = new or (self.new(m, factor), self.new(m, factor))
+        di = None if idx is None else torch.tensor(np.asarray(idx), dtype=torch.int32, device="cuda")
+        self.ctx.d2c_q8_update([B().Q8Seq(self.cache, L, m, idx=di, new_k=dk, new_v=dv)])
+        self.ref.update(np.arange(L - m, L) if idx is None else idx, nk, nv, L)
+        torch.cuda.synchronize()
+
+    def fill(self):
+        self.update(None, m=self.L)
+        return self
+
+    def check(self, L=None):
+        """Codes of the first L rows and scales, bit for bit."""
+        L = self.L if L is None else L
+        nb = -(-L // 64)
+        for name, t in (("k", self.ref.k), ("v", self.ref.v)):
+            got_s = getattr(self.cache, name + "_scale").cpu().numpy().astype(np.float64)[:nb]
+            assert np.array_equal(got_s, t.scale[:nb]), name + " scales"
+            raw = getattr(self.cache, name + "_codes").cpu().numpy()
+            c = raw.reshape(-1, self.Hkv, self.D // 16, 64, 16).transpose(0, 3, 1, 2, 4) if name == "k" else \
+                raw.reshape(-1, self.Hkv, 16, self.D, 4).transpose(0, 2, 4, 1, 3)
+            c = c.reshape(-1, self.Hkv, self.D).astype(np.int64) - 128
+            assert np.array_equal(c[:L], t.codes[:L]), name + " codes"
+
+    def queries(self, m, factor=1.0):
+        return dev(self.rng.standard_normal((m, self.H * self.D)) * factor, self.dtype)
+
+    def expect(self, q, out, avg, L=None):
+        L = self.L if L is None else L
+        check_attention(q, self.ref.k.values(L), self.ref.v.values(L), out, avg, self)
+
+
+def check_attention(q, k, v, out, avg, c):
+    m = q.shape[0]
+    o, a, mag, share = R.attention(f64(q).reshape(m, c.H, c.D), k, v)
+    if out is not None:
+        # each term's share twice (numerator and denominator), its rounding, D / 64 blocks of fp32 sums, the result's rounding
+        n = k.shape[0]
+        # a probability below 2^-29 of its row's largest is a subnormal fp16 number (it is rounded times 2^15; fp16 is normal from 2^-14 on):
+        # its rounding is at most half of 2^-24 there, 2^-25 / 2^15 = 2^-40 of the row's largest, which is at most the row's sum
+        below = 2.0 ** -40 * np.repeat(np.abs(v).sum(0), c.H // c.Hkv, 0)[None]
+        tol = HALF[c.dtype] * np.abs(o) + (1 + HALF[c.dtype]) * (mag * (2 * share + P_HALF[c.dtype] + (n ** 0.5 + 70) * 2.0 ** -24) + below) + 1e-30
+        err = np.abs(f64(out).reshape(m, c.H, c.D) - o)
+        assert (err <= tol).all(), "out: %g times the bound" % (err / tol).max()
+    if avg is not None:
+        tol = a * (2 * share + (k.shape[0] ** 0.5 + c.H + 16) * 2.0 ** -24) + 1e-30
+        err = np.abs(f64(avg) - a)
+        assert (err <= tol).all(), "average: %g times the bound" % (err / tol).max()
+
+
+# ---------------------------------------------------------------------- update and read
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("geo", ["mha", "dream"])
+@pytest.mark.parametrize("L", [1, 3, 63, 64, 65, 200, 1000])
+def test_fill_and_refresh(geo, dtype, L):
+    say(f"q8 update {geo} {dtype} L={L}")
+    c = Case(geo, dtype, L).fill()
+    c.check()
+    for m, factor in ((1, 1.0), (min(L, 3), 2.5), (min(L, 20), 0.1), ((L + 1) // 2, 1.5), (L, 0.7)):
+        idx = np.sort(c.rng.permutation(L)[:m])
+        c.update(idx, factor=factor)
+        c.check()
+
+
+@pytest.mark.parametrize("L", [4099, 20000])
+def test_refresh_of_long_caches(L):
+    """Few scattered rows (a workgroup per row) and more rows than blocks (a workgroup per block, its rows searched)."""
+    say(f"q8 update long {L}")
+    c = Case((2, 1, 64), "bf16", L).fill()
+    for m in (5, L // 64, L // 64 + 1, 700, L - 1):
+        c.update(np.sort(c.rng.permutation(L)[:m]), factor=1.3)
+        c.check()
+    c.update(np.arange(64 * 10, 64 * 20), factor=0.2)       # whole blocks among the others
+    c.check()
+
+
+def test_append_row_by_row():
+    """A cache that grows: the first row of a block sets its scale, whatever lay there."""
+    say("q8 append")
+    c = Case("gqa", "bf16", 130, capacity=200)
+    c.cache.k_scale.fill_(float("nan"))
+    c.cache.v_scale.fill_(1e30)
+    c.update(None, m=61, L=61)
+    for L in range(62, 131):
+        c.update(None, m=1, L=L, factor=1.0 + 0.01 * L)
+    c.check(130)
+
+
+def test_borders_and_values_that_are_not_finite():
+    say("q8 borders")
+    c = Case("mha", "f32", 128)
+    s = float(np.float32(127.0 * 0.75) / np.float32(127))
+    x = np.zeros((64, c.Hkv, c.D))
+    x[0, :, 0] = 127 * 0.75
+    x[1:] = (c.rng.integers(-127, 127, size=(63, c.Hkv, c.D)) + 0.5) * s                       # exactly between two codes
+    x[2:4] = np.nextafter(x[2:4].astype(np.float32), np.float32(0))                             # and just beside
+    x[4:6] = np.nextafter(x[4:6].astype(np.float32), np.float32(1e9))
+    x = x.astype(np.float32)
+    d = dev(x, "f32").reshape(64, -1)
+    c.update(np.arange(64), new=((d, f64(d).reshape(x.shape)), (d, f64(d).reshape(x.shape))))
+    c.check(64)
+    y = np.zeros((64, c.Hkv, c.D), np.float32)
+    y[3, 0, 5], y[4, 1, 6], y[5, 2, 7], y[6] = np.nan, np.inf, -np.inf, 0.25
+    y[7, 3] = 1e-38                                                                             # far below the others
+    d = dev(y, "f32").reshape(64, -1)
+    c.update(np.arange(64, 128), new=((d, f64(d).reshape(y.shape)), (d, f64(d).reshape(y.shape))))
+    c.check(128)
+    tiny = np.full((64, c.Hkv, c.D), 1e-36, np.float32)                                         # below 2^-100: zeros, scale 0
+    d = dev(tiny, "f32").reshape(64, -1)
+    c.update(np.arange(64), new=((d, f64(d).reshape(y.shape)), (d, f64(d).reshape(y.shape))))
+    assert (c.cache.k_scale[0] == 0).all()
+    c.update([9], factor=1.0)                                                                   # and a row beside them
+    c.check(128)
+    big = np.full((1, c.Hkv, c.D), 3e38, np.float32)
+    d = dev(big, "f32").reshape(1, -1)
+    c.update([10], new=((d, f64(d).reshape(big.shape)), (d, f64(d).reshape(big.shape))))
+    c.check(128)
+
+
+@pytest.mark.parametrize("L", [100, 1000])
+def test_indices_outside_are_left_out(L):
+    say(f"q8 indices outside L={L}")
+    c = Case("mha", "bf16", L, capacity=L + 28).fill()
+    c.update([-70, -1, 5, 64, L, L + 27, 1 << 30])                                               # L = 1000: fewer than blocks
+    c.check()
+    c.update(np.r_[[-9], np.arange(0, L, 3), [L, 5000]])                                         # the searched form
+    c.check()
+
+
+def test_batch_of_updates():
+    say("q8 batch of 11 updates")
+    first = Case("gqa", "bf16", 700, max_batch=11)
+    cs = [first] + [Case("gqa", "bf16", 100 + 50 * i, seed=i, ctx=first.ctx) for i in range(10)]
+    seqs = []
+    for i, c in enumerate(cs):
+        c.fill()
+        m = 0 if i == 4 else 1 + 9 * i
+        (dk, nk), (dv, nv) = c.new(m, 1.5), c.new(m, 1.5)
+        idx = np.sort(c.rng.permutation(c.L)[:m])
+        seqs.append(B().Q8Seq(c.cache, c.L, m, idx=torch.tensor(idx, dtype=torch.int32, device="cuda"), new_k=dk, new_v=dv))
+        c.ref.update(idx, nk, nv, c.L)
+    first.ctx.d2c_q8_update(seqs)
+    torch.cuda.synchronize()
+    for c in cs:
+        c.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("geo", ["mha", "dream"])
+def test_read(geo, dtype):
+    say(f"q8 read {geo} {dtype}")
+    c = Case(geo, dtype, 201).fill()
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    for idx in (None, [0], [200, 3, 3, 64, 63], [-1, 5, 201, 1 << 30], list(range(0, 201, 7))):
+        n = 201 if idx is None else len(idx)
+        k, v = (torch.full((n, c.Hkv * c.D), 7.0, dtype=t, device="cuda") for _ in range(2))
+        c.ctx.d2c_q8_read(c.cache, 201, None if idx is None else torch.tensor(idx, dtype=torch.int32, device="cuda"), k, v)
+        at = np.arange(n) if idx is None else np.asarray(idx)
+        ok = (at >= 0) & (at < 201)
+        for got, ref in ((k, c.ref.k), (v, c.ref.v)):
+            want = np.where(ok[:, None], ref.values().astype(np.float32)[np.where(ok, at, 0)].reshape(n, -1), 0.0)
+            assert torch.equal(got.cpu(), torch.from_numpy(want.astype(np.float32)).to(t))
+    only = torch.zeros((3, c.Hkv * c.D), dtype=t, device="cuda")
+    c.ctx.d2c_q8_read(c.cache, 201, None, None, only)
+    assert torch.equal(only.cpu(), torch.from_numpy(c.ref.v.values(3).astype(np.float32).reshape(3, -1)).to(t))
+
+
+# ---------------------------------------------------------------------- attention
+
+def attend(c, m, L=None, avg=True, q=None, batch=None):
+    L = c.L if L is None else L
+    q = c.queries(m) if q is None else q
+    out = torch.full_like(q, 9.0)
+    a = torch.full((m, L), 9.0, device="cuda") if avg else None
+    c.ctx.d2c_q8_attention([B().Q8Seq(c.cache, L, m, q=q, out=out, attn_avg=a)])
+    torch.cuda.synchronize()
+    return q, out, a
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("geo", list(GEOS))
+@pytest.mark.parametrize("m,L", [(1, 1), (1, 2), (3, 63), (2, 64), (33, 65), (32, 128), (1, 257), (31, 500), (130, 320), (64, 1030)])
+def test_attention(geo, dtype, m, L):
+    say(f"q8 attention {geo} {dtype} m={m} L={L}")
+    c = Case(geo, dtype, L).fill()
+    q, out, avg = attend(c, m)
+    c.expect(q, out, avg)
+    _, again, _ = attend(c, m, avg=False, q=q)
+    assert torch.equal(again, out)                      # the average changes nothing, and the same call gives the same bits
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("geo,m,L", [("dream", 1, 70001), ("odd", 7, 33333), ("llada", 2, 9000), ("mha", 256, 4100)])
+def test_attention_long(geo, dtype, m, L):
+    say(f"q8 attention long {geo} {dtype} m={m} L={L}")
+    c = Case(geo, dtype, L)
+    c.update(None, m=L)
+    q, out, avg = attend(c, m, avg=m < 100)
+    c.expect(q, out, avg)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_refreshes_first_and_a_shorter_length_reads_less(dtype):
+    say(f"q8 attention with update {dtype}")
+    c = Case("gqa", dtype, 300).fill()
+    idx = np.sort(c.rng.permutation(300)[:40])
+    (dk, nk), (dv, nv) = c.new(40, 2.0), c.new(40, 2.0)
+    q = c.queries(40)
+    out, avg = torch.zeros_like(q), torch.zeros((40, 300), device="cuda")
+    c.ctx.d2c_q8_attention([B().Q8Seq(c.cache, 300, 40, idx=torch.tensor(idx, dtype=torch.int32, device="cuda"), new_k=dk, new_v=dv, q=q,
+                                      out=out, attn_avg=avg)])
+    c.ref.update(idx, nk, nv, 300)
+    c.check()
+    c.expect(q, out, avg)
+    q, out, avg = attend(c, 5, L=130)
+    c.expect(q, out, avg, L=130)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_batch(dtype):
+    """Eleven sequences of different sizes in one call, one of them empty, some without the average."""
+    say(f"q8 attention batch {dtype}")
+    first = Case("gqa", dtype, 900, max_batch=11, max_rows=600)
+    cs = [first] + [Case("gqa", dtype, 1 + 97 * i, seed=i, ctx=first.ctx) for i in range(10)]
+    seqs, got = [], []
+    for i, c in enumerate(cs):
+        c.fill()
+        m = 0 if i == 4 else 1 + 11 * i
+        q = c.queries(m)
+        out, avg = torch.zeros_like(q), torch.zeros((m, c.L), device="cuda") if i % 3 else None
+        seqs.append(B().Q8Seq(c.cache, c.L, m, q=q, out=out, attn_avg=avg))
+        got.append((q, out, avg))
+    first.ctx.d2c_q8_attention(seqs)
+    torch.cuda.synchronize()
+    for i, (c, (q, out, avg)) in enumerate(zip(cs, got)):
+        if i != 4:
+            c.expect(q, out, avg)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_of_extreme_sizes(dtype):
+    """Loud and silent blocks, one key that takes all, queries far from 1, zeros: nothing overflows and nothing is lost."""
+    say(f"q8 attention extremes {dtype}")
+    c = Case("mha", dtype, 400).fill()
+    c.update(np.arange(64), factor=1e-6)
+    c.update(np.arange(64, 128), factor=0.0)
+    c.update(np.arange(192, 256), factor=20.0)
+    c.check()
+    for factor in (1e-30, 1e-3, 1.0, 30.0):
+        q = c.queries(19, factor)
+        q[3] = 0
+        q, out, avg = attend(c, 19, q=q)
+        c.expect(q, out, avg)
+    q = c.queries(5)
+    q[1, 7], q[2, 70], q[3, 200] = float("nan"), float("inf"), -float("inf")
+    _, out, avg = attend(c, 5, q=q)
+    assert torch.isnan(out[1, : c.D]).all() and torch.isnan(avg[1:4]).all()
+    assert torch.isfinite(out[1, c.D:]).all()                                           # the other heads' columns
+    c.expect(q[[0, 4]].contiguous(), out[[0, 4]], avg[[0, 4]])
+
+
+def test_attention_of_a_flat_row_over_a_long_cache():
+    """Equal scores: each of 50000 probabilities is 2e-5 of the sum; none may be lost in its rounding."""
+    say("q8 attention flat")
+    c = Case((2, 1, 64), "bf16", 50000)
+    c.update(None, m=50000)
+    q = c.queries(3)
+    q[0] = 0
+    q[1] *= 1e-4
+    q, out, avg = attend(c, 3, q=q)
+    c.expect(q, out, avg)
+
+
+# ---------------------------------------------------------------------- linear
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,N,K", [(1, 1, 8), (1, 16, 64), (2, 17, 72), (15, 33, 256), (16, 768, 1000), (17, 100, 320), (33, 250, 2048),
+                                   (64, 64, 4096), (65, 129, 136), (100, 1000, 512), (130, 72, 8192), (200, 300, 640), (257, 513, 576),
+                                   (520, 520, 264)])
+def test_linear(dtype, m, N, K):
+    say(f"q8 linear {dtype} m={m} N={N} K={K}")
+    rng = np.random.default_rng([m, N, K])
+    a, w = dev(rng.standard_normal((m, K)), dtype), dev(0.02 * rng.standard_normal((N, K)) * np.exp(rng.standard_normal((N, 1))), dtype)
+    if m > 3:
+        a[1] = 0
+        a[2] = 0
+        a[2, K // 2] = -5
+    ctx = B().Q8Context(4, 4, 64, dtype, max_rows=m, max_k=K, max_n=N)
+    p = ctx.d2c_q8_pack(w)
+    guard = torch.full((m + 2, N), 123.0, device="cuda")
+    out = torch.full((m, N), 9.0, device="cuda")
+    ctx.d2c_q8_linear(a, p, out)
+    want, _, sw = R.linear(f64(a), f64(w))
+    assert np.array_equal(p.scale.cpu().numpy(), sw)
+    assert np.array_equal(out.cpu().numpy(), want)
+    flat = guard.view(-1)[: m * N].view(m, N)                          # nothing behind the last row or column is written
+    ctx.d2c_q8_linear(a, p, flat)
+    assert torch.equal(flat, out) and (guard.view(-1)[m * N:] == 123.0).all()
+
+
+def test_linear_float_rows_of_four_more():
+    say("q8 linear f32 K % 8 == 4")
+    for m, N, K in ((5, 40, 4), (3, 20, 12), (70, 90, 1028)):
+        rng = np.random.default_rng([m, N, K])
+        a, w = dev(rng.standard_normal((m, K)), "f32"), dev(rng.standard_normal((N, K)), "f32")
+        ctx = B().Q8Context(4, 4, 64, "f32", max_rows=m, max_k=K, max_n=N)
+        out = torch.zeros((m, N), device="cuda")
+        ctx.d2c_q8_linear(a, ctx.d2c_q8_pack(w), out)
+        assert np.array_equal(out.cpu().numpy(), R.linear(f64(a), f64(w))[0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m", [5, 70, 300])
+def test_linear_rows_and_channels_that_are_not_finite(dtype, m):
+    say(f"q8 linear not finite {dtype} m={m}")
+    rng = np.random.default_rng(m)
+    N, K = 150, 512
+    a, w = dev(rng.standard_normal((m, K)), dtype), dev(rng.standard_normal((N, K)), dtype)
+    a[1, 3], a[3, 511], w[7, 0], w[149, 77] = float("nan"), -float("inf"), float("inf"), float("nan")
+    ctx = B().Q8Context(4, 4, 64, dtype, max_rows=m, max_k=K, max_n=N)
+    out = torch.zeros((m, N), device="cuda")
+    ctx.d2c_q8_linear(a, ctx.d2c_q8_pack(w), out)
+    assert np.array_equal(out.cpu().numpy(), R.linear(f64(a), f64(w))[0], equal_nan=True)
+    assert int(torch.isnan(out).sum()) == 2 * N + 2 * (m - 2)
+
+
+def test_linear_near_the_largest_sum():
+    """All products 127 * 127 over the longest contraction: 1.06e9 still fits the 32-bit sum."""
+    say("q8 linear largest sum")
+    ctx = B().Q8Context(4, 4, 64, "bf16", max_rows=20, max_k=1 << 16, max_n=48)
+    a, w = (torch.ones((r, 1 << 16), dtype=torch.bfloat16, device="cuda") for r in (20, 48))
+    w[5] = -1
+    out = torch.zeros((20, 48), device="cuda")
+    ctx.d2c_q8_linear(a, ctx.d2c_q8_pack(w), out)
+    assert np.array_equal(out.cpu().numpy(), R.linear(f64(a), f64(w))[0])
+
+
+# ---------------------------------------------------------------------- weigh and evict
+
+@pytest.mark.parametrize("m,L", [(1, 1), (3, 63), (17, 64), (64, 65), (130, 1000), (300, 5000), (2, 70000)])
+def test_weigh(m, L):
+    say(f"q8 weigh m={m} L={L}")
+    rng = np.random.default_rng([m, L])
+    avg = rng.random((m, L), dtype=np.float32) ** 8
+    avg[0, 0] = 1.0
+    w = rng.integers(0, 1 << 40, size=L)
+    if L > 10:
+        avg[0, 1:7] = [np.nan, np.inf, -np.inf, -1.0, 2.0, 1e-12]
+    d = torch.from_numpy(w.copy()).cuda()
+    ctx = B().Q8Context(4, 4, 64, "f32")
+    ctx.d2c_q8_weigh(torch.from_numpy(avg).cuda(), d)
+    assert np.array_equal(d.cpu().numpy(), R.weigh(avg, w))
+
+
+def weights(rng, L, kind):
+    if kind == "spread":
+        return (np.exp(2 * rng.standard_normal(L)) * 2 ** 30).astype(np.int64)
+    if kind == "ties":
+        return rng.integers(0, 4, size=L) * (1 << 33)
+    if kind == "equal":
+        return np.full(L, 12345)
+    if kind == "wide":
+        return rng.integers(0, (1 << 63) - 1, size=L) >> rng.integers(0, 63, size=L)
+    w = rng.integers(-5, 3, size=L)                     # zeros and negative ones
+    return w
+
+
+@pytest.mark.parametrize("kind", ["spread", "ties", "equal", "wide", "negative"])
+@pytest.mark.parametrize("L", [1, 2, 64, 65, 1000, 5000, 20481, 140000])
+def test_evict(kind, L):
+    say(f"q8 evict {kind} L={L}")
+    geo = (1, 1, 64) if L > 10000 else "gqa"
+    c = Case(geo, "bf16", L).fill()
+    w = weights(c.rng, L, kind)
+    protect = (c.rng.random(L) < 0.2).astype(np.uint8) * 3
+    dw = torch.from_numpy(w).cuda()
+    for n, p in ((1, None), (L, None), ((L + 1) // 2, None), ((L + 1) // 2, protect), (max(1, L // 10), protect), (max(1, int((protect > 0).sum())), protect)):
+        dst = B().Q8Cache(c.ctx, n)
+        kept = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+        kw = torch.full((n,), -1, dtype=torch.int64, device="cuda")
+        c.ctx.d2c_q8_evict(c.cache, L, dw, None if p is None else torch.from_numpy(p).cuda(), dst, kept, kw)
+        want = R.keep(w, p, n)
+        assert np.array_equal(kept.cpu().numpy(), want), f"n={n}"
+        assert np.array_equal(kw.cpu().numpy(), w[want])
+        o = Case.__new__(Case)
+        o.__dict__.update(c.__dict__)
+        o.cache, o.ref, o.L = dst, c.ref.evict(want), n
+        o.check()
+
+
+# ---------------------------------------------------------------------- together
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_few_steps_together(dtype):
+    """Projection of selected rows -> refresh + attention -> weights -> eviction -> the next step on the smaller cache."""
+    say(f"q8 together {dtype}")
+    d, m, L = 256, 21, 333
+    c = Case("gqa", dtype, L, max_rows=64)
+    lin = B().Q8Context(c.H, c.Hkv, c.D, dtype, max_rows=64, max_k=d, max_n=c.H * c.D + 2 * c.Hkv * c.D)
+    w = dev(0.06 * c.rng.standard_normal((lin.d_q + 2 * lin.d_kv, d)), dtype)
+    pack = lin.d2c_q8_pack(w)
+    c.fill()
+    weight = torch.zeros(L, dtype=torch.int64, device="cuda")
+    ref_w, t = np.zeros(L, np.int64), torch.bfloat16 if dtype == "bf16" else torch.float32
+    for step in range(4):
+        h = dev(c.rng.standard_normal((m, d)), dtype)
+        qkv = torch.zeros((m, lin.d_q + 2 * lin.d_kv), device="cuda")
+        lin.d2c_q8_linear(h, pack, qkv)
+        assert np.array_equal(qkv.cpu().numpy(), R.linear(f64(h), f64(w))[0])
+        q, k, v = (x.to(t).contiguous() for x in qkv.split([lin.d_q, lin.d_kv, lin.d_kv], 1))
+        idx = np.sort(c.rng.permutation(c.L)[:m])
+        out, avg = torch.zeros_like(q), torch.zeros((m, c.L), device="cuda")
+        c.ctx.d2c_q8_attention([B().Q8Seq(c.cache, c.L, m, idx=torch.tensor(idx, dtype=torch.int32, device="cuda"), new_k=k, new_v=v, q=q,
+                                          out=out, attn_avg=avg)])
+        c.ref.update(idx, f64(k).reshape(m, c.Hkv, c.D), f64(v).reshape(m, c.Hkv, c.D), c.L)
+        c.check()
+        c.expect(q, out, avg)
+        c.ctx.d2c_q8_weigh(avg, weight)
+        ref_w = R.weigh(f64(avg), ref_w)
+        assert np.array_equal(weight.cpu().numpy(), ref_w)
+        n = c.L - 40 if step % 2 else c.L
+        if n < c.L:
+            dst, kept = B().Q8Cache(c.ctx, n), torch.zeros(n, dtype=torch.int32, device="cuda")
+            kw = torch.zeros(n, dtype=torch.int64, device="cuda")
+            c.ctx.d2c_q8_evict(c.cache, c.L, weight, None, dst, kept, kw)
+            want = R.keep(ref_w, None, n)
+            assert np.array_equal(kept.cpu().numpy(), want)
+            c.cache, c.ref, c.L, weight, ref_w = dst, c.ref.evict(want), n, kw, ref_w[want]
+            c.check()
+
+
+def test_captured_and_replayed_on_another_stream():
+    """One graph of all calls, replayed with eager work in between, against eager results."""
+    say("q8 graph")
+    L, m, n, dtype = 500, 30, 300, "bf16"
+    c = Case("gqa", dtype, L, max_rows=64).fill()
+    lin = B().Q8Context(8, 2, 64, dtype, max_rows=300, max_k=512, max_n=256)
+    w, a = dev(c.rng.standard_normal((256, 512)), dtype), dev(c.rng.standard_normal((300, 512)), dtype)
+    pack, y = lin.d2c_q8_pack(w), torch.zeros((300, 256), device="cuda")
+    idx = torch.tensor(np.sort(c.rng.permutation(L)[:m]), dtype=torch.int32, device="cuda")
+    (dk, _), (dv, _) = c.new(m), c.new(m)
+    q = c.queries(m)
+    out, avg = torch.zeros_like(q), torch.zeros((m, L), device="cuda")
+    weight, kept, kw = torch.zeros(L, dtype=torch.int64, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int64, device="cuda")
+    dst = B().Q8Cache(c.ctx, n)
+    rk, rv = (torch.zeros((n, c.ctx.d_kv), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    batch = B().Q8Batch(c.ctx, [B().Q8Seq(c.cache, L, m, idx=idx, new_k=dk, new_v=dv, q=q, out=out, attn_avg=avg)])
+
+    def step():
+        lin.d2c_q8_linear(a, pack, y)
+        c.ctx.d2c_q8_attention(batch)
+        c.ctx.d2c_q8_weigh(avg, weight)
+        c.ctx.d2c_q8_evict(c.cache, L, weight, None, dst, kept, kw)
+        c.ctx.d2c_q8_read(dst, n, None, rk, rv)
+
+    state = [c.cache.k_codes, c.cache.v_codes, c.cache.k_scale, c.cache.v_scale, out, avg, weight, kept, kw, dst.k_codes, dst.v_codes,
+             dst.k_scale, dst.v_scale, rk, rv, y]
+    start = [t.clone() for t in state]
+
+    def reset(i):
+        for t, s in zip(state, start):
+            t.copy_(s)
+        for t, seed in ((dk, 10), (dv, 20), (q, 30)):
+            g = torch.Generator(device="cuda").manual_seed(seed + i)
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+
+    want = []
+    for i in range(4):
+        reset(i)
+        step()
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in state])
+    reset(0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for i in (0, 1, 2, 3, 1):
+        reset(i)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for k, (t, s) in enumerate(zip(state, want[i])):
+            assert torch.equal(t, s), f"replay {i}, tensor {k}"
+        reset((i + 1) % 4)                              # eager work between the replays
+        step()
+        torch.cuda.synchronize()
+        for k, (t, s) in enumerate(zip(state, want[(i + 1) % 4])):
+            assert torch.equal(t, s), f"eager {i}, tensor {k}"
+    side2 = torch.cuda.Stream()
+    reset(2)
+    side2.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side2):
+        step()
+    torch.cuda.synchronize()
+    for t, s in zip(state, want[2]):
+        assert torch.equal(t, s)
+
+
+def test_refusals():
+    say("q8 refusals")
+    b = B()
+    c = Case("gqa", "bf16", 100, max_rows=10, max_batch=2).fill()
+    ctx, q = c.ctx, c.queries(4)
+    out = torch.zeros_like(q)
+
+    def refused(code, f):
+        with pytest.raises(b.D2CError) as e:
+            f()
+        assert e.value.code == code and str(e.value)
+
+    seq = lambda **kw: b.Q8Seq(c.cache, kw.pop("L", 100), kw.pop("m", 4), **kw)
+    (dk, _), (dv, _) = c.new(4), c.new(4)
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_attention([seq(q=q)]))                                     # no out
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_attention([seq(q=q, out=out, new_k=dk)]))                  # no new_v
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_update([seq()]))                                           # nothing to write
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_attention([seq(q=q, out=out, L=0)]))
+    refused(b.D2C_ESHAPE, lambda: ctx.d2c_q8_attention([b.Q8Seq(c.cache, 128, 4, q=q, out=out)]))       # the cache holds it, the handle does not
+    refused(b.D2C_ESHAPE, lambda: seq(L=129))                                                           # beyond the cache
+    refused(b.D2C_ESHAPE, lambda: ctx.d2c_q8_attention([seq(q=q, out=out)] * 3))                        # more than max_batch
+    q11 = c.queries(11)
+    refused(b.D2C_ESHAPE, lambda: ctx.d2c_q8_attention([seq(q=q11, out=torch.zeros_like(q11), m=11)]))  # more than max_rows
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_update([seq(new_k=dk, new_v=dv, L=3)]))                    # more rows than L
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_update([seq(new_k=dk, new_v=dv), seq(new_k=dk, new_v=dv)]))  # one cache twice
+    off = torch.zeros(4 * ctx.d_q + 1, dtype=torch.bfloat16, device="cuda")[1:].view(4, ctx.d_q)
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_attention([seq(q=off, out=out)]))                          # not 16-byte aligned
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_read(c.cache, 100, None, torch.zeros((101, ctx.d_kv), dtype=torch.bfloat16, device="cuda"), None))
+    wt, kept = torch.zeros(100, dtype=torch.int64, device="cuda"), torch.zeros(50, dtype=torch.int32, device="cuda")
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_evict(c.cache, 100, wt, None, c.cache, kept))              # onto itself
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_evict(c.cache, 100, wt, None, b.Q8Cache(ctx, 128), torch.zeros(101, dtype=torch.int32, device="cuda")))
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_evict(c.cache, 100, wt.int(), None, b.Q8Cache(ctx, 50), kept))
+    refused(b.D2C_ESHAPE, lambda: ctx.d2c_q8_evict(c.cache, 100, wt, None, b.Q8Cache(ctx, 49), torch.zeros(65, dtype=torch.int32, device="cuda")))
+    lin = b.Q8Context(4, 4, 64, "bf16", max_rows=8, max_k=64, max_n=32)
+    w = torch.zeros((32, 64), dtype=torch.bfloat16, device="cuda")
+    p = lin.d2c_q8_pack(w)
+    a = torch.zeros((9, 64), dtype=torch.bfloat16, device="cuda")
+    refused(b.D2C_ESHAPE, lambda: lin.d2c_q8_linear(a, p, torch.zeros((9, 32), device="cuda")))
+    refused(b.D2C_EINVAL, lambda: lin.d2c_q8_linear(a[:8], p, torch.zeros((8, 31), device="cuda")))
+    refused(b.D2C_ESHAPE, lambda: lin.d2c_q8_pack(torch.zeros((4, 4), dtype=torch.bfloat16, device="cuda")))
+    refused(b.D2C_ESHAPE, lambda: lin.d2c_q8_evict(c.cache, 100, wt, None, b.Q8Cache(ctx, 50), kept))
+    c.check()                                                                                            # none of them wrote anything
+    ctx.d2c_q8_attention([])
+    ctx.d2c_q8_update([seq(m=0)])
+    lin.d2c_q8_linear(a[:0], p, torch.zeros((0, 32), device="cuda"))
+    c.check()

@@ -1,0 +1,140 @@
+"""CPU-side checks of the 8-bit operators: the header against the library and the binding, refusals that need no GPU, and what the plain
+64-bit forms (which the GPU tests compare with) promise."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+
+import q8_reference as R
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_2509_23094_amd", "libd2c.so")
+built = pytest.mark.skipif(not os.path.exists(LIB), reason="libd2c.so not built (run __graft_entry__.build())")
+
+
+@built
+def test_header_library_and_binding_agree():
+    from paper_2509_23094_amd import binding as B
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "d2c_q8.h")).read(), flags=re.S)
+    names = sorted(set(re.findall(r"\b(d2c_q8_[a-z_0-9]+)\s*\(", text)))
+    assert names == sorted(B.Q8_EXPORTS)
+    for n in names:
+        assert getattr(B._lib, n) is not None
+    for n in ("update", "attention", "read", "pack", "linear", "weigh", "evict"):
+        assert hasattr(B.Q8Context, "d2c_q8_" + n)
+    assert ctypes.sizeof(B.d2c_q8_seq) == 10 * 8 + 8 and ctypes.sizeof(B.d2c_q8_dims) == 36
+
+
+@built
+@pytest.mark.parametrize("field,value,code", [
+    ("n_heads", 0, -1), ("n_kv_heads", 0, -1), ("n_kv_heads", 3, -1), ("n_heads", 2048, -1), ("head_dim", 96, -4), ("dtype", 2, -1),
+    ("max_seq", -1, -1), ("max_seq", (1 << 24) + 1, -1), ("max_rows", -1, -1), ("max_rows", (1 << 16) + 1, -1), ("max_batch", 257, -1),
+    ("max_k", (1 << 16) + 1, -1), ("max_n", -5, -1)])
+def test_init_refuses(field, value, code):
+    from paper_2509_23094_amd import binding as B
+    d = B.d2c_q8_dims(4, 4, 64, B.D2C_BF16, 128, 16, 1, 0, 0)
+    setattr(d, field, value)
+    out = ctypes.c_void_p()
+    assert B._lib.d2c_q8_init(ctypes.byref(d), ctypes.byref(out)) == code
+    assert B._lib.d2c_q8_last_error(None) and not out
+
+
+@built
+def test_null_arguments_are_refused():
+    from paper_2509_23094_amd import binding as B
+    lib, out = B._lib, ctypes.c_void_p()
+    assert lib.d2c_q8_init(None, ctypes.byref(out)) == B.D2C_EINVAL
+    assert lib.d2c_q8_destroy(None) == B.D2C_OK
+    assert lib.d2c_q8_workspace_bytes(None) == 0
+    assert lib.d2c_q8_update(None, None, 1, None) == B.D2C_EINVAL
+    assert lib.d2c_q8_attention(None, None, 1, None) == B.D2C_EINVAL
+    assert lib.d2c_q8_read(None, None, 1, None, 1, None, None, None) == B.D2C_EINVAL
+    assert lib.d2c_q8_pack(None, None, 1, 8, None, None, None) == B.D2C_EINVAL
+    assert lib.d2c_q8_linear(None, None, 1, None, None, 1, 8, None, None) == B.D2C_EINVAL
+    assert lib.d2c_q8_weigh(None, None, 1, 1, None, None) == B.D2C_EINVAL
+    assert lib.d2c_q8_evict(None, None, 1, None, None, 1, None, None, None, None) == B.D2C_EINVAL
+    assert lib.d2c_q8_cache_size(None, 1, None, None) == B.D2C_EINVAL
+    assert lib.d2c_q8_weight_bytes(17, 65) == 32 * 128 and lib.d2c_q8_weight_bytes(0, 8) == 0
+
+
+@built
+def test_binding_refuses_tensors_of_another_kind():
+    import torch
+    from paper_2509_23094_amd import binding as B
+
+    class Ctx:                                   # geometry of a handle, no device needed
+        torch_dtype, device, d_kv, d_q = torch.bfloat16, -1, 128, 256
+
+    class Cache:
+        c = B.d2c_q8_cache()
+
+        def holds(self, L):
+            pass
+
+    def batch(**kw):
+        return B.Q8Batch(Ctx, [B.Q8Seq(Cache(), 64, 3, **kw)])
+
+    batch(q=torch.zeros(3, 256, dtype=torch.bfloat16))
+    for bad in (dict(q=torch.zeros(3, 256)), dict(q=torch.zeros(2, 256, dtype=torch.bfloat16)),
+                dict(new_k=torch.zeros(3, 64, dtype=torch.bfloat16)), dict(idx=torch.zeros(3, dtype=torch.int64)),
+                dict(attn_avg=torch.zeros(3, 63)), dict(out=torch.zeros(256, 3, dtype=torch.bfloat16).t())):
+        with pytest.raises(B.D2CError) as e:
+            batch(**bad)
+        assert e.value.code == B.D2C_EINVAL
+
+
+# ---------------------------------------------------------------------- the plain forms
+
+def test_codes_are_within_half_a_step_and_ties_go_to_even():
+    rng = np.random.default_rng(0)
+    x = rng.standard_normal(4000).astype(np.float32).astype(np.float64)
+    s = R.scale(np.abs(x).max())
+    assert np.abs(R.code(x, s) * s - x).max() <= s / 2 * (1 + 1e-12)
+    assert list(R.code(np.array([0.5, 1.5, 2.5, -0.5, -1.5, 300.0, np.inf, -np.inf, np.nan]), 1.0)) == [0, 2, 2, 0, -2, 127, 127, -127, 0]
+    assert R.scale(2.0 ** -101) == 0 and R.scale(0.0) == 0 and R.code(1e-40, 0.0) == 0
+
+
+def test_many_small_growths_do_not_carry_a_value_away():
+    """A row that is never refreshed beside one that grows by a little 600 times: each growth of the scale is a factor of 1.25 or more
+    and rounds by half a step, so the whole drift stays below half a last step / (1 - 1/1.25) = 2.5 of them."""
+    t = R.Tensor8(64, 1, 16)
+    rng = np.random.default_rng(1)
+    first = rng.standard_normal((64, 1, 16))
+    t.update(np.arange(64), first, 64)
+    size = np.abs(first).max()
+    for _ in range(600):
+        size *= 1.01
+        t.update([7], np.full((1, 1, 16), size), 64)
+    others = np.delete(np.arange(64), 7)
+    assert np.abs(t.values()[others] - first[others]).max() <= 2.5 * t.scale[0, 0] + 1e-9
+    assert abs(t.values()[7, 0, 0] - size) <= t.scale[0, 0] / 2 + 1e-9
+
+
+def test_a_refreshed_block_takes_the_scale_of_its_rows_again():
+    t = R.Tensor8(70, 2, 16)
+    t.update(np.arange(70), np.full((70, 2, 16), 8.0), 70)
+    t.update(np.arange(64, 70), np.full((6, 2, 16), 0.5), 70)              # all rows below L of the second block
+    assert (t.scale[1] == R.scale(0.5)).all() and (t.scale[0] == R.scale(8.0)).all()
+    t.update(np.arange(63), np.full((63, 2, 16), 0.5), 70)                 # one row of the first stays
+    assert (t.scale[0] == R.scale(8.0)).all()
+
+
+def test_byte_order_is_the_documented_one():
+    rng = np.random.default_rng(2)
+    heads, D, nb = 3, 64, 2
+    c = rng.integers(-127, 128, size=(nb * 64, heads, D))
+    k, v = R.k_bytes(c), R.v_bytes(c)
+    for _ in range(200):
+        b, h, t, d = rng.integers(nb), rng.integers(heads), rng.integers(64), rng.integers(D)
+        base = (b * heads + h) * 64 * D
+        assert k[base + d // 16 * 1024 + t * 16 + d % 16] == c[b * 64 + t, h, d] + 128
+        assert v[base + t // 4 * 4 * D + d * 4 + t % 4] == c[b * 64 + t, h, d] + 128
+
+
+def test_keep_orders_protected_weight_and_index():
+    assert list(R.keep([5, 9, 5, 1], None, 2)) == [0, 1]
+    assert list(R.keep([5, 9, 5, 1], [0, 0, 0, 1], 2)) == [1, 3]
+    assert list(R.keep([5, 9, 5, 1], [1, 0, 1, 1], 2)) == [0, 2]
+    assert list(R.keep([-3, 0, -1], None, 2)) == [0, 1]
