@@ -43,8 +43,8 @@ size_t q8_attention_bytes(const Q8Shape& s, int max_rows, int max_batch);
 hipError_t launch_q8_attention(const Q8Shape& s, const Q8Attend* calls, int n, int max_rows, int max_batch, void* ws, hipStream_t st);
 
 inline int q8_kpad(int K) { return (K + 63) & ~63; }
-// bytes of workspace for products of up to max_rows rows, contractions of up to max_k and max_n outputs
-size_t q8_linear_bytes(int max_rows, int max_k, int max_n);
+// bytes of workspace for products of up to max_rows rows and contractions of up to max_k
+size_t q8_linear_bytes(int max_rows, int max_k);
 hipError_t launch_q8_pack(int dtype, const void* w, int N, int K, int8_t* codes, float* scale, hipStream_t st);
 hipError_t launch_q8_linear(int dtype, const void* a, int m, const int8_t* codes, const float* scale, int N, int K, float* out,
                             void* ws, hipStream_t st);

@@ -127,7 +127,7 @@ int d2c_q8_init(const d2c_q8_dims* dims, d2c_q8** out) {
   }
   size_t bytes = 256;
   if (D.max_seq > 0 && D.max_rows > 0) bytes = std::max(bytes, q8_attention_bytes(c->shape, D.max_rows, c->max_batch));
-  if (D.max_k > 0 && D.max_n > 0 && D.max_rows > 0) bytes = std::max(bytes, q8_linear_bytes(D.max_rows, D.max_k, D.max_n));
+  if (D.max_k > 0 && D.max_n > 0 && D.max_rows > 0) bytes = std::max(bytes, q8_linear_bytes(D.max_rows, D.max_k));
   const hipError_t e = hipMalloc(&c->ws, bytes);
   if (e != hipSuccess) {
     (void)hipGetLastError();
