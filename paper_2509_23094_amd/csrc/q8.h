@@ -56,23 +56,24 @@ __device__ __forceinline__ float q8_inverse(float s) { return s > 0.f ? 1.f / s 
 
 // The whole number nearest to x / s (s > 0, inv about 1 / s), ties to even, in [-127, 127].  The product with inv can land on
 // the wrong side of a border; the remainder x - n s tells, and has no rounding: it is a multiple of half of s's last place, and
-// about s / 2 at most.
+// about s / 2 at most.  (Borders are not rare: half of a row's largest magnitude is one.)  No branches.
 __device__ __forceinline__ int q8_code(float x, float s, float inv) {
-  if (!(x == x) || s == 0.f) return 0;
-  float n = fminf(fmaxf(rintf(x * inv), -127.f), 127.f);
+  const float n = fminf(fmaxf(rintf(x * inv), -127.f), 127.f);
   const float e = fmaf(-n, s, x), e2 = 2.f * fabsf(e);
-  if (e2 > s || (e2 == s && ((int)n & 1))) n += e > 0.f ? 1.f : -1.f;
-  return (int)fminf(fmaxf(n, -127.f), 127.f);
+  const bool odd = (__builtin_bit_cast(uint32_t, n + 12582912.f) & 1u) != 0;
+  const bool over = (e2 > s) | ((e2 == s) & odd);
+  const float c = fminf(fmaxf(n + (over ? copysignf(1.f, e) : 0.f), -127.f), 127.f);
+  return (x == x) & (s > 0.f) ? (int)c : 0;
 }
 // code(c * old, s): the product has 31 bits
 __device__ __forceinline__ int q8_recode(int c, float old, float s, float inv) {
-  if (s == 0.f) return 0;
   const double x = (double)c * (double)old;
-  double n = rint((double)((float)x * inv));
-  n = fmin(fmax(n, -127.0), 127.0);
-  const double e = fma(-n, (double)s, x), e2 = 2.0 * fabs(e);
-  if (e2 > (double)s || (e2 == (double)s && ((int)n & 1))) n += e > 0.0 ? 1.0 : -1.0;
-  return (int)fmin(fmax(n, -127.0), 127.0);
+  const float n = fminf(fmaxf(rintf((float)x * inv), -127.f), 127.f);
+  const double e = fma(-(double)n, (double)s, x), e2 = 2.0 * fabs(e);
+  const bool odd = (__builtin_bit_cast(uint32_t, n + 12582912.f) & 1u) != 0;
+  const bool over = (e2 > (double)s) | ((e2 == (double)s) & odd);
+  const float r = fminf(fmaxf(n + (over ? copysignf(1.f, (float)e) : 0.f), -127.f), 127.f);
+  return s > 0.f ? (int)r : 0;
 }
 // eight neighbouring values of T as floats (16 bytes of bf16, 32 of float)
 __device__ __forceinline__ void q8_load8(const bf16* p, float* x) {

@@ -21,10 +21,11 @@ typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 // Rows quantised by their largest magnitude; a row that holds a NaN or an infinity gets the scale NaN and codes 0.  What pads
 // the last tile is not written, or holds the last row again: it gives outputs that nothing stores.
 //
-// A workgroup of 16 waves takes 16 / WAVES rows and the part blockIdx.y of their columns; every part looks at the whole row for its
-// largest magnitude (integer maxima of the bits without sign: infinities and NaN are the largest), 16 columns per thread at a time,
-// one lane's piece of a tile.  Few rows have all waves on one row and several parts, as the rounding is what takes the time then
-// (37 x 18944: XXX us; one part 7.8); many rows go four to a workgroup, so that 64 bytes of a tile are written together.
+// A workgroup takes a row, or a part of its columns (blockIdx.y) while there are few rows, 16 columns per thread at a time: one lane's piece
+// of a tile.  It looks at the whole row for its largest magnitude -- integer maxima of the bits without sign: infinities and NaN are the
+// largest -- and rounds its part from registers.  What bounds it: one chain of load, maximum, barrier and store; 37 x 18944 4.3 us, 1536 x
+// 4096 11 us (4 waves a row; 16 waves 17).  Sixteen rows per workgroup with lanes as in a tile, so that codes leave a kilobyte
+// at a time, took longer (20 and 19 us): their loads are 128-byte pieces of 16 rows.
 //
 // Rounding: the sum with 1.5 * 2^23 leaves the whole number nearest to x / s (or its neighbour, next to a border) in its low byte, and the
 // remainder x - n s, which has no rounding (see q8_code), says if all 16 are the nearest: only where a remainder is half a step or more
@@ -59,16 +60,21 @@ template <> struct Raw16<float> {
     return __builtin_bit_cast(float, x);
   }
 };
+// (read from a place inside where there is nothing, and set to 0 afterwards: loads under a condition would come one after the other)
 template <typename T>
 __device__ __forceinline__ Raw16<T> load16(const T* row, int k, int K) {
   constexpr int kEach = 16 / sizeof(T), kN = sizeof(Raw16<T>) / 16;         // K is a multiple of 16 bytes
   Raw16<T> v;
 #pragma unroll
-  for (int i = 0; i < kN; ++i) {
-    v.w[i] = u32x4{0, 0, 0, 0};
-    if (k + i * kEach < K) v.w[i] = ld16(row + k + i * kEach);
-  }
+  for (int i = 0; i < kN; ++i) v.w[i] = ld16(row + min(k + i * kEach, K - kEach));
   return v;
+}
+template <typename T>
+__device__ __forceinline__ void zero_past(Raw16<T>& v, int k, int K) {
+  constexpr int kEach = 16 / sizeof(T), kN = sizeof(Raw16<T>) / 16;
+#pragma unroll
+  for (int i = 0; i < kN; ++i)
+    if (k + i * kEach >= K) v.w[i] = u32x4{0, 0, 0, 0};
 }
 template <typename T>
 __device__ __forceinline__ u32x4 round16(const Raw16<T>& v, float s, float inv) {
@@ -97,43 +103,54 @@ __device__ __forceinline__ u32x4 round16(const Raw16<T>& v, float s, float inv) 
   }
   return c;
 }
-template <typename T, int WAVES, int PIECES>
-__global__ __launch_bounds__(1024) void q8_rows_kernel(const T* x, int n_rows, int K, int kc, int per_part, int8_t* codes, float* scale) {
-  constexpr int kThreads = 64 * WAVES;
-  const int wave = threadIdx.x >> 6, r = blockIdx.x * (16 / WAVES) + wave / WAVES, tid = threadIdx.x % kThreads;
-  const T* row = x + (size_t)min(r, n_rows - 1) * K;
-  const int p0 = blockIdx.y * per_part, p1 = min(4 * kc, p0 + per_part);      // pieces of 16 columns
-  __shared__ uint32_t red[16];
-  Raw16<T> v[PIECES];
+__device__ __forceinline__ uint32_t wave_max_bits(uint32_t v) {
 #pragma unroll
-  for (int i = 0; i < PIECES; ++i) v[i] = load16(row, 16 * (p0 + tid + i * kThreads), K);
-  uint32_t bits = 0;
-#pragma unroll
-  for (int i = 0; i < PIECES; ++i) bits = max(bits, v[i].largest());
-  // what this part has not in registers
-  for (int p = tid; 16 * p < K; p += kThreads)
-    if (p < p0 || p >= p0 + PIECES * kThreads) bits = max(bits, load16(row, 16 * p, K).largest());
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) bits = max(bits, (uint32_t)__shfl_xor((int)bits, o, 64));
-  if ((threadIdx.x & 63) == 0) red[wave] = bits;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) bits = max(bits, red[wave / WAVES * WAVES + w]);
-  const bool nan_row = bits >= 0x7f800000u;
-  const float s = nan_row ? 0.f : q8_scale(__builtin_bit_cast(float, bits)), inv = q8_inverse(s);
-  if (tid == 0 && p0 == 0 && r < n_rows) scale[r] = nan_row ? __builtin_nanf("") : s;
-  int8_t* to = codes + (size_t)(r / 16) * kc * 1024 + r % 16 * 16;
-  auto put = [&](int p, const Raw16<T>& w) __attribute__((always_inline)) {
+  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+  return v;
+}
+// the scale that a row's largest bits give, the row's scale as it is stored, and the codes of a piece
+struct RowScale {
+  float s, inv;
+  bool bad;
+  __device__ explicit RowScale(uint32_t bits) : bad(bits >= 0x7f800000u) {
+    s = bad ? 0.f : q8_scale(__builtin_bit_cast(float, bits));
+    inv = q8_inverse(s);
+  }
+  __device__ float stored() const { return bad ? __builtin_nanf("") : s; }
+  template <typename T> __device__ void put(int8_t* to, const Raw16<T>& w) const {
     u32x4 c = {0, 0, 0, 0};
     if (s > 0.f) c = round16(w, s, inv);
-    *reinterpret_cast<u32x4*>(to + (size_t)(p / 4) * 1024 + p % 4 * 256) = c;
-  };
-#pragma unroll
-  for (int i = 0; i < PIECES; ++i) {
-    const int p = p0 + tid + i * kThreads;
-    if (p < p1) put(p, v[i]);
+    *reinterpret_cast<u32x4*>(to) = c;
   }
-  for (int p = p0 + tid + PIECES * kThreads; p < p1; p += kThreads) put(p, load16(row, 16 * p, K));
+};
+
+template <typename T, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void q8_rows_kernel(const T* x, int K, int kc, int per_part, int8_t* codes, float* scale) {
+  const int r = blockIdx.x, tid = threadIdx.x;
+  const T* row = x + (size_t)r * K;
+  const int p0 = blockIdx.y * per_part, p1 = min(4 * kc, p0 + per_part);      // pieces of 16 columns
+  __shared__ uint32_t red[WAVES];
+  Raw16<T> v = load16(row, 16 * (p0 + tid), K);
+  zero_past(v, 16 * (p0 + tid), K);
+  uint32_t bits = v.largest();
+  // what this part has not in registers (what load16 repeats at the end is the row's own)
+  for (int p = tid; 16 * p < K; p += 64 * WAVES)
+    if (p < p0 || p >= p0 + 64 * WAVES) bits = max(bits, load16(row, 16 * p, K).largest());
+  bits = wave_max_bits(bits);
+  if ((tid & 63) == 0) red[tid >> 6] = bits;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) bits = max(bits, red[w]);
+  const RowScale s(bits);
+  if (tid == 0 && p0 == 0) scale[r] = s.stored();
+  int8_t* to = codes + (size_t)(r / 16) * kc * 1024 + r % 16 * 16;
+  auto at = [&](int p) { return to + (size_t)(p / 4) * 1024 + p % 4 * 256; };
+  if (p0 + tid < p1) s.put(at(p0 + tid), v);
+  for (int p = p0 + tid + 64 * WAVES; p < p1; p += 64 * WAVES) {
+    v = load16(row, 16 * p, K);
+    zero_past(v, 16 * p, K);
+    s.put(at(p), v);
+  }
 }
 
 __device__ __forceinline__ i32x4 mfma_i8(const u32x4& a, const u32x4& b, const i32x4& c) {
@@ -336,7 +353,7 @@ __global__ __launch_bounds__(512, 1) void q8_tile_kernel(const int8_t* a, const 
   __builtin_amdgcn_s_waitcnt(0x70 | 0xf00);                 // no staging may write LDS any more
   __syncthreads();
   // Outputs leave through LDS, 16 rows at a time, in whole rows of the workgroup's columns: from the accumulators they would leave in
-  // pieces of 64 bytes (XXX)
+  // pieces of 64 bytes (1536 x 24576 x 4096 178 us, this way 157)
   float sn[NT][4];
 #pragma unroll
   for (int n = 0; n < NT; ++n)
@@ -461,12 +478,12 @@ hipError_t run_tile(const Operands& o, const TilePlan& p, hipStream_t st) {
 
 template <typename T>
 hipError_t rows_t(const T* x, int rows, int K, int kc, int8_t* codes, float* scale, hipStream_t st) {
-  if (rows > 256) {
-    q8_rows_kernel<T, 4, 2><<<(rows + 3) / 4, 1024, 0, st>>>(x, rows, K, kc, 4 * kc, codes, scale);
+  if (4 * kc <= 256) {
+    q8_rows_kernel<T, 4><<<rows, 256, 0, st>>>(x, K, kc, 4 * kc, codes, scale);
   } else {
     // parts of 256 pieces at least, as many as the chip has room for
     const int parts = std::max(1, std::min((4 * kc + 255) / 256, 512 / rows)), per = (4 * kc + parts - 1) / parts;
-    q8_rows_kernel<T, 16, 1><<<dim3(rows, parts), 1024, 0, st>>>(x, rows, K, kc, per, codes, scale);
+    q8_rows_kernel<T, 16><<<dim3(rows, parts), 1024, 0, st>>>(x, K, kc, per, codes, scale);
   }
   return hipGetLastError();
 }
