@@ -8,8 +8,8 @@
 //   permutation and one packed addition for two codes).  q enters as fp16 too, exactly: a row is scaled by a power of two so that its
 //   largest magnitude lies in [2^14, 2^15); bf16 has 8 bits, float takes two pieces of 11.  The product's scale (row, block and
 //   log2(e) / sqrt(D)) is applied to the fp32 score, V's scale when a block's O^T joins the running one.
-//   probabilities times 2^15 are rounded to fp16 (float: two pieces): 11 (22) bits down to 2^-29 of a row's largest, below that to
-//   the nearest 2^-39 of it; the running sum takes them before that rounding.
+//   probabilities are rounded to fp16 (float: two pieces): 11 (22) bits down to 2^-25 (2^-14) of a row's largest, below that to
+//   the nearest 2^-35 of it; the running sum takes them before that rounding.
 // The waves' maxima, sums and O^T are merged through LDS; where the key range is split over workgroups, by a second launch.
 // The head average has a pass of its own over the scores, from the same fp16 q and the final (maximum, sum) of every row.
 #include <algorithm>
@@ -25,7 +25,9 @@ typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kTile = 32;                 // query rows per workgroup
-constexpr float kPScale = 32768.f;        // probabilities before their rounding to fp16
+constexpr int kWaves = 8;
+// Probabilities are rounded to fp16 times 2^kPBits, relative to a reference that a score may pass by kSlack: 2^15 at most.
+constexpr float kPBits = 11.f, kSlack = 4.f;
 
 struct AttendSeq {
   Q8CachePtr c;
@@ -73,18 +75,13 @@ __device__ __forceinline__ float pow2_for(float amax) {
 
 // D / 16 operands of one query row half (16 dimensions of each 32), scaled; returns the scale
 template <typename T, int D, int QP>
-__device__ __forceinline__ float load_q(const T* q, bool valid, h8 (&f)[QP][D / 16]) {
+__device__ __forceinline__ float load_q(const T* q, h8 (&f)[QP][D / 16]) {
   float x[D / 2], amax = 0.f;
   const int g = (threadIdx.x & 63) >> 5;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) {
-    if (valid) {
-      q8_load8(q + 32 * c + 16 * g, &x[16 * c]);
-      q8_load8(q + 32 * c + 16 * g + 8, &x[16 * c + 8]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) x[16 * c + j] = 0.f;
-    }
+    q8_load8(q + 32 * c + 16 * g, &x[16 * c]);
+    q8_load8(q + 32 * c + 16 * g + 8, &x[16 * c + 8]);
   }
 #pragma unroll
   for (int j = 0; j < D / 2; ++j) amax = fmaxf(amax, fabsf(x[j]));
@@ -122,11 +119,23 @@ __device__ __forceinline__ void load_k(const uint8_t* k, int key, u32x4 (&raw)[D
   for (int c = 0; c < D / 32; ++c) raw[c] = ld16(k + (2 * c + g) * 1024 + key * 16);
 }
 
+// Pieces of V of a block: eight times four rows of this lane's D / 32 dimensions (D = 64: eight bytes of each)
+template <int D>
+__device__ __forceinline__ void load_v(const uint8_t* v, u32x4 (&raw)[8]) {
+  const int g = (threadIdx.x & 63) >> 5, r32 = threadIdx.x & 31;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint8_t* at = v + (2 * i + g) * 4 * D + r32 * (D / 8);
+    if constexpr (D == 128) raw[i] = ld16(at);
+    else { const u32x2 w = ld8(at); raw[i][0] = w[0]; raw[i][1] = w[1]; }
+  }
+}
+
 template <typename T, int D>
-__global__ __launch_bounds__(256) void q8_attend_kernel(AttendArgs args) {
+__global__ __launch_bounds__(64 * kWaves) void q8_attend_kernel(AttendArgs args) {
   constexpr int QP = sizeof(T) == 2 ? 1 : 2;      // fp16 pieces of q and of a probability
   constexpr int DT = D / 32;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, r32 = lane & 31;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
   int si = 0;
   while (si + 1 < args.n && (int)blockIdx.x >= args.s[si + 1].first_wg) ++si;
   const AttendSeq& s = args.s[si];
@@ -136,11 +145,28 @@ __global__ __launch_bounds__(256) void q8_attend_kernel(AttendArgs args) {
   const int G = args.H / args.Hkv, R = s.m * G, n_blocks = (s.L + kQ8Rows - 1) / kQ8Rows;
   const int b0 = split * s.per_split, b1 = min(n_blocks, b0 + s.per_split);
   const int r = tile * kTile + r32;
-  const bool valid = r < R;
+  const bool valid = r < R;                        // past the last: the first row again, not stored
   const int row = valid ? r / G : 0, head = hk * G + (valid ? r % G : 0);
 
+  u32x4 kr[2][D / 32], vr[8];
+  float ks_next, vs_next;
+  // the next block's keys are requested as soon as this block's are used (float, whose q takes twice the registers: when they are
+  // needed), its values likewise; behind the last block that one again
+  auto want_k = [&](int b) __attribute__((always_inline)) {
+    const size_t blk = (size_t)min(b, b1 - 1) * args.Hkv + hk;
+    load_k<D>(s.c.k + blk * kQ8Rows * D, r32, kr[0]);
+    load_k<D>(s.c.k + blk * kQ8Rows * D, 32 + r32, kr[1]);
+    ks_next = s.c.ks[blk];
+  };
+  auto want_v = [&](int b) __attribute__((always_inline)) {
+    const size_t blk = (size_t)min(b, b1 - 1) * args.Hkv + hk;
+    load_v<D>(s.c.v + blk * kQ8Rows * D, vr);
+    vs_next = s.c.vs[blk];
+  };
+  if (QP == 1) want_k(b0 + wave);
+  want_v(b0 + wave);
   h8 q[QP][D / 16];
-  const float p2 = load_q<T, D, QP>((const T*)s.q + ((size_t)row * args.H + head) * D, valid, q);
+  const float p2 = load_q<T, D, QP>((const T*)s.q + ((size_t)row * args.H + head) * D, q);
   const float factor = 1.4426950408889634f / (sqrtf((float)D) * p2);
   if (s.avg && split == 0 && wave == 0 && valid) {
     _Float16* to = args.q16 + s.q16 + (((size_t)head * s.avg_tiles + row / kTile) * (QP * D / 16) * 64 + g * 32 + row % kTile) * 8;
@@ -150,53 +176,65 @@ __global__ __launch_bounds__(256) void q8_attend_kernel(AttendArgs args) {
       for (int f = 0; f < D / 16; ++f) *reinterpret_cast<h8*>(to + (size_t)(p * (D / 16) + f) * 512) = q[p][f];
   }
 
+  // o and l are relative to 2^ref; ref is raised only where a score passes it by more than kSlack
   f32x16 o[DT] = {};
-  float mx = -INFINITY, l = 0.f;
-  for (int b = b0 + wave; b < b1; b += 4) {
-    const size_t blk = (size_t)b * args.Hkv + hk;
-    const uint8_t *k = s.c.k + blk * kQ8Rows * D, *v = s.c.v + blk * kQ8Rows * D;
-    u32x4 kr[2][D / 32];
-    load_k<D>(k, r32, kr[0]);
-    load_k<D>(k, 32 + r32, kr[1]);
-    u32x4 vr[8];                           // D = 64: eight bytes of each
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint8_t* at = v + (2 * i + g) * 4 * D + r32 * (D / 8);
-      if constexpr (D == 128) vr[i] = ld16(at);
-      else { const u32x2 w = ld8(at); vr[i][0] = w[0]; vr[i][1] = w[1]; }
-    }
-    const float ks = s.c.ks[blk] * factor, vs = s.c.vs[blk];
+  float ref = -INFINITY, l = 0.f;
+  for (int b = b0 + wave; b < b1; b += kWaves) {
+    if (QP > 1) want_k(b);
+    const float ks = ks_next * factor;
     f32x16 x[2];
     x[0] = scores<D, QP>(kr[0], q);
     x[1] = scores<D, QP>(kr[1], q);
-    float bm = -INFINITY;
+    if (QP == 1) want_k(b + kWaves);
     const int left = s.L - b * kQ8Rows;    // keys of this block that exist
+    float top = -3.4e38f;
+    if (left >= kQ8Rows) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, x[t][i]);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (32 * t + 8 * (i / 4) + 4 * g + i % 4 < left) top = fmaxf(top, x[t][i]);
+    }
+    top = fmaxf(top, __shfl_xor(top, 32, 64)) * ks;
+    if (__any(top > ref + kSlack)) {
+      const float to = top > ref + kSlack ? top : ref, alpha = exp2_hw(ref - to);
+      ref = to;
+      l *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
+    }
+    const float base = kPBits - ref;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float y = x[t][i] * ks;
-        if (left < kQ8Rows && 32 * t + 8 * (i / 4) + 4 * g + i % 4 >= left) y = -INFINITY;
-        x[t][i] = y;
-        bm = fmaxf(bm, y);
-      }
-    bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
-    const float m_new = fmaxf(mx, bm), ref = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = exp2_hw(mx - ref);
-    mx = m_new;
+      for (int i = 0; i < 16; ++i) x[t][i] = exp2_hw(fmaf(x[t][i], ks, base));
+    if (left < kQ8Rows) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (32 * t + 8 * (i / 4) + 4 * g + i % 4 >= left) x[t][i] = 0.f;
+    }
     h8 p[QP][4];
     float sum = 0.f;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float e = exp2_hw(x[t][i] - ref) * kPScale;
-        sum += e;
-        const _Float16 hi = (_Float16)e;
+        sum += x[t][i];
+        const _Float16 hi = (_Float16)x[t][i];
         p[0][2 * t + i / 8][i % 8] = hi;
-        if constexpr (QP > 1) p[1][2 * t + i / 8][i % 8] = (_Float16)(e - (float)hi);
+        if constexpr (QP > 1) p[1][2 * t + i / 8][i % 8] = (_Float16)(x[t][i] - (float)hi);
       }
-    l = l * alpha + sum;
+    l += sum;
+    const float vs = vs_next;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
       f32x16 acc = {};
@@ -207,28 +245,44 @@ __global__ __launch_bounds__(256) void q8_attend_kernel(AttendArgs args) {
         for (int pp = 0; pp < QP; ++pp) acc = mfma(a, p[pp][i], acc);
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[dt][i] = o[dt][i] * alpha + vs * acc[i];
+      for (int i = 0; i < 16; ++i) o[dt][i] = fmaf(vs, acc[i], o[dt][i]);
     }
+    want_v(b + kWaves);
   }
   l += __shfl_xor(l, 32, 64);
 
-  // merge the waves: each adds up a quarter of every accumulator, 16 neighbouring dimensions of a row (D = 64: 8)
+  // merge the waves: half of them hand theirs to the other half, until four are left; each of these adds up a quarter of every accumulator,
+  // 16 neighbouring dimensions of a row (D = 64: 8)
   __shared__ float lds[4][DT * 16][64];
-  __shared__ float wm[4][kTile], wl[4][kTile];
-  if (g == 0) { wm[wave][r32] = mx; wl[wave][r32] = l; }
+  __shared__ float wref[kWaves][kTile], wl[kWaves][kTile];
+  if (g == 0) { wref[wave][r32] = ref; wl[wave][r32] = l; }
   __syncthreads();
-  const float M = fmaxf(fmaxf(wm[0][r32], wm[1][r32]), fmaxf(wm[2][r32], wm[3][r32]));
-  const float ref = M == -INFINITY ? 0.f : M;
-  const float own = exp2_hw(mx - ref);
-  float sum = 0.f;
+  float M = wref[0][r32], sum = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) sum += wl[w][r32] * exp2_hw(wm[w][r32] - ref);
+  for (int w = 1; w < kWaves; ++w) M = fmaxf(M, wref[w][r32]);
+  const float to_m = M == -INFINITY ? 0.f : M, own = exp2_hw(ref - to_m);
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) sum += wl[w][r32] * exp2_hw(wref[w][r32] - to_m);
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) lds[wave][dt * 16 + i][lane] = o[dt][i] * own;
+    for (int i = 0; i < 16; ++i) o[dt][i] *= own;
+  if (wave >= 4)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) lds[wave - 4][dt * 16 + i][lane] = o[dt][i];
   __syncthreads();
-  if (!valid) return;
+  if (wave < 4)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        o[dt][i] += lds[wave][dt * 16 + i][lane];
+        lds[wave][dt * 16 + i][lane] = o[dt][i];
+      }
+  __syncthreads();
+  if (!valid || wave >= 4) return;
   float y[4 * DT];
 #pragma unroll
   for (int j = 0; j < 4; ++j)
@@ -252,41 +306,58 @@ __global__ __launch_bounds__(256) void q8_attend_kernel(AttendArgs args) {
 #pragma unroll
     for (int j = 0; j < DT; ++j) q8_store4(to + 4 * j, y + 4 * j);
   }
-  if (s.avg && wave == 0 && g == 0 && (s.splits == 1 || split == 0))
-    args.row[slot] = make_float2(factor, ref + log2f(sum / kPScale));       // (the sum of a split row: the merge puts it right)
+  if (s.avg && wave == 0 && g == 0 && split == 0)
+    args.row[slot] = make_float2(factor, to_m + log2f(sum) - kPBits);       // (the sum of a split row: the merge puts it right)
 }
 
-// Splits of a row joined in order.  A workgroup per 256 / (D / 4) rows.
+// Splits of a row joined.  A workgroup per row, a thread per (four dimensions, every kJoin-th split).
+constexpr int kJoin = 8;
 template <typename T, int D>
-__global__ __launch_bounds__(256) void q8_join_kernel(AttendArgs args) {
-  const int t = threadIdx.x % (D / 4) * 4;
-  const size_t slot = (size_t)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
-  if (slot >= args.slots) return;
+__global__ __launch_bounds__(kJoin * D / 4) void q8_join_kernel(AttendArgs args) {
+  const int t = threadIdx.x % (D / 4), part = threadIdx.x / (D / 4);
+  const size_t slot = blockIdx.x;
   int si = 0;
   while (si + 1 < args.n && slot >= (size_t)args.s[si + 1].row0) ++si;
   const AttendSeq& s = args.s[si];
   if (s.splits <= 1) return;
   float M = -INFINITY, sum = 0.f;
-  for (int i = 0; i < s.splits; ++i) M = fmaxf(M, args.ml[(size_t)i * args.slots + slot].x);
-  const float ref = M == -INFINITY ? 0.f : M;
   f32x4 y = {};
-  for (int i = 0; i < s.splits; ++i) {
+  for (int i = part; i < s.splits; i += kJoin) {
     const float2 ml = args.ml[(size_t)i * args.slots + slot];
-    const float w = exp2_hw(ml.x - ref);
-    sum += ml.y * w;
-    y += w * *reinterpret_cast<const f32x4*>(args.part + ((size_t)i * args.slots + slot) * D + t);
+    const f32x4 z = *reinterpret_cast<const f32x4*>(args.part + ((size_t)i * args.slots + slot) * D + 4 * t);
+    const float m = fmaxf(M, ml.x), ref = m == -INFINITY ? 0.f : m, a = exp2_hw(M - ref), w = exp2_hw(ml.x - ref);
+    M = m;
+    sum = sum * a + ml.y * w;
+    y = y * a + z * w;
+  }
+  __shared__ float sm[kJoin], ss[kJoin];
+  __shared__ f32x4 sy[kJoin][D / 4];
+  if (t == 0) { sm[part] = M; ss[part] = sum; }
+  sy[part][t] = y;
+  __syncthreads();
+  if (part) return;
+#pragma unroll
+  for (int i = 1; i < kJoin; ++i) M = fmaxf(M, sm[i]);
+  const float ref = M == -INFINITY ? 0.f : M;
+  sum = 0.f;
+  y = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kJoin; ++i) {
+    const float w = exp2_hw(sm[i] - ref);
+    sum += ss[i] * w;
+    y += sy[i][t] * w;
   }
   y *= 1.f / sum;
   float z[4] = {y[0], y[1], y[2], y[3]};
-  q8_store4((T*)s.out + (slot - s.row0) * D + t, z);
-  if (s.avg && t == 0) args.row[slot].y = ref + log2f(sum / kPScale);
+  q8_store4((T*)s.out + (slot - s.row0) * D + 4 * t, z);
+  if (s.avg && t == 0) args.row[slot].y = ref + log2f(sum) - kPBits;
 }
 
 // attn_avg of 32 rows x one block of keys: the four waves take the heads in turn and are added up at the end.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void q8_average_kernel(AttendArgs args) {
   constexpr int QP = sizeof(T) == 2 ? 1 : 2;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, r32 = lane & 31;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
   int si = 0;
   while (si + 1 < args.n && (int)blockIdx.x >= args.s[si + 1].avg_first_wg) ++si;
   const AttendSeq& s = args.s[si];
@@ -331,10 +402,18 @@ __global__ __launch_bounds__(256) void q8_average_kernel(AttendArgs args) {
   }
 }
 
-// Workgroups over the keys: enough to fill the chip about twice, each with a block for each of its waves.
+// Workgroups over the keys.  A wave takes about 1.2 us for a block beside another on its SIMD, a workgroup 3 us at its ends, a split row
+// 4 us and its way to memory and back; a compute unit holds one workgroup.
 constexpr int kTargetWgs = 512;
 int plan_splits(int workgroups, int n_blocks) {
-  return std::max(1, std::min(kTargetWgs / workgroups, n_blocks / 4));
+  int best = 1;
+  float best_cost = 1e30f;
+  for (int s = 1; s <= 64 && (s == 1 || (s * workgroups <= kTargetWgs && s * kWaves < 2 * n_blocks)); ++s) {
+    const int per = (n_blocks + s - 1) / s;
+    const float cost = (s * workgroups + 255) / 256 * ((per + kWaves - 1) / kWaves * 1.2f + 3.f) + (s > 1 ? 4.f + s * workgroups * 0.008f : 0.f);
+    if (cost < best_cost) { best_cost = cost; best = s; }
+  }
+  return best;
 }
 int row_tiles(const Q8Shape& s, int m) { return (m * (s.H / s.Hkv) + kTile - 1) / kTile; }
 
@@ -355,10 +434,10 @@ Layout layout(const Q8Shape& s, size_t max_rows, size_t max_batch) {
 
 template <typename T, int D>
 hipError_t run(const AttendArgs& a, int wgs, int avg_wgs, bool join, hipStream_t st) {
-  q8_attend_kernel<T, D><<<wgs, 256, 0, st>>>(a);
+  q8_attend_kernel<T, D><<<wgs, 64 * kWaves, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && join) {
-    q8_join_kernel<T, D><<<(unsigned)((a.slots + 1024 / D - 1) / (1024 / D)), 256, 0, st>>>(a);
+    q8_join_kernel<T, D><<<(unsigned)a.slots, kJoin * D / 4, 0, st>>>(a);
     e = hipGetLastError();
   }
   if (e == hipSuccess && avg_wgs) {

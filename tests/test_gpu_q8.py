@@ -90,9 +90,9 @@ def check_attention(q, k, v, out, avg, c):
     if out is not None:
         # each term's share twice (numerator and denominator), its rounding, D / 64 blocks of fp32 sums, the result's rounding
         n = k.shape[0]
-        # a probability below 2^-29 of its row's largest is a subnormal fp16 number (it is rounded times 2^15; fp16 is normal from 2^-14 on):
-        # its rounding is at most half of 2^-24 there, 2^-25 / 2^15 = 2^-40 of the row's largest, which is at most the row's sum
-        below = 2.0 ** -40 * np.repeat(np.abs(v).sum(0), c.H // c.Hkv, 0)[None]
+        # a probability is rounded to fp16 times 2^11, relative to a reference that is at most the row's largest.  Where that is a subnormal
+        # number (below 2^-14) its rounding is at most half of 2^-24: 2^-25 / 2^11 = 2^-36 of the largest, which is at most the row's sum
+        below = 2.0 ** -36 * np.repeat(np.abs(v).sum(0), c.H // c.Hkv, 0)[None]
         tol = HALF[c.dtype] * np.abs(o) + (1 + HALF[c.dtype]) * (mag * (2 * share + P_HALF[c.dtype] + (n ** 0.5 + 70) * 2.0 ** -24) + below) + 1e-30
         err = np.abs(f64(out).reshape(m, c.H, c.D) - o)
         assert (err <= tol).all(), "out: %g times the bound" % (err / tol).max()
