@@ -75,6 +75,44 @@ __device__ __forceinline__ int q8_recode(int c, float old, float s, float inv) {
   const float r = fminf(fmaxf(n + (over ? copysignf(1.f, (float)e) : 0.f), -127.f), 127.f);
   return s > 0.f ? (int)r : 0;
 }
+// Sixteen codes at a time, as cache bytes.  The sum with 1.5 * 2^23 leaves the whole number nearest to x / s (or its neighbour, next to a
+// border) in its low bits; the remainders say if all sixteen are the nearest: only where one is half a step or more (values that are
+// not finite among them) is each done by itself.  byte[i]: code(x[i], s) + 128 in the low byte, other bits anything.
+__device__ __forceinline__ void q8_bytes16(const float (&x)[16], float s, float inv, uint32_t (&byte)[16]) {
+  constexpr float kMagic = 12582912.f + 128.f;
+  float worst = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float n = fmaf(x[i], inv, kMagic);
+    worst = fmaxf(worst, fabsf(fmaf(-(n - kMagic), s, x[i])));
+    byte[i] = __builtin_bit_cast(uint32_t, n);
+    worst = fabsf(x[i]) <= 3.402823466e38f ? worst : INFINITY;
+  }
+  if (!(worst < 0.5f * s))
+#pragma unroll
+    for (int i = 0; i < 16; ++i) byte[i] = (uint32_t)(q8_code(x[i], s, inv) + 128);
+}
+// low bytes of four words in one
+__device__ __forceinline__ uint32_t q8_pack(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
+}
+// Four bytes of a word of old codes (scale old) as codes for s; inv about 1 / s, ratio about old / s.  The remainder in 32 bits is off by less than
+// 1e-5 s (127 old 2^-24, old <= s): where one is that near to a border, all four are done in 64 bits.
+__device__ __forceinline__ uint32_t q8_reword(uint32_t word, float old, float s, float inv, float ratio) {
+  constexpr float kMagic = 12582912.f + 128.f;
+  float worst = 0.f;
+  uint32_t b[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float c = (float)(word >> (8 * j) & 255u) - 128.f, n = fmaf(c, ratio, kMagic);
+    worst = fmaxf(worst, fabsf(fmaf(-(n - kMagic), s, c * old)));
+    b[j] = __builtin_bit_cast(uint32_t, n);
+  }
+  if (!(worst < 0.49998f * s))
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = (uint32_t)(q8_recode((int)(word >> (8 * j) & 255u) - 128, old, s, inv) + 128);
+  return q8_pack(b[0], b[1], b[2], b[3]);
+}
 // eight neighbouring values of T as floats (16 bytes of bf16, 32 of float)
 __device__ __forceinline__ void q8_load8(const bf16* p, float* x) {
   const bf16x8 v = __builtin_bit_cast(bf16x8, ld16(p));
@@ -106,7 +144,6 @@ __device__ __forceinline__ void q8_store4(bf16* p, const float* x) {
 __device__ __forceinline__ void q8_store4(float* p, const float* x) {
   *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
 }
-__device__ __forceinline__ uint32_t q8_byte(int code) { return (uint32_t)(code + 128); }
 __device__ __forceinline__ int q8_code_of(uint32_t word, int byte) { return (int)((word >> (8 * byte)) & 255u) - 128; }
 #endif
 

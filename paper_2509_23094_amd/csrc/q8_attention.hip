@@ -14,6 +14,10 @@
 // The head average has a pass of its own over the scores, from the same fp16 q and the final (maximum, sum) of every row.
 #include <algorithm>
 #include <cmath>
+#ifdef Q8_DEV
+#include <cstdio>
+#include <cstdlib>
+#endif
 
 #include "q8.h"
 
@@ -131,6 +135,60 @@ __device__ __forceinline__ void load_v(const uint8_t* v, u32x4 (&raw)[8]) {
   }
 }
 
+// Scores of a block (`left` of its keys exist) -> probabilities in operand order.  o and l are relative to 2^ref; ref is raised only where
+// a score passes it by more than kSlack.
+template <int QP, int DT>
+__device__ __forceinline__ void softmax_step(f32x16 (&x)[2], float ks, int left, float& ref, float& l, f32x16 (&o)[DT], h8 (&p)[QP][4]) {
+  const int g = (threadIdx.x & 63) >> 5;
+  float top = -3.4e38f;
+  if (left >= kQ8Rows) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, x[t][i]);
+  } else {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (32 * t + 8 * (i / 4) + 4 * g + i % 4 < left) top = fmaxf(top, x[t][i]);
+  }
+  top = fmaxf(top, __shfl_xor(top, 32, 64)) * ks;
+  if (__any(top > ref + kSlack)) {
+    const float to = top > ref + kSlack ? top : ref, alpha = exp2_hw(ref - to);
+    ref = to;
+    l *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
+  }
+  const float base = kPBits - ref;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[t][i] = exp2_hw(fmaf(x[t][i], ks, base));
+  if (left < kQ8Rows) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (32 * t + 8 * (i / 4) + 4 * g + i % 4 >= left) x[t][i] = 0.f;
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      sum += x[t][i];
+      const _Float16 hi = (_Float16)x[t][i];
+      p[0][2 * t + i / 8][i % 8] = hi;
+      if constexpr (QP > 1) p[1][2 * t + i / 8][i % 8] = (_Float16)(x[t][i] - (float)hi);
+    }
+  l += sum;
+}
+
+// One tile of rows per workgroup: its waves take blocks in turn, operands straight from memory.
 template <typename T, int D>
 __global__ __launch_bounds__(64 * kWaves) void q8_attend_kernel(AttendArgs args) {
   constexpr int QP = sizeof(T) == 2 ? 1 : 2;      // fp16 pieces of q and of a probability
@@ -176,9 +234,9 @@ __global__ __launch_bounds__(64 * kWaves) void q8_attend_kernel(AttendArgs args)
       for (int f = 0; f < D / 16; ++f) *reinterpret_cast<h8*>(to + (size_t)(p * (D / 16) + f) * 512) = q[p][f];
   }
 
-  // o and l are relative to 2^ref; ref is raised only where a score passes it by more than kSlack
   f32x16 o[DT] = {};
   float ref = -INFINITY, l = 0.f;
+  if (wave & 4) __builtin_amdgcn_s_setprio(2);
   for (int b = b0 + wave; b < b1; b += kWaves) {
     if (QP > 1) want_k(b);
     const float ks = ks_next * factor;
@@ -186,54 +244,8 @@ __global__ __launch_bounds__(64 * kWaves) void q8_attend_kernel(AttendArgs args)
     x[0] = scores<D, QP>(kr[0], q);
     x[1] = scores<D, QP>(kr[1], q);
     if (QP == 1) want_k(b + kWaves);
-    const int left = s.L - b * kQ8Rows;    // keys of this block that exist
-    float top = -3.4e38f;
-    if (left >= kQ8Rows) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, x[t][i]);
-    } else {
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (32 * t + 8 * (i / 4) + 4 * g + i % 4 < left) top = fmaxf(top, x[t][i]);
-    }
-    top = fmaxf(top, __shfl_xor(top, 32, 64)) * ks;
-    if (__any(top > ref + kSlack)) {
-      const float to = top > ref + kSlack ? top : ref, alpha = exp2_hw(ref - to);
-      ref = to;
-      l *= alpha;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
-    }
-    const float base = kPBits - ref;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[t][i] = exp2_hw(fmaf(x[t][i], ks, base));
-    if (left < kQ8Rows) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (32 * t + 8 * (i / 4) + 4 * g + i % 4 >= left) x[t][i] = 0.f;
-    }
     h8 p[QP][4];
-    float sum = 0.f;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sum += x[t][i];
-        const _Float16 hi = (_Float16)x[t][i];
-        p[0][2 * t + i / 8][i % 8] = hi;
-        if constexpr (QP > 1) p[1][2 * t + i / 8][i % 8] = (_Float16)(x[t][i] - (float)hi);
-      }
-    l += sum;
+    softmax_step<QP, DT>(x, ks, s.L - b * kQ8Rows, ref, l, o, p);
     const float vs = vs_next;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
@@ -353,40 +365,55 @@ __global__ __launch_bounds__(kJoin * D / 4) void q8_join_kernel(AttendArgs args)
   if (s.avg && t == 0) args.row[slot].y = ref + log2f(sum) - kPBits;
 }
 
-// attn_avg of 32 rows x one block of keys: the four waves take the heads in turn and are added up at the end.
+// attn_avg of 32 rows x one block of keys: the waves take a run of heads each and are added up at the end.  The next head's keys and
+// queries are on their way while one head's are used.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void q8_average_kernel(AttendArgs args) {
+__global__ __launch_bounds__(64 * kWaves) void q8_average_kernel(AttendArgs args) {
   constexpr int QP = sizeof(T) == 2 ? 1 : 2;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
   int si = 0;
   while (si + 1 < args.n && (int)blockIdx.x >= args.s[si + 1].avg_first_wg) ++si;
   const AttendSeq& s = args.s[si];
   const int n_blocks = (s.L + kQ8Rows - 1) / kQ8Rows, local = blockIdx.x - s.avg_first_wg;
-  const int b = local % n_blocks, tile = local / n_blocks, row = tile * kTile + r32, G = args.H / args.Hkv;
-  const int per = (args.H + 3) / 4, h0 = wave * per, h1 = min(args.H, h0 + per);
+  const int b = local % n_blocks, tile = local / n_blocks, row = min(tile * kTile + r32, s.m - 1), G = args.H / args.Hkv;
+  const int h0 = wave * args.H / kWaves, h1 = (wave + 1) * args.H / kWaves;
   f32x16 acc[2] = {};
-  for (int h = h0; h < h1; ++h) {
+  u32x4 kr[2][D / 32];
+  h8 q[QP][D / 16];
+  float2 rw = {};
+  float ks = 0.f;
+  auto want_k = [&](int h) __attribute__((always_inline)) {
     const size_t blk = (size_t)b * args.Hkv + h / G;
-    const uint8_t* k = s.c.k + blk * kQ8Rows * D;
-    u32x4 kr[2][D / 32];
-    load_k<D>(k, r32, kr[0]);
-    load_k<D>(k, 32 + r32, kr[1]);
-    h8 q[QP][D / 16];
+    load_k<D>(s.c.k + blk * kQ8Rows * D, r32, kr[0]);
+    load_k<D>(s.c.k + blk * kQ8Rows * D, 32 + r32, kr[1]);
+    ks = s.c.ks[blk];
+  };
+  auto want_q = [&](int h) __attribute__((always_inline)) {
     const _Float16* from = args.q16 + s.q16 + (((size_t)h * s.avg_tiles + tile) * (QP * D / 16) * 64 + lane) * 8;
 #pragma unroll
     for (int p = 0; p < QP; ++p)
 #pragma unroll
       for (int f = 0; f < D / 16; ++f) q[p][f] = __builtin_bit_cast(h8, ld16(from + (size_t)(p * (D / 16) + f) * 512));
-    const float2 rw = row < s.m ? args.row[(size_t)s.row0 + (size_t)row * args.H + h] : make_float2(0.f, 0.f);
-    const float ks = s.c.ks[blk] * rw.x;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const f32x16 x = scores<D, QP>(kr[t], q);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[t][i] += exp2_hw(x[i] * ks - rw.y);
-    }
+    rw = args.row[(size_t)s.row0 + (size_t)row * args.H + h];
+  };
+  if (h0 < h1) {
+    want_k(h0);
+    want_q(h0);
   }
-  __shared__ float lds[4][kTile][kQ8Rows + 1];
+  for (int h = h0; h < h1; ++h) {
+    const float c = ks * rw.x, base = -rw.y;
+    f32x16 x[2];
+    x[0] = scores<D, QP>(kr[0], q);
+    x[1] = scores<D, QP>(kr[1], q);
+    const int next = min(h + 1, h1 - 1);
+    want_k(next);
+    want_q(next);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[t][i] += exp2_hw(fmaf(x[t][i], c, base));
+  }
+  __shared__ float lds[kWaves][kTile][kQ8Rows + 1];
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -396,21 +423,27 @@ __global__ __launch_bounds__(256) void q8_average_kernel(AttendArgs args) {
   if (key >= s.L) return;
   const float inv = 1.f / args.H;
 #pragma unroll
-  for (int i = 0; i < kTile / 4; ++i) {
-    const int rr = 4 * i + wave, at = tile * kTile + rr;
-    if (at < s.m) s.avg[(size_t)at * s.L + key] = ((lds[0][rr][lane] + lds[1][rr][lane]) + (lds[2][rr][lane] + lds[3][rr][lane])) * inv;
+  for (int i = 0; i < kTile / kWaves; ++i) {
+    const int rr = kWaves * i + wave, at = tile * kTile + rr;
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) sum += lds[w][rr][lane];
+    if (at < s.m) s.avg[(size_t)at * s.L + key] = sum * inv;
   }
 }
 
-// Workgroups over the keys.  A wave takes about 1.2 us for a block beside another on its SIMD, a workgroup 3 us at its ends, a split row
-// 4 us and its way to memory and back; a compute unit holds one workgroup.
+// Workgroups over the keys, by an estimate of the time in us: a compute unit holds one workgroup, a round over eight blocks takes it about
+// 2.6, its ends 5; a split row takes a launch of 4 and its way to memory and back.
 constexpr int kTargetWgs = 512;
-int plan_splits(int workgroups, int n_blocks) {
+int plan_splits(int workgroups, int most_blocks) {
+#ifdef Q8_DEV
+  if (const char* f = getenv("Q8_ATT")) return atoi(f);
+#endif
   int best = 1;
   float best_cost = 1e30f;
-  for (int s = 1; s <= 64 && (s == 1 || (s * workgroups <= kTargetWgs && s * kWaves < 2 * n_blocks)); ++s) {
-    const int per = (n_blocks + s - 1) / s;
-    const float cost = (s * workgroups + 255) / 256 * ((per + kWaves - 1) / kWaves * 1.2f + 3.f) + (s > 1 ? 4.f + s * workgroups * 0.008f : 0.f);
+  for (int s = 1; s <= 64 && (s == 1 || (s * workgroups <= kTargetWgs && s * kWaves < 2 * most_blocks)); ++s) {
+    const int rounds = ((most_blocks + s - 1) / s + kWaves - 1) / kWaves;
+    const float cost = (s * workgroups + 255) / 256 * (rounds * 2.6f + 5.f) + (s > 1 ? 4.f + s * workgroups * 0.008f : 0.f);
     if (cost < best_cost) { best_cost = cost; best = s; }
   }
   return best;
@@ -441,7 +474,7 @@ hipError_t run(const AttendArgs& a, int wgs, int avg_wgs, bool join, hipStream_t
     e = hipGetLastError();
   }
   if (e == hipSuccess && avg_wgs) {
-    q8_average_kernel<T, D><<<avg_wgs, 256, 0, st>>>(a);
+    q8_average_kernel<T, D><<<avg_wgs, 64 * kWaves, 0, st>>>(a);
     e = hipGetLastError();
   }
   return e;
@@ -463,16 +496,20 @@ hipError_t launch_q8_attention(const Q8Shape& s, const Q8Attend* calls, int n, i
     a.ml = (float2*)((char*)ws + l.ml);
     a.row = (float2*)((char*)ws + l.row);
     a.q16 = (_Float16*)((char*)ws + l.q16);
-    int base = 0, wgs = 0, avg_wgs = 0;
+    int base = 0, most = 0, wgs = 0, avg_wgs = 0;
     size_t rows = 0;
     bool join = false;
-    for (int i = 0; i < a.n; ++i) base += row_tiles(s, calls[c0 + i].m) * s.Hkv;
+    for (int i = 0; i < a.n; ++i) {
+      base += row_tiles(s, calls[c0 + i].m) * s.Hkv;
+      most = std::max(most, q8_blocks(calls[c0 + i].L));
+    }
+    const int splits = plan_splits(base, most);
     for (int i = 0; i < a.n; ++i) {
       const Q8Attend& c = calls[c0 + i];
       AttendSeq& q = a.s[i];
       const int nb = q8_blocks(c.L);
       q.c = c.cache; q.q = c.q; q.out = c.out; q.avg = c.avg; q.m = c.m; q.L = c.L;
-      q.splits = plan_splits(base, nb);
+      q.splits = std::min(splits, nb);
       q.per_split = (nb + q.splits - 1) / q.splits;
       q.splits = (nb + q.per_split - 1) / q.per_split;      // none empty
       q.first_wg = wgs;

@@ -1,6 +1,7 @@
 // The 8-bit K/V cache apart from its attention: refreshed rows in, rows out as values, attention weight summed, rows kept and
 // the cache compacted.  All of it moves bytes: one pass over the codes and rows concerned, 16 bytes per access.
 #include <algorithm>
+#include <type_traits>
 
 #include "q8.h"
 
@@ -90,32 +91,42 @@ __global__ __launch_bounds__(256) void q8_update_kernel(UpdateArgs args, int Hkv
   float* scale = (is_v ? c.cache.vs : c.cache.ks) + (size_t)b * Hkv + h;
   const float s_old = *scale;
 
+  // (rows that are not there are read as the first one and set to 0: loads under a condition would come one after the other)
   float x[P::kPerThread][16];
-  float amax = 0.f;
 #pragma unroll
   for (int i = 0; i < P::kPerThread; ++i) {
     const int p = tid + 256 * i;
     if (is_v) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int r = row_of[P::v_row(p) + j];
-        if (r >= 0) q8_load4(rows + r * pitch + P::v_dim(p), &x[i][4 * j]);
-        else x[i][4 * j] = x[i][4 * j + 1] = x[i][4 * j + 2] = x[i][4 * j + 3] = 0.f;
+        float y[4];
+        q8_load4(rows + max(row_of[P::v_row(p) + j], 0) * pitch + P::v_dim(p), y);
+#pragma unroll
+        for (int d = 0; d < 4; ++d) x[i][4 * d + j] = y[d];                  // in the order of the piece's bytes
       }
     } else {
-      const int r = row_of[P::k_row(p)];
-      if (r >= 0) {
-        q8_load8(rows + r * pitch + P::k_dim(p), &x[i][0]);
-        q8_load8(rows + r * pitch + P::k_dim(p) + 8, &x[i][8]);
-      } else {
+      const T* from = rows + max(row_of[P::k_row(p)], 0) * pitch + P::k_dim(p);
+      float y[8];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) x[i][j] = 0.f;
+      for (int h = 0; h < 2; ++h) {
+        q8_load8(from + 8 * h, y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[i][8 * h + j] = y[j];
       }
     }
+  }
+  // which rows of a piece are new: V its four rows, K all four bits alike
+  uint32_t is_new[P::kPerThread];
+  float amax = 0.f;
+#pragma unroll
+  for (int i = 0; i < P::kPerThread; ++i) {
+    const int p = tid + 256 * i;
+    is_new[i] = is_v ? (uint32_t)(fresh >> P::v_row(p)) & 15u : (fresh >> P::k_row(p) & 1) ? 15u : 0u;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
+      if (!(is_new[i] >> (j & 3) & 1u)) x[i][j] = 0.f;
       const float a = fabsf(x[i][j]);
-      if (a <= 3.402823466e38f) amax = fmaxf(amax, a);
+      amax = fmaxf(amax, a <= 3.402823466e38f ? a : 0.f);
     }
   }
   amax = wave_max(amax);
@@ -125,47 +136,24 @@ __global__ __launch_bounds__(256) void q8_update_kernel(UpdateArgs args, int Hkv
   const float want = q8_scale(amax);
   const float s = whole ? want : want > s_old ? fmaxf(want, s_old * 1.25f) : s_old;
   const bool moved = !whole && s != s_old;
-  const float inv = q8_inverse(s);
+  const float inv = q8_inverse(s), ratio = s_old * inv;
 #pragma unroll
   for (int i = 0; i < P::kPerThread; ++i) {
     const int p = tid + 256 * i;
-    if (is_v) {
-      const int t = P::v_row(p);
-      const uint32_t f4 = (uint32_t)(fresh >> t) & 15u;
-      if (f4 == 0 && !moved) continue;
-      u32x4 w = {0, 0, 0, 0};
-      u32x4* at = reinterpret_cast<u32x4*>(codes + P::v_at(p));
-      if (f4 != 15u) w = *at;
+    if (is_new[i] == 0 && !moved) continue;
+    u32x4* at = reinterpret_cast<u32x4*>(codes + (is_v ? P::v_at(p) : P::k_at(p)));
+    u32x4 w = {0, 0, 0, 0};
+    if (is_new[i] != 15u) w = *at;
+    uint32_t byte[16];
+    q8_bytes16(x[i], s, inv, byte);
+    const uint32_t keep = (is_new[i] & 1u ? 0u : 0xffu) | (is_new[i] & 2u ? 0u : 0xff00u) | (is_new[i] & 4u ? 0u : 0xff0000u) | (is_new[i] & 8u ? 0u : 0xff000000u);
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        uint32_t word = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int old = q8_code_of(w[d], j);
-          const int code = (f4 >> j & 1u) ? q8_code(x[i][4 * j + d], s, inv) : moved ? q8_recode(old, s_old, s, inv) : old;
-          word |= q8_byte(code) << (8 * j);
-        }
-        w[d] = word;
-      }
-      *at = w;
-    } else {
-      const bool is_new = fresh >> P::k_row(p) & 1;
-      if (!is_new && !moved) continue;
-      u32x4 w = {0, 0, 0, 0};
-      u32x4* at = reinterpret_cast<u32x4*>(codes + P::k_at(p));
-      if (!is_new) w = *at;
-#pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        uint32_t word = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int code = is_new ? q8_code(x[i][4 * d + j], s, inv) : q8_recode(q8_code_of(w[d], j), s_old, s, inv);
-          word |= q8_byte(code) << (8 * j);
-        }
-        w[d] = word;
-      }
-      *at = w;
+    for (int d = 0; d < 4; ++d) {
+      uint32_t old = w[d];
+      if (moved) old = q8_reword(old, s_old, s, inv, ratio);
+      w[d] = (q8_pack(byte[4 * d], byte[4 * d + 1], byte[4 * d + 2], byte[4 * d + 3]) & ~keep) | (old & keep);
     }
+    *at = w;
   }
   if (tid == 0 && s != s_old) *scale = s;      // every thread has read the old one before the barrier above
 }
@@ -252,7 +240,7 @@ __device__ __forceinline__ unsigned long long wg_scan(unsigned long long v, unsi
 // The chosen class's n-th largest weight is found digit by digit (11 bits, from the highest bit in which its weights differ), with a
 // histogram in LDS and an early end when a digit's rows all stay.  Then the kept positions are numbered in order.
 // What bounds it: a chain of barriers and LDS atomics per digit; the other compute units idle.
-template <int PER>
+template <int PER, bool PROTECT>
 __global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* weight, const uint8_t* protect, int L, int n_keep,
                                                               int32_t* kept, int64_t* kept_weight) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -261,13 +249,16 @@ __global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* we
   __shared__ int found_bin;
   __shared__ uint32_t found_above, found_in;
   unsigned long long reg[PER ? PER : 1];                // weight, top bit: protected
+  // (read at a place inside where there is none: loads under a condition would come one after the other)
   auto load = [&](int i) -> unsigned long long {
+    i = min(i, L - 1);
     const int64_t w = weight[i];
-    return (w < 0 ? 0ull : (unsigned long long)w) | (protect && protect[i] ? 1ull << 63 : 0ull);
+    const bool p = PROTECT && protect[i] != 0;
+    return (w < 0 ? 0ull : (unsigned long long)w) | (p ? 1ull << 63 : 0ull);
   };
   if constexpr (PER > 0) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) reg[i] = tid + 1024 * i < L ? load(tid + 1024 * i) : 0ull;
+    for (int i = 0; i < PER; ++i) reg[i] = load(tid + 1024 * i);
   }
   auto each = [&](auto f) {                             // f(key) for this thread's positions
     if constexpr (PER > 0) {
@@ -280,7 +271,7 @@ __global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* we
   };
   constexpr unsigned long long kTop = 1ull << 63;
   unsigned long long n_prot = 0, total;
-  if (protect) {
+  if (PROTECT) {
     each([&](unsigned long long k) { n_prot += k >> 63; });
     wg_scan(n_prot, scratch, &total);
     n_prot = total;
@@ -334,7 +325,7 @@ __global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* we
   for (int c0 = 0; c0 < L; c0 += kKeepChunk) {
     const int n_j = min(64, (L - c0 + kKeepThreads - 1) / kKeepThreads);
     auto key_at = [&](int j, int i) -> unsigned long long {
-      if constexpr (PER > 0) { (void)i; return reg[j]; } else { (void)j; return i < L ? load(i) : 0ull; }
+      if constexpr (PER > 0) { (void)i; return reg[j]; } else { (void)j; return load(i); }
     };
     auto pass = [&](auto f) {
       if constexpr (PER > 0) {
@@ -392,48 +383,48 @@ __global__ __launch_bounds__(256) void q8_compact_kernel(Q8CachePtr src, const i
   }
   __syncthreads();
   const float s = wave_max(scale_of[tid & 63]), inv = q8_inverse(s);
+  // (places past the last are read as the first row and set to code 0)
   uint8_t* out = (is_v ? dst.v : dst.k) + ((size_t)b * Hkv + h) * kQ8Rows * D;
 #pragma unroll
   for (int i = 0; i < P::kPerThread; ++i) {
     const int p = tid + 256 * i;
+    u32x4 r;
     if (is_v) {
       u32x4 w[4];
+      float old[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int pos = from[P::v_row(p) + j];
-        w[j] = u32x4{0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
-        if (pos >= 0)
-          w[j] = ld16(codes + ((size_t)(pos / kQ8Rows) * Hkv + h) * kQ8Rows * D + pos % kQ8Rows / 4 * 4 * D + P::v_dim(p) * 4);
+        const int pos = max(from[P::v_row(p) + j], 0);
+        old[j] = scale_of[P::v_row(p) + j];
+        w[j] = ld16(codes + ((size_t)(pos / kQ8Rows) * Hkv + h) * kQ8Rows * D + pos % kQ8Rows / 4 * 4 * D + P::v_dim(p) * 4);
       }
-      u32x4 r = {0, 0, 0, 0};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int t = P::v_row(p) + j, byte = from[t] & 3;
-        const float old = scale_of[t];
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          int code = q8_code_of(w[j][d], byte);
-          if (old != s) code = q8_recode(code, old, s, inv);
-          r[d] |= q8_byte(code) << (8 * j);
-        }
+        const int t = P::v_row(p) + j;
+        // the row's bytes of its four words, as one word
+        const uint32_t sel = 0x0c0c0000u | (from[t] & 3) | (4 + (from[t] & 3)) << 8;
+        uint32_t x = __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[j][3], w[j][2], sel), __builtin_amdgcn_perm(w[j][1], w[j][0], sel), 0x05040100u);
+        if (old[j] != s) x = q8_reword(x, old[j], s, inv, old[j] * inv);
+        if (from[t] < 0) x = 0x80808080u;
+        w[j][0] = x;
       }
+      // four rows of four dimensions -> four dimensions of four rows
+      const uint32_t lo0 = __builtin_amdgcn_perm(w[1][0], w[0][0], 0x05010400u), lo1 = __builtin_amdgcn_perm(w[1][0], w[0][0], 0x07030602u);
+      const uint32_t hi0 = __builtin_amdgcn_perm(w[3][0], w[2][0], 0x05010400u), hi1 = __builtin_amdgcn_perm(w[3][0], w[2][0], 0x07030602u);
+      r[0] = __builtin_amdgcn_perm(hi0, lo0, 0x05040100u);
+      r[1] = __builtin_amdgcn_perm(hi0, lo0, 0x07060302u);
+      r[2] = __builtin_amdgcn_perm(hi1, lo1, 0x05040100u);
+      r[3] = __builtin_amdgcn_perm(hi1, lo1, 0x07060302u);
       *reinterpret_cast<u32x4*>(out + P::v_at(p)) = r;
     } else {
-      const int t = P::k_row(p), pos = from[t];
-      u32x4 w = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
-      if (pos >= 0)
-        w = ld16(codes + ((size_t)(pos / kQ8Rows) * Hkv + h) * kQ8Rows * D + P::k_dim(p) * kQ8Rows + pos % kQ8Rows * 16);
-      const float old = scale_of[t];
-      if (old != s) {
+      const int t = P::k_row(p), pos = max(from[t], 0);
+      r = ld16(codes + ((size_t)(pos / kQ8Rows) * Hkv + h) * kQ8Rows * D + P::k_dim(p) * kQ8Rows + pos % kQ8Rows * 16);
+      const float old = scale_of[t], ratio = old * inv;
+      if (old != s)
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          uint32_t word = 0;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) word |= q8_byte(q8_recode(q8_code_of(w[d], j), old, s, inv)) << (8 * j);
-          w[d] = word;
-        }
-      }
-      *reinterpret_cast<u32x4*>(out + P::k_at(p)) = w;
+        for (int d = 0; d < 4; ++d) r[d] = q8_reword(r[d], old, s, inv, ratio);
+      if (from[t] < 0) r = u32x4{0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
+      *reinterpret_cast<u32x4*>(out + P::k_at(p)) = r;
     }
   }
   if (tid == 0) (is_v ? dst.vs : dst.ks)[(size_t)b * Hkv + h] = s;
@@ -489,11 +480,14 @@ hipError_t launch_q8_weigh(const float* avg, int m, int L, int64_t* weight, hipS
 hipError_t launch_q8_keep(const int64_t* weight, const uint8_t* protect, int L, int n_keep, int32_t* kept, int64_t* kept_weight,
                           hipStream_t st) {
   const int per = (L + kKeepThreads - 1) / kKeepThreads;
-  if (per <= 4) q8_keep_kernel<4><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
-  else if (per <= 8) q8_keep_kernel<8><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
-  else if (per <= 20) q8_keep_kernel<20><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
-  else q8_keep_kernel<0><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
-  return hipGetLastError();
+  auto go = [&](auto prot) {
+    constexpr bool P = decltype(prot)::value;
+    if (per <= 4) q8_keep_kernel<4, P><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
+    else if (per <= 20) q8_keep_kernel<20, P><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
+    else q8_keep_kernel<0, P><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
+    return hipGetLastError();
+  };
+  return protect ? go(std::true_type{}) : go(std::false_type{});
 }
 
 hipError_t launch_q8_compact(const Q8Shape& s, const Q8CachePtr& src, const int32_t* kept, int n, const Q8CachePtr& dst,
