@@ -115,8 +115,8 @@ int d2c_q8_weigh(d2c_q8* ctx, const float* attn_avg, int32_t m, int32_t L, int64
 /* Keeps n_keep of the L rows of a cache: those of largest weight (negative ones count as 0), ties to the lowest index; rows
  * with protect[j] != 0 (protect may be NULL) come before all others.  kept [n_keep] out: their positions, ascending.
  * Row i of dst is row kept[i] of src: a block of dst has the largest scale its rows had, codes of rows with another scale
- * become code(code * old, new).  kept_weight [n_keep] out (may be NULL): weight[kept].  dst holds ceil(n_keep / 64) blocks
- * and must not overlap src. */
+ * become code(code * old, new).  kept_weight [n_keep] out (may be NULL): weight[kept], negative ones as 0.  dst holds
+ * ceil(n_keep / 64) blocks and must not overlap src. */
 int d2c_q8_evict(d2c_q8* ctx, const d2c_q8_cache* src, int32_t L, const int64_t* weight, const uint8_t* protect,
                  int32_t n_keep, const d2c_q8_cache* dst, int32_t* kept, int64_t* kept_weight, void* stream);
 

@@ -387,7 +387,7 @@ def _checked(t: Optional[torch.Tensor], what: str, dtype: torch.dtype, shape, de
     """The pointer of a tensor that has to have this type and shape: a call must not read past it."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.get_device() != device:
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
         raise D2CError(D2C_EINVAL, "%s: contiguous %s of shape %s on device %d expected, got %s %s on %s"
                        % (what, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
     return t.data_ptr()

@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void q8_update_kernel(UpdateArgs args, int Hkv
   const Q8Update c = args.c[blockIdx.z];
   const int h = blockIdx.y >> 1, is_v = blockIdx.y & 1, tid = threadIdx.x, slot = blockIdx.x;
   const int n_blocks = (c.L + kQ8Rows - 1) / kQ8Rows;
-  __shared__ int row_of[kQ8Rows];
+  __shared__ int row_of[kQ8Rows], near[kQ8Rows + 1];
   __shared__ float wave_amax[4];
   int b;
   if (tid < kQ8Rows) row_of[tid] = -1;
@@ -61,20 +61,22 @@ __global__ __launch_bounds__(256) void q8_update_kernel(UpdateArgs args, int Hkv
     if (tid < kQ8Rows && pos >= first && pos < c.L) row_of[tid] = pos - first;
   } else {
     int lo = slot;
-    if (c.m < n_blocks) {                       // a slot is a row
+    if (c.m < n_blocks) {                       // a slot is a row; near: its index behind the one before
       if (slot >= c.m) return;
-      const int pos = c.idx[slot];
+      if (tid <= kQ8Rows) near[tid] = c.idx[min(max(slot - 1 + tid, 0), c.m - 1)];
+      __syncthreads();
+      const int pos = near[1];
       if (pos < 0 || pos >= c.L) return;
       b = pos / kQ8Rows;
-      if (slot > 0 && (c.idx[slot - 1] >> 6) == b) return;
-      __syncthreads();
+      if (slot > 0 && (near[0] >> 6) == b) return;
     } else {                                    // a slot is a block
       b = slot;
       if (b >= n_blocks) return;
       lo = lower_bound_wide(c.idx, c.m, b * kQ8Rows);
+      if (tid < kQ8Rows) near[1 + tid] = c.idx[min(lo + tid, c.m - 1)];        // (read by the thread that wrote it)
     }
     if (tid < kQ8Rows && lo + tid < c.m) {
-      const int pos = c.idx[lo + tid];
+      const int pos = near[1 + tid];
       if (pos >= 0 && pos < c.L && pos / kQ8Rows == b) atomicMax(&row_of[pos % kQ8Rows], lo + tid);
     }
   }
@@ -115,13 +117,19 @@ __global__ __launch_bounds__(256) void q8_update_kernel(UpdateArgs args, int Hkv
       }
     }
   }
-  // which rows of a piece are new: V its four rows, K all four bits alike
+  // which rows of a piece are new: V its four rows, K all four bits alike; a V piece that stays in part is read now
   uint32_t is_new[P::kPerThread];
+  u32x4 was[P::kPerThread];
   float amax = 0.f;
 #pragma unroll
   for (int i = 0; i < P::kPerThread; ++i) {
     const int p = tid + 256 * i;
     is_new[i] = is_v ? (uint32_t)(fresh >> P::v_row(p)) & 15u : (fresh >> P::k_row(p) & 1) ? 15u : 0u;
+    was[i] = u32x4{0, 0, 0, 0};
+    if (is_new[i] != 0 && is_new[i] != 15u) was[i] = ld16(codes + P::v_at(p));
+  }
+#pragma unroll
+  for (int i = 0; i < P::kPerThread; ++i) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
       if (!(is_new[i] >> (j & 3) & 1u)) x[i][j] = 0.f;
@@ -142,8 +150,8 @@ __global__ __launch_bounds__(256) void q8_update_kernel(UpdateArgs args, int Hkv
     const int p = tid + 256 * i;
     if (is_new[i] == 0 && !moved) continue;
     u32x4* at = reinterpret_cast<u32x4*>(codes + (is_v ? P::v_at(p) : P::k_at(p)));
-    u32x4 w = {0, 0, 0, 0};
-    if (is_new[i] != 15u) w = *at;
+    u32x4 w = was[i];
+    if (is_new[i] == 0) w = *at;
     uint32_t byte[16];
     q8_bytes16(x[i], s, inv, byte);
     const uint32_t keep = (is_new[i] & 1u ? 0u : 0xffu) | (is_new[i] & 2u ? 0u : 0xff00u) | (is_new[i] & 4u ? 0u : 0xff0000u) | (is_new[i] & 8u ? 0u : 0xff000000u);
@@ -210,161 +218,140 @@ __global__ __launch_bounds__(256) void q8_weigh_kernel(const float* avg, int m, 
 }
 
 // ---- the rows to keep: one workgroup of 16 waves
-constexpr int kKeepThreads = 1024;
-constexpr int kKeepChunk = 64 * kKeepThreads;      // positions numbered at once: 64 per thread
+constexpr int kKeepWaves = 16, kKeepThreads = 64 * kKeepWaves;
 
-// exclusive sum over the workgroup's threads of v, and the total; scratch: 16 values
-__device__ __forceinline__ unsigned long long wg_scan(unsigned long long v, unsigned long long* scratch, unsigned long long* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  unsigned long long s = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const unsigned long long t = __shfl_up(s, o, 64);
-    if (lane >= o) s += t;
-  }
-  __syncthreads();
-  if (lane == 63) scratch[wave] = s;
-  __syncthreads();
-  unsigned long long before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kKeepThreads / 64; ++w) {
-    if (w < wave) before += scratch[w];
-    all += scratch[w];
-  }
-  *total = all;
-  return before + s - v;
-}
-
-// Thread t holds positions t + 1024 i, in registers where there are at most PER of them (PER = 0: read again for each pass).  The
-// protected rows fill up first: if they are more than n_keep the choice is among them, else all of them stay and it is among the others.
-// The chosen class's n-th largest weight is found digit by digit (11 bits, from the highest bit in which its weights differ), with a
-// histogram in LDS and an early end when a digit's rows all stay.  Then the kept positions are numbered in order.
-// What bounds it: a chain of barriers and LDS atomics per digit; the other compute units idle.
+// Wave w takes a run of positions, lane by lane; in registers where that is at most PER rounds of it (PER = 0: read again for each pass).
+// The protected rows fill up first: if they are n_keep or more the choice is among them, else all of them stay and it is among the others.
+// The chosen class's n-th largest weight is found digit by digit (11 bits, from its highest bit on), with a histogram in LDS and an early
+// end when a digit's rows all stay.  Then each wave numbers its kept positions behind those of the waves before.
+// What bounds it: a chain of barriers and LDS atomics per digit in one compute unit; 767 rows XXX us, 20001 XXX.
 template <int PER, bool PROTECT>
 __global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* weight, const uint8_t* protect, int L, int n_keep,
                                                               int32_t* kept, int64_t* kept_weight) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  __shared__ uint32_t hist[2048];
-  __shared__ unsigned long long scratch[16], red[2][16], counts[1024];
-  __shared__ int found_bin;
-  __shared__ uint32_t found_above, found_in;
+  constexpr unsigned long long kTop = 1ull << 63;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rounds = ((L + kKeepWaves - 1) / kKeepWaves + 63) / 64, first = wave * rounds * 64 + lane;
+  __shared__ uint32_t hist[2][2048], wave_sum[kKeepWaves], wave_bits[kKeepWaves], wave_up[kKeepWaves], wave_eq[kKeepWaves];
+  __shared__ uint32_t found_bin, found_above, found_in;
   unsigned long long reg[PER ? PER : 1];                // weight, top bit: protected
-  // (read at a place inside where there is none: loads under a condition would come one after the other)
-  auto load = [&](int i) -> unsigned long long {
-    i = min(i, L - 1);
-    const int64_t w = weight[i];
-    const bool p = PROTECT && protect[i] != 0;
-    return (w < 0 ? 0ull : (unsigned long long)w) | (p ? 1ull << 63 : 0ull);
+  // (through buffers that end with the arrays, which answer 0 past them: loads under a condition would come one after the other)
+  const __amdgpu_buffer_rsrc_t w_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int64_t*>(weight), 0, L * 8, 0x00020000);
+  const __amdgpu_buffer_rsrc_t p_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(protect), 0, PROTECT ? L : 0, 0x00020000);
+  auto load = [&](int j) __attribute__((always_inline)) -> unsigned long long {
+    const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(w_rsrc, first * 8, j * 512, 0);
+    uint32_t hi = (int)w[1] < 0 ? 0u : w[1], lo = (int)w[1] < 0 ? 0u : w[0];
+    if (PROTECT && __builtin_amdgcn_raw_buffer_load_b8(p_rsrc, first, j * 64, 0) != 0) hi |= 1u << 31;
+    return (unsigned long long)hi << 32 | lo;
   };
   if constexpr (PER > 0) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) reg[i] = load(tid + 1024 * i);
+    for (int j = 0; j < PER; ++j) reg[j] = load(j);
   }
-  auto each = [&](auto f) {                             // f(key) for this thread's positions
+  // f(key, whether there is one, round).  (`left` is opaque to the compiler in each pass: it would keep 20 comparisons' results for all of
+  // them, and spill.)
+  auto each = [&](auto f) __attribute__((always_inline)) {
+    int left = L - first;
+    asm volatile("" : "+v"(left));
     if constexpr (PER > 0) {
 #pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (tid + 1024 * i < L) f(reg[i]);
+      for (int j = 0; j < PER; ++j)
+        if (j < rounds) f(reg[j], 64 * j < left, j);
     } else {
-      for (int i = tid; i < L; i += kKeepThreads) f(load(i));
+      for (int j = 0; j < rounds; ++j) f(load(j), 64 * j < left, j);
     }
   };
-  constexpr unsigned long long kTop = 1ull << 63;
-  unsigned long long n_prot = 0, total;
-  if (PROTECT) {
-    each([&](unsigned long long k) { n_prot += k >> 63; });
-    wg_scan(n_prot, scratch, &total);
-    n_prot = total;
+  for (int b = tid; b < 2048; b += kKeepThreads) hist[0][b] = 0;
+  // how many are protected, and how many bits each class's weights have
+  uint32_t n_prot = 0;
+  unsigned long long any[2] = {0, 0};
+  each([&](unsigned long long k, bool valid, int) {
+    const bool p = PROTECT && valid && (k & kTop);
+    n_prot += p;
+    any[0] |= valid && !p ? k : 0ull;
+    if (PROTECT) any[1] |= p ? k & ~kTop : 0ull;
+  });
+  const uint32_t bits[2] = {(uint32_t)(any[0] ? 64 - __clzll((long long)any[0]) : 0), (uint32_t)(any[1] ? 64 - __clzll((long long)any[1]) : 0)};
+  uint32_t both = bits[0] | bits[1] << 16;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const uint32_t x = __shfl_xor(both, o, 64);
+    both = max(both & 0xffffu, x & 0xffffu) | max(both & 0xffff0000u, x & 0xffff0000u);
+    if (PROTECT) n_prot += __shfl_xor(n_prot, o, 64);
   }
-  const bool among_protected = n_prot >= (unsigned long long)n_keep;
+  if (lane == 0) { wave_sum[wave] = n_prot; wave_bits[wave] = both; }
+  __syncthreads();
+  n_prot = both = 0;
+#pragma unroll
+  for (int w = 0; w < kKeepWaves; ++w) {
+    const uint32_t x = wave_bits[w];
+    n_prot += wave_sum[w];
+    both = max(both & 0xffffu, x & 0xffffu) | max(both & 0xffff0000u, x & 0xffff0000u);
+  }
+  const bool among_protected = n_prot >= (uint32_t)n_keep;
   const unsigned long long cls = among_protected ? kTop : 0ull;                        // n_keep > 0
-  uint32_t need = among_protected ? (uint32_t)n_keep : (uint32_t)(n_keep - (int)n_prot);   // of the class `cls`
-  const uint32_t size = cls ? (uint32_t)n_prot : (uint32_t)(L - (int)n_prot);
-  // threshold: keys of the class above `thr` stay, of those equal to it (under the mask of the digits looked at) the first `need`
+  uint32_t need = among_protected ? (uint32_t)n_keep : (uint32_t)n_keep - n_prot;      // of the class `cls`
+  const uint32_t size = among_protected ? n_prot : (uint32_t)L - n_prot;
+  // keys of the class above `thr` stay, of those equal to it under the mask of the digits looked at the first `need`
   unsigned long long thr = cls, mask = kTop;
   if (need < size) {
-    unsigned long long all_or = 0, all_and = ~0ull;
-    each([&](unsigned long long k) { if ((k & kTop) == cls) { all_or |= k; all_and &= k; } });
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      all_or |= __shfl_xor(all_or, o, 64);
-      all_and &= __shfl_xor(all_and, o, 64);
-    }
-    if (lane == 0) { red[0][wave] = all_or; red[1][wave] = all_and; }
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 16; ++w) { all_or |= red[0][w]; all_and &= red[1][w]; }
-    const unsigned long long differ = all_or & ~all_and;
-    int hi = differ ? 64 - __clzll((long long)differ) : 0;     // bits hi .. 63 are common
-    mask = hi >= 64 ? 0ull : ~0ull << hi;
-    thr = all_and & mask;
-    while (hi > 0) {
-      const int lo = max(0, hi - 11), bins = 1 << (hi - lo);
-      for (int b = tid; b < 2048; b += kKeepThreads) hist[b] = 0;
-      __syncthreads();
-      each([&](unsigned long long k) { if ((k & mask) == thr) atomicAdd(&hist[(uint32_t)(k >> lo) & (bins - 1)], 1u); });
+    int hi = among_protected ? both >> 16 : both & 0xffffu;     // bits hi .. 62 are 0 throughout
+    mask = ~0ull << hi;
+    for (int pass = 0; hi > 0; ++pass) {
+      const int lo = max(0, hi - 11);
+      const uint32_t bins = 1u << (hi - lo);
+      uint32_t* h = hist[pass & 1];
+      each([&](unsigned long long k, bool valid, int) { if (valid && (k & mask) == thr) atomicAdd(&h[(uint32_t)(k >> lo) & (bins - 1)], 1u); });
+      for (int b = tid; b < 2048; b += kKeepThreads) hist[(pass & 1) ^ 1][b] = 0;
       __syncthreads();
       // thread t holds bins 2047 - 2t and below: prefix sums run from the largest digit down
-      const uint32_t a = hist[2047 - 2 * tid], c = hist[2046 - 2 * tid];
-      const uint32_t before = (uint32_t)wg_scan((unsigned long long)a + c, scratch, &total);
+      const uint32_t a = h[2047 - 2 * tid], c = h[2046 - 2 * tid];
+      uint32_t s = a + c;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t t = __shfl_up(s, o, 64);
+        if (lane >= o) s += t;
+      }
+      if (lane == 63) wave_sum[wave] = s;
+      __syncthreads();
+      uint32_t before = s - a - c;
+#pragma unroll
+      for (int w = 0; w < kKeepWaves; ++w) before += w < wave ? wave_sum[w] : 0u;
       if (before < need && before + a >= need) { found_bin = 2047 - 2 * tid; found_above = before; found_in = a; }
       else if (before + a < need && before + a + c >= need) { found_bin = 2046 - 2 * tid; found_above = before + a; found_in = c; }
       __syncthreads();
       need -= found_above;
       thr |= (unsigned long long)found_bin << lo;
-      mask = lo ? ~0ull << lo : ~0ull;
-      const bool done = need == found_in;
+      mask = ~0ull << lo;
       hi = lo;
-      __syncthreads();
-      if (done) break;
+      if (need == found_in) break;
     }
   }
-  // above: stays; equal under the mask: the first `need` stay
-  const uint32_t ties = need;
-  unsigned long long base = 0;                            // kept above in the low half, equal ones in the high half
-  for (int c0 = 0; c0 < L; c0 += kKeepChunk) {
-    const int n_j = min(64, (L - c0 + kKeepThreads - 1) / kKeepThreads);
-    auto key_at = [&](int j, int i) -> unsigned long long {
-      if constexpr (PER > 0) { (void)i; return reg[j]; } else { (void)j; return load(i); }
-    };
-    auto pass = [&](auto f) {
-      if constexpr (PER > 0) {
+  uint32_t n_up = 0, n_eq = 0;
+  each([&](unsigned long long k, bool valid, int) {
+    n_up += __popcll(__ballot(valid && (k & mask) > thr));
+    n_eq += __popcll(__ballot(valid && (k & mask) == thr));
+  });
+  if (lane == 0) { wave_up[wave] = n_up; wave_eq[wave] = n_eq; }
+  __syncthreads();
+  uint32_t up = 0, eq = 0;
 #pragma unroll
-        for (int j = 0; j < PER; ++j)
-          if (j < n_j) f(j);
-      } else {
-        for (int j = 0; j < n_j; ++j) f(j);
-      }
-    };
-    __syncthreads();
-    counts[tid] = 0;
-    __syncthreads();
-    pass([&](int j) {
-      const int i = c0 + j * kKeepThreads + tid;
-      const unsigned long long k = key_at(j, i) & mask;
-      const uint64_t up = __ballot(i < L && k > thr), eq = __ballot(i < L && k == thr);
-      if (lane == 0) counts[j * 16 + wave] = (unsigned long long)__popcll(up) | (unsigned long long)__popcll(eq) << 32;
-    });
-    __syncthreads();
-    const unsigned long long own = counts[tid], pre = wg_scan(own, scratch, &total) + base;
-    __syncthreads();
-    counts[tid] = pre;
-    __syncthreads();
-    pass([&](int j) {
-      const int i = c0 + j * kKeepThreads + tid;
-      const unsigned long long key = key_at(j, i), k = key & mask;
-      const bool is_up = i < L && k > thr, is_eq = i < L && k == thr;
-      const uint64_t up = __ballot(is_up), eq = __ballot(is_eq), below = (1ull << lane) - 1;
-      const unsigned long long p = counts[j * 16 + wave];
-      const uint32_t up_before = (uint32_t)p + (uint32_t)__popcll(up & below), eq_before = (uint32_t)(p >> 32) + (uint32_t)__popcll(eq & below);
-      if (is_up || (is_eq && eq_before < ties)) {
-        const uint32_t at = up_before + min(eq_before, ties);
-        kept[at] = i;
-        if (kept_weight) kept_weight[at] = weight[i];
-      }
-    });
-    base += total;
+  for (int w = 0; w < kKeepWaves; ++w) {
+    up += w < wave ? wave_up[w] : 0u;
+    eq += w < wave ? wave_eq[w] : 0u;
   }
+  each([&](unsigned long long key, bool valid, int j) {
+    const int i = first + 64 * j;
+    const bool is_up = valid && (key & mask) > thr, is_eq = valid && (key & mask) == thr;
+    const uint64_t u = __ballot(is_up), e = __ballot(is_eq), below = (1ull << lane) - 1;
+    const uint32_t up_at = up + __popcll(u & below), eq_at = eq + __popcll(e & below);
+    if (is_up || (is_eq && eq_at < need)) {
+      const uint32_t at = up_at + min(eq_at, need);
+      kept[at] = i;
+      if (kept_weight) kept_weight[at] = (int64_t)(key & ~kTop);
+    }
+    up += __popcll(u);
+    eq += __popcll(e);
+  });
 }
 
 // Row i of dst is row kept[i] of src.  A workgroup per (block of dst, kv head, K or V): 16 KB read (V: more, its pieces hold four rows
@@ -479,7 +466,7 @@ hipError_t launch_q8_weigh(const float* avg, int m, int L, int64_t* weight, hipS
 
 hipError_t launch_q8_keep(const int64_t* weight, const uint8_t* protect, int L, int n_keep, int32_t* kept, int64_t* kept_weight,
                           hipStream_t st) {
-  const int per = (L + kKeepThreads - 1) / kKeepThreads;
+  const int per = ((L + kKeepWaves - 1) / kKeepWaves + 63) / 64;             // rounds of a wave
   auto go = [&](auto prot) {
     constexpr bool P = decltype(prot)::value;
     if (per <= 4) q8_keep_kernel<4, P><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
