@@ -263,60 +263,50 @@ __global__ __launch_bounds__(64 * kWaves) void q8_attend_kernel(AttendArgs args)
   }
   l += __shfl_xor(l, 32, 64);
 
-  // merge the waves: half of them hand theirs to the other half, until four are left; each of these adds up a quarter of every accumulator,
-  // 16 neighbouring dimensions of a row (D = 64: 8)
-  __shared__ float lds[4][DT * 16][64];
+  // merge the waves: each adds up an eighth of every accumulator, two times D / 32 neighbouring dimensions of a row
+  __shared__ float lds[kWaves][DT * 16][64];
   __shared__ float wref[kWaves][kTile], wl[kWaves][kTile];
   if (g == 0) { wref[wave][r32] = ref; wl[wave][r32] = l; }
-  __syncthreads();
-  float M = wref[0][r32], sum = 0.f;
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) M = fmaxf(M, wref[w][r32]);
-  const float to_m = M == -INFINITY ? 0.f : M, own = exp2_hw(ref - to_m);
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) sum += wl[w][r32] * exp2_hw(wref[w][r32] - to_m);
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) o[dt][i] *= own;
-  if (wave >= 4)
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) lds[wave - 4][dt * 16 + i][lane] = o[dt][i];
+    for (int i = 0; i < 16; ++i) lds[wave][dt * 16 + i][lane] = o[dt][i];
   __syncthreads();
-  if (wave < 4)
+  if (!valid) return;
+  float M = wref[0][r32], sum = 0.f, weight[kWaves];
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+  for (int w = 1; w < kWaves; ++w) M = fmaxf(M, wref[w][r32]);
+  const float to_m = M == -INFINITY ? 0.f : M;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        o[dt][i] += lds[wave][dt * 16 + i][lane];
-        lds[wave][dt * 16 + i][lane] = o[dt][i];
-      }
-  __syncthreads();
-  if (!valid || wave >= 4) return;
-  float y[4 * DT];
+  for (int w = 0; w < kWaves; ++w) {
+    weight[w] = exp2_hw(wref[w][r32] - to_m);
+    sum += wl[w][r32] * weight[w];
+  }
+  float y[2 * DT];
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int j = 0; j < 2; ++j)
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      const int e = dt * 16 + 4 * wave + j;
-      y[j * DT + dt] = (lds[0][e][lane] + lds[1][e][lane]) + (lds[2][e][lane] + lds[3][e][lane]);
+      float t = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) t = fmaf(lds[w][dt * 16 + 2 * wave + j][lane], weight[w], t);
+      y[j * DT + dt] = t;
     }
-  const int d0 = (8 * wave + 4 * g) * DT;        // row 8 w + 4 g + j of tile dt is dimension DT * (that) + dt
+  // row 8 (wave / 2) + 4 g + 2 (wave % 2) + j of tile dt is dimension DT * (that) + dt
+  const int d0 = (wave / 2 * 8 + 4 * g + wave % 2 * 2) * DT;
   const size_t slot = (size_t)s.row0 + (size_t)row * args.H + head;
   if (s.splits > 1) {
     float* to = args.part + ((size_t)split * args.slots + slot) * D + d0;
 #pragma unroll
-    for (int j = 0; j < DT; ++j) q8_store4(to + 4 * j, y + 4 * j);
+    for (int j = 0; j < DT / 2; ++j) q8_store4(to + 4 * j, y + 4 * j);
     if (wave == 0 && g == 0) args.ml[(size_t)split * args.slots + slot] = make_float2(M, sum);
   } else {
     const float inv = 1.f / sum;
 #pragma unroll
-    for (int j = 0; j < 4 * DT; ++j) y[j] *= inv;
+    for (int j = 0; j < 2 * DT; ++j) y[j] *= inv;
     T* to = (T*)s.out + ((size_t)row * args.H + head) * D + d0;
 #pragma unroll
-    for (int j = 0; j < DT; ++j) q8_store4(to + 4 * j, y + 4 * j);
+    for (int j = 0; j < DT / 2; ++j) q8_store4(to + 4 * j, y + 4 * j);
   }
   if (s.avg && wave == 0 && g == 0 && split == 0)
     args.row[slot] = make_float2(factor, to_m + log2f(sum) - kPBits);       // (the sum of a split row: the merge puts it right)

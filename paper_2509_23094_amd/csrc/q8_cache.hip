@@ -26,6 +26,8 @@ struct UpdateArgs {
   Q8Update c[kQ8Launch];
 };
 
+constexpr int kScan = 1024;                  // so many indices are compared with a block's range each
+
 // Number of idx entries below `limit`, by all 256 threads together (idx ascending; in bounds whatever it holds).
 __device__ int lower_bound_wide(const int32_t* idx, int m, int limit) {
   const int step = (m + 255) / 256, t = threadIdx.x;
@@ -60,7 +62,6 @@ __global__ __launch_bounds__(256) void q8_update_kernel(UpdateArgs args, int Hkv
     const int pos = b * kQ8Rows + tid;
     if (tid < kQ8Rows && pos >= first && pos < c.L) row_of[tid] = pos - first;
   } else {
-    int lo = slot;
     if (c.m < n_blocks) {                       // a slot is a row; near: its index behind the one before
       if (slot >= c.m) return;
       if (tid <= kQ8Rows) near[tid] = c.idx[min(max(slot - 1 + tid, 0), c.m - 1)];
@@ -72,12 +73,22 @@ __global__ __launch_bounds__(256) void q8_update_kernel(UpdateArgs args, int Hkv
     } else {                                    // a slot is a block
       b = slot;
       if (b >= n_blocks) return;
-      lo = lower_bound_wide(c.idx, c.m, b * kQ8Rows);
-      if (tid < kQ8Rows) near[1 + tid] = c.idx[min(lo + tid, c.m - 1)];        // (read by the thread that wrote it)
     }
-    if (tid < kQ8Rows && lo + tid < c.m) {
-      const int pos = near[1 + tid];
-      if (pos >= 0 && pos < c.L && pos / kQ8Rows == b) atomicMax(&row_of[pos % kQ8Rows], lo + tid);
+    auto take = [&](int i, int pos) {
+      if (i < c.m && pos >= 0 && pos < c.L && pos / kQ8Rows == b) atomicMax(&row_of[pos % kQ8Rows], i);
+    };
+    if (c.m < n_blocks) {
+      if (tid < kQ8Rows) take(slot + tid, near[1 + tid]);
+    } else if (c.m <= kScan) {                  // looked at one and all: one latency instead of the search's three
+      int pos[kScan / 256];
+#pragma unroll
+      for (int i = 0; i < kScan / 256; ++i) pos[i] = c.idx[min(tid + 256 * i, c.m - 1)];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kScan / 256; ++i) take(tid + 256 * i, pos[i]);
+    } else {
+      const int lo = lower_bound_wide(c.idx, c.m, b * kQ8Rows);
+      if (tid < kQ8Rows) take(lo + tid, c.idx[min(lo + tid, c.m - 1)]);
     }
   }
   __syncthreads();
