@@ -101,20 +101,30 @@ __device__ __forceinline__ float load_q(const T* q, h8 (&f)[QP][D / 16]) {
   return p2;
 }
 
-// S^T of 32 keys of a block: raw[c] = 16 dimensions of this lane's key in chunk 2c + g
-template <int D, int QP>
-__device__ __forceinline__ f32x16 scores(const u32x4 (&raw)[D / 32], const h8 (&q)[QP][D / 16]) {
-  f32x16 acc = {};
+// Operands of 32 keys: raw[c] = 16 dimensions of this lane's key in chunk 2c + g
+template <int D>
+__device__ __forceinline__ void convert_k(const u32x4 (&raw)[D / 32], h8 (&k)[D / 16]) {
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) {
-    const h8 lo = codes8(raw[c][0], raw[c][1]), hi = codes8(raw[c][2], raw[c][3]);
-#pragma unroll
-    for (int p = 0; p < QP; ++p) {
-      acc = mfma(lo, q[p][2 * c], acc);
-      acc = mfma(hi, q[p][2 * c + 1], acc);
-    }
+    k[2 * c] = codes8(raw[c][0], raw[c][1]);
+    k[2 * c + 1] = codes8(raw[c][2], raw[c][3]);
   }
+}
+// S^T of 32 keys
+template <int D, int QP>
+__device__ __forceinline__ f32x16 product(const h8 (&k)[D / 16], const h8 (&q)[QP][D / 16]) {
+  f32x16 acc = {};
+#pragma unroll
+  for (int f = 0; f < D / 16; ++f)
+#pragma unroll
+    for (int p = 0; p < QP; ++p) acc = mfma(k[f], q[p][f], acc);
   return acc;
+}
+template <int D, int QP>
+__device__ __forceinline__ f32x16 scores(const u32x4 (&raw)[D / 32], const h8 (&q)[QP][D / 16]) {
+  h8 k[D / 16];
+  convert_k<D>(raw, k);
+  return product<D, QP>(k, q);
 }
 template <int D>
 __device__ __forceinline__ void load_k(const uint8_t* k, int key, u32x4 (&raw)[D / 32]) {
@@ -369,14 +379,14 @@ __global__ __launch_bounds__(64 * kWaves) void q8_average_kernel(AttendArgs args
   const int h0 = wave * args.H / kWaves, h1 = (wave + 1) * args.H / kWaves;
   f32x16 acc[2] = {};
   u32x4 kr[2][D / 32];
-  h8 q[QP][D / 16];
+  h8 k[2][D / 16], q[QP][D / 16];
   float2 rw = {};
-  float ks = 0.f;
-  auto want_k = [&](int h) __attribute__((always_inline)) {
-    const size_t blk = (size_t)b * args.Hkv + h / G;
+  float ks_next = 0.f, ks = 0.f;
+  auto want_k = [&](int hk) __attribute__((always_inline)) {
+    const size_t blk = (size_t)b * args.Hkv + hk;
     load_k<D>(s.c.k + blk * kQ8Rows * D, r32, kr[0]);
     load_k<D>(s.c.k + blk * kQ8Rows * D, 32 + r32, kr[1]);
-    ks = s.c.ks[blk];
+    ks_next = s.c.ks[blk];
   };
   auto want_q = [&](int h) __attribute__((always_inline)) {
     const _Float16* from = args.q16 + s.q16 + (((size_t)h * s.avg_tiles + tile) * (QP * D / 16) * 64 + lane) * 8;
@@ -387,17 +397,21 @@ __global__ __launch_bounds__(64 * kWaves) void q8_average_kernel(AttendArgs args
     rw = args.row[(size_t)s.row0 + (size_t)row * args.H + h];
   };
   if (h0 < h1) {
-    want_k(h0);
+    want_k(h0 / G);
     want_q(h0);
   }
   for (int h = h0; h < h1; ++h) {
+    if (h == h0 || h % G == 0) {                     // the heads of a kv head share its operands
+      convert_k<D>(kr[0], k[0]);
+      convert_k<D>(kr[1], k[1]);
+      ks = ks_next;
+      want_k(min(h / G + 1, args.Hkv - 1));
+    }
     const float c = ks * rw.x, base = -rw.y;
     f32x16 x[2];
-    x[0] = scores<D, QP>(kr[0], q);
-    x[1] = scores<D, QP>(kr[1], q);
-    const int next = min(h + 1, h1 - 1);
-    want_k(next);
-    want_q(next);
+    x[0] = product<D, QP>(k[0], q);
+    x[1] = product<D, QP>(k[1], q);
+    want_q(min(h + 1, h1 - 1));
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
