@@ -9,7 +9,8 @@
  *     at d2c_q8_init, and calls with another device current are refused (D2C_EINVAL);
  *   - no call but d2c_q8_init allocates, copies to the host or waits, so each can be captured into a HIP graph;
  *   - a handle is not thread-safe, and calls (or replays of graphs captured from calls) that share a handle must not
- *     overlap in time: they share its workspace.  d2c_q8_update, _read, _weigh and _pack use no workspace;
+ *     overlap in time: they share its workspace.  d2c_q8_update, _read, _weigh, _evict and _pack use no workspace;
+ *   - what a call writes must not overlap what it reads (but the caches that it refreshes) or other outputs;
  *   - T is float (D2C_F32) or bfloat16 (D2C_BF16), as the handle's dtype says: queries, K/V rows, outputs, activations
  *     and the weights given to d2c_q8_pack;
  *   - pointers to T and to codes are multiples of 16 bytes, others of their element's size (D2C_EINVAL).
@@ -18,7 +19,8 @@
  * code(x, s) = the whole number in [-127, 127] nearest to the real quotient x / s, ties to even; 0 where s = 0.
  *
  * The cache of n rows has ceil(n / 64) blocks, each n_kv_heads * 64 * head_dim bytes of K and as many of V; the last
- * block is whole even if n is not a multiple of 64.  A byte is its code + 128.  With block b, kv head h, row t of the
+ * block is whole even if n is not a multiple of 64.  It starts as bytes of 128 and scales of 0 (every value 0), or with an
+ * update of all its rows.  A byte is its code + 128.  With block b, kv head h, row t of the
  * block and dimension d (D = head_dim), base = (b * n_kv_heads + h) * 64 * D:
  *   K at base + (d / 16) * 1024 + t * 16 + d % 16          V at base + (t / 4) * 4 * D + d * 4 + t % 4
  *   scales at b * n_kv_heads + h.  value = code * scale.
@@ -84,16 +86,19 @@ int d2c_q8_cache_size(const d2c_q8* ctx, int64_t rows, int64_t* code_bytes, int6
  * becomes max(scale(new rows), 1.25 * old scale) and the other rows' codes become code(code * old, new) -- at least a quarter
  * at a time, so that many small growths cannot let a value drift away with its scale.  A value that is not finite counts
  * for no scale: NaN is stored as 0, an infinity as the largest code of its sign.  Indices outside [0, L) are left out;
- * indices that are not ascending and distinct leave the refreshed rows undefined and nothing else. */
+ * indices that are not ascending and distinct leave the blocks of 64 rows that they name undefined, and nothing else.  Two
+ * sequences of a call must not refresh the same cache (D2C_EINVAL). */
 int d2c_q8_update(d2c_q8* ctx, const d2c_q8_seq* seqs, int32_t batch, void* stream);
 
-/* d2c_q8_update where new_k / new_v are given, then attention of each sequence's m query rows against all L rows of its
- * cache, no mask.  Scores, softmax and sums are fp32; q enters exactly (as fp16 pieces of a row scaled by a power of two:
- * one for bf16, two for float), probabilities are rounded to 11 bits for bf16 and 22 bits for float. */
+/* d2c_q8_update of the sequences that give new_k / new_v, then attention of each sequence's m query rows against all L rows
+ * of its cache, no mask; sequences may share a cache that at most one of them refreshes.  Scores, softmax and sums are fp32.
+ * q enters as fp16 pieces of a row scaled by a power of two, one for bf16 (exact down to 2^-32 of the row's largest
+ * magnitude, to the nearest 2^-39 of it below), two for float (within 2^-23, or 2^-39 of the largest).  Probabilities are
+ * rounded to 11 bits for bf16 and 22 for float, those below 2^-25 (2^-14) of a row's largest to the nearest 2^-35 of it. */
 int d2c_q8_attention(d2c_q8* ctx, const d2c_q8_seq* seqs, int32_t batch, void* stream);
 
 /* Values of cache rows: out_k / out_v T [n, d_kv] (either may be NULL) = rows idx[0 .. n) of the cache of L rows, or rows
- * 0 .. n - 1 where idx is NULL.  An index outside [0, L) gives zeros. */
+ * 0 .. n - 1 where idx is NULL; n up to 2^24.  An index outside [0, L) gives zeros. */
 int d2c_q8_read(d2c_q8* ctx, const d2c_q8_cache* cache, int32_t L, const int32_t* idx, int32_t n,
                 void* out_k, void* out_v, void* stream);
 
@@ -109,7 +114,7 @@ int d2c_q8_linear(d2c_q8* ctx, const void* a, int32_t m, const int8_t* codes, co
                   float* out, void* stream);
 
 /* Accumulated attention: weight[j] += sum_r floor(clamp(attn_avg[r, j], 0, 1) * 2^32) for j < L (NaN counts as 0).
- * attn_avg: float [m, L], as the attention calls leave it.  Whole numbers: the order of the sum does not matter. */
+ * attn_avg: float [m, L], as the attention calls leave it, m and L up to 2^24; the sums hold 2^31 such rows.  Whole numbers: the order of the sum does not matter. */
 int d2c_q8_weigh(d2c_q8* ctx, const float* attn_avg, int32_t m, int32_t L, int64_t* weight, void* stream);
 
 /* Keeps n_keep of the L rows of a cache: those of largest weight (negative ones count as 0), ties to the lowest index; rows

@@ -393,6 +393,11 @@ def _checked(t: Optional[torch.Tensor], what: str, dtype: torch.dtype, shape, de
     return t.data_ptr()
 
 
+def _same_geometry(ctx: "Q8Context", cache: "Q8Cache") -> None:
+    if cache.geo != ctx.geo:
+        raise D2CError(D2C_ESHAPE, "the cache was made for (n_kv_heads, head_dim, device) %s, the handle has %s" % (cache.geo, ctx.geo))
+
+
 class Q8Context:
     """Owns a d2c_q8 handle on the current device."""
 
@@ -403,6 +408,7 @@ class Q8Context:
         self.d_q, self.d_kv = self.n_heads * self.head_dim, self.n_kv_heads * self.head_dim
         self.handle = C.c_void_p()
         self.device = torch.cuda.current_device()
+        self.geo = (self.n_kv_heads, self.head_dim, self.device)
         d = d2c_q8_dims(n_heads, n_kv_heads, head_dim, D2C_BF16 if dtype == "bf16" else D2C_F32, max_seq, max_rows, max_batch,
                         max_k, max_n)
         rc = _lib.d2c_q8_init(C.byref(d), C.byref(self.handle))
@@ -427,21 +433,31 @@ class Q8Context:
     def workspace_bytes(self) -> int:
         return int(_lib.d2c_q8_workspace_bytes(self.handle))
 
+    def _batch(self, seqs) -> "Q8Batch":
+        if not isinstance(seqs, Q8Batch):
+            return Q8Batch(self, seqs)
+        if seqs.kind != (self.geo, self.d_q, self.torch_dtype):
+            raise D2CError(D2C_ESHAPE, "the batch was made for a handle of another geometry")
+        return seqs
+
     # ------------------------------------------------------------------ C ABI calls
     def d2c_q8_update(self, seqs) -> None:
         """seqs: a Q8Batch (made once, used again) or a list of Q8Seq."""
-        b = seqs if isinstance(seqs, Q8Batch) else Q8Batch(self, seqs)
+        b = self._batch(seqs)
         self._check(_lib.d2c_q8_update(self.handle, b.arr, b.n, _stream()))
 
     def d2c_q8_attention(self, seqs) -> None:
-        b = seqs if isinstance(seqs, Q8Batch) else Q8Batch(self, seqs)
+        b = self._batch(seqs)
         self._check(_lib.d2c_q8_attention(self.handle, b.arr, b.n, _stream()))
 
     def d2c_q8_read(self, cache: "Q8Cache", L: int, idx: Optional[torch.Tensor], out_k: Optional[torch.Tensor],
                     out_v: Optional[torch.Tensor]) -> None:
         """Rows idx (None: 0, 1, ...) as values; as many as the outputs have rows."""
+        if out_k is None and out_v is None:
+            raise D2CError(D2C_EINVAL, "neither out_k nor out_v")
         n = (out_k if out_k is not None else out_v).shape[0]
         cache.holds(L)
+        _same_geometry(self, cache)
         shape = (n, self.d_kv)
         self._check(_lib.d2c_q8_read(self.handle, cache.ref, L, _checked(idx, "idx", torch.int32, (n,), self.device), n,
                                      _checked(out_k, "out_k", self.torch_dtype, shape, self.device),
@@ -458,6 +474,8 @@ class Q8Context:
 
     def d2c_q8_linear(self, a: torch.Tensor, w: "Q8Weights", out: torch.Tensor) -> None:
         m = a.shape[0]
+        if w.device != self.device:
+            raise D2CError(D2C_EINVAL, "the weights are on device %d, the handle is on %d" % (w.device, self.device))
         self._check(_lib.d2c_q8_linear(self.handle, _checked(a, "a", self.torch_dtype, (m, w.K), self.device), m, w.codes_ptr,
                                        w.scale_ptr, w.N, w.K, _checked(out, "out", torch.float32, (m, w.N), self.device),
                                        _stream()))
@@ -473,6 +491,8 @@ class Q8Context:
         n = kept.shape[0]
         src.holds(L)
         dst.holds(n)
+        _same_geometry(self, src)
+        _same_geometry(self, dst)
         self._check(_lib.d2c_q8_evict(self.handle, src.ref, L, _checked(weight, "weight", torch.int64, (L,), self.device),
                                       _checked(protect, "protect", torch.uint8, (L,), self.device), n, dst.ref,
                                       _checked(kept, "kept", torch.int32, (n,), self.device),
@@ -484,7 +504,7 @@ class Q8Weights:
 
     def __init__(self, N: int, K: int, codes: torch.Tensor, scale: torch.Tensor):
         self.N, self.K, self.codes, self.scale = N, K, codes, scale
-        self.codes_ptr, self.scale_ptr = codes.data_ptr(), scale.data_ptr()
+        self.codes_ptr, self.scale_ptr, self.device = codes.data_ptr(), scale.data_ptr(), codes.get_device()
 
 
 class Q8Cache:
@@ -496,7 +516,7 @@ class Q8Cache:
         if rc != D2C_OK:
             raise D2CError(rc, "d2c_q8_cache_size: bad arguments")
         dev = torch.device("cuda", ctx.device)
-        self.rows = int(rows)
+        self.rows, self.geo = int(rows), ctx.geo
         self.k_codes, self.v_codes = (torch.full((nb.value,), 128, dtype=torch.uint8, device=dev) for _ in range(2))
         self.k_scale, self.v_scale = (torch.zeros((ns.value // ctx.n_kv_heads, ctx.n_kv_heads), device=dev) for _ in range(2))
         self.c = d2c_q8_cache(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr())
@@ -523,9 +543,11 @@ class Q8Batch:
 
     def __init__(self, ctx: Q8Context, seqs: Sequence[Q8Seq]):
         self.n, self.seqs = len(seqs), list(seqs)
+        self.kind = (ctx.geo, ctx.d_q, ctx.torch_dtype)
         arr = (d2c_q8_seq * max(1, self.n))()
         t, dev = ctx.torch_dtype, ctx.device
         for c, s in zip(arr, self.seqs):
+            _same_geometry(ctx, s.cache)
             c.cache = s.cache.c
             c.idx = _checked(s.idx, "idx", torch.int32, (s.m,), dev)
             c.new_k = _checked(s.new_k, "new_k", t, (s.m, ctx.d_kv), dev)

@@ -38,6 +38,18 @@ int hip(d2c_q8* c, hipError_t e, const char* what) {
 }
 
 bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return a && b && x < y + nb && y < x + na;
+}
+// any buffer of a cache of na rows with any of the same kind of one of nb rows
+bool caches_overlap(const d2c_q8* c, const d2c_q8_cache& a, int na, const d2c_q8_cache& b, int nb) {
+  const size_t block = (size_t)c->dims.n_kv_heads * D2C_Q8_BLOCK * c->dims.head_dim, scales = (size_t)c->dims.n_kv_heads * 4;
+  const size_t ca = q8_blocks(na) * block, cb = q8_blocks(nb) * block, sa = q8_blocks(na) * scales, sb = q8_blocks(nb) * scales;
+  return overlap(a.k_codes, ca, b.k_codes, cb) || overlap(a.v_codes, ca, b.v_codes, cb) || overlap(a.k_codes, ca, b.v_codes, cb) ||
+         overlap(a.v_codes, ca, b.k_codes, cb) || overlap(a.k_scale, sa, b.k_scale, sb) || overlap(a.v_scale, sa, b.v_scale, sb) ||
+         overlap(a.k_scale, sa, b.v_scale, sb) || overlap(a.v_scale, sa, b.k_scale, sb);
+}
 Q8CachePtr ptr(const d2c_q8_cache& c) { return Q8CachePtr{c.k_codes, c.v_codes, c.k_scale, c.v_scale}; }
 
 int check_device(d2c_q8* c) {
@@ -73,7 +85,7 @@ int check_seqs(d2c_q8* c, const d2c_q8_seq* seqs, int batch, bool attend) {
         return fail(c, D2C_EINVAL, "new_k / new_v must be aligned to 16 bytes");
       // two sequences of a call must not refresh one cache: their order is not defined
       for (int j = 0; j < i; ++j)
-        if (seqs[j].m > 0 && seqs[j].new_k && (seqs[j].cache.k_codes == s.cache.k_codes || seqs[j].cache.v_codes == s.cache.v_codes))
+        if (seqs[j].m > 0 && seqs[j].new_k && caches_overlap(c, seqs[j].cache, seqs[j].L, s.cache, s.L))
           return fail(c, D2C_EINVAL, "two sequences of the call refresh the same cache");
     }
     if (attend) {
@@ -93,10 +105,6 @@ int do_update(d2c_q8* c, const d2c_q8_seq* seqs, int batch, hipStream_t st) {
     if (seqs[i].m > 0 && seqs[i].new_k)
       u[n++] = Q8Update{ptr(seqs[i].cache), seqs[i].idx, seqs[i].new_k, seqs[i].new_v, seqs[i].m, seqs[i].L};
   return n ? hip(c, launch_q8_update(c->shape, u, n, st), "update") : D2C_OK;
-}
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return x < y + nb && y < x + na;
 }
 
 }  // namespace
@@ -184,6 +192,7 @@ int d2c_q8_read(d2c_q8* c, const d2c_q8_cache* cache, int32_t L, const int32_t* 
   if (!cache) return fail(c, D2C_EINVAL, "null cache");
   if ((rc = check_cache(c, *cache, L))) return rc;
   if (n < 0 || (!idx && n > L)) return fail(c, D2C_EINVAL, "n outside [0, L]");
+  if (n > 1 << 24) return fail(c, D2C_ESHAPE, "more than 2^24 rows");
   if (!aligned(out_k, 16) || !aligned(out_v, 16) || !aligned(idx, 4)) return fail(c, D2C_EINVAL, "outputs must be aligned to 16 bytes");
   if (n == 0 || (!out_k && !out_v)) return D2C_OK;
   return hip(c, launch_q8_read(c->shape, ptr(*cache), L, idx, n, out_k, out_v, (hipStream_t)stream), "read");
@@ -219,6 +228,8 @@ int d2c_q8_linear(d2c_q8* c, const void* a, int32_t m, const int8_t* codes, cons
   if (!a || !codes || !scale || !out) return fail(c, D2C_EINVAL, "null buffer");
   if (!aligned(a, 16) || !aligned(codes, 16) || !aligned(scale, 4) || !aligned(out, 16))
     return fail(c, D2C_EINVAL, "a, codes and out must be aligned to 16 bytes");
+  // (workgroups read rows that others have finished)
+  if (overlap(a, (size_t)m * K * (c->dims.dtype == D2C_BF16 ? 2 : 4), out, (size_t)m * N * 4)) return fail(c, D2C_EINVAL, "out overlaps a");
   return hip(c, launch_q8_linear(c->dims.dtype, a, m, codes, scale, N, K, out, c->ws, (hipStream_t)stream), "linear");
 }
 
@@ -227,6 +238,7 @@ int d2c_q8_weigh(d2c_q8* c, const float* avg, int32_t m, int32_t L, int64_t* wei
   int rc = check_device(c);
   if (rc) return rc;
   if (m < 0 || L <= 0) return fail(c, D2C_EINVAL, "bad m or L");
+  if (m > 1 << 24 || L > 1 << 24) return fail(c, D2C_ESHAPE, "m or L above 2^24");
   if (m == 0) return D2C_OK;
   if (!avg || !weight) return fail(c, D2C_EINVAL, "null buffer");
   if (!aligned(avg, 4) || !aligned(weight, 8)) return fail(c, D2C_EINVAL, "attn_avg or weight not aligned");
@@ -245,14 +257,11 @@ int d2c_q8_evict(d2c_q8* c, const d2c_q8_cache* src, int32_t L, const int64_t* w
   if ((rc = check_cache(c, *dst, n_keep))) return rc;
   if (!weight || !kept) return fail(c, D2C_EINVAL, "null buffer");
   if (!aligned(weight, 8) || !aligned(kept, 4) || !aligned(kept_weight, 8)) return fail(c, D2C_EINVAL, "weight or kept not aligned");
-  const size_t block = (size_t)c->dims.n_kv_heads * D2C_Q8_BLOCK * c->dims.head_dim, scales = (size_t)c->dims.n_kv_heads * 4;
-  const size_t ns = q8_blocks(L), nd = q8_blocks(n_keep);
-  if (overlap(src->k_codes, ns * block, dst->k_codes, nd * block) || overlap(src->v_codes, ns * block, dst->v_codes, nd * block) ||
-      overlap(src->k_codes, ns * block, dst->v_codes, nd * block) || overlap(src->v_codes, ns * block, dst->k_codes, nd * block) ||
-      overlap(src->k_scale, ns * scales, dst->k_scale, nd * scales) || overlap(src->v_scale, ns * scales, dst->v_scale, nd * scales) ||
-      overlap(src->k_scale, ns * scales, dst->v_scale, nd * scales) || overlap(src->v_scale, ns * scales, dst->k_scale, nd * scales) ||
-      (kept_weight && overlap(weight, (size_t)L * 8, kept_weight, (size_t)n_keep * 8)))
-    return fail(c, D2C_EINVAL, "dst overlaps src");
+  if (caches_overlap(c, *src, L, *dst, n_keep)) return fail(c, D2C_EINVAL, "dst overlaps src");
+  const size_t nl = (size_t)L, nk = (size_t)n_keep;
+  if (overlap(kept, nk * 4, weight, nl * 8) || overlap(kept, nk * 4, protect, nl) || overlap(kept, nk * 4, kept_weight, nk * 8) ||
+      overlap(kept_weight, nk * 8, weight, nl * 8) || overlap(kept_weight, nk * 8, protect, nl))
+    return fail(c, D2C_EINVAL, "kept or kept_weight overlaps another buffer of the call");
   hipStream_t st = (hipStream_t)stream;
   if ((rc = hip(c, launch_q8_keep(weight, protect, L, n_keep, kept, kept_weight, st), "evict"))) return rc;
   return hip(c, launch_q8_compact(c->shape, ptr(*src), kept, n_keep, ptr(*dst), st), "evict");

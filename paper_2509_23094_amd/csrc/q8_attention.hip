@@ -1,12 +1,13 @@
 // Attention of a few query rows against a whole K/V cache held in 8 bits.
 //
 // A workgroup takes 32 query rows of one kv head (with grouped heads: rows of all its query heads) and a range of the cache's 64-row
-// blocks, four waves one block each at a time.  A wave forms S^T[64 keys x 32 rows] = K Q^T, its softmax terms, and
+// blocks, eight waves one block each at a time.  A wave forms S^T[64 keys x 32 rows] = K Q^T, its softmax terms, and
 // O^T[D x 32 rows] += V^T P^T, all in registers: an accumulator of S^T holds, for one query row, the keys 8a + 4g + j (g = lane / 32),
 // and V's codes lie in the cache as four rows of four dimensions, so that they are the other operand in just that order.
 //   codes -> fp16 exactly: a byte u under the high byte 0x64 is the fp16 number 1024 + u, less 1152 gives code = u - 128 (one byte
-//   permutation and one packed addition for two codes).  q enters as fp16 too, exactly: a row is scaled by a power of two so that its
-//   largest magnitude lies in [2^14, 2^15); bf16 has 8 bits, float takes two pieces of 11.  The product's scale (row, block and
+//   permutation and one packed addition for two codes).  q enters as fp16 too: a row is scaled by a power of two so that its largest
+//   magnitude lies in [2^14, 2^15).  bf16's 8 bits fit in whole down to 2^-32 of the largest (below: to the nearest 2^-39 of it);
+//   float takes two pieces of 11 bits, which leave 2^-23 of each value and 2^-39 of the largest.  The product's scale (row, block and
 //   log2(e) / sqrt(D)) is applied to the fp32 score, V's scale when a block's O^T joins the running one.
 //   probabilities are rounded to fp16 (float: two pieces): 11 (22) bits down to 2^-25 (2^-14) of a row's largest, below that to
 //   the nearest 2^-35 of it; the running sum takes them before that rounding.
@@ -14,10 +15,6 @@
 // The head average has a pass of its own over the scores, from the same fp16 q and the final (maximum, sum) of every row.
 #include <algorithm>
 #include <cmath>
-#ifdef Q8_DEV
-#include <cstdio>
-#include <cstdlib>
-#endif
 
 #include "q8.h"
 
@@ -246,7 +243,6 @@ __global__ __launch_bounds__(64 * kWaves) void q8_attend_kernel(AttendArgs args)
 
   f32x16 o[DT] = {};
   float ref = -INFINITY, l = 0.f;
-  if (wave & 4) __builtin_amdgcn_s_setprio(2);
   for (int b = b0 + wave; b < b1; b += kWaves) {
     if (QP > 1) want_k(b);
     const float ks = ks_next * factor;
@@ -440,9 +436,6 @@ __global__ __launch_bounds__(64 * kWaves) void q8_average_kernel(AttendArgs args
 // 2.6, its ends 5; a split row takes a launch of 4 and its way to memory and back.
 constexpr int kTargetWgs = 512;
 int plan_splits(int workgroups, int most_blocks) {
-#ifdef Q8_DEV
-  if (const char* f = getenv("Q8_ATT")) return atoi(f);
-#endif
   int best = 1;
   float best_cost = 1e30f;
   for (int s = 1; s <= 64 && (s == 1 || (s * workgroups <= kTargetWgs && s * kWaves < 2 * most_blocks)); ++s) {

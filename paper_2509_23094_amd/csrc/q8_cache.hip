@@ -235,7 +235,8 @@ constexpr int kKeepWaves = 16, kKeepThreads = 64 * kKeepWaves;
 // The protected rows fill up first: if they are n_keep or more the choice is among them, else all of them stay and it is among the others.
 // The chosen class's n-th largest weight is found digit by digit (11 bits, from its highest bit on), with a histogram in LDS and an early
 // end when a digit's rows all stay.  Then each wave numbers its kept positions behind those of the waves before.
-// What bounds it: a chain of barriers and LDS atomics per digit in one compute unit; 767 rows XXX us, 20001 XXX.
+// What bounds it: a chain of barriers and LDS atomics per digit in one compute unit, and its instructions where there are many rows; 767 rows
+// 6.5 us, 20001 18.4.
 template <int PER, bool PROTECT>
 __global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* weight, const uint8_t* protect, int L, int n_keep,
                                                               int32_t* kept, int64_t* kept_weight) {

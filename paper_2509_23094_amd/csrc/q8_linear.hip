@@ -2,13 +2,9 @@
 //
 // Both operands lie in the order in which the matrix cores take them (v_mfma_i32_16x16x64_i8): tiles of 16 rows x 64 of the
 // contraction, 1 KB each, lane l's 16 bytes (row l % 16, contraction 16 (l / 16) ..) at 16 l; rows and contraction are padded with
-// zeros to whole tiles.  Weights are brought into that order once (q8_pack_kernel), activations in a launch of their own in front of
-// each product (q8_rows_kernel), with a scale per row.
+// zeros to whole tiles.  Weights are brought into that order once, activations in a launch of their own in front of each product (both
+// q8_rows_kernel), with a scale per row; a few short rows are rounded inside the product's launch.
 #include <algorithm>
-#ifdef Q8_DEV
-#include <cstdio>
-#include <cstdlib>
-#endif
 
 #include "q8.h"
 
@@ -23,9 +19,9 @@ typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 //
 // A workgroup takes a row, or a part of its columns (blockIdx.y) while there are few rows, 16 columns per thread at a time: one lane's piece
 // of a tile.  It looks at the whole row for its largest magnitude -- integer maxima of the bits without sign: infinities and NaN are the
-// largest -- and rounds its part from registers.  What bounds it: one chain of load, maximum, barrier and store; 37 x 18944 4.3 us, 1536 x
-// 4096 11 us (4 waves a row; 16 waves 17).  Sixteen rows per workgroup with lanes as in a tile, so that codes leave a kilobyte
-// at a time, took longer (20 and 19 us): their loads are 128-byte pieces of 16 rows.
+// largest -- and rounds its part from registers.  What bounds it: one chain of load, maximum, barrier and store; 37 x 18944 5 us, 1536 x
+// 4096 10 us (4 waves a row; 16 waves 17).  Sixteen rows per workgroup with lanes as in a tile, so that codes leave a kilobyte
+// at a time, took longer (22 and 18 us): their loads are 128-byte pieces of 16 rows.
 //
 // Rounding: the sum with 1.5 * 2^23 leaves the whole number nearest to x / s (or its neighbour, next to a border) in its low byte, and the
 // remainder x - n s, which has no rounding (see q8_code), says if all 16 are the nearest: only where a remainder is half a step or more
@@ -247,7 +243,8 @@ __global__ __launch_bounds__(64 * WAVES) void q8_stream_kernel(const int8_t* a, 
 
 // Few rows and a short contraction (m <= 16 MT, MT * kc <= 32): one launch.  Every workgroup rounds all the rows into LDS by itself, a wave a row at a
 // time, while its weights -- a tile of 16 outputs, two steps of the contraction per wave at most -- are on their way.
-// 5 x 768 x 256: XXX us a call, in two launches 9.
+// What bounds it: launching, and one chain of load, maximum, code, barrier, product, barrier.  5 x 768 x 256: 5.3 us a call, in two
+// launches 9.
 template <typename T, int MT>
 __global__ __launch_bounds__(1024) void q8_small_kernel(const T* x, const int8_t* w, const float* sw, int m, int N, int K, int kc, float* out) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -319,6 +316,8 @@ __global__ __launch_bounds__(256) void q8_sum_kernel(const int* part, int splits
 // registers from the order they lie in and are refilled as soon as a step is done.  LDS reads run three groups of NT matrix-core instructions
 // ahead of their use.  Each XCD takes a run of tiles in an order in which neighbours share activations and weights in its L2.  Splits of the
 // contraction write their sums to `part`.
+// What bounds it: what a compute unit gets from its L2, 65-80 KB/us, and the clock (1536 x 24576 x 4096: 147-157 us, 1.97-2.1 POP/s,
+// matrix cores busy 43 % of the time).  Two chunks on their way instead of one gave nothing.
 constexpr int kStepsPerChunk = 4;
 template <int MT, int NT>
 __global__ __launch_bounds__(512, 1) void q8_tile_kernel(const int8_t* a, const float* sa, const int8_t* w, const float* sw, int m, int N,
@@ -492,11 +491,11 @@ hipError_t tile(const Operands& o, int splits, hipStream_t st) {
   return e != hipSuccess || splits == 1 ? e : sum_parts(o, splits, st);
 }
 
-// The tile kernel's shape and splits by an estimate of its time in us, fitted to 90 sizes (1-1536 rows, 64-37888 outputs, contractions of
+// The tile kernel's shape and splits by an estimate of its time in us, fitted to 87 sizes (1-1536 rows, 64-37888 outputs, contractions of
 // 64-18944; all shapes and splits measured on each).  A chunk takes a workgroup c0 + c1 MT NT + c2 NT alone (c1 is the matrix cores'
 // time), and as long as its bytes take from the L2 where all compute units pull: 80 KB/us each; then its outputs' way to memory.
-// Splits cost a launch and the parts' way out and in.  What it picks is 1.7 % behind the best on average, 13 % at most; always
-// taking MT = 8, NT = 2 without splits loses 40 % on average.
+// Splits cost a launch and the parts' way out and in.  What it picks is 1.1 % behind the best on average, 6.5 % at most; always
+// taking MT = 8, NT = 2 without splits is 38 % behind at 128 rows and more.
 struct TilePlan { int mt, nt, splits; };
 TilePlan plan_tile(int m, int N, int ka) {
   constexpr float c0 = 0.25f, c1 = 0.05f, c2 = 0.05f, l2 = 80.f, out = 0.4f, split_launch = 8.f, split_bytes = 6e6f;
@@ -582,18 +581,9 @@ hipError_t launch_q8_linear(int dtype, const void* a, int m, const int8_t* codes
   const hipError_t e = launch_rows(dtype, a, m, K, ka, qa, sa, st);
   if (e != hipSuccess) return e;
   const Operands o{qa, sa, codes, scale, m, N, kc, ka, out, (int*)p};
-#ifdef Q8_DEV
-  if (const char* f = getenv("Q8_PLAN")) {
-    int kind, mt, nt, splits = 1;
-    sscanf(f, "%d,%d,%d,%d", &kind, &mt, &nt, &splits);
-    if (kind == 1) {
-      if ((size_t)splits * m * N * 4 > kPartBytes && splits > 1) return hipErrorInvalidValue;
-      return run_tile(o, TilePlan{mt, nt, splits}, st);
-    }
-  }
-#endif
-  // Up to two tiles of rows the activations come along from the L2 without weighing (32 x 4096 x 12288: 17.7 us, tiles 18.2); from
-  // three on a compute unit pulls more of them than of weights (64 x 4096 x 12288: 23, tiles 18.9).
+  // Up to two tiles of rows the activations come along from the L2 without weighing (a call of 1 x 3584 x 18944 18.3 us, through tiles
+  // 19.9; 31 x 4096 x 12288 18.2 and 19.0); from three on a compute unit pulls more of them than of weights (37 x 3584 x 18944 25.4 and
+  // 23.3, 63 x 12288 x 4096 21.2 and 17.6).
   if (m <= kStreamRows) {
     const bool two = n_tiles >= 512;                  // two column tiles where that leaves a workgroup for each compute unit
     if (m_tiles == 1) return two ? stream<1, 2, 8>(o, st) : stream<1, 1, 16>(o, st);

@@ -599,3 +599,131 @@ def test_refusals():
     ctx.d2c_q8_update([seq(m=0)])
     lin.d2c_q8_linear(a[:0], p, torch.zeros((0, 32), device="cuda"))
     c.check()
+
+
+def test_places_past_32_bits():
+    """A cache whose last rows lie more than 4 GiB behind its first: refresh, read, attention, weight, eviction.  All but three rows are
+    zeros, so the plain form needs only those three."""
+    say("q8 places past 32 bits")
+    H, D, L = 32, 128, (1 << 20) + 12345
+    idx = np.array([5, (1 << 20) + 3, L - 1])
+    rng, t = np.random.default_rng(11), lambda a: torch.from_numpy(np.ascontiguousarray(a, np.float32)).cuda()
+    ctx = B().Q8Context(H, H, D, "f32", max_seq=L, max_rows=3)
+    cache = B().Q8Cache(ctx, L)
+    assert cache.k_codes.numel() > 1 << 32
+    k, v, q = t(3.0 * rng.standard_normal((3, H * D))), t(rng.standard_normal((3, H * D))), t(rng.standard_normal((3, H * D)))
+    out, avg = torch.zeros_like(q), torch.zeros((3, L), device="cuda")
+    ctx.d2c_q8_attention([B().Q8Seq(cache, L, 3, idx=torch.tensor(idx, dtype=torch.int32, device="cuda"), new_k=k, new_v=v, q=q, out=out,
+                                    attn_avg=avg)])
+    ref = R.Cache8(192, H, D)                          # each of the three alone in its block, as it is in the cache
+    at = np.array([5, 67, 191])
+    ref.update(at, f64(k).reshape(3, H, D), f64(v).reshape(3, H, D), 192)
+    rk, rv = torch.zeros((4, H * D), device="cuda"), torch.zeros((4, H * D), device="cuda")
+    ctx.d2c_q8_read(cache, L, torch.tensor(list(idx) + [L - 2], dtype=torch.int32, device="cuda"), rk, rv)
+    for got, want in ((rk, ref.k), (rv, ref.v)):
+        assert np.array_equal(got[:3].cpu().numpy(), want.values()[at].reshape(3, -1).astype(np.float32)) and not got[3].any()
+    kk, vv, qq = ref.k.values()[at], ref.v.values()[at], f64(q).reshape(3, H, D)
+    s = np.einsum("mhd,nhd->mhn", qq, kk) / D ** 0.5
+    sums = np.einsum("mhd,nhd->mhn", np.abs(qq), np.abs(kk)) / D ** 0.5
+    share = float((D + 4) * sums.max() + 6 * np.abs(s).max() + 8) * 2.0 ** -24         # as R.attention has it
+    den = (L - 3) + np.exp(s).sum(2)
+    p = np.exp(s) / den[:, :, None]
+    o, mag = np.einsum("mhn,nhd->mhd", p, vv), np.einsum("mhn,nhd->mhd", p, np.abs(vv))
+    tol = HALF["f32"] * np.abs(o) + mag * (2 * share + P_HALF["f32"] + (L ** 0.5 + 70) * 2.0 ** -24) * 1.001 + 2.0 ** -36 * np.abs(vv).sum(0)[None]
+    assert (np.abs(f64(out).reshape(3, H, D) - o) <= tol).all()
+    a = f64(avg)
+    for cols, want in ((idx, p.mean(1)), ([0, 1 << 20, L - 2], np.repeat((1 / den).mean(1)[:, None], 3, 1))):
+        assert (np.abs(a[:, cols] - want) <= want * (2 * share + (L ** 0.5 + H + 16) * 2.0 ** -24)).all()
+    weight = torch.zeros(L, dtype=torch.int64, device="cuda")
+    ctx.d2c_q8_weigh(avg, weight)
+    assert np.array_equal(weight.cpu().numpy(), R.weigh(a, np.zeros(L, np.int64)))
+    weight[torch.from_numpy(idx).cuda()] += 1 << 40
+    dst, kept = B().Q8Cache(ctx, 3), torch.zeros(3, dtype=torch.int32, device="cuda")
+    ctx.d2c_q8_evict(cache, L, weight, None, dst, kept)
+    assert np.array_equal(kept.cpu().numpy(), idx)
+    small = ref.evict(at)
+    ctx.d2c_q8_read(dst, 3, None, rk[:3], rv[:3])
+    for got, want in ((rk, small.k), (rv, small.v)):
+        assert np.array_equal(got[:3].cpu().numpy(), want.values(3).reshape(3, -1).astype(np.float32))
+
+
+def test_a_cache_that_one_sequence_refreshes_and_others_read():
+    """All of a call's refreshes come before its attention, in whatever order the sequences stand."""
+    say("q8 shared cache")
+    c = Case("gqa", "bf16", 400, max_batch=12).fill()
+    (dk, nk), (dv, nv) = c.new(7), c.new(7)
+    idx = np.sort(c.rng.permutation(400)[:7])
+    seqs, got = [], []
+    for i in range(12):
+        q = c.queries(7)
+        out = torch.zeros_like(q)
+        new = dict(idx=torch.tensor(idx, dtype=torch.int32, device="cuda"), new_k=dk, new_v=dv) if i == 10 else {}
+        seqs.append(B().Q8Seq(c.cache, 400, 7, q=q, out=out, **new))
+        got.append((q, out))
+    c.ctx.d2c_q8_attention(seqs)
+    c.ref.update(idx, nk, nv, 400)
+    c.check()
+    for q, out in got:
+        c.expect(q, out, None)
+
+
+def test_two_handles_at_once():
+    """Two handles on two streams, their calls overlapping in time, give what each gives alone."""
+    say("q8 two handles at once")
+    cs = [Case("dream", "bf16", 3000 + 500 * i, seed=i).fill() for i in range(2)]
+    qs = [c.queries(40 + i) for i, c in enumerate(cs)]
+    alone = [attend(c, q.shape[0], q=q)[1:] for c, q in zip(cs, qs)]
+    outs = [[(torch.zeros_like(q), torch.zeros((q.shape[0], c.L), device="cuda")) for _ in range(10)] for c, q in zip(cs, qs)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cs]
+    for j in range(10):
+        for c, q, o, st in zip(cs, qs, outs, streams):
+            with torch.cuda.stream(st):
+                c.ctx.d2c_q8_attention([B().Q8Seq(c.cache, c.L, q.shape[0], q=q, out=o[j][0], attn_avg=o[j][1])])
+    torch.cuda.synchronize()
+    for (x, a), o in zip(alone, outs):
+        for y, b in o:
+            assert torch.equal(x, y) and torch.equal(a, b)
+
+
+def test_refusals_of_overlaps_and_other_geometries():
+    say("q8 refusals of overlaps")
+    b = B()
+    c = Case("gqa", "bf16", 200, max_rows=10, max_batch=2).fill()
+    ctx = c.ctx
+
+    def refused(code, f):
+        with pytest.raises(b.D2CError) as e:
+            f()
+        assert e.value.code == code and str(e.value)
+
+    q = c.queries(4)
+    batch = b.Q8Batch(ctx, [b.Q8Seq(c.cache, 200, 4, q=q, out=torch.zeros_like(q))])
+    other = b.Q8Context(8, 4, 64, "bf16", max_seq=300, max_rows=10)
+    refused(b.D2C_ESHAPE, lambda: other.d2c_q8_attention(batch))                        # a batch of another handle's geometry
+    refused(b.D2C_ESHAPE, lambda: other.d2c_q8_attention([b.Q8Seq(c.cache, 200, 4, q=q, out=torch.zeros_like(q))]))
+    rk = torch.zeros((4, other.d_kv), dtype=torch.bfloat16, device="cuda")
+    refused(b.D2C_ESHAPE, lambda: other.d2c_q8_read(c.cache, 200, None, rk, None))
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_read(c.cache, 200, None, None, None))
+    # the second cache begins inside the first
+    (dk, _), (dv, _) = c.new(4), c.new(4)
+    inner = b.Q8Cache(ctx, 64)
+    inner.c.v_codes = c.cache.v_codes.data_ptr() + 64 * ctx.d_kv
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_update([b.Q8Seq(c.cache, 200, 4, new_k=dk, new_v=dv), b.Q8Seq(inner, 64, 4, new_k=dk, new_v=dv)]))
+    wt = torch.zeros(200, dtype=torch.int64, device="cuda")
+    kept = torch.zeros(50, dtype=torch.int32, device="cuda")
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_evict(c.cache, 200, wt, None, inner, kept))
+    dst = b.Q8Cache(ctx, 50)
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_evict(c.cache, 200, wt, None, dst, kept, wt[10:60]))
+    refused(b.D2C_EINVAL, lambda: ctx.d2c_q8_evict(c.cache, 200, wt, None, dst, wt[:25].view(torch.int32)))
+    lin = b.Q8Context(4, 4, 64, "f32", max_rows=8, max_k=64, max_n=64)
+    p = lin.d2c_q8_pack(torch.ones((64, 64), device="cuda"))
+    a = torch.ones((8, 64), device="cuda")
+    refused(b.D2C_EINVAL, lambda: lin.d2c_q8_linear(a, p, a))
+    assert (a == 1).all() and not wt.any() and not kept.any()
+    big = torch.zeros(1, device="cuda")
+    lib, h, st = b._lib, ctx.handle, torch.cuda.current_stream().cuda_stream
+    assert lib.d2c_q8_weigh(h, big.data_ptr(), 1, (1 << 24) + 1, wt.data_ptr(), st) == b.D2C_ESHAPE
+    assert lib.d2c_q8_weigh(h, big.data_ptr(), (1 << 24) + 1, 1, wt.data_ptr(), st) == b.D2C_ESHAPE
+    assert lib.d2c_q8_read(h, c.cache.ref, 200, kept.data_ptr(), (1 << 24) + 1, rk.data_ptr(), None, st) == b.D2C_ESHAPE
+    c.check()

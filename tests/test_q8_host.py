@@ -65,10 +65,10 @@ def test_binding_refuses_tensors_of_another_kind():
     from paper_2509_23094_amd import binding as B
 
     class Ctx:                                   # geometry of a handle, no device needed
-        torch_dtype, device, d_kv, d_q = torch.bfloat16, -1, 128, 256
+        torch_dtype, device, d_kv, d_q, geo = torch.bfloat16, -1, 128, 256, (2, 64, -1)
 
     class Cache:
-        c = B.d2c_q8_cache()
+        c, geo = B.d2c_q8_cache(), (2, 64, -1)
 
         def holds(self, L):
             pass
@@ -83,6 +83,10 @@ def test_binding_refuses_tensors_of_another_kind():
         with pytest.raises(B.D2CError) as e:
             batch(**bad)
         assert e.value.code == B.D2C_EINVAL
+    Cache.geo = (2, 128, -1)                     # a cache of another geometry
+    with pytest.raises(B.D2CError) as e:
+        batch(q=torch.zeros(3, 256, dtype=torch.bfloat16))
+    assert e.value.code == B.D2C_ESHAPE
 
 
 # ---------------------------------------------------------------------- the plain forms
