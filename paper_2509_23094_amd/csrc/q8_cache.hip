@@ -236,7 +236,7 @@ constexpr int kKeepWaves = 16, kKeepThreads = 64 * kKeepWaves;
 // The chosen class's n-th largest weight is found digit by digit (11 bits, from its highest bit on), with a histogram in LDS and an early
 // end when a digit's rows all stay.  Then each wave numbers its kept positions behind those of the waves before.
 // What bounds it: a chain of barriers and LDS atomics per digit in one compute unit, and its instructions where there are many rows; 767 rows
-// 6.5 us, 20001 18.4.
+// 6.2 us, 20001 16.1 (with equal keys told apart in every pass over them, not only where a part of them stays, 6.7 and 18.7).
 template <int PER, bool PROTECT>
 __global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* weight, const uint8_t* protect, int L, int n_keep,
                                                               int32_t* kept, int64_t* kept_weight) {
@@ -276,12 +276,15 @@ __global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* we
   // how many are protected, and how many bits each class's weights have
   uint32_t n_prot = 0;
   unsigned long long any[2] = {0, 0};
-  each([&](unsigned long long k, bool valid, int) {
-    const bool p = PROTECT && valid && (k & kTop);
-    n_prot += p;
-    any[0] |= valid && !p ? k : 0ull;
-    if (PROTECT) any[1] |= p ? k & ~kTop : 0ull;
+  each([&](unsigned long long k, bool, int) {           // (what is not there is 0)
+    const unsigned long long p = PROTECT ? (unsigned long long)((long long)k >> 63) : 0ull;
+    any[0] |= k & ~p;
+    if (PROTECT) {
+      any[1] |= k & p;
+      n_prot += (uint32_t)(k >> 63);
+    }
   });
+  any[1] &= ~kTop;
   const uint32_t bits[2] = {(uint32_t)(any[0] ? 64 - __clzll((long long)any[0]) : 0), (uint32_t)(any[1] ? 64 - __clzll((long long)any[1]) : 0)};
   uint32_t both = bits[0] | bits[1] << 16;
 #pragma unroll
@@ -303,9 +306,12 @@ __global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* we
   const unsigned long long cls = among_protected ? kTop : 0ull;                        // n_keep > 0
   uint32_t need = among_protected ? (uint32_t)n_keep : (uint32_t)n_keep - n_prot;      // of the class `cls`
   const uint32_t size = among_protected ? n_prot : (uint32_t)L - n_prot;
-  // keys of the class above `thr` stay, of those equal to it under the mask of the digits looked at the first `need`
+  // keys of the class above `thr` stay, of those equal to it under the mask of the digits looked at the first `need`: all of them, or, where
+  // the last digit has been looked at, of equal keys the first
   unsigned long long thr = cls, mask = kTop;
+  bool some = false;
   if (need < size) {
+    some = true;
     int hi = among_protected ? both >> 16 : both & 0xffffu;     // bits hi .. 62 are 0 throughout
     mask = ~0ull << hi;
     for (int pass = 0; hi > 0; ++pass) {
@@ -335,14 +341,19 @@ __global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* we
       thr |= (unsigned long long)found_bin << lo;
       mask = ~0ull << lo;
       hi = lo;
-      if (need == found_in) break;
+      some = need != found_in;
+      if (!some) break;
     }
   }
   uint32_t n_up = 0, n_eq = 0;
-  each([&](unsigned long long k, bool valid, int) {
-    n_up += __popcll(__ballot(valid && (k & mask) > thr));
-    n_eq += __popcll(__ballot(valid && (k & mask) == thr));
-  });
+  if (some) {
+    each([&](unsigned long long k, bool valid, int) {
+      n_up += __popcll(__ballot(valid && k > thr));
+      n_eq += __popcll(__ballot(valid && k == thr));
+    });
+  } else {
+    each([&](unsigned long long k, bool valid, int) { n_up += __popcll(__ballot(valid && k >= thr)); });
+  }
   if (lane == 0) { wave_up[wave] = n_up; wave_eq[wave] = n_eq; }
   __syncthreads();
   uint32_t up = 0, eq = 0;
@@ -351,19 +362,28 @@ __global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* we
     up += w < wave ? wave_up[w] : 0u;
     eq += w < wave ? wave_eq[w] : 0u;
   }
-  each([&](unsigned long long key, bool valid, int j) {
-    const int i = first + 64 * j;
-    const bool is_up = valid && (key & mask) > thr, is_eq = valid && (key & mask) == thr;
-    const uint64_t u = __ballot(is_up), e = __ballot(is_eq), below = (1ull << lane) - 1;
-    const uint32_t up_at = up + __popcll(u & below), eq_at = eq + __popcll(e & below);
-    if (is_up || (is_eq && eq_at < need)) {
-      const uint32_t at = up_at + min(eq_at, need);
-      kept[at] = i;
-      if (kept_weight) kept_weight[at] = (int64_t)(key & ~kTop);
-    }
-    up += __popcll(u);
-    eq += __popcll(e);
-  });
+  auto put = [&](uint32_t at, int j, unsigned long long key) __attribute__((always_inline)) {
+    kept[at] = first + 64 * j;
+    if (kept_weight) kept_weight[at] = (int64_t)(key & ~kTop);
+  };
+  auto below = [](uint64_t b) { return (uint32_t)__builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0u)); };
+  if (some) {
+    each([&](unsigned long long key, bool valid, int j) {
+      const bool is_up = valid && key > thr, is_eq = valid && key == thr;
+      const uint64_t u = __ballot(is_up), e = __ballot(is_eq);
+      const uint32_t eq_at = eq + below(e);
+      if (is_up || (is_eq && eq_at < need)) put(up + below(u) + min(eq_at, need), j, key);
+      up += __popcll(u);
+      eq += __popcll(e);
+    });
+  } else {
+    each([&](unsigned long long key, bool valid, int j) {
+      const bool stays = valid && key >= thr;
+      const uint64_t u = __ballot(stays);
+      if (stays) put(up + below(u), j, key);
+      up += __popcll(u);
+    });
+  }
 }
 
 // Row i of dst is row kept[i] of src.  A workgroup per (block of dst, kv head, K or V): 16 KB read (V: more, its pieces hold four rows
