@@ -241,64 +241,54 @@ __global__ __launch_bounds__(64 * WAVES) void q8_stream_kernel(const int8_t* a, 
   }
 }
 
-// Few rows and a short contraction (m <= 16 MT, MT * kc <= 32): one launch.  Every workgroup rounds all the rows into LDS by itself, a wave a row at a
-// time, while its weights -- a tile of 16 outputs, two steps of the contraction per wave at most -- are on their way.
-// What bounds it: launching, and one chain of load, maximum, code, barrier, product, barrier.  5 x 768 x 256: 5.3 us a call, in two
-// launches 9.
-template <typename T, int MT>
+// Up to 16 rows and a short contraction (kc <= 32): one launch.  Every workgroup rounds all the rows into LDS by itself, a wave a row, while
+// its weights -- a tile of 16 outputs, two steps of the contraction per wave at most -- are on their way.
+// What bounds it: launching, and one chain of load, maximum, code, barrier, product, barrier (times in launch_q8_linear).
+template <typename T>
 __global__ __launch_bounds__(1024) void q8_small_kernel(const T* x, const int8_t* w, const float* sw, int m, int N, int K, int kc, float* out) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  __shared__ __attribute__((aligned(16))) int8_t codes[32 * 1024];      // [row tile][step][1 KB]
-  __shared__ int sums[MT][256];
-  __shared__ float scale[MT * 16];
+  __shared__ __attribute__((aligned(16))) int8_t codes[32 * 1024];      // [step][1 KB]
+  __shared__ int sums[256];
+  __shared__ float scale[16];
   const int8_t* wp = w + (size_t)blockIdx.x * kc * 1024 + lane * 16;
   u32x4 wf[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) wf[u] = ld16(wp + (size_t)min(wave + 16 * u, kc - 1) * 1024);
-  for (int i = threadIdx.x; i < MT * 256; i += 1024) (&sums[0][0])[i] = 0;
+  if (threadIdx.x < 256) sums[threadIdx.x] = 0;
+  const T* row = x + (size_t)min(wave, m - 1) * K;                      // past the last row that one again, not stored
+  Raw16<T> v[2];
+  uint32_t bits = 0;
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int r = 16 * t + wave;
-    const T* row = x + (size_t)min(r, m - 1) * K;                       // past the last row that one again, not stored
-    Raw16<T> v[2];
-    uint32_t bits = 0;
+  for (int u = 0; u < 2; ++u) v[u] = load16(row, 16 * (lane + 64 * u), K);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) v[u] = load16(row, 16 * (lane + 64 * u), K);
+  for (int u = 0; u < 2; ++u) {
+    zero_past(v[u], 16 * (lane + 64 * u), K);
+    bits = max(bits, v[u].largest());
+  }
+  const RowScale s(wave_max_bits(bits));
+  if (lane == 0) scale[wave] = s.stored();
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      zero_past(v[u], 16 * (lane + 64 * u), K);
-      bits = max(bits, v[u].largest());
-    }
-    const RowScale s(wave_max_bits(bits));
-    if (lane == 0) scale[r] = s.stored();
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int p = lane + 64 * u;
-      if (p < 4 * kc) s.put(codes + (t * kc + p / 4) * 1024 + p % 4 * 256 + wave * 16, v[u]);
-    }
+  for (int u = 0; u < 2; ++u) {
+    const int p = lane + 64 * u;
+    if (p < 4 * kc) s.put(codes + p / 4 * 1024 + p % 4 * 256 + wave * 16, v[u]);
   }
   __syncthreads();
-  i32x4 acc[MT] = {};
+  i32x4 acc = {};
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int k = wave + 16 * u;
-    if (k < kc)
-#pragma unroll
-      for (int t = 0; t < MT; ++t) acc[t] = mfma_i8(wf[u], *reinterpret_cast<const u32x4*>(codes + (t * kc + k) * 1024 + lane * 16), acc[t]);
+    if (k < kc) acc = mfma_i8(wf[u], *reinterpret_cast<const u32x4*>(codes + k * 1024 + lane * 16), acc);
   }
   if (wave < kc)
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) atomicAdd(&sums[t][j * 64 + lane], acc[t][j]);
+    for (int j = 0; j < 4; ++j) atomicAdd(&sums[j * 64 + lane], acc[j]);
   __syncthreads();
-  if (wave >= MT) return;
-  const int row = wave * 16 + lane % 16, col = blockIdx.x * 16 + lane / 16 * 4;
-  if (row >= m) return;
-  float* to = out + (size_t)row * N + col;
+  const int r = lane % 16, col = blockIdx.x * 16 + lane / 16 * 4;
+  if (wave || r >= m) return;
+  float* to = out + (size_t)r * N + col;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    if (col + j < N) to[j] = (float)sums[wave][j * 64 + lane] * scale[row] * sw[col + j];
+    if (col + j < N) to[j] = (float)sums[j * 64 + lane] * scale[r] * sw[col + j];
 }
 
 // out = the parts' sums, scaled.  A workgroup per (row, 256 outputs): with one index over all outputs, and its division by N, a call of
@@ -551,10 +541,8 @@ hipError_t rows_t(const T* x, int rows, int K, int kc, int8_t* codes, float* sca
   return hipGetLastError();
 }
 template <typename T>
-hipError_t small(const T* a, int m, int m_tiles, const int8_t* codes, const float* scale, int N, int K, int kc, float* out, hipStream_t st) {
-  const int groups = (N + 15) / 16;
-  if (m_tiles == 1) q8_small_kernel<T, 1><<<groups, 1024, 0, st>>>(a, codes, scale, m, N, K, kc, out);
-  else q8_small_kernel<T, 2><<<groups, 1024, 0, st>>>(a, codes, scale, m, N, K, kc, out);
+hipError_t small(const T* a, int m, const int8_t* codes, const float* scale, int N, int K, int kc, float* out, hipStream_t st) {
+  q8_small_kernel<T><<<(N + 15) / 16, 1024, 0, st>>>(a, codes, scale, m, N, K, kc, out);
   return hipGetLastError();
 }
 hipError_t launch_rows(int dtype, const void* x, int rows, int K, int kc, int8_t* codes, float* scale, hipStream_t st) {
@@ -574,10 +562,12 @@ hipError_t launch_q8_pack(int dtype, const void* w, int N, int K, int8_t* codes,
 hipError_t launch_q8_linear(int dtype, const void* a, int m, const int8_t* codes, const float* scale, int N, int K, float* out,
                             void* ws, hipStream_t st) {
   const int kc = q8_kpad(K) / 64, ka = (kc + 3) & ~3, m_tiles = (m + 15) / 16, n_tiles = (N + 15) / 16;
-  // every workgroup rounds the rows again: up to two workgroups for each compute unit
-  if (m_tiles <= 2 && m_tiles * kc <= 32 && n_tiles <= 512)
-    return dtype == kBF16 ? small((const bf16*)a, m, m_tiles, codes, scale, N, K, kc, out, st)
-                          : small((const float*)a, m, m_tiles, codes, scale, N, K, kc, out, st);
+  // One launch; every workgroup rounds the rows again, so only up to three workgroups for two compute units.  In a captured loop of calls, us, one
+  // launch and two: 5 x 768 x 256 3.9 and 5.4, 16 x 4096 x 1024 5.5 and 6.9, 16 x 4096 x 2048 7.2 and 8.1, 16 x 6144 x 1024 7.2 and 7.4,
+  // 16 x 8192 x 2048 10.3 and 9.5 (two tiles of rows in one launch: 32 x 768 x 256 6.1 and 6.4, 32 x 2048 x 1024 7.2 and 6.8).
+  if (m_tiles == 1 && kc <= 32 && n_tiles <= 384)
+    return dtype == kBF16 ? small((const bf16*)a, m, codes, scale, N, K, kc, out, st)
+                          : small((const float*)a, m, codes, scale, N, K, kc, out, st);
   char* p = (char*)ws;
   int8_t* qa = (int8_t*)p;
   p += up256((size_t)m_tiles * 16 * ka * 64);
@@ -590,7 +580,9 @@ hipError_t launch_q8_linear(int dtype, const void* a, int m, const int8_t* codes
   // 19.9; 31 x 4096 x 12288 18.2 and 19.0); from three on a compute unit pulls more of them than of weights (37 x 3584 x 18944 25.4 and
   // 23.3, 63 x 12288 x 4096 21.2 and 17.6).
   if (m <= kStreamRows) {
-    const bool two = n_tiles >= 512;                  // two column tiles where that leaves a workgroup for each compute unit
+    // Two column tiles a workgroup where that leaves a workgroup for each compute unit (2 x 12288 x 4096 15.1 us, with one 15.9, 18 x 14851
+    // x 984 11.0 and 12.5; 31 x 4096 x 12288 22.6, with one 18.2)
+    const bool two = n_tiles >= 512;
     if (m_tiles == 1) return two ? stream<1, 2, 8>(o, st) : stream<1, 1, 16>(o, st);
     return two ? stream<2, 2, 8>(o, st) : stream<2, 1, 16>(o, st);
   }

@@ -329,7 +329,7 @@ def test_attention_of_a_flat_row_over_a_long_cache():
 # ---------------------------------------------------------------------- linear
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("m,N,K", [(1, 1, 8), (1, 16, 64), (2, 17, 72), (15, 33, 256), (16, 768, 1000), (17, 100, 320), (33, 250, 2048),
+@pytest.mark.parametrize("m,N,K", [(1, 1, 8), (16, 6144, 2048), (13, 6145, 64), (17, 80, 2048), (1, 16, 64), (2, 17, 72), (15, 33, 256), (16, 768, 1000), (17, 100, 320), (33, 250, 2048),
                                    (64, 64, 4096), (65, 129, 136), (100, 1000, 512), (130, 72, 8192), (200, 300, 640), (257, 513, 576),
                                    (520, 520, 264)])
 def test_linear(dtype, m, N, K):
