@@ -486,14 +486,14 @@ hipError_t tile(const Operands& o, int splits, hipStream_t st) {
   return e != hipSuccess || splits == 1 ? e : sum_parts(o, splits, st);
 }
 
-// The tile kernel's shape and splits by an estimate of its time in us, fitted to 87 sizes (1-1536 rows, 64-37888 outputs, contractions of
-// 64-18944; all shapes and splits measured on each).  A chunk takes a workgroup c0 + c1 MT NT + c2 NT alone (c1 is the matrix cores'
-// time), and as long as its bytes take from the L2 where all compute units pull: 80 KB/us each; then its outputs' way to memory.
-// Splits cost a launch and the parts' way out and in.  What it picks is 1.1 % behind the best on average, 6.5 % at most; always
-// taking MT = 8, NT = 2 without splits is 38 % behind at 128 rows and more.
+// The tile kernel's shape and splits by an estimate of its time in us, fitted to 159 sizes (33-1536 rows, 64-37888 outputs, contractions of
+// 64-18944; all shapes and splits measured on each).  A round of workgroups starts in `round`; a chunk takes a workgroup c0 + c1 MT NT +
+// c2 NT, and as long as its bytes take from the L2 where all compute units pull; then its outputs' way to memory.  Splits cost a
+// launch and the parts' way out and in.  What it picks is 1.0 % behind the best on average, 16 % at most; always taking MT = 8, NT = 2
+// without splits is 50 % behind at 128 rows and more.
 struct TilePlan { int mt, nt, splits; };
 TilePlan plan_tile(int m, int N, int ka) {
-  constexpr float c0 = 0.25f, c1 = 0.05f, c2 = 0.05f, l2 = 80.f, out = 0.4f, split_launch = 8.f, split_bytes = 6e6f;
+  constexpr float round = 0.83f, c0 = 0.29f, c1 = 0.09f, c2 = 0.04f, l2 = 120.f, out = 0.55f, split_launch = 2.7f, split_bytes = 5.5e6f;
   static constexpr int8_t shapes[][2] = {{1, 1}, {2, 1}, {3, 1}, {4, 1}, {6, 1}, {8, 1}, {4, 2}, {6, 2}, {8, 2}, {8, 3}};
   static constexpr int8_t counts[] = {1, 2, 3, 4, 6, 8, 12};
   const int chunks = ka / kStepsPerChunk, m_tiles = (m + 15) / 16;
@@ -502,14 +502,14 @@ TilePlan plan_tile(int m, int N, int ka) {
   for (const auto& sh : shapes) {
     const int mt = sh[0], nt = sh[1];
     if (mt > 1 && mt / 2 >= m_tiles) continue;            // more than half of the rows idle
-    if (mt < 4 && m_tiles > 16) continue;
     const int groups = ((m_tiles + mt - 1) / mt) * ((N + 128 * nt - 1) / (128 * nt));
+    if (mt < 4 && groups > 2048) continue;                // not measured
     for (int n : counts) {
       if (n > 1 && (n > chunks || (size_t)n * m * N * 4 > kPartBytes || groups * n > 1024)) break;
       const int per = (chunks + n - 1) / n, splits = (chunks + per - 1) / per, wgs = groups * splits;
       const float share = std::min(1.f, wgs / 256.f);
       const float chunk = std::max(c0 + c1 * mt * nt + c2 * nt, 4.f * (mt + 8 * nt) / l2 * share);
-      float cost = (wgs + 255) / 256 * (per * chunk + out * mt * nt * share);
+      float cost = (wgs + 255) / 256 * (round + per * chunk + out * mt * nt * share);
       if (splits > 1) cost += split_launch + 8.f * splits * m * N / split_bytes;
       if (cost < best_cost) { best_cost = cost; best = TilePlan{mt, nt, n}; }
     }
