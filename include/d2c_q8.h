@@ -114,7 +114,8 @@ int d2c_q8_linear(d2c_q8* ctx, const void* a, int32_t m, const int8_t* codes, co
                   float* out, void* stream);
 
 /* Accumulated attention: weight[j] += sum_r floor(clamp(attn_avg[r, j], 0, 1) * 2^32) for j < L (NaN counts as 0).
- * attn_avg: float [m, L], as the attention calls leave it, m and L up to 2^24; the sums hold 2^31 such rows.  Whole numbers: the order of the sum does not matter. */
+ * attn_avg: float [m, L], as the attention calls leave it, m and L up to 2^24; the sums hold 2^31 such rows.  Whole numbers:
+ * the order of the sum does not matter. */
 int d2c_q8_weigh(d2c_q8* ctx, const float* attn_avg, int32_t m, int32_t L, int64_t* weight, void* stream);
 
 /* Keeps n_keep of the L rows of a cache: those of largest weight (negative ones count as 0), ties to the lowest index; rows

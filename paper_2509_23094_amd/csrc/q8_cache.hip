@@ -43,7 +43,8 @@ __device__ int lower_bound_wide(const int32_t* idx, int m, int limit) {
 // A workgroup per (block, kv head, K or V, sequence).  Its refreshed rows are found first: blocks are counted from the first refreshed
 // one where the rows are consecutive or many; few scattered rows get a workgroup each, of which the first of a block's does the block.
 // Rows and, where the scale moves, the old codes are then read once and the codes written once.
-// What bounds it: bytes for a whole prompt, the chain index -> rows -> maximum -> codes for a decode step.
+// What bounds it: bytes for a whole prompt (2500 rows of 32 heads of 128, bf16: 21 us, 61 MB), the chain index -> rows -> maximum -> codes for a
+// decode step (45 rows among 1823: 9.5 us).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void q8_update_kernel(UpdateArgs args, int Hkv) {
   using P = Pieces<D>;
@@ -179,6 +180,7 @@ __global__ __launch_bounds__(256) void q8_update_kernel(UpdateArgs args, int Hkv
 
 // A thread per (row, four dimensions of a kv head).  A workgroup's rows are neighbours, so that the four rows of a V piece, and the
 // pieces of K in one line, come from the L1.
+// What bounds it: bytes; 2500 rows of 32 heads of 128, bf16: 13.6 us, 61 MB.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void q8_read_kernel(Q8CachePtr c, int L, const int32_t* idx, int n, int Hkv, T* out_k, T* out_v) {
   const int r = blockIdx.x * (1024 / D) + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4, h = blockIdx.y;
@@ -208,6 +210,7 @@ __global__ __launch_bounds__(256) void q8_read_kernel(Q8CachePtr c, int L, const
 
 // Column sums of [m, L] in fixed point.  A workgroup takes 64 columns, its four waves every fourth of its rows.  Where several
 // workgroups share columns they add with integer atomics: any order gives the same sum.
+// What bounds it: launching and one or two latencies; 130 x 20001 5.0 us (10 MB).
 __global__ __launch_bounds__(256) void q8_weigh_kernel(const float* avg, int m, int L, int rows_per_wg, unsigned long long* weight) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = blockIdx.x * 64 + lane;
   const int r0 = blockIdx.y * rows_per_wg, r1 = min(m, r0 + rows_per_wg);
@@ -387,7 +390,7 @@ __global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* we
 }
 
 // Row i of dst is row kept[i] of src.  A workgroup per (block of dst, kv head, K or V): 16 KB read (V: more, its pieces hold four rows
-// of which some go), 8 KB written.
+// of which some go), 8 KB written.  What bounds it: the chain kept -> scales -> rows; 500 rows of 32 heads of 128 7.6 us, 9999 of 4 heads 10.3.
 template <int D>
 __global__ __launch_bounds__(256) void q8_compact_kernel(Q8CachePtr src, const int32_t* kept, int n, Q8CachePtr dst, int Hkv) {
   using P = Pieces<D>;
