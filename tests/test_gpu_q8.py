@@ -182,6 +182,17 @@ def test_indices_outside_are_left_out(L):
     c.check()
 
 
+@pytest.mark.parametrize("idx", ["all", "one before", "one behind", "gap"])
+def test_as_many_indices_as_rows(idx):
+    """More than a thousand indices, as many as there are rows: each in its place, or some left out and the others shifted."""
+    say(f"q8 as many indices as rows, {idx}")
+    L = 1300
+    c = Case("gqa", "bf16", L, capacity=L + 28).fill()
+    at = np.arange(L)
+    c.update({"all": at, "one before": at - 1, "one behind": at + 1, "gap": np.r_[at[:700], at[701:], [L + 3]]}[idx])
+    c.check()
+
+
 def test_batch_of_updates():
     say("q8 batch of 11 updates")
     first = Case("gqa", "bf16", 700, max_batch=11)
