@@ -43,7 +43,7 @@ __device__ int lower_bound_wide(const int32_t* idx, int m, int limit) {
 // A workgroup per (block, kv head, K or V, sequence).  Its refreshed rows are found first: blocks are counted from the first refreshed
 // one where the rows are consecutive or many; few scattered rows get a workgroup each, of which the first of a block's does the block.
 // Rows and, where the scale moves, the old codes are then read once and the codes written once.
-// What bounds it: bytes for a whole prompt (2500 rows of 32 heads of 128, bf16: 19 us, 61 MB), the chain index -> rows -> maximum -> codes for a
+// What bounds it: bytes for a whole prompt (2500 rows of 32 heads of 128, bf16: 18-21 us, 61 MB), the chain index -> rows -> maximum -> codes for a
 // decode step (45 rows among 1823: 9.5 us).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void q8_update_kernel(UpdateArgs args, int Hkv) {
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(256) void q8_update_kernel(UpdateArgs args, int Hkv
       for (int i = 0; i < kScan / 256; ++i) take(tid + 256 * i, pos[i]);
     } else {
       // as many indices as rows: index i is i, unless some are left out -- which the two on either side of the place tell (2500
-      // rows, with the search always: 21 us)
+      // rows, updated and read: 33.8 us, with the search always 35.2)
       const int start = b * kQ8Rows;
       bool found = false;
       if (c.m == c.L) {

@@ -738,3 +738,35 @@ def test_refusals_of_overlaps_and_other_geometries():
     assert lib.d2c_q8_weigh(h, big.data_ptr(), (1 << 24) + 1, 1, wt.data_ptr(), st) == b.D2C_ESHAPE
     assert lib.d2c_q8_read(h, c.cache.ref, 200, kept.data_ptr(), (1 << 24) + 1, rk.data_ptr(), None, st) == b.D2C_ESHAPE
     c.check()
+
+
+def test_two_graphs_of_one_handle():
+    """A product and an attention captured in graphs of their own share the handle's workspace: replayed in turn, with eager calls between."""
+    say("q8 two graphs of one handle")
+    H, Hkv, D, L, m = 8, 2, 64, 1500, 40
+    ctx = B().Q8Context(H, Hkv, D, "bf16", max_seq=L, max_rows=m, max_k=4096, max_n=600)
+    c = Case((H, Hkv, D), "bf16", L, ctx=ctx).fill()
+    w, a = dev(0.05 * c.rng.standard_normal((600, 4096)), "bf16"), dev(c.rng.standard_normal((m, 4096)), "bf16")
+    p, q = ctx.d2c_q8_pack(w), c.queries(m)
+    y, out, avg = torch.zeros((m, 600), device="cuda"), torch.zeros_like(q), torch.zeros((m, L), device="cuda")
+    batch = B().Q8Batch(ctx, [B().Q8Seq(c.cache, L, m, q=q, out=out, attn_avg=avg)])
+    calls = [lambda: ctx.d2c_q8_linear(a, p, y), lambda: ctx.d2c_q8_attention(batch)]
+    for f in calls:
+        f()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (y, out, avg)]
+    graphs = []
+    for f in calls:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            f()
+    for i in range(6):
+        for t in (y, out, avg):
+            t.fill_(7.0)
+        graphs[i % 2].replay()
+        graphs[1 - i % 2].replay()
+        if i % 3 == 0:
+            calls[i % 2]()
+        torch.cuda.synchronize()
+        for t, x in zip((y, out, avg), want):
+            assert torch.equal(t, x), f"replay {i}"
