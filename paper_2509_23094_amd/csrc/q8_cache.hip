@@ -261,13 +261,14 @@ __global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* we
   __shared__ uint32_t hist[2][2048], wave_sum[kKeepWaves], wave_bits[kKeepWaves], wave_up[kKeepWaves], wave_eq[kKeepWaves];
   __shared__ uint32_t found_bin, found_above, found_in;
   unsigned long long reg[PER ? PER : 1];                // weight, top bit: protected
-  // (through buffers that end with the arrays, which answer 0 past them: loads under a condition would come one after the other)
+  // (through buffers that end with the arrays, which answer 0 past them: loads under a condition would come one after the other.  The round
+  // is part of the vector offset, which is compared with the buffer's end; the compiler's documentation leaves a scalar offset out of that)
   const __amdgpu_buffer_rsrc_t w_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int64_t*>(weight), 0, L * 8, 0x00020000);
   const __amdgpu_buffer_rsrc_t p_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(protect), 0, PROTECT ? L : 0, 0x00020000);
   auto load = [&](int j) __attribute__((always_inline)) -> unsigned long long {
-    const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(w_rsrc, first * 8, j * 512, 0);
+    const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(w_rsrc, (first + 64 * j) * 8, 0, 0);
     uint32_t hi = (int)w[1] < 0 ? 0u : w[1], lo = (int)w[1] < 0 ? 0u : w[0];
-    if (PROTECT && __builtin_amdgcn_raw_buffer_load_b8(p_rsrc, first, j * 64, 0) != 0) hi |= 1u << 31;
+    if (PROTECT && __builtin_amdgcn_raw_buffer_load_b8(p_rsrc, first + 64 * j, 0, 0) != 0) hi |= 1u << 31;
     return (unsigned long long)hi << 32 | lo;
   };
   if constexpr (PER > 0) {
@@ -291,7 +292,8 @@ __global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* we
   // how many are protected, and how many bits each class's weights have
   uint32_t n_prot = 0;
   unsigned long long any[2] = {0, 0};
-  each([&](unsigned long long k, bool, int) {           // (what is not there is 0)
+  each([&](unsigned long long k, bool valid, int) {
+    k = valid ? k : 0ull;
     const unsigned long long p = PROTECT ? (unsigned long long)((long long)k >> 63) : 0ull;
     any[0] |= k & ~p;
     if (PROTECT) {

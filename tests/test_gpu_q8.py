@@ -770,3 +770,22 @@ def test_two_graphs_of_one_handle():
         torch.cuda.synchronize()
         for t, x in zip((y, out, avg), want):
             assert torch.equal(t, x), f"replay {i}"
+
+
+@pytest.mark.parametrize("L", [1, 65, 191, 1100, 5000, 20481])
+def test_evict_looks_at_nothing_behind_its_arrays(L):
+    """Weights and protection as views of longer arrays that hold large weights and protected rows behind them; what lies behind kept stays."""
+    say(f"q8 evict views L={L}")
+    c = Case((1, 1, 64), "bf16", L).fill()
+    w, p = weights(c.rng, L, "spread"), (c.rng.random(L) < 0.2).astype(np.uint8)
+    long_w = torch.full((L + 40000,), (1 << 63) - 1, dtype=torch.int64, device="cuda")
+    long_p = torch.full((L + 40000,), 255, dtype=torch.uint8, device="cuda")
+    long_w[:L], long_p[:L] = torch.from_numpy(w).cuda(), torch.from_numpy(p).cuda()
+    for n, q in ((1, None), ((L + 1) // 2, None), (L, None), (1, p), ((L + 1) // 2, p), (max(1, int(p.sum())), p), (L, p)):
+        kept = torch.full((n + 64,), -7, dtype=torch.int32, device="cuda")
+        kw = torch.full((n + 64,), -7, dtype=torch.int64, device="cuda")
+        c.ctx.d2c_q8_evict(c.cache, L, long_w[:L], None if q is None else long_p[:L], B().Q8Cache(c.ctx, n), kept[:n], kw[:n])
+        want = R.keep(w, q, n)
+        assert np.array_equal(kept[:n].cpu().numpy(), want), f"n={n}"
+        assert np.array_equal(kw[:n].cpu().numpy(), w[want])
+        assert (kept[n:] == -7).all() and (kw[n:] == -7).all()
