@@ -94,7 +94,8 @@ int d2c_q8_update(d2c_q8* ctx, const d2c_q8_seq* seqs, int32_t batch, void* stre
  * of its cache, no mask; sequences may share a cache that at most one of them refreshes.  Scores, softmax and sums are fp32.
  * q enters as fp16 pieces of a row scaled by a power of two, one for bf16 (exact down to 2^-32 of the row's largest
  * magnitude, to the nearest 2^-39 of it below), two for float (within 2^-23, or 2^-39 of the largest).  Probabilities are
- * rounded to 11 bits for bf16 and 22 for float, those below 2^-25 (2^-14) of a row's largest to the nearest 2^-35 of it. */
+ * rounded to 11 bits for bf16 and 22 for float, those below 2^-25 (float: 2^-18) of a row's largest to the nearest 2^-35
+ * (2^-39) of it. */
 int d2c_q8_attention(d2c_q8* ctx, const d2c_q8_seq* seqs, int32_t batch, void* stream);
 
 /* Values of cache rows: out_k / out_v T [n, d_kv] (either may be NULL) = rows idx[0 .. n) of the cache of L rows, or rows

@@ -9,8 +9,8 @@
 //   magnitude lies in [2^14, 2^15).  bf16's 8 bits fit in whole down to 2^-32 of the largest (below: to the nearest 2^-39 of it);
 //   float takes two pieces of 11 bits, which leave 2^-23 of each value and 2^-39 of the largest.  The product's scale (row, block and
 //   log2(e) / sqrt(D)) is applied to the fp32 score, V's scale when a block's O^T joins the running one.
-//   probabilities are rounded to fp16 (float: two pieces): 11 (22) bits down to 2^-25 (2^-14) of a row's largest, below that to
-//   the nearest 2^-35 of it; the running sum takes them before that rounding.
+//   probabilities are rounded to fp16 (float: two pieces): 11 (22) bits down to 2^-25 (2^-18) of a row's largest, below that to
+//   the nearest 2^-35 (2^-39) of it; the running sum takes them before that rounding.
 // The waves' maxima, sums and O^T are merged through LDS; where the key range is split over workgroups, by a second launch.
 // The head average has a pass of its own over the scores, from the same fp16 q and the final (maximum, sum) of every row.
 #include <algorithm>
@@ -27,8 +27,10 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kTile = 32;                 // query rows per workgroup
 constexpr int kWaves = 8;
-// Probabilities are rounded to fp16 times 2^kPBits, relative to a reference that a score may pass by kSlack: 2^15 at most.
-constexpr float kPBits = 11.f, kSlack = 4.f;
+// Probabilities are rounded to fp16 times 2^bits, relative to a reference that a score may pass by slack: 2^15 at most.  bf16 gives four bits
+// of the range for a reference that is seldom raised; float, whose second piece would be a subnormal number sooner, keeps them (32 heads of 128,
+// 256 x 2048 in float: 28.7 us, with bf16's 11 bits and slack 28.3).
+template <int QP> struct Base { static constexpr float bits = QP == 1 ? 11.f : 15.f, slack = 15.f - bits; };
 
 struct AttendSeq {
   Q8CachePtr c;
@@ -143,9 +145,10 @@ __device__ __forceinline__ void load_v(const uint8_t* v, u32x4 (&raw)[8]) {
 }
 
 // Scores of a block (`left` of its keys exist) -> probabilities in operand order.  o and l are relative to 2^ref; ref is raised only where
-// a score passes it by more than kSlack.
+// a score passes it by more than the slack.
 template <int QP, int DT>
 __device__ __forceinline__ void softmax_step(f32x16 (&x)[2], float ks, int left, float& ref, float& l, f32x16 (&o)[DT], h8 (&p)[QP][4]) {
+  constexpr float kSlack = Base<QP>::slack;
   const int g = (threadIdx.x & 63) >> 5;
   float top = -3.4e38f;
   if (left >= kQ8Rows) {
@@ -170,7 +173,7 @@ __device__ __forceinline__ void softmax_step(f32x16 (&x)[2], float ks, int left,
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
   }
-  const float base = kPBits - ref;
+  const float base = Base<QP>::bits - ref;
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -320,7 +323,7 @@ __global__ __launch_bounds__(64 * kWaves) void q8_attend_kernel(AttendArgs args)
     for (int j = 0; j < DT / 2; ++j) q8_store4(to + 4 * j, y + 4 * j);
   }
   if (s.avg && wave == 0 && g == 0 && split == 0)
-    args.row[slot] = make_float2(factor, to_m + log2f(sum) - kPBits);       // (the sum of a split row: the merge puts it right)
+    args.row[slot] = make_float2(factor, to_m + log2f(sum) - Base<QP>::bits);       // (the sum of a split row: the merge puts it right)
 }
 
 // Splits of a row joined.  A workgroup per row and head, a thread per (four dimensions, every kJoin-th split).  What bounds it: launching and
@@ -364,7 +367,7 @@ __global__ __launch_bounds__(kJoin * D / 4) void q8_join_kernel(AttendArgs args)
   y *= 1.f / sum;
   float z[4] = {y[0], y[1], y[2], y[3]};
   q8_store4((T*)s.out + (slot - s.row0) * D + 4 * t, z);
-  if (s.avg && t == 0) args.row[slot].y = ref + log2f(sum) - kPBits;
+  if (s.avg && t == 0) args.row[slot].y = ref + log2f(sum) - Base<sizeof(T) == 2 ? 1 : 2>::bits;
 }
 
 // attn_avg of 32 rows x one block of keys: the waves take a run of heads each and are added up at the end.  The next head's keys and

@@ -789,3 +789,32 @@ def test_evict_looks_at_nothing_behind_its_arrays(L):
         assert np.array_equal(kept[:n].cpu().numpy(), want), f"n={n}"
         assert np.array_equal(kw[:n].cpu().numpy(), w[want])
         assert (kept[n:] == -7).all() and (kw[n:] == -7).all()
+
+
+@pytest.mark.parametrize("L", [64, 700, 20001])
+def test_float_attention_beside_keys_that_take_nearly_all(L):
+    """One key of each block has a value of 0 and a score 20 to 26 bits above the others' 0: the output is what the far smaller probabilities,
+    all alike, leave of their bits.  A probability is rounded as two fp16 pieces times 2^15 of the row's largest: where the second is a
+    subnormal number, by at most half of 2^-24, that is 2^-40 of the largest, which is at most a block's share of the row's sum.  Of a
+    score's 64 products one is not 0."""
+    say(f"q8 attention float, small probabilities L={L}")
+    D, m = 64, 48
+    c = Case((1, 1, D), "f32", L, max_rows=m)
+    k, v = np.zeros((L, 1, D)), 1.0 + c.rng.random((L, 1, D))
+    k[::64, 0, 0], v[::64] = 3.0, 0.0
+    k, v = (dev(x, "f32").reshape(L, D) for x in (k, v))
+    c.update(None, m=L, new=((k, f64(k).reshape(L, 1, D)), (v, f64(v).reshape(L, 1, D))))
+    c.check()
+    q = np.zeros((m, D))
+    q[:, 0] = np.linspace(20, 26, m) * np.log(2) * np.sqrt(D) / 3
+    q, out, avg = attend(c, m, q=dev(q, "f32"))
+    vv = c.ref.v.values(L)
+    o, a, mag, _ = R.attention(f64(q).reshape(m, 1, D), c.ref.k.values(L), vv)
+    s = 26 * np.log(2)
+    share = ((1 + 4) * s + 6 * s + 8) * 2.0 ** -24             # as R.attention has it, of one product
+    below = 2.0 ** -40 * vv.sum(0)[None] / -(-L // 64)
+    tol = HALF["f32"] * o + (1 + HALF["f32"]) * (mag * (2 * share + P_HALF["f32"] + (L ** 0.5 + 70) * 2.0 ** -24) + below)
+    err = np.abs(f64(out).reshape(m, 1, D) - o)
+    assert (err <= tol).all(), "out: %g times the bound" % (err / tol).max()
+    err = np.abs(f64(avg) - a)
+    assert (err <= a * (2 * share + (L ** 0.5 + 17) * 2.0 ** -24)).all()
