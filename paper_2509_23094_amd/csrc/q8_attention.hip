@@ -32,6 +32,9 @@ constexpr int kWaves = 8;
 // 256 x 2048 in float: 28.7 us, with bf16's 11 bits and slack 28.3).
 template <int QP> struct Base { static constexpr float bits = QP == 1 ? 11.f : 15.f, slack = 15.f - bits; };
 
+// log2(e) / sqrt(D)
+template <int D> constexpr float kScore = 1.4426950408889634f / (D == 128 ? 11.313708498984761f : 8.f);
+
 struct AttendSeq {
   Q8CachePtr c;
   const void* q;
@@ -50,7 +53,7 @@ struct AttendArgs {
   float* part;                            // [split][slot][D]
   float2* ml;                             // [split][slot]: maximum (base 2), sum
   _Float16* q16;
-  float2* row;                            // [slot]: score factor of the row, log2 of its sum of exponentials
+  float2* row;                            // [slot]: 1 / (power of two on the row), log2 of its sum of exponentials
   size_t slots;                           // of the whole launch
 };
 
@@ -240,7 +243,8 @@ __global__ __launch_bounds__(64 * kWaves) void q8_attend_kernel(AttendArgs args)
   want_v(b0 + wave);
   h8 q[QP][D / 16];
   const float p2 = load_q<T, D, QP>((const T*)s.q + ((size_t)row * args.H + head) * D, q);
-  const float factor = 1.4426950408889634f / (sqrtf((float)D) * p2);
+  // a block's scores take ks * kScore * rp2, in this order: the row's power of two alone can be near the ends of the range (2^126 on tiny rows)
+  const float rp2 = 1.f / p2;
   if (s.avg && split == 0 && wave == 0 && valid) {
     _Float16* to = args.q16 + s.q16 + (((size_t)head * s.avg_tiles + row / kTile) * (QP * D / 16) * 64 + g * 32 + row % kTile) * 8;
 #pragma unroll
@@ -253,7 +257,7 @@ __global__ __launch_bounds__(64 * kWaves) void q8_attend_kernel(AttendArgs args)
   float ref = -INFINITY, l = 0.f;
   for (int b = b0 + wave; b < b1; b += kWaves) {
     if (QP > 1) want_k(b);
-    const float ks = ks_next * factor;
+    const float ks = ks_next * kScore<D> * rp2;
     f32x16 x[2];
     x[0] = scores<D, QP>(kr[0], q);
     x[1] = scores<D, QP>(kr[1], q);
@@ -323,7 +327,7 @@ __global__ __launch_bounds__(64 * kWaves) void q8_attend_kernel(AttendArgs args)
     for (int j = 0; j < DT / 2; ++j) q8_store4(to + 4 * j, y + 4 * j);
   }
   if (s.avg && wave == 0 && g == 0 && split == 0)
-    args.row[slot] = make_float2(factor, to_m + log2f(sum) - Base<QP>::bits);       // (the sum of a split row: the merge puts it right)
+    args.row[slot] = make_float2(rp2, to_m + log2f(sum) - Base<QP>::bits);       // (the sum of a split row: the merge puts it right)
 }
 
 // Splits of a row joined.  A workgroup per row and head, a thread per (four dimensions, every kJoin-th split).  What bounds it: launching and
@@ -413,7 +417,7 @@ __global__ __launch_bounds__(64 * kWaves) void q8_average_kernel(AttendArgs args
       ks = ks_next;
       want_k(min(h / G + 1, args.Hkv - 1));
     }
-    const float c = ks * rw.x, base = -rw.y;
+    const float c = ks * kScore<D> * rw.x, base = -rw.y;
     f32x16 x[2];
     x[0] = product<D, QP>(k[0], q);
     x[1] = product<D, QP>(k[1], q);

@@ -818,3 +818,17 @@ def test_float_attention_beside_keys_that_take_nearly_all(L):
     assert (err <= tol).all(), "out: %g times the bound" % (err / tol).max()
     err = np.abs(f64(avg) - a)
     assert (err <= a * (2 * share + (L ** 0.5 + 17) * 2.0 ** -24)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_size,k_size", [(1e-36, 1e36), (1e-38, 1e37), (1e30, 1e-30), (1e-30, 1e-6)])
+def test_attention_of_tiny_queries_on_huge_keys(dtype, q_size, k_size):
+    """Queries near the type's smallest numbers and keys that make ordinary scores of them, and the other way round."""
+    say(f"q8 attention {dtype} queries of {q_size}, keys of {k_size}")
+    c = Case("gqa", dtype, 200)
+    k, (dv, nv) = rows(c.rng, 200, c.Hkv, c.D) * k_size, c.new(200)
+    dk = dev(k, dtype).reshape(200, c.Hkv * c.D)
+    c.update(None, m=200, new=((dk, f64(dk).reshape(k.shape)), (dv, nv)))
+    c.check()
+    q, out, avg = attend(c, 9, q=c.queries(9, q_size))
+    c.expect(q, out, avg)
