@@ -10,7 +10,8 @@
  *   - no call but d2c_q8_init allocates, copies to the host or waits, so each can be captured into a HIP graph;
  *   - a handle is not thread-safe, and calls (or replays of graphs captured from calls) that share a handle must not
  *     overlap in time: they share its workspace.  d2c_q8_update, _read, _weigh, _evict and _pack use no workspace;
- *   - what a call writes must not overlap what it reads (but the caches that it refreshes) or other outputs;
+ *   - what a call writes must not overlap what it reads (but the caches that it refreshes, which it may read for other
+ *     sequences) or other outputs: refused with D2C_EINVAL, as far as the call's own sizes tell;
  *   - T is float (D2C_F32) or bfloat16 (D2C_BF16), as the handle's dtype says: queries, K/V rows, outputs, activations
  *     and the weights given to d2c_q8_pack;
  *   - pointers to T and to codes are multiples of 16 bytes, others of their element's size (D2C_EINVAL).

@@ -10,7 +10,14 @@
 
 using namespace d2c;
 
-constexpr int kMaxBatch = 256;
+constexpr int kMaxBatch = 256, kSeqBuffers = 10;
+
+// A buffer of a call: where it lies, and what the call does with it.  Calls may read a cache that they refresh for another sequence.
+enum Use { kReads, kWrites, kReadsCache, kRefreshes };
+struct Range {
+  uintptr_t at, end;
+  Use use;
+};
 
 struct d2c_q8 {
   d2c_q8_dims dims{};
@@ -18,6 +25,8 @@ struct d2c_q8 {
   int device = 0, max_batch = 1;
   void* ws = nullptr;            // shared by attention and linear: calls do not overlap
   int64_t ws_bytes = 0;
+  Range ranges[kMaxBatch * kSeqBuffers];   // of the call that is checked
+  int n_ranges = 0;
   char err[256] = {};
 };
 
@@ -38,17 +47,34 @@ int hip(d2c_q8* c, hipError_t e, const char* what) {
 }
 
 bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return a && b && x < y + nb && y < x + na;
+
+void add(d2c_q8* c, const void* p, size_t bytes, Use use) {
+  if (p && bytes) c->ranges[c->n_ranges++] = Range{(uintptr_t)p, (uintptr_t)p + bytes, use};
 }
-// any buffer of a cache of na rows with any of the same kind of one of nb rows
-bool caches_overlap(const d2c_q8* c, const d2c_q8_cache& a, int na, const d2c_q8_cache& b, int nb) {
-  const size_t block = (size_t)c->dims.n_kv_heads * D2C_Q8_BLOCK * c->dims.head_dim, scales = (size_t)c->dims.n_kv_heads * 4;
-  const size_t ca = q8_blocks(na) * block, cb = q8_blocks(nb) * block, sa = q8_blocks(na) * scales, sb = q8_blocks(nb) * scales;
-  return overlap(a.k_codes, ca, b.k_codes, cb) || overlap(a.v_codes, ca, b.v_codes, cb) || overlap(a.k_codes, ca, b.v_codes, cb) ||
-         overlap(a.v_codes, ca, b.k_codes, cb) || overlap(a.k_scale, sa, b.k_scale, sb) || overlap(a.v_scale, sa, b.v_scale, sb) ||
-         overlap(a.k_scale, sa, b.v_scale, sb) || overlap(a.v_scale, sa, b.k_scale, sb);
+void add_cache(d2c_q8* c, const d2c_q8_cache& k, int rows, Use use) {
+  const size_t codes = (size_t)q8_blocks(rows) * c->dims.n_kv_heads * D2C_Q8_BLOCK * c->dims.head_dim;
+  const size_t scales = (size_t)q8_blocks(rows) * c->dims.n_kv_heads * 4;
+  add(c, k.k_codes, codes, use);
+  add(c, k.v_codes, codes, use);
+  add(c, k.k_scale, scales, use);
+  add(c, k.v_scale, scales, use);
+}
+size_t row_bytes(const d2c_q8* c, int heads) { return (size_t)heads * c->dims.head_dim * (c->dims.dtype == D2C_BF16 ? 2 : 4); }
+// What is written must not overlap anything else of the call.  In the order of their addresses a buffer overlaps one before it if that
+// one, or any other of its use, ends behind its start.
+int check_overlap(d2c_q8* c) {
+  static constexpr bool kClash[4][4] = {{false, true, false, true}, {true, true, true, true}, {false, true, false, false}, {true, true, false, true}};
+  std::sort(c->ranges, c->ranges + c->n_ranges, [](const Range& a, const Range& b) { return a.at < b.at; });
+  uintptr_t end[4] = {};
+  for (int i = 0; i < c->n_ranges; ++i) {
+    const Range& r = c->ranges[i];
+    for (int u = 0; u < 4; ++u)
+      if (kClash[r.use][u] && end[u] > r.at)
+        return fail(c, D2C_EINVAL, r.use == kRefreshes && u == kRefreshes ? "buffers of the caches that the call refreshes overlap"
+                                                                          : "a buffer that the call writes overlaps another of its buffers");
+    end[r.use] = std::max(end[r.use], r.end);
+  }
+  return D2C_OK;
 }
 Q8CachePtr ptr(const d2c_q8_cache& c) { return Q8CachePtr{c.k_codes, c.v_codes, c.k_scale, c.v_scale}; }
 
@@ -71,6 +97,7 @@ int check_seqs(d2c_q8* c, const d2c_q8_seq* seqs, int batch, bool attend) {
   if (batch < 0 || (batch > 0 && !seqs)) return fail(c, D2C_EINVAL, "bad batch");
   if (batch > c->max_batch) return fail(c, D2C_ESHAPE, "batch exceeds max_batch of the handle");
   int64_t rows = 0;
+  c->n_ranges = 0;
   for (int i = 0; i < batch; ++i) {
     const d2c_q8_seq& s = seqs[i];
     if (s.m < 0) return fail(c, D2C_EINVAL, "m must not be negative");
@@ -83,20 +110,23 @@ int check_seqs(d2c_q8* c, const d2c_q8_seq* seqs, int batch, bool attend) {
       if (s.m > s.L) return fail(c, D2C_EINVAL, "more refreshed rows than L");
       if (!aligned(s.new_k, 16) || !aligned(s.new_v, 16) || !aligned(s.idx, 4))
         return fail(c, D2C_EINVAL, "new_k / new_v must be aligned to 16 bytes");
-      // two sequences of a call must not refresh one cache: their order is not defined
-      for (int j = 0; j < i; ++j)
-        if (seqs[j].m > 0 && seqs[j].new_k && caches_overlap(c, seqs[j].cache, seqs[j].L, s.cache, s.L))
-          return fail(c, D2C_EINVAL, "two sequences of the call refresh the same cache");
+      add(c, s.idx, (size_t)s.m * 4, kReads);
+      add(c, s.new_k, s.m * row_bytes(c, c->dims.n_kv_heads), kReads);
+      add(c, s.new_v, s.m * row_bytes(c, c->dims.n_kv_heads), kReads);
     }
+    add_cache(c, s.cache, s.L, s.new_k ? kRefreshes : kReadsCache);
     if (attend) {
       if (!s.q || !s.out) return fail(c, D2C_EINVAL, "null q or out");
       if (!aligned(s.q, 16) || !aligned(s.out, 16) || !aligned(s.attn_avg, 4))
         return fail(c, D2C_EINVAL, "q and out must be aligned to 16 bytes");
       rows += s.m;
+      add(c, s.q, s.m * row_bytes(c, c->dims.n_heads), kReads);
+      add(c, s.out, s.m * row_bytes(c, c->dims.n_heads), kWrites);
+      add(c, s.attn_avg, (size_t)s.m * s.L * 4, kWrites);
     }
   }
   if (rows > c->dims.max_rows) return fail(c, D2C_ESHAPE, "query rows exceed max_rows of the handle");
-  return D2C_OK;
+  return check_overlap(c);         // (two sequences must not refresh one cache: their order is not defined)
 }
 int do_update(d2c_q8* c, const d2c_q8_seq* seqs, int batch, hipStream_t st) {
   Q8Update u[kMaxBatch];
@@ -195,6 +225,12 @@ int d2c_q8_read(d2c_q8* c, const d2c_q8_cache* cache, int32_t L, const int32_t* 
   if (n > 1 << 24) return fail(c, D2C_ESHAPE, "more than 2^24 rows");
   if (!aligned(out_k, 16) || !aligned(out_v, 16) || !aligned(idx, 4)) return fail(c, D2C_EINVAL, "outputs must be aligned to 16 bytes");
   if (n == 0 || (!out_k && !out_v)) return D2C_OK;
+  c->n_ranges = 0;
+  add_cache(c, *cache, L, kReads);
+  add(c, idx, (size_t)n * 4, kReads);
+  add(c, out_k, n * row_bytes(c, c->dims.n_kv_heads), kWrites);
+  add(c, out_v, n * row_bytes(c, c->dims.n_kv_heads), kWrites);
+  if ((rc = check_overlap(c))) return rc;
   return hip(c, launch_q8_read(c->shape, ptr(*cache), L, idx, n, out_k, out_v, (hipStream_t)stream), "read");
 }
 
@@ -215,6 +251,11 @@ int d2c_q8_pack(d2c_q8* c, const void* w, int32_t N, int32_t K, int8_t* codes, f
   if (rc || (rc = check_linear(c, 0, N, K))) return rc;
   if (!w || !codes || !scale) return fail(c, D2C_EINVAL, "null buffer");
   if (!aligned(w, 16) || !aligned(codes, 16) || !aligned(scale, 4)) return fail(c, D2C_EINVAL, "w and codes must be aligned to 16 bytes");
+  c->n_ranges = 0;
+  add(c, w, (size_t)N * K * (c->dims.dtype == D2C_BF16 ? 2 : 4), kReads);
+  add(c, codes, (size_t)d2c_q8_weight_bytes(N, K), kWrites);
+  add(c, scale, (size_t)N * 4, kWrites);
+  if ((rc = check_overlap(c))) return rc;
   return hip(c, launch_q8_pack(c->dims.dtype, w, N, K, codes, scale, (hipStream_t)stream), "pack");
 }
 
@@ -228,8 +269,12 @@ int d2c_q8_linear(d2c_q8* c, const void* a, int32_t m, const int8_t* codes, cons
   if (!a || !codes || !scale || !out) return fail(c, D2C_EINVAL, "null buffer");
   if (!aligned(a, 16) || !aligned(codes, 16) || !aligned(scale, 4) || !aligned(out, 16))
     return fail(c, D2C_EINVAL, "a, codes and out must be aligned to 16 bytes");
-  // (workgroups read rows that others have finished)
-  if (overlap(a, (size_t)m * K * (c->dims.dtype == D2C_BF16 ? 2 : 4), out, (size_t)m * N * 4)) return fail(c, D2C_EINVAL, "out overlaps a");
+  c->n_ranges = 0;
+  add(c, a, (size_t)m * K * (c->dims.dtype == D2C_BF16 ? 2 : 4), kReads);
+  add(c, codes, (size_t)d2c_q8_weight_bytes(N, K), kReads);
+  add(c, scale, (size_t)N * 4, kReads);
+  add(c, out, (size_t)m * N * 4, kWrites);
+  if ((rc = check_overlap(c))) return rc;
   return hip(c, launch_q8_linear(c->dims.dtype, a, m, codes, scale, N, K, out, c->ws, (hipStream_t)stream), "linear");
 }
 
@@ -242,6 +287,10 @@ int d2c_q8_weigh(d2c_q8* c, const float* avg, int32_t m, int32_t L, int64_t* wei
   if (m == 0) return D2C_OK;
   if (!avg || !weight) return fail(c, D2C_EINVAL, "null buffer");
   if (!aligned(avg, 4) || !aligned(weight, 8)) return fail(c, D2C_EINVAL, "attn_avg or weight not aligned");
+  c->n_ranges = 0;
+  add(c, avg, (size_t)m * L * 4, kReads);
+  add(c, weight, (size_t)L * 8, kWrites);
+  if ((rc = check_overlap(c))) return rc;
   return hip(c, launch_q8_weigh(avg, m, L, weight, (hipStream_t)stream), "weigh");
 }
 
@@ -257,11 +306,14 @@ int d2c_q8_evict(d2c_q8* c, const d2c_q8_cache* src, int32_t L, const int64_t* w
   if ((rc = check_cache(c, *dst, n_keep))) return rc;
   if (!weight || !kept) return fail(c, D2C_EINVAL, "null buffer");
   if (!aligned(weight, 8) || !aligned(kept, 4) || !aligned(kept_weight, 8)) return fail(c, D2C_EINVAL, "weight or kept not aligned");
-  if (caches_overlap(c, *src, L, *dst, n_keep)) return fail(c, D2C_EINVAL, "dst overlaps src");
-  const size_t nl = (size_t)L, nk = (size_t)n_keep;
-  if (overlap(kept, nk * 4, weight, nl * 8) || overlap(kept, nk * 4, protect, nl) || overlap(kept, nk * 4, kept_weight, nk * 8) ||
-      overlap(kept_weight, nk * 8, weight, nl * 8) || overlap(kept_weight, nk * 8, protect, nl))
-    return fail(c, D2C_EINVAL, "kept or kept_weight overlaps another buffer of the call");
+  c->n_ranges = 0;
+  add_cache(c, *src, L, kReads);
+  add(c, weight, (size_t)L * 8, kReads);
+  add(c, protect, (size_t)L, kReads);
+  add_cache(c, *dst, n_keep, kWrites);
+  add(c, kept, (size_t)n_keep * 4, kWrites);
+  add(c, kept_weight, (size_t)n_keep * 8, kWrites);
+  if ((rc = check_overlap(c))) return rc;
   hipStream_t st = (hipStream_t)stream;
   if ((rc = hip(c, launch_q8_keep(weight, protect, L, n_keep, kept, kept_weight, st), "evict"))) return rc;
   return hip(c, launch_q8_compact(c->shape, ptr(*src), kept, n_keep, ptr(*dst), st), "evict");

@@ -832,3 +832,76 @@ def test_attention_of_tiny_queries_on_huge_keys(dtype, q_size, k_size):
     c.check()
     q, out, avg = attend(c, 9, q=c.queries(9, q_size))
     c.expect(q, out, avg)
+
+
+def test_what_is_written_must_not_overlap_anything():
+    """Every call whose output lies over an input or another output is refused, and nothing is written; neighbours are not."""
+    say("q8 overlaps")
+    b, L, m = B(), 200, 4
+    c = Case("gqa", "bf16", L, max_rows=300, max_batch=8).fill()
+    ctx, t = c.ctx, torch.bfloat16
+
+    def refused(f):
+        with pytest.raises(b.D2CError) as e:
+            f()
+        assert e.value.code == b.D2C_EINVAL and "overlap" in str(e.value)
+
+    def seq(cache=None, **kw):
+        q = c.queries(m)
+        args = dict(q=q, out=torch.zeros_like(q), attn_avg=torch.zeros((m, L), device="cuda")) | kw
+        return b.Q8Seq(cache or c.cache, L, m, **args)
+
+    attend_ = lambda *s: ctx.d2c_q8_attention(list(s))
+    (dk, _), (dv, _) = c.new(m), c.new(m)
+    idx = torch.arange(m, dtype=torch.int32, device="cuda")
+    fresh = dict(idx=idx, new_k=dk, new_v=dv)
+    first = seq()
+    refused(lambda: attend_(seq(q=first.q, out=first.q)))
+    refused(lambda: attend_(first, seq(out=first.out)))
+    refused(lambda: attend_(first, seq(attn_avg=first.attn_avg)))
+    refused(lambda: attend_(first, seq(out=first.q)))
+    refused(lambda: attend_(seq(attn_avg=torch.zeros(m * max(L, ctx.d_q), device="cuda")[: m * L].view(m, L), out=first.out), first))
+    over_k = c.cache.k_codes[: m * ctx.d_q * 2].view(t).view(m, ctx.d_q)
+    refused(lambda: attend_(seq(out=over_k)))
+    other = b.Q8Cache(ctx, L)
+    refused(lambda: attend_(seq(out=over_k, cache=other), seq(**fresh)))
+    refused(lambda: ctx.d2c_q8_update([seq(idx=idx, new_k=c.cache.v_codes[: m * ctx.d_kv * 2].view(t).view(m, ctx.d_kv), new_v=dv)]))
+    refused(lambda: ctx.d2c_q8_update([seq(idx=c.cache.k_scale.view(-1)[:m].view(torch.int32), new_k=dk, new_v=dv)]))
+    refused(lambda: ctx.d2c_q8_update([seq(**fresh), seq(**fresh)]))
+    both = b.Q8Cache(ctx, L)
+    both.c.v_codes = both.c.k_codes
+    refused(lambda: ctx.d2c_q8_update([seq(cache=both, **fresh)]))
+    rk, rv = (torch.zeros((m, ctx.d_kv), dtype=t, device="cuda") for _ in range(2))
+    refused(lambda: ctx.d2c_q8_read(c.cache, L, idx, rk, rk))
+    refused(lambda: ctx.d2c_q8_read(c.cache, L, idx, c.cache.v_codes[: m * ctx.d_kv * 2].view(t).view(m, ctx.d_kv), rv))
+    refused(lambda: ctx.d2c_q8_read(c.cache, L, rk.view(-1).view(torch.int32)[:m], rk, rv))
+    c.check()
+
+    lin = b.Q8Context(4, 4, 64, "f32", max_rows=300, max_k=64, max_n=64)
+    w, a = torch.ones((64, 64), device="cuda"), torch.ones((64, 64), device="cuda")
+    p = lin.d2c_q8_pack(w)
+    refused(lambda: lin.d2c_q8_linear(a, p, a))
+    refused(lambda: lin.d2c_q8_linear(a[:16], p, p.codes.view(torch.float32).view(16, 64)))
+    refused(lambda: lin.d2c_q8_linear(a[:1], p, p.scale.view(1, 64)))
+    rc = b._lib.d2c_q8_pack(lin.handle, w.data_ptr(), 64, 64, w.data_ptr(), p.scale.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert rc == b.D2C_EINVAL and (w == 1).all() and (a == 1).all()
+
+    weight, kept = torch.zeros(L, dtype=torch.int64, device="cuda"), torch.zeros(50, dtype=torch.int32, device="cuda")
+    kw, dst = torch.zeros(50, dtype=torch.int64, device="cuda"), b.Q8Cache(ctx, 50)
+    refused(lambda: ctx.d2c_q8_weigh(weight.view(torch.float32)[:L].view(1, L), weight))
+    refused(lambda: ctx.d2c_q8_evict(c.cache, L, weight, None, dst, c.cache.k_codes[:200].view(torch.int32), kw))
+    refused(lambda: ctx.d2c_q8_evict(c.cache, L, weight, None, dst, dst.k_codes[:200].view(torch.int32), kw))
+    refused(lambda: ctx.d2c_q8_evict(c.cache, L, weight, None, dst, kept, c.cache.v_codes[:400].view(torch.int64)))
+    c.check()
+    assert not weight.any() and not kept.any() and (dst.k_codes == 128).all()
+
+    # neighbours in one allocation, a shared input, and a cache that others read are no overlap
+    both = torch.zeros((4 * m, ctx.d_q), dtype=t, device="cuda")
+    both[: 2 * m] = c.queries(2 * m)
+    s = [seq(q=both[:m], out=both[2 * m: 3 * m]), seq(q=both[m: 2 * m], out=both[3 * m:]), seq(q=both[:m], **fresh)]
+    attend_(*s)
+    ref = c.ref
+    ref.update(np.arange(m), f64(dk).reshape(m, c.Hkv, c.D), f64(dv).reshape(m, c.Hkv, c.D), L)
+    c.check()
+    for x in s:
+        c.expect(x.q, x.out, x.attn_avg)
