@@ -68,7 +68,8 @@ typedef struct {
   const void* new_v;
   const void* q;         /* T [m, d_q]                                    (d2c_q8_attention)    */
   void*  out;            /* T [m, d_q]                                    (d2c_q8_attention)    */
-  float* attn_avg;       /* [m, L] mean over the heads of the softmax rows, or NULL (as above)  */
+  float* attn_avg;       /* [m, L] mean over the heads of the softmax rows, or NULL (as above);
+                            a call's averages have fewer than 2^23 tiles of 32 rows x 64 keys   */
   int32_t m, L;          /* (host) m = 0 is legal and leaves the sequence alone                 */
 } d2c_q8_seq;
 

@@ -96,7 +96,7 @@ int check_cache(d2c_q8* c, const d2c_q8_cache& k, int L) {
 int check_seqs(d2c_q8* c, const d2c_q8_seq* seqs, int batch, bool attend) {
   if (batch < 0 || (batch > 0 && !seqs)) return fail(c, D2C_EINVAL, "bad batch");
   if (batch > c->max_batch) return fail(c, D2C_ESHAPE, "batch exceeds max_batch of the handle");
-  int64_t rows = 0;
+  int64_t rows = 0, tiles = 0;
   c->n_ranges = 0;
   for (int i = 0; i < batch; ++i) {
     const d2c_q8_seq& s = seqs[i];
@@ -120,12 +120,15 @@ int check_seqs(d2c_q8* c, const d2c_q8_seq* seqs, int batch, bool attend) {
       if (!aligned(s.q, 16) || !aligned(s.out, 16) || !aligned(s.attn_avg, 4))
         return fail(c, D2C_EINVAL, "q and out must be aligned to 16 bytes");
       rows += s.m;
+      if (s.attn_avg) tiles += (int64_t)((s.m + 31) / 32) * q8_blocks(s.L);
       add(c, s.q, s.m * row_bytes(c, c->dims.n_heads), kReads);
       add(c, s.out, s.m * row_bytes(c, c->dims.n_heads), kWrites);
       add(c, s.attn_avg, (size_t)s.m * s.L * 4, kWrites);
     }
   }
   if (rows > c->dims.max_rows) return fail(c, D2C_ESHAPE, "query rows exceed max_rows of the handle");
+  // a workgroup of 512 for each of these, and a launch holds fewer than 2^32 threads
+  if (tiles >= 1 << 23) return fail(c, D2C_ESHAPE, "the averages of the call have 2^23 or more tiles of 32 rows x 64 keys");
   return check_overlap(c);         // (two sequences must not refresh one cache: their order is not defined)
 }
 int do_update(d2c_q8* c, const d2c_q8_seq* seqs, int batch, hipStream_t st) {

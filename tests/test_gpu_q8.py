@@ -905,3 +905,19 @@ def test_what_is_written_must_not_overlap_anything():
     c.check()
     for x in s:
         c.expect(x.q, x.out, x.attn_avg)
+
+
+def test_averages_of_more_tiles_than_a_launch_has_room_for_are_refused():
+    """2^23 workgroups of 512 threads do not fit a launch: refused before anything is looked at (the sizes are claimed, no such buffer is)."""
+    say("q8 averages too large")
+    b = B()
+    ctx = b.Q8Context(1, 1, 64, "bf16", max_seq=1 << 24, max_rows=1 << 12, max_batch=2)
+    cache, x = b.Q8Cache(ctx, 64), torch.zeros(1024, device="cuda")
+    st, p = torch.cuda.current_stream().cuda_stream, x.data_ptr()
+    for sizes in ([(1 << 10, 1 << 24)], [(1 << 10, (1 << 23) + 1), (993, 1 << 23)], [(1, 1 << 24), (1 << 11, 1 << 23)]):
+        arr = (b.d2c_q8_seq * len(sizes))()
+        for s, (m, L) in zip(arr, sizes):
+            s.cache, s.q, s.out, s.attn_avg, s.m, s.L = cache.c, p, p, p, m, L
+        assert b._lib.d2c_q8_attention(ctx.handle, arr, len(sizes), st) == b.D2C_ESHAPE
+        assert b"tiles" in b._lib.d2c_q8_last_error(ctx.handle)
+    assert not x.any()
