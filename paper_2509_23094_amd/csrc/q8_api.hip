@@ -238,7 +238,7 @@ int d2c_q8_read(d2c_q8* c, const d2c_q8_cache* cache, int32_t L, const int32_t* 
 }
 
 int64_t d2c_q8_weight_bytes(int32_t N, int32_t K) {
-  return N <= 0 || K <= 0 ? 0 : (int64_t)((N + 15) / 16 * 16) * q8_kpad(K);
+  return N <= 0 || K <= 0 ? 0 : ((int64_t)N + 15) / 16 * 16 * (((int64_t)K + 63) / 64 * 64);
 }
 
 static int check_linear(d2c_q8* c, int m, int N, int K) {

@@ -142,3 +142,11 @@ def test_keep_orders_protected_weight_and_index():
     assert list(R.keep([5, 9, 5, 1], [0, 0, 0, 1], 2)) == [1, 3]
     assert list(R.keep([5, 9, 5, 1], [1, 0, 1, 1], 2)) == [0, 2]
     assert list(R.keep([-3, 0, -1], None, 2)) == [0, 1]
+
+
+@built
+def test_weight_bytes_of_the_largest_sizes():
+    from paper_2509_23094_amd import binding as B
+    big = (1 << 31) - 1
+    for N, K in ((big, 8), (1, big), (big, big), (1 << 20, 1 << 16)):
+        assert B._lib.d2c_q8_weight_bytes(N, K) == -(-N // 16) * 16 * (-(-K // 64) * 64)
