@@ -75,7 +75,7 @@ typedef struct {
 
 int d2c_q8_init(const d2c_q8_dims* dims, d2c_q8** out);
 int d2c_q8_destroy(d2c_q8* ctx);
-/* Text of the last error of this handle (or of d2c_q8_init when ctx is NULL). */
+/* Text of the last error of this handle (ctx NULL: of this thread's last d2c_q8_init that failed). */
 const char* d2c_q8_last_error(const d2c_q8* ctx);
 /* Bytes of device workspace the handle holds. */
 int64_t d2c_q8_workspace_bytes(const d2c_q8* ctx);

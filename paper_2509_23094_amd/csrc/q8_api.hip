@@ -32,7 +32,7 @@ struct d2c_q8 {
 
 namespace {
 
-char g_err[256] = {};
+thread_local char g_err[256] = {};     // of this thread's last d2c_q8_init
 
 // Text without allocation: nothing here can throw.
 int fail(d2c_q8* c, int code, const char* msg, const char* more = "") {

@@ -150,3 +150,24 @@ def test_weight_bytes_of_the_largest_sizes():
     big = (1 << 31) - 1
     for N, K in ((big, 8), (1, big), (big, big), (1 << 20, 1 << 16)):
         assert B._lib.d2c_q8_weight_bytes(N, K) == -(-N // 16) * 16 * (-(-K // 64) * 64)
+
+
+@built
+def test_init_errors_of_two_threads_keep_apart():
+    """The text of a failed d2c_q8_init belongs to the thread that called it."""
+    import threading
+    from paper_2509_23094_amd import binding as B
+
+    def fail(field, value):
+        d, out = B.d2c_q8_dims(4, 4, 64, B.D2C_BF16, 128, 16, 1, 0, 0), ctypes.c_void_p()
+        setattr(d, field, value)
+        assert B._lib.d2c_q8_init(ctypes.byref(d), ctypes.byref(out)) < 0
+        return B._lib.d2c_q8_last_error(None)
+
+    mine, seen = fail("head_dim", 96), []
+    assert b"head_dim" in mine
+    other = threading.Thread(target=lambda: seen.append((B._lib.d2c_q8_last_error(None), fail("dtype", 7))))
+    other.start()
+    other.join()
+    assert seen[0][0] == b"" and b"dtype" in seen[0][1]
+    assert B._lib.d2c_q8_last_error(None) == mine
