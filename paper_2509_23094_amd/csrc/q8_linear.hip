@@ -417,6 +417,7 @@ __global__ __launch_bounds__(512, 1) void q8_tile_kernel(const int8_t* a, const 
     }
   const int row_base = mt0 * 16, col_base = cg * 8 * NT * 16;
   int* to = (part ? part + (size_t)split * m * N : (int*)out) + (size_t)row_base * N + col_base;
+  const bool whole = N % 4 == 0 && ((uintptr_t)to & 15) == 0;              // four outputs of a row are 16 aligned bytes
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
     int* o = (int*)(lds + (t & 1) * kOut);
@@ -439,7 +440,7 @@ __global__ __launch_bounds__(512, 1) void q8_tile_kernel(const int8_t* a, const 
       if (row_base + t * 16 + row >= m || col_base + col >= N) continue;
       const i32x4 y = *reinterpret_cast<const i32x4*>(o + row * kPitch + col);
       int* at = to + (size_t)(t * 16 + row) * N + col;
-      if (N % 4 == 0) {
+      if (whole) {
         *reinterpret_cast<i32x4*>(at) = y;
       } else {
 #pragma unroll

@@ -921,3 +921,18 @@ def test_averages_of_more_tiles_than_a_launch_has_room_for_are_refused():
         assert b._lib.d2c_q8_attention(ctx.handle, arr, len(sizes), st) == b.D2C_ESHAPE
         assert b"tiles" in b._lib.d2c_q8_last_error(ctx.handle)
     assert not x.any()
+
+
+@pytest.mark.parametrize("m,N,K", [(5, 768, 256), (20, 512, 4096), (37, 256, 4096), (300, 512, 256), (100, 1000, 512)])
+def test_linear_into_outputs_of_any_alignment(m, N, K):
+    """out is float: any multiple of 4 bytes will do."""
+    say(f"q8 linear out anywhere m={m} N={N} K={K}")
+    rng = np.random.default_rng([m, N, K])
+    a, w = dev(rng.standard_normal((m, K)), "bf16"), dev(rng.standard_normal((N, K)), "bf16")
+    ctx = B().Q8Context(4, 4, 64, "bf16", max_rows=m, max_k=K, max_n=N)
+    p, want = ctx.d2c_q8_pack(w), R.linear(f64(a), f64(w))[0]
+    for shift in (0, 1, 2, 3):
+        room = torch.full((m * N + 8,), 5.0, device="cuda")
+        ctx.d2c_q8_linear(a, p, room[shift: shift + m * N].view(m, N))
+        assert np.array_equal(room[shift: shift + m * N].view(m, N).cpu().numpy(), want)
+        assert (room[:shift] == 5.0).all() and (room[shift + m * N:] == 5.0).all()
