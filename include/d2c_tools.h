@@ -72,6 +72,12 @@ int d2c_ctx_set_tunable(d2c_ctx* ctx, const char* name, int32_t value);
  * Returns D2C_EINVAL for a null pointer, a dtype other than D2C_F32 / D2C_BF16 or non-positive sizes. */
 int d2c_plan_projection(int32_t dtype, int32_t m, int32_t N, int32_t K, int32_t single_split, int32_t shape[7]);
 
+/* The same for d2c_q8_linear (include/d2c_q8.h) of m rows with weights [N, K], as shape[0..4] = kernel (0: one launch, 1: weights
+ * streamed past up to two tiles of rows, 2: tiles of rows and columns), row tiles per workgroup, column tiles per wave
+ * (kernel 1: per workgroup), waves per workgroup, splits of the contraction.  D2C_EINVAL for a null pointer or sizes that
+ * d2c_q8_linear refuses whatever the handle. */
+int d2c_q8_plan_linear(int32_t m, int32_t N, int32_t K, int32_t shape[5]);
+
 /* Device memory the context holds, in bytes: bytes[0] everything, bytes[1] of which the pre-tiled weight
  * copies, bytes[2] head averages / per-head probability rows / rollout scratch, bytes[3] attention partials. */
 int d2c_memory_info(const d2c_ctx* ctx, int64_t bytes[4]);

@@ -78,7 +78,7 @@ class d2c_q8_seq(C.Structure):
 EXPORTS = ["d2c_init", "d2c_destroy", "d2c_last_error", "d2c_seq_reset", "d2c_select", "d2c_refresh_layer",
            "d2c_attention", "d2c_influence", "d2c_linear", "d2c_step", "d2c_workspace_bytes", "d2c_select_static"]
 TOOL_EXPORTS = ["d2c_profile_begin", "d2c_profile_end", "d2c_init_tuned", "d2c_ctx_set_tunable",
-                "d2c_plan_projection", "d2c_memory_info"]
+                "d2c_plan_projection", "d2c_q8_plan_linear", "d2c_memory_info"]
 # include/d2c_q8.h (the 8-bit operators)
 Q8_EXPORTS = ["d2c_q8_init", "d2c_q8_destroy", "d2c_q8_last_error", "d2c_q8_workspace_bytes", "d2c_q8_cache_size",
               "d2c_q8_update", "d2c_q8_attention", "d2c_q8_read", "d2c_q8_weight_bytes", "d2c_q8_pack", "d2c_q8_linear",
@@ -115,6 +115,7 @@ def load_library() -> C.CDLL:
     lib.d2c_ctx_set_tunable.argtypes = [vp, C.c_char_p, i32]
     lib.d2c_memory_info.argtypes = [vp, C.POINTER(C.c_int64)]
     lib.d2c_plan_projection.argtypes = [i32, i32, i32, i32, i32, C.POINTER(i32)]
+    lib.d2c_q8_plan_linear.argtypes = [i32, i32, i32, C.POINTER(i32)]
     i64 = C.c_int64
     lib.d2c_q8_init.argtypes = [C.POINTER(d2c_q8_dims), C.POINTER(vp)]
     lib.d2c_q8_destroy.argtypes = [vp]
@@ -171,6 +172,15 @@ def d2c_plan_projection(dtype: str, m: int, N: int, K: int, single_split: bool =
         raise D2CError(rc, "d2c_plan_projection: bad arguments")
     return dict(zip(("row_tiles", "col_tiles_per_wave", "waves", "splits", "k_per_split", "row_chunks", "workgroups"),
                     [int(x) for x in shape]))
+
+
+def d2c_q8_plan_linear(m: int, N: int, K: int) -> Dict[str, int]:
+    """Launch shape of d2c_q8_linear for m rows of a [N, K] matrix (host arithmetic, no GPU)."""
+    shape = (C.c_int32 * 5)()
+    rc = _lib.d2c_q8_plan_linear(int(m), int(N), int(K), shape)
+    if rc != 0:
+        raise D2CError(rc, "d2c_q8_plan_linear: bad arguments")
+    return dict(zip(("kernel", "row_tiles", "col_tiles", "waves", "splits"), [int(x) for x in shape]))
 
 
 def make_params(sigma=10.0, k=32, p=0.1, block_len=32, n_unmask=1, cand_mode=0, threshold=0.0, conf_decode=0,

@@ -42,6 +42,10 @@ size_t q8_attention_bytes(const Q8Shape& s, int max_rows, int max_batch);
 // calls with m > 0; max_rows and max_batch as the workspace was sized for
 hipError_t launch_q8_attention(const Q8Shape& s, const Q8Attend* calls, int n, int max_rows, int max_batch, void* ws, hipStream_t st);
 
+// How a product is launched: in one launch, or its rows rounded first and the product by weights streamed past few rows or by tiles
+enum { kQ8Small = 0, kQ8Stream = 1, kQ8Tile = 2 };
+struct Q8LinearPlan { int kernel, mt, nt, waves, splits; };   // row tiles per workgroup, column tiles per wave; waves of a workgroup, splits of the contraction
+Q8LinearPlan q8_plan_linear(int m, int N, int K);
 inline int q8_kpad(int K) { return (K + 63) & ~63; }
 // bytes of workspace for products of up to max_rows rows and contractions of up to max_k
 size_t q8_linear_bytes(int max_rows, int max_k);

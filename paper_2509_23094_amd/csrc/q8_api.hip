@@ -6,6 +6,7 @@
 #include <new>
 
 #include "../../include/d2c_q8.h"
+#include "../../include/d2c_tools.h"
 #include "q8.h"
 
 using namespace d2c;
@@ -245,6 +246,17 @@ static int check_linear(d2c_q8* c, int m, int N, int K) {
   if (m < 0 || N <= 0 || K <= 0) return fail(c, D2C_EINVAL, "bad m, N or K");
   if (N > 1 << 20 || K > 1 << 16) return fail(c, D2C_ESHAPE, "N or K too large");
   if (K % (c->dims.dtype == D2C_BF16 ? 8 : 4)) return fail(c, D2C_ESHAPE, "K must be a multiple of 16 bytes of T");
+  return D2C_OK;
+}
+
+int d2c_q8_plan_linear(int32_t m, int32_t N, int32_t K, int32_t shape[5]) {
+  if (!shape || m <= 0 || m > 1 << 16 || N <= 0 || N > 1 << 20 || K <= 0 || K > 1 << 16) return D2C_EINVAL;
+  const Q8LinearPlan p = q8_plan_linear(m, N, K);
+  shape[0] = p.kernel;
+  shape[1] = p.mt;
+  shape[2] = p.nt;
+  shape[3] = p.waves;
+  shape[4] = p.splits;
   return D2C_OK;
 }
 

@@ -463,13 +463,16 @@ hipError_t sum_parts(const Operands& o, int splits, hipStream_t st) {
   q8_sum_kernel<<<dim3(o.m, (o.N + 255) / 256), 256, 0, st>>>(o.part, splits, o.sa, o.sw, o.m, o.N, o.out);
   return hipGetLastError();
 }
-template <int MT, int NT, int WAVES>
-hipError_t stream(const Operands& o, hipStream_t st) {
-  const int groups = ((o.N + 15) / 16 + NT - 1) / NT;
-  // splits: a workgroup for each compute unit, while each wave has two steps and more and the parts have room
+// splits: a workgroup for each compute unit, while each wave has two steps and more and the parts have room
+int plan_stream(int m, int N, int kc, int nt, int waves) {
+  const int groups = ((N + 15) / 16 + nt - 1) / nt;
   int splits = 1;
-  while (groups * splits * 2 <= 256 && o.kc / (2 * splits) >= 2 * WAVES && (size_t)2 * splits * o.m * o.N * 4 <= kPartBytes) splits *= 2;
-  const int per = (o.kc + splits - 1) / splits;
+  while (groups * splits * 2 <= 256 && kc / (2 * splits) >= 2 * waves && (size_t)2 * splits * m * N * 4 <= kPartBytes) splits *= 2;
+  return splits;
+}
+template <int MT, int NT, int WAVES>
+hipError_t stream(const Operands& o, int splits, hipStream_t st) {
+  const int groups = ((o.N + 15) / 16 + NT - 1) / NT, per = (o.kc + splits - 1) / splits;
   q8_stream_kernel<MT, NT, WAVES><<<dim3(groups, splits), 64 * WAVES, 0, st>>>(o.a, o.sa, o.w, o.sw, o.m, o.N, o.kc, o.ka, per, o.out,
                                                                                 splits > 1 ? o.part : nullptr);
   const hipError_t e = hipGetLastError();
@@ -479,7 +482,6 @@ template <int MT, int NT>
 hipError_t tile(const Operands& o, int splits, hipStream_t st) {
   const int rows = 16 * MT, cols = 128 * NT, rg = (o.m + rows - 1) / rows, cg = (o.N + cols - 1) / cols, chunks = o.ka / kStepsPerChunk;
   const int per = (chunks + splits - 1) / splits;
-  splits = (chunks + per - 1) / per;                  // none empty
   const int per_xcd = (rg * cg * splits + 7) / 8;
   q8_tile_kernel<MT, NT><<<8 * per_xcd, 512, 0, st>>>(o.a, o.sa, o.w, o.sw, o.m, o.N, o.kc, o.ka, per, rg, cg, splits, o.out,
                                                       splits > 1 ? o.part : nullptr);
@@ -492,13 +494,12 @@ hipError_t tile(const Operands& o, int splits, hipStream_t st) {
 // c2 NT, and as long as its bytes take from the L2 where all compute units pull; then its outputs' way to memory.  Splits cost a
 // launch and the parts' way out and in.  What it picks is 1.0 % behind the best on average, 16 % at most; always taking MT = 8, NT = 2
 // without splits is 50 % behind at 128 rows and more.
-struct TilePlan { int mt, nt, splits; };
-TilePlan plan_tile(int m, int N, int ka) {
+Q8LinearPlan plan_tile(int m, int N, int ka) {
   constexpr float round = 0.83f, c0 = 0.29f, c1 = 0.09f, c2 = 0.04f, l2 = 120.f, out = 0.55f, split_launch = 2.7f, split_bytes = 5.5e6f;
   static constexpr int8_t shapes[][2] = {{1, 1}, {2, 1}, {3, 1}, {4, 1}, {6, 1}, {8, 1}, {4, 2}, {6, 2}, {8, 2}, {8, 3}};
   static constexpr int8_t counts[] = {1, 2, 3, 4, 6, 8, 12};
   const int chunks = ka / kStepsPerChunk, m_tiles = (m + 15) / 16;
-  TilePlan best{8, 2, 1};
+  Q8LinearPlan best{kQ8Tile, 8, 2, 8, 1};
   float best_cost = 1e30f;
   for (const auto& sh : shapes) {
     const int mt = sh[0], nt = sh[1];
@@ -512,12 +513,12 @@ TilePlan plan_tile(int m, int N, int ka) {
       const float chunk = std::max(c0 + c1 * mt * nt + c2 * nt, 4.f * (mt + 8 * nt) / l2 * share);
       float cost = (wgs + 255) / 256 * (round + per * chunk + out * mt * nt * share);
       if (splits > 1) cost += split_launch + 8.f * splits * m * N / split_bytes;
-      if (cost < best_cost) { best_cost = cost; best = TilePlan{mt, nt, n}; }
+      if (cost < best_cost) { best_cost = cost; best = Q8LinearPlan{kQ8Tile, mt, nt, 8, splits}; }
     }
   }
   return best;
 }
-hipError_t run_tile(const Operands& o, const TilePlan& p, hipStream_t st) {
+hipError_t run_tile(const Operands& o, const Q8LinearPlan& p, hipStream_t st) {
   if (p.nt == 3) return tile<8, 3>(o, p.splits, st);
   if (p.nt == 2) return p.mt == 4 ? tile<4, 2>(o, p.splits, st) : p.mt == 6 ? tile<6, 2>(o, p.splits, st) : tile<8, 2>(o, p.splits, st);
   switch (p.mt) {
@@ -560,13 +561,29 @@ hipError_t launch_q8_pack(int dtype, const void* w, int N, int K, int8_t* codes,
   return launch_rows(dtype, w, N, K, q8_kpad(K) / 64, codes, scale, st);
 }
 
-hipError_t launch_q8_linear(int dtype, const void* a, int m, const int8_t* codes, const float* scale, int N, int K, float* out,
-                            void* ws, hipStream_t st) {
+Q8LinearPlan q8_plan_linear(int m, int N, int K) {
   const int kc = q8_kpad(K) / 64, ka = (kc + 3) & ~3, m_tiles = (m + 15) / 16, n_tiles = (N + 15) / 16;
   // One launch; every workgroup rounds the rows again, so only up to three workgroups for two compute units.  In a captured loop of calls, us, one
   // launch and two: 5 x 768 x 256 3.9 and 5.4, 16 x 4096 x 1024 5.5 and 6.9, 16 x 4096 x 2048 7.2 and 8.1, 16 x 6144 x 1024 7.2 and 7.4,
   // 16 x 8192 x 2048 10.3 and 9.5 (two tiles of rows in one launch: 32 x 768 x 256 6.1 and 6.4, 32 x 2048 x 1024 7.2 and 6.8).
-  if (m_tiles == 1 && kc <= 32 && n_tiles <= 384)
+  if (m_tiles == 1 && kc <= 32 && n_tiles <= 384) return Q8LinearPlan{kQ8Small, 1, 1, 16, 1};
+  // Up to two tiles of rows the activations come along from the L2 without weighing (a call of 1 x 3584 x 18944 18.3 us, through tiles
+  // 19.9; 31 x 4096 x 12288 18.2 and 19.0); from three on a compute unit pulls more of them than of weights (37 x 3584 x 18944 25.4 and
+  // 23.3, 63 x 12288 x 4096 21.2 and 17.6).
+  if (m <= kStreamRows) {
+    // Two column tiles a workgroup where that leaves a workgroup for each compute unit (2 x 12288 x 4096 15.1 us, with one 15.9, 18 x 14851
+    // x 984 11.0 and 12.5; 31 x 4096 x 12288 22.6, with one 18.2)
+    const int nt = n_tiles >= 512 ? 2 : 1, waves = nt == 2 ? 8 : 16;
+    return Q8LinearPlan{kQ8Stream, m_tiles, nt, waves, plan_stream(m, N, kc, nt, waves)};
+  }
+  return plan_tile(m, N, ka);
+}
+
+hipError_t launch_q8_linear(int dtype, const void* a, int m, const int8_t* codes, const float* scale, int N, int K, float* out,
+                            void* ws, hipStream_t st) {
+  const int kc = q8_kpad(K) / 64, ka = (kc + 3) & ~3, m_tiles = (m + 15) / 16;
+  const Q8LinearPlan plan = q8_plan_linear(m, N, K);
+  if (plan.kernel == kQ8Small)
     return dtype == kBF16 ? small((const bf16*)a, m, codes, scale, N, K, kc, out, st)
                           : small((const float*)a, m, codes, scale, N, K, kc, out, st);
   char* p = (char*)ws;
@@ -577,17 +594,9 @@ hipError_t launch_q8_linear(int dtype, const void* a, int m, const int8_t* codes
   const hipError_t e = launch_rows(dtype, a, m, K, ka, qa, sa, st);
   if (e != hipSuccess) return e;
   const Operands o{qa, sa, codes, scale, m, N, kc, ka, out, (int*)p};
-  // Up to two tiles of rows the activations come along from the L2 without weighing (a call of 1 x 3584 x 18944 18.3 us, through tiles
-  // 19.9; 31 x 4096 x 12288 18.2 and 19.0); from three on a compute unit pulls more of them than of weights (37 x 3584 x 18944 25.4 and
-  // 23.3, 63 x 12288 x 4096 21.2 and 17.6).
-  if (m <= kStreamRows) {
-    // Two column tiles a workgroup where that leaves a workgroup for each compute unit (2 x 12288 x 4096 15.1 us, with one 15.9, 18 x 14851
-    // x 984 11.0 and 12.5; 31 x 4096 x 12288 22.6, with one 18.2)
-    const bool two = n_tiles >= 512;
-    if (m_tiles == 1) return two ? stream<1, 2, 8>(o, st) : stream<1, 1, 16>(o, st);
-    return two ? stream<2, 2, 8>(o, st) : stream<2, 1, 16>(o, st);
-  }
-  return run_tile(o, plan_tile(m, N, ka), st);
+  if (plan.kernel == kQ8Tile) return run_tile(o, plan, st);
+  if (plan.mt == 1) return plan.nt == 2 ? stream<1, 2, 8>(o, plan.splits, st) : stream<1, 1, 16>(o, plan.splits, st);
+  return plan.nt == 2 ? stream<2, 2, 8>(o, plan.splits, st) : stream<2, 1, 16>(o, plan.splits, st);
 }
 
 }  // namespace d2c

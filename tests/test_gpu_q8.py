@@ -936,3 +936,37 @@ def test_linear_into_outputs_of_any_alignment(m, N, K):
         ctx.d2c_q8_linear(a, p, room[shift: shift + m * N].view(m, N))
         assert np.array_equal(room[shift: shift + m * N].view(m, N).cpu().numpy(), want)
         assert (room[:shift] == 5.0).all() and (room[shift + m * N:] == 5.0).all()
+
+
+def _linear_sizes():
+    from q8_sizes import LINEAR
+    return [(key, size) for key, sizes in LINEAR.items() for size in sizes]
+
+
+@pytest.mark.parametrize("key,size", _linear_sizes(), ids=lambda x: "-".join(map(str, x)))
+def test_linear_in_every_kernel(key, size):
+    """Each kernel of the product, by sizes that leave a part of its last tiles; rows and channels that are not finite stay among themselves."""
+    from q8_sizes import linear
+    m, N, K = size
+    say(f"q8 linear kernel {key} size {size}")
+    p = B().d2c_q8_plan_linear(m, N, K)
+    assert (p["kernel"], p["row_tiles"], p["col_tiles"], p["splits"] > 1) == key
+    for dtype in ("bf16", "f32") if N * K < 10 ** 8 else ("bf16",):
+        t, g = torch.bfloat16 if dtype == "bf16" else torch.float32, torch.Generator(device="cuda").manual_seed(m + N + K)
+        a = torch.randn((m, K), generator=g, device="cuda").to(t)
+        w = (0.02 * torch.exp(torch.randn((N, 1), generator=g, device="cuda")) * torch.randn((N, K), generator=g, device="cuda")).to(t)
+        if m > 5:
+            a[1], a[2] = 0, 0
+            a[2, K // 2], a[m - 2, K - 1], w[N - 1, 0], w[3, K - 1] = -5, float("nan"), float("inf"), float("nan")
+        ctx = B().Q8Context(4, 4, 64, dtype, max_rows=m, max_k=K, max_n=N)
+        pack = ctx.d2c_q8_pack(w)
+        room = torch.full((m * N + 2048,), 123.0, device="cuda")
+        out = room[1024: 1024 + m * N].view(m, N)
+        ctx.d2c_q8_linear(a, pack, out)
+        want, sw = linear(a, w)
+        assert torch.equal(pack.scale.nan_to_num(nan=-1.0), sw.nan_to_num(nan=-1.0))
+        assert torch.equal(out.isnan(), want.isnan()) and torch.equal(out.nan_to_num(nan=0.0), want.nan_to_num(nan=0.0))
+        assert (room[:1024] == 123.0).all() and (room[1024 + m * N:] == 123.0).all()
+        room.fill_(7.0)
+        ctx.d2c_q8_linear(a, pack, out)
+        assert torch.equal(out.nan_to_num(nan=0.0), want.nan_to_num(nan=0.0))

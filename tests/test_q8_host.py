@@ -171,3 +171,62 @@ def test_init_errors_of_two_threads_keep_apart():
     other.join()
     assert seen[0][0] == b"" and b"dtype" in seen[0][1]
     assert B._lib.d2c_q8_last_error(None) == mine
+
+
+# ---------------------------------------------------------------------- the product's kernels and the sizes that test them
+
+def _linear_kernel(m, N, K):
+    from paper_2509_23094_amd import binding as B
+    p = B.d2c_q8_plan_linear(m, N, K)
+    return (p["kernel"], p["row_tiles"], p["col_tiles"], p["splits"] > 1), p
+
+
+@built
+def test_every_kernel_of_the_product_has_a_tested_size():
+    """The sizes that the GPU tests multiply reach the kernels they are listed for, and sizes all over the range reach no other."""
+    from q8_sizes import LINEAR
+    for key, sizes in LINEAR.items():
+        for size in sizes:
+            assert _linear_kernel(*size)[0] == key, size
+    rng = np.random.default_rng(3)
+    sizes = np.exp(rng.uniform(0, 1, (60000, 3)) * np.log([4096, 65536, 8192])).astype(np.int64)
+    seen = {_linear_kernel(int(m), int(n), 8 * int(k))[0] for m, n, k in sizes}
+    assert seen <= set(LINEAR), seen - set(LINEAR)
+
+
+@built
+def test_linear_plan_covers_the_contraction_and_fits_its_parts():
+    rng = np.random.default_rng(4)
+    for m, n, k in np.exp(rng.uniform(0, 1, (20000, 3)) * np.log([65536, 1 << 20, 8192])).astype(np.int64):
+        m, n, k = int(m), int(n), 8 * int(k)
+        (kernel, mt, nt, split), p = _linear_kernel(m, n, k)
+        steps = -(-k // 64)
+        units = -(-steps // 4) if kernel == 2 else steps                  # what a split takes whole numbers of
+        per = -(-units // p["splits"])
+        assert p["splits"] >= 1 and per * (p["splits"] - 1) < units, (m, n, k, p)          # none empty
+        assert not split or 4 * p["splits"] * m * n <= 32 << 20, (m, n, k, p)
+        assert p["waves"] in (8, 16)
+        if kernel == 0:
+            assert m <= 16 and k <= 2048 and not split
+        if kernel == 1:
+            assert mt == -(-m // 16) <= 2
+
+
+@built
+def test_linear_plan_rejects_bad_arguments():
+    from paper_2509_23094_amd import binding as B
+    shape = (ctypes.c_int32 * 5)()
+    for m, n, k in ((0, 16, 16), (1, 0, 16), (1, 16, 0), ((1 << 16) + 1, 16, 16), (1, (1 << 20) + 1, 16), (1, 16, (1 << 16) + 1)):
+        assert B._lib.d2c_q8_plan_linear(m, n, k, shape) == B.D2C_EINVAL
+    assert B._lib.d2c_q8_plan_linear(1, 16, 16, None) == B.D2C_EINVAL
+
+
+def test_the_product_in_torch_is_the_one_in_numpy():
+    import torch
+    from q8_sizes import linear
+    g = torch.Generator().manual_seed(0)
+    a, w = torch.randn((9, 72), generator=g), 0.02 * torch.randn((33, 72), generator=g)
+    a[1], a[2, 3], a[4, 5], w[6, 7], a[7] = 0, float("nan"), float("-inf"), float("inf"), 2.0 ** -101
+    want, _, sw = R.linear(a.numpy(), w.numpy())
+    got, s = linear(a, w)
+    assert np.array_equal(got.numpy(), want, equal_nan=True) and np.array_equal(s.numpy(), sw, equal_nan=True)
