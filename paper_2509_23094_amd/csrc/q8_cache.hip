@@ -515,13 +515,17 @@ hipError_t launch_q8_weigh(const float* avg, int m, int L, int64_t* weight, hipS
 
 hipError_t launch_q8_keep(const int64_t* weight, const uint8_t* protect, int L, int n_keep, int32_t* kept, int64_t* kept_weight,
                           hipStream_t st) {
-  // Rounds of a wave.  Rounds that are not there cost nearly what others do, and keys that are read again their way from the L2: 767 rows with
-  // 4 rounds in registers 5.8 us, with 20 12.0; 4096 rows 6.4, 12.7, read again 9.0; 20001 rows with 20 17.0, read again 25.5.
+  // Rounds of a wave.  Rounds that are not there cost nearly what others do, and keys that are read again their way from the L2.  A call that keeps
+  // 64 rows of one head (choice and compaction, in a captured loop), us, with protected rows:
+  //   rows              767  2000  4096  4097  5000  6000  8000  10000  12000  16000  20001  20480
+  //   4 in registers    7.4   7.6   8.2
+  //   20 in registers  11.1  11.3  11.8  12.0  12.0  12.3  12.8   15.2   13.4   14.5   17.8   15.4
+  //   read again        7.5   8.5  10.0  10.7  10.9  11.7  13.2   17.7   16.3   19.0   26.7   22.2
   const int per = ((L + kKeepWaves - 1) / kKeepWaves + 63) / 64;
   auto go = [&](auto prot) {
     constexpr bool P = decltype(prot)::value;
     if (per <= 4) q8_keep_kernel<4, P><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
-    else if (per <= 20) q8_keep_kernel<20, P><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
+    else if (per > 6 && per <= 20) q8_keep_kernel<20, P><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
     else q8_keep_kernel<0, P><<<1, kKeepThreads, 0, st>>>(weight, protect, L, n_keep, kept, kept_weight);
     return hipGetLastError();
   };

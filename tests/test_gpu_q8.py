@@ -970,3 +970,18 @@ def test_linear_in_every_kernel(key, size):
         room.fill_(7.0)
         ctx.d2c_q8_linear(a, pack, out)
         assert torch.equal(out.nan_to_num(nan=0.0), want.nan_to_num(nan=0.0))
+
+
+@pytest.mark.parametrize("L", [4096, 4097, 6144, 6145, 9000, 20480])
+def test_evict_where_the_choice_changes_its_form(L):
+    """On both sides of the sizes at which keys are held in registers or read again."""
+    say(f"q8 evict forms L={L}")
+    c = Case((1, 1, 64), "bf16", L).fill()
+    for kind in ("spread", "ties", "wide"):
+        w, p = weights(c.rng, L, kind), (c.rng.random(L) < 0.1).astype(np.uint8)
+        dw, dp = torch.from_numpy(w).cuda(), torch.from_numpy(p).cuda()
+        for n, q in ((L // 3, None), (L // 3, p), (L // 50, p), (L, p)):
+            dst, kept, kw = B().Q8Cache(c.ctx, n), torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int64, device="cuda")
+            c.ctx.d2c_q8_evict(c.cache, L, dw, None if q is None else dp, dst, kept, kw)
+            want = R.keep(w, q, n)
+            assert np.array_equal(kept.cpu().numpy(), want) and np.array_equal(kw.cpu().numpy(), w[want]), f"{kind} n={n}"
