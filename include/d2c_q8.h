@@ -88,12 +88,14 @@ int d2c_q8_cache_size(const d2c_q8* ctx, int64_t rows, int64_t* code_bytes, int6
  * becomes max(scale(new rows), 1.25 * old scale) and the other rows' codes become code(code * old, new) -- at least a quarter
  * at a time, so that many small growths cannot let a value drift away with its scale.  A value that is not finite counts
  * for no scale: NaN is stored as 0, an infinity as the largest code of its sign.  Indices outside [0, L) are left out;
- * indices that are not ascending and distinct leave the blocks of 64 rows that they name undefined, and nothing else.  Two
- * sequences of a call must not refresh the same cache (D2C_EINVAL). */
+ * indices that are not ascending and distinct leave the blocks of 64 rows that they name undefined, and nothing else.  L is
+ * the cache's length: rows from L on of the block that holds row L - 1 have no defined values once that block is refreshed.
+ * Two sequences of a call must not refresh the same cache (D2C_EINVAL). */
 int d2c_q8_update(d2c_q8* ctx, const d2c_q8_seq* seqs, int32_t batch, void* stream);
 
 /* d2c_q8_update of the sequences that give new_k / new_v, then attention of each sequence's m query rows against all L rows
- * of its cache, no mask; sequences may share a cache that at most one of them refreshes.  Scores, softmax and sums are fp32.
+ * of its cache, no mask; sequences may share a cache that at most one of them refreshes.  Scores, softmax and sums are fp32;
+ * scores (q k^T / sqrt(D)) are meant to stay within 2^22, beyond which a row can turn NaN.
  * q enters as fp16 pieces of a row scaled by a power of two, one for bf16 (exact down to 2^-32 of the row's largest
  * magnitude, to the nearest 2^-39 of it below), two for float (within 2^-23, or 2^-39 of the largest).  Probabilities are
  * rounded to 11 bits for bf16 and 22 for float, those below 2^-25 (float: 2^-18) of a row's largest to the nearest 2^-35
@@ -111,7 +113,7 @@ int64_t d2c_q8_weight_bytes(int32_t N, int32_t K);
 int d2c_q8_pack(d2c_q8* ctx, const void* w, int32_t N, int32_t K, int8_t* codes, float* scale, void* stream);
 
 /* out[m, N] (float) = a[m, K] w[N, K]^T with each row of a quantised to 8 bits by its own largest magnitude: the sums are
- * exact whole numbers, times the row's and the channel's scale.  A row of a, or a channel of w, that holds a NaN or an
+ * exact whole numbers, made float, times the row's scale, times the channel's.  A row of a, or a channel of w, that holds a NaN or an
  * infinity gives NaN in its outputs and in no others. */
 int d2c_q8_linear(d2c_q8* ctx, const void* a, int32_t m, const int8_t* codes, const float* scale, int32_t N, int32_t K,
                   float* out, void* stream);

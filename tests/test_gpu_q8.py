@@ -985,3 +985,24 @@ def test_evict_where_the_choice_changes_its_form(L):
             c.ctx.d2c_q8_evict(c.cache, L, dw, None if q is None else dp, dst, kept, kw)
             want = R.keep(w, q, n)
             assert np.array_equal(kept.cpu().numpy(), want) and np.array_equal(kw.cpu().numpy(), w[want]), f"{kind} n={n}"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_of_the_largest_scores(dtype):
+    """Scores up to 2^22: a key that leads by 64 takes all (the scores' own rounding is (D + 10) 2^-24 of 2^22, below 20)."""
+    say(f"q8 attention largest scores {dtype}")
+    c = Case("gqa", dtype, 300).fill()
+    k, v, m = c.ref.k.values(300), c.ref.v.values(300), 40
+    q = c.queries(m)
+    group = np.arange(c.H) // (c.H // c.Hkv)
+    score = lambda q: np.einsum("mhd,nhd->mhn", f64(q).reshape(m, c.H, c.D), k[:, group]) / c.D ** 0.5
+    q = (q.float() * float(0.9 * 2 ** 22 / np.abs(score(q)).max())).to(q.dtype)
+    s = np.sort(score(q), 2)
+    assert 2 ** 21 < np.abs(s).max() < 2 ** 22
+    clear, first = s[:, :, -1] - s[:, :, -2] > 64, score(q).argmax(2)
+    assert clear.mean() > 0.9
+    q, out, avg = attend(c, m, q=q)
+    assert torch.isfinite(out).all() and torch.isfinite(avg).all()
+    want, got = v[first, group[None]], f64(out).reshape(m, c.H, c.D)
+    tol = (HALF[dtype] + P_HALF[dtype] + 2.0 ** -20) * np.abs(want) + 1e-12
+    assert (np.abs(got - want) <= tol)[clear].all()
