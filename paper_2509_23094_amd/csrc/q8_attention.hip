@@ -27,10 +27,13 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kTile = 32;                 // query rows per workgroup
 constexpr int kWaves = 8;
-// Probabilities are rounded to fp16 times 2^bits, relative to a reference that a score may pass by slack: 2^15 at most.  bf16 gives four bits
-// of the range for a reference that is seldom raised; float, whose second piece would be a subnormal number sooner, keeps them (32 heads of 128,
-// 256 x 2048 in float: 28.7 us, with bf16's 11 bits and slack 28.3).
-template <int QP> struct Base { static constexpr float bits = QP == 1 ? 11.f : 15.f, slack = 15.f - bits; };
+// Probabilities are rounded to fp16 relative to a reference that a score may pass by `slack`, times a power of two that takes them to 2^15 at most.
+// bf16: 2^11 in the exponent, and a reference that is seldom raised.  Float, whose second piece would be a subnormal number sooner,
+// keeps the four bits and multiplies by 2^15 behind the exponential, whose argument stays small (near 15 its rounding alone is 2^-21).
+template <int QP> struct Base {
+  static constexpr float bits = QP == 1 ? 11.f : 0.f, times = QP == 1 ? 1.f : 0x1p15f, slack = QP == 1 ? 4.f : 0.f;
+  static constexpr float unit = QP == 1 ? 0x1p-11f : 1.f;       // 2^-bits
+};
 
 // log2(e) / sqrt(D)
 template <int D> constexpr float kScore = 1.4426950408889634f / (D == 128 ? 11.313708498984761f : 8.f);
@@ -53,7 +56,7 @@ struct AttendArgs {
   float* part;                            // [split][slot][D]
   float2* ml;                             // [split][slot]: maximum (base 2), sum
   _Float16* q16;
-  float2* row;                            // [slot]: 1 / (power of two on the row), log2 of its sum of exponentials
+  f32x4* row;                             // [slot]: 1 / (power of two on the row), its reference, 1 / its sum of exponentials
   size_t slots;                           // of the whole launch
 };
 
@@ -194,9 +197,9 @@ __device__ __forceinline__ void softmax_step(f32x16 (&x)[2], float ks, int left,
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       sum += x[t][i];
-      const _Float16 hi = (_Float16)x[t][i];
+      const _Float16 hi = (_Float16)(x[t][i] * Base<QP>::times);
       p[0][2 * t + i / 8][i % 8] = hi;
-      if constexpr (QP > 1) p[1][2 * t + i / 8][i % 8] = (_Float16)(x[t][i] - (float)hi);
+      if constexpr (QP > 1) p[1][2 * t + i / 8][i % 8] = (_Float16)fmaf(x[t][i], Base<QP>::times, -(float)hi);
     }
   l += sum;
 }
@@ -264,7 +267,7 @@ __global__ __launch_bounds__(64 * kWaves) void q8_attend_kernel(AttendArgs args)
     if (QP == 1) want_k(b + kWaves);
     h8 p[QP][4];
     softmax_step<QP, DT>(x, ks, s.L - b * kQ8Rows, ref, l, o, p);
-    const float vs = vs_next;
+    const float vs = vs_next * (1.f / Base<QP>::times);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
       f32x16 acc = {};
@@ -327,7 +330,7 @@ __global__ __launch_bounds__(64 * kWaves) void q8_attend_kernel(AttendArgs args)
     for (int j = 0; j < DT / 2; ++j) q8_store4(to + 4 * j, y + 4 * j);
   }
   if (s.avg && wave == 0 && g == 0 && split == 0)
-    args.row[slot] = make_float2(rp2, to_m + log2f(sum) - Base<QP>::bits);       // (the sum of a split row: the merge puts it right)
+    args.row[slot] = f32x4{rp2, to_m, 1.f / (sum * Base<QP>::unit), 0.f};      // (of a split row: the merge puts it right)
 }
 
 // Splits of a row joined.  A workgroup per row and head, a thread per (four dimensions, every kJoin-th split).  What bounds it: launching and
@@ -371,7 +374,10 @@ __global__ __launch_bounds__(kJoin * D / 4) void q8_join_kernel(AttendArgs args)
   y *= 1.f / sum;
   float z[4] = {y[0], y[1], y[2], y[3]};
   q8_store4((T*)s.out + (slot - s.row0) * D + 4 * t, z);
-  if (s.avg && t == 0) args.row[slot].y = ref + log2f(sum) - Base<sizeof(T) == 2 ? 1 : 2>::bits;
+  if (s.avg && t == 0) {
+    args.row[slot][1] = ref;
+    args.row[slot][2] = 1.f / (sum * Base<sizeof(T) == 2 ? 1 : 2>::unit);
+  }
 }
 
 // attn_avg of 32 rows x one block of keys: the waves take a run of heads each and are added up at the end.  The next head's keys and
@@ -390,7 +396,7 @@ __global__ __launch_bounds__(64 * kWaves) void q8_average_kernel(AttendArgs args
   f32x16 acc[2] = {};
   u32x4 kr[2][D / 32];
   h8 k[2][D / 16], q[QP][D / 16];
-  float2 rw = {};
+  f32x4 rw = {};
   float ks_next = 0.f, ks = 0.f;
   auto want_k = [&](int hk) __attribute__((always_inline)) {
     const size_t blk = (size_t)b * args.Hkv + hk;
@@ -417,7 +423,7 @@ __global__ __launch_bounds__(64 * kWaves) void q8_average_kernel(AttendArgs args
       ks = ks_next;
       want_k(min(h / G + 1, args.Hkv - 1));
     }
-    const float c = ks * kScore<D> * rw.x, base = -rw.y;
+    const float c = ks * kScore<D> * rw[0], base = -rw[1], inv = rw[2];
     f32x16 x[2];
     x[0] = product<D, QP>(k[0], q);
     x[1] = product<D, QP>(k[1], q);
@@ -425,7 +431,7 @@ __global__ __launch_bounds__(64 * kWaves) void q8_average_kernel(AttendArgs args
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[t][i] += exp2_hw(fmaf(x[t][i], c, base));
+      for (int i = 0; i < 16; ++i) acc[t][i] = fmaf(exp2_hw(fmaf(x[t][i], c, base)), inv, acc[t][i]);
   }
   __shared__ float lds[kWaves][kTile][kQ8Rows + 1];
 #pragma unroll
@@ -466,7 +472,7 @@ int plan_splits(int workgroups, int most_blocks) {
 int row_tiles(const Q8Shape& s, int m) { return (m * (s.H / s.Hkv) + kTile - 1) / kTile; }
 
 // Workspace: partial sums of split rows -- splits x rows is at most kTargetWgs tiles, as rows are at most 32 per unsplit
-// workgroup -- and, for the average, (factor, log-sum) and fp16 rows of every query row and head.
+// workgroup -- and, for the average, the softmax's numbers and fp16 rows of every query row and head.
 struct Layout { size_t ml, row, q16, total; };
 Layout layout(const Q8Shape& s, size_t max_rows, size_t max_batch) {
   const size_t split_rows = (size_t)kTargetWgs * kTile, pieces = s.dtype == kBF16 ? 1 : 2;
@@ -475,7 +481,7 @@ Layout layout(const Q8Shape& s, size_t max_rows, size_t max_batch) {
   Layout l;
   l.ml = up(split_rows * s.D * 4);
   l.row = l.ml + up(split_rows * 8);
-  l.q16 = l.row + up(max_rows * s.H * 8);
+  l.q16 = l.row + up(max_rows * s.H * 16);
   l.total = l.q16 + up(q_rows * s.H * pieces * s.D * 2);
   return l;
 }
@@ -509,7 +515,7 @@ hipError_t launch_q8_attention(const Q8Shape& s, const Q8Attend* calls, int n, i
     a.Hkv = s.Hkv;
     a.part = (float*)ws;
     a.ml = (float2*)((char*)ws + l.ml);
-    a.row = (float2*)((char*)ws + l.row);
+    a.row = (f32x4*)((char*)ws + l.row);
     a.q16 = (_Float16*)((char*)ws + l.q16);
     int base = 0, most = 0, wgs = 0, avg_wgs = 0;
     size_t rows = 0;

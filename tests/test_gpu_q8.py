@@ -1006,3 +1006,19 @@ def test_attention_of_the_largest_scores(dtype):
     want, got = v[first, group[None]], f64(out).reshape(m, c.H, c.D)
     tol = (HALF[dtype] + P_HALF[dtype] + 2.0 ** -20) * np.abs(want) + 1e-12
     assert (np.abs(got - want) <= tol)[clear].all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_average_of_equal_scores_is_one_over_the_length(dtype):
+    """Equal scores: the exponentials are 1 and their sum is L, both exact; two roundings are left, of 1 / L and of its product, and as many
+    again are allowed (the instructions' own).  The float output of values that are all 1 likewise, with its sum's product beside them."""
+    say(f"q8 average of equal scores {dtype}")
+    c = Case((1, 1, 64), dtype, 4200)
+    one = dev(np.ones((4200, 64)), dtype)
+    c.update(None, m=4200, new=((one, f64(one).reshape(4200, 1, 64)),) * 2)
+    value = float(c.ref.v.values(1)[0, 0, 0])
+    for L in [1, 3, 7] + list(range(70, 260, 9)) + [1000, 1023, 2500, 4199]:
+        q, out, avg = attend(c, 2, L=L, q=torch.zeros((2, 64), dtype=c.ctx.torch_dtype, device="cuda"))
+        assert np.abs(f64(avg) * L - 1).max() <= 4 * 2.0 ** -24, L
+        if dtype == "f32":
+            assert np.abs(f64(out) / value - 1).max() <= (8 + L ** 0.5) * 2.0 ** -24, L
