@@ -205,9 +205,12 @@ __device__ __forceinline__ void softmax_step(f32x16 (&x)[2], float ks, int left,
 }
 
 // One tile of rows per workgroup: its waves take blocks in turn, operands straight from memory.
-// What bounds it: vector instructions (611 for 32 rows x 64 keys, 256 of them to make fp16 of codes) beside the matrix cores (busy 28 % of the
-// time), with the two waves per SIMD that the registers allow, and 5 us at its ends.  32 heads, 4 x 45 rows x 1823 keys 18.6 us, 256 x 2048
-// 19.2; 28 heads on 4, 19 rows x 60001 keys 34.7.  Tried without gain: codes shared in LDS by the tiles of rows, keys requested two blocks
+// What bounds it: a wave's chain through a block, keys -> scores -> maximum -> exponentials -> values, which the two waves per SIMD that the
+// registers allow do not hide, and 5 us at its ends.  28 heads on 4, 19 rows x 60001 keys: vector units busy 72 % of the time, matrix cores 29 %, waves
+// waiting 32 %, with 571 vector instructions per wave and block (256 of them to make fp16 of codes); 32 heads, 256 x 2048, where the ends weigh more, 64,
+// 22 and 31 %.  Times: 36 us, 18-20 us, 4 sequences of up to 45 rows x 1823 keys 18.7 us (their 192 workgroups have 29 to 13 blocks
+// each and all wait for the longest); float 256 x 2048 29 us.  Of D = 128 bf16 spills 2 registers around the loop, float 10, one of which is
+// loaded again for each block.  Tried without gain: codes shared in LDS by the tiles of rows, keys requested two blocks
 // ahead, priorities for half the waves.  Codes left 1152 too large, with the sums put right afterwards, is a fifth fewer vector instructions,
 // 2-6 % faster, and loses up to 2^-12 of a step of the codes: not kept.
 template <typename T, int D>
@@ -381,8 +384,9 @@ __global__ __launch_bounds__(kJoin * D / 4) void q8_join_kernel(AttendArgs args)
 }
 
 // attn_avg of 32 rows x one block of keys: the waves take a run of heads each and are added up at the end.  The next head's keys and
-// queries are on their way while one head's are used.  What bounds it: what a compute unit gets from its L2 (16 KB of codes and queries for each head
-// and block, 50 KB/us); 32 heads, 256 rows x 2048 keys 11.6 us, 4 x 45 x 1823 12.2.
+// queries are on their way while one head's are used.  What bounds it: the same chain without the values: vector units busy 44 % of the
+// time, matrix cores 18 %, waves waiting 40 % (32 heads, 256 rows x 2048 keys, 11.7 us; a compute unit gets 45 KB/us of codes and queries from
+// its L2).  4 sequences of up to 45 x 1823 12.4 us.
 template <typename T, int D>
 __global__ __launch_bounds__(64 * kWaves) void q8_average_kernel(AttendArgs args) {
   constexpr int QP = sizeof(T) == 2 ? 1 : 2;

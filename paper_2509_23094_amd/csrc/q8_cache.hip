@@ -44,7 +44,8 @@ __device__ int lower_bound_wide(const int32_t* idx, int m, int limit) {
 // one where the rows are consecutive or many; few scattered rows get a workgroup each, of which the first of a block's does the block.
 // Rows and, where the scale moves, the old codes are then read once and the codes written once.
 // What bounds it: bytes for a whole prompt (2500 rows of 32 heads of 128, bf16: 18-21 us, 61 MB), the chain index -> rows -> maximum -> codes for a
-// decode step (45 rows among 1823: 9.5 us).
+// decode step (45 rows among 1823: 8.6 us where all fit their blocks' scales; 16.9 where the scale of every block they touch grows,
+// which is then read and written whole).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void q8_update_kernel(UpdateArgs args, int Hkv) {
   using P = Pieces<D>;
@@ -251,7 +252,7 @@ constexpr int kKeepWaves = 16, kKeepThreads = 64 * kKeepWaves;
 // The chosen class's n-th largest weight is found digit by digit (11 bits, from its highest bit on), with a histogram in LDS and an early
 // end when a digit's rows all stay.  Then each wave numbers its kept positions behind those of the waves before.
 // What bounds it: a chain of barriers and LDS atomics per digit in one compute unit, and its instructions where there are many rows; 767 rows
-// 6.2 us, 20001 16.1 (with equal keys told apart in every pass over them, not only where a part of them stays, 6.7 and 18.7).
+// 6.3 us, 20001 16.4 (with equal keys told apart in every pass over them, not only where a part of them stays, 0.5 and 2.6 us more).
 template <int PER, bool PROTECT>
 __global__ __launch_bounds__(kKeepThreads) void q8_keep_kernel(const int64_t* weight, const uint8_t* protect, int L, int n_keep,
                                                               int32_t* kept, int64_t* kept_weight) {

@@ -311,8 +311,8 @@ __global__ __launch_bounds__(256) void q8_sum_kernel(const int* part, int splits
 // registers from the order they lie in and are refilled as soon as a step is done.  LDS reads run three groups of NT matrix-core instructions
 // ahead of their use.  Each XCD takes a run of tiles in an order in which neighbours share activations and weights in its L2.  Splits of the
 // contraction write their sums to `part`.
-// What bounds it: what a compute unit gets from its L2, 65-80 KB/us, and the clock (1536 x 24576 x 4096: 147-157 us, 1.97-2.1 POP/s,
-// matrix cores busy 43 % of the time).  Two chunks on their way instead of one gave nothing.
+// What bounds it: the matrix cores, busy 62 % of the time that waves are there (1536 x 24576 x 4096: 146-162 us, 1.9-2.1 POP/s), and the barrier of each chunk,
+// with one workgroup per compute unit: waves wait 34 % of their time.  Two chunks on their way instead of one gave nothing.
 constexpr int kStepsPerChunk = 4;
 template <int MT, int NT>
 __global__ __launch_bounds__(512, 1) void q8_tile_kernel(const int8_t* a, const float* sa, const int8_t* w, const float* sw, int m, int N,
