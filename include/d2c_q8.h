@@ -95,7 +95,8 @@ int d2c_q8_update(d2c_q8* ctx, const d2c_q8_seq* seqs, int32_t batch, void* stre
 
 /* d2c_q8_update of the sequences that give new_k / new_v, then attention of each sequence's m query rows against all L rows
  * of its cache, no mask; sequences may share a cache that at most one of them refreshes.  Scores, softmax and sums are fp32;
- * scores (q k^T / sqrt(D)) are meant to stay within 2^22, beyond which a row can turn NaN.
+ * scores (q k^T / sqrt(D)) are meant to stay within 2^22, and L times the values of V within 2^112: beyond, a row can turn NaN
+ * or infinite.
  * q enters as fp16 pieces of a row scaled by a power of two, one for bf16 (exact down to 2^-32 of the row's largest
  * magnitude, to the nearest 2^-39 of it below), two for float (within 2^-23, or 2^-39 of the largest).  Probabilities are
  * rounded to 11 bits for bf16 and 22 for float, those below 2^-25 (float: 2^-18) of a row's largest to the nearest 2^-35

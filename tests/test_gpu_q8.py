@@ -1022,3 +1022,19 @@ def test_average_of_equal_scores_is_one_over_the_length(dtype):
         assert np.abs(f64(avg) * L - 1).max() <= 4 * 2.0 ** -24, L
         if dtype == "f32":
             assert np.abs(f64(out) / value - 1).max() <= (8 + L ** 0.5) * 2.0 ** -24, L
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_of_the_largest_values(dtype):
+    """Values of V up to 2^112 / L: sums over the keys stay in float's range."""
+    say(f"q8 attention largest values {dtype}")
+    for L in (64, 1100):
+        c = Case("gqa", dtype, L)
+        v = c.rng.uniform(0.5, 1.0, (L, c.Hkv, c.D)) * 2.0 ** 112 / L
+        dv = dev(v, dtype).reshape(L, c.Hkv * c.D)
+        c.update(None, m=L, new=(c.new(L), (dv, f64(dv).reshape(v.shape))))
+        c.check()
+        q = c.queries(9)
+        q[0] = 0
+        q, out, avg = attend(c, 9, q=q)
+        c.expect(q, out, avg)
