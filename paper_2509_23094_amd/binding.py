@@ -74,6 +74,30 @@ class d2c_q8_seq(C.Structure):
                [("m", C.c_int32), ("L", C.c_int32)]
 
 
+class d2c_pg_dims(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_heads", "n_kv_heads", "head_dim", "dtype", "page_rows", "max_rows", "max_batch",
+                                          "n_pairs", "n_axes", "pairing")] + [("freq", C.c_double * 64), ("axis", C.c_uint8 * 64)]
+
+
+class d2c_pg_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int32)]
+
+
+class d2c_pg_batch(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("row_start", "length", "pages", "at", "origin")] + \
+               [(n, C.c_int32) for n in ("batch", "n_rows", "page_cols")]
+
+
+class d2c_pg_new(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v")] + [(n, C.c_int64) for n in ("q_ld", "k_ld", "v_ld")] + \
+               [("dtype", C.c_int32), ("pos", C.c_void_p), ("q_out", C.c_void_p), ("q_out_ld", C.c_int64)]
+
+
+class d2c_pg_attend(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_ld", C.c_int64), ("out", C.c_void_p), ("out_ld", C.c_int64), ("attn_avg", C.c_void_p),
+                ("avg_ld", C.c_int64), ("block", C.c_int32), ("window", C.c_int32), ("scale", C.c_float)]
+
+
 # include/d2c.h (the method's calls) and include/d2c_tools.h (timing, tunables, planner)
 EXPORTS = ["d2c_init", "d2c_destroy", "d2c_last_error", "d2c_seq_reset", "d2c_select", "d2c_refresh_layer",
            "d2c_attention", "d2c_influence", "d2c_linear", "d2c_step", "d2c_workspace_bytes", "d2c_select_static"]
@@ -84,6 +108,10 @@ Q8_EXPORTS = ["d2c_q8_init", "d2c_q8_destroy", "d2c_q8_last_error", "d2c_q8_work
               "d2c_q8_update", "d2c_q8_attention", "d2c_q8_read", "d2c_q8_weight_bytes", "d2c_q8_pack", "d2c_q8_linear",
               "d2c_q8_weigh", "d2c_q8_evict"]
 Q8_BLOCK = 64
+# include/d2c_pg.h (the paged cache)
+PG_EXPORTS = ["d2c_pg_init", "d2c_pg_destroy", "d2c_pg_last_error", "d2c_pg_workspace_bytes", "d2c_pg_cache_size",
+              "d2c_pg_rotate", "d2c_pg_append", "d2c_pg_read", "d2c_pg_attention"]
+D2C_PG_HALVES, D2C_PG_NEIGHBOURS = 0, 1
 
 
 def load_library() -> C.CDLL:
@@ -133,9 +161,20 @@ def load_library() -> C.CDLL:
     lib.d2c_q8_linear.argtypes = [vp, vp, i32, vp, vp, i32, i32, vp, vp]
     lib.d2c_q8_weigh.argtypes = [vp, vp, i32, i32, vp, vp]
     lib.d2c_q8_evict.argtypes = [vp, vp, i32, vp, vp, i32, vp, vp, vp, vp]
-    for name in EXPORTS + TOOL_EXPORTS + Q8_EXPORTS:
+    lib.d2c_pg_init.argtypes = [C.POINTER(d2c_pg_dims), C.POINTER(vp)]
+    lib.d2c_pg_destroy.argtypes = [vp]
+    lib.d2c_pg_last_error.argtypes = [vp]
+    lib.d2c_pg_last_error.restype = C.c_char_p
+    lib.d2c_pg_workspace_bytes.argtypes = [vp]
+    lib.d2c_pg_workspace_bytes.restype = i64
+    lib.d2c_pg_cache_size.argtypes = [vp, i64, C.POINTER(i64)]
+    lib.d2c_pg_rotate.argtypes = [vp, vp, i64, i32, i32, i32, vp, i32, vp, i64, vp]
+    lib.d2c_pg_append.argtypes = [vp, vp, vp, vp, vp]
+    lib.d2c_pg_read.argtypes = [vp, vp, vp, vp, i64, vp, i64, vp]
+    lib.d2c_pg_attention.argtypes = [vp, vp, vp, vp, vp]
+    for name in EXPORTS + TOOL_EXPORTS + Q8_EXPORTS + PG_EXPORTS:
         if name not in ("d2c_last_error", "d2c_workspace_bytes", "d2c_q8_last_error", "d2c_q8_workspace_bytes",
-                        "d2c_q8_weight_bytes"):
+                        "d2c_q8_weight_bytes", "d2c_pg_last_error", "d2c_pg_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
     return lib
 
@@ -567,3 +606,175 @@ class Q8Batch:
             c.attn_avg = _checked(s.attn_avg, "attn_avg", torch.float32, (s.m, s.L), dev)
             c.m, c.L = s.m, s.L
         self.arr = arr
+
+
+# ---------------------------------------------------------------------- the paged cache (include/d2c_pg.h)
+
+def _rows(t: torch.Tensor, what: str, dtypes, n: int, width: Optional[int], device: int):
+    """(pointer, pitch in elements) of rows [n, width] whose elements lie together; the rows may lie apart."""
+    if t.dtype not in dtypes or t.dim() != 2 or t.shape[0] != n or (width is not None and t.shape[1] != width) or \
+            (t.shape[1] > 1 and t.stride(1) != 1) or t.get_device() != device:
+        raise D2CError(D2C_EINVAL, "%s: rows of %s, %s x %s on device %d expected, got %s %s strides %s on %s"
+                       % (what, " or ".join(map(str, dtypes)), n, width, device, t.dtype, tuple(t.shape), t.stride(), t.device))
+    if n <= 1:
+        return t.data_ptr(), t.shape[1]              # (a single row's stride can be anything)
+    return t.data_ptr(), t.stride(0)
+
+
+class Rotary:
+    """How a head's pairs turn: pairs[a] of them by axis a, frequencies theta ** -(i / n) over all n pairs (ladder "shared") or over each
+    axis's own ("own"); the rest of the head stays.  Or any freq and axis per pair."""
+
+    def __init__(self, pairs: Optional[Sequence[int]] = None, theta: float = 10000.0, ladder: str = "shared", pairing: str = "halves",
+                 freq: Optional[Sequence[float]] = None, axis: Optional[Sequence[int]] = None):
+        if ladder not in ("shared", "own") or pairing not in ("halves", "neighbours") or (pairs is None) == (freq is None):
+            raise D2CError(D2C_EINVAL, "bad ladder or pairing, or not one of pairs and freq")
+        self.pairing = D2C_PG_HALVES if pairing == "halves" else D2C_PG_NEIGHBOURS
+        if freq is not None:
+            self.freq = [float(f) for f in freq]
+            self.axis = [int(a) for a in axis] if axis is not None else [0] * len(self.freq)
+            self.n_axes = max(self.axis, default=0) + 1
+        else:
+            n = sum(pairs)
+            self.axis = [a for a, count in enumerate(pairs) for _ in range(count)]
+            self.freq = [float(theta) ** -(i / n) for i in range(n)] if ladder == "shared" else \
+                [float(theta) ** -(i / count) for count in pairs for i in range(count)]
+            self.n_axes = max(1, len(pairs))
+        if len(self.axis) != len(self.freq) or len(self.freq) > 64 or any(not 0 <= a < 4 for a in self.axis) or self.n_axes > 4:
+            raise D2CError(D2C_EINVAL, "at most 64 pairs, each with one of at most 4 axes")
+
+
+class PgContext:
+    """Owns a d2c_pg handle on the current device."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, dtype: str, page_rows: int = 64, max_rows: int = 0, max_batch: int = 1,
+                 rotary: Optional[Rotary] = None):
+        self.handle = C.c_void_p()
+        self.n_heads, self.n_kv_heads, self.head_dim, self.dtype = int(n_heads), int(n_kv_heads), int(head_dim), dtype
+        self.page_rows, self.rotary = int(page_rows), rotary
+        self.torch_dtype = torch_dtype(dtype)
+        self.d_q, self.d_kv = self.n_heads * self.head_dim, self.n_kv_heads * self.head_dim
+        self.device = torch.cuda.current_device()
+        self.geo = (self.n_kv_heads, self.head_dim, self.page_rows, dtype, self.device)
+        d = d2c_pg_dims(n_heads, n_kv_heads, head_dim, D2C_BF16 if dtype == "bf16" else D2C_F32, page_rows, max_rows, max_batch)
+        self.n_axes = 1
+        if rotary is not None:
+            d.n_pairs, d.n_axes, d.pairing, self.n_axes = len(rotary.freq), rotary.n_axes, rotary.pairing, rotary.n_axes
+            for i, (f, a) in enumerate(zip(rotary.freq, rotary.axis)):
+                d.freq[i], d.axis[i] = f, a
+        rc = _lib.d2c_pg_init(C.byref(d), C.byref(self.handle))
+        if rc != D2C_OK:
+            raise D2CError(rc, (_lib.d2c_pg_last_error(None) or b"").decode())
+
+    def _check(self, rc: int) -> None:
+        if rc != D2C_OK:
+            raise D2CError(rc, (_lib.d2c_pg_last_error(self.handle) or b"").decode())
+
+    def close(self) -> None:
+        if self.handle:
+            _lib.d2c_pg_destroy(self.handle)
+            self.handle = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def workspace_bytes(self) -> int:
+        return int(_lib.d2c_pg_workspace_bytes(self.handle))
+
+    def _source(self, t: torch.Tensor, what: str):
+        if t.dtype not in (torch.float32, self.torch_dtype):
+            raise D2CError(D2C_EINVAL, "%s: float32 or %s expected, got %s" % (what, self.torch_dtype, t.dtype))
+        return D2C_F32 if t.dtype is torch.float32 else D2C_BF16
+
+    def _pos(self, pos: Optional[torch.Tensor], n: int) -> Optional[int]:
+        return _checked(pos, "pos", torch.int32, (self.n_axes, n), self.device)
+
+    def _match(self, cache: "PgCache", batch: "PgBatch") -> None:
+        if cache.geo != self.geo or batch.device != self.device:
+            raise D2CError(D2C_ESHAPE, "the cache was made for (n_kv_heads, head_dim, page_rows, dtype, device) %s, the batch for device %d, "
+                           "the handle has %s" % (cache.geo, batch.device, self.geo))
+
+    # ------------------------------------------------------------------ C ABI calls
+    def d2c_pg_rotate(self, x: torch.Tensor, pos: torch.Tensor, out: torch.Tensor, inverse: bool = False) -> None:
+        """x [n, heads * head_dim] (float32 or the storage type) turned by pos [n_axes, n] into out (storage type; may be x)."""
+        n, width = x.shape
+        kind = self._source(x, "x")
+        if width % self.head_dim:
+            raise D2CError(D2C_EINVAL, "x: whole heads expected")
+        xp, x_ld = _rows(x, "x", (x.dtype,), n, width, self.device)
+        op, o_ld = _rows(out, "out", (self.torch_dtype,), n, width, self.device)
+        self._check(_lib.d2c_pg_rotate(self.handle, xp, x_ld, kind, n, width // self.head_dim, self._pos(pos, n), int(inverse), op, o_ld,
+                                       _stream()))
+
+    def d2c_pg_append(self, cache: "PgCache", batch: "PgBatch", k: torch.Tensor, v: torch.Tensor, pos: Optional[torch.Tensor] = None,
+                      q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> None:
+        """Rows k, v [n_rows, d_kv] into the pages, k turned by pos [n_axes, n_rows] (None: the rows' indices); q likewise into q_out."""
+        self._match(cache, batch)
+        n, t = batch.n_rows, (k.dtype,)
+        a = d2c_pg_new(dtype=self._source(k, "k"), pos=self._pos(pos, n))
+        a.k, a.k_ld = _rows(k, "k", t, n, self.d_kv, self.device)
+        a.v, a.v_ld = _rows(v, "v", t, n, self.d_kv, self.device)
+        if q is not None:
+            a.q, a.q_ld = _rows(q, "q", t, n, self.d_q, self.device)
+        if q_out is not None:
+            a.q_out, a.q_out_ld = _rows(q_out, "q_out", (self.torch_dtype,), n, self.d_q, self.device)
+        self._check(_lib.d2c_pg_append(self.handle, cache.ref, batch.ref, C.byref(a), _stream()))
+
+    def d2c_pg_read(self, cache: "PgCache", batch: "PgBatch", out_k: Optional[torch.Tensor], out_v: Optional[torch.Tensor]) -> None:
+        """Values of the cache rows that the batch's rows stand for."""
+        self._match(cache, batch)
+        kp, k_ld = _rows(out_k, "out_k", (self.torch_dtype,), batch.n_rows, self.d_kv, self.device) if out_k is not None else (None, 0)
+        vp, v_ld = _rows(out_v, "out_v", (self.torch_dtype,), batch.n_rows, self.d_kv, self.device) if out_v is not None else (None, 0)
+        self._check(_lib.d2c_pg_read(self.handle, cache.ref, batch.ref, kp, k_ld, vp, v_ld, _stream()))
+
+    def d2c_pg_attention(self, cache: "PgCache", batch: "PgBatch", q: torch.Tensor, out: torch.Tensor, block: int = 0, window: int = 0,
+                         scale: Optional[float] = None, attn_avg: Optional[torch.Tensor] = None) -> None:
+        """Rows of q [n_rows, d_q] against their sequences' pages: block 0 no mask, 1 causal, more: blocks that see each other in whole."""
+        self._match(cache, batch)
+        n, t = batch.n_rows, (self.torch_dtype,)
+        if scale is not None and not scale > 0:
+            raise D2CError(D2C_EINVAL, "scale must be positive")
+        a = d2c_pg_attend(block=block, window=window, scale=0.0 if scale is None else scale)
+        a.q, a.q_ld = _rows(q, "q", t, n, self.d_q, self.device)
+        a.out, a.out_ld = _rows(out, "out", t, n, self.d_q, self.device)
+        if attn_avg is not None:
+            if attn_avg.dim() != 2 or attn_avg.shape[1] < 1:
+                raise D2CError(D2C_EINVAL, "attn_avg: [n_rows, columns] expected, got %s" % (tuple(attn_avg.shape),))
+            a.attn_avg, a.avg_ld = _checked(attn_avg, "attn_avg", torch.float32, (n, attn_avg.shape[-1]), self.device), attn_avg.shape[-1]
+        self._check(_lib.d2c_pg_attention(self.handle, cache.ref, batch.ref, C.byref(a), _stream()))
+
+
+class PgCache:
+    """Pages of one layer's cache (allocated with torch; what they hold before an append does not matter)."""
+
+    def __init__(self, ctx: PgContext, n_pages: int):
+        n = C.c_int64()
+        rc = _lib.d2c_pg_cache_size(ctx.handle, int(n_pages), C.byref(n))
+        if rc != D2C_OK:
+            raise D2CError(rc, "d2c_pg_cache_size: bad arguments")
+        shape = (int(n_pages), ctx.n_kv_heads, ctx.page_rows * ctx.head_dim)
+        self.n_pages, self.geo = int(n_pages), ctx.geo
+        self.k, self.v = (torch.empty(shape, dtype=ctx.torch_dtype, device=torch.device("cuda", ctx.device)) for _ in range(2))
+        assert self.k.numel() * self.k.element_size() == n.value
+        self.c = d2c_pg_cache(self.k.data_ptr(), self.v.data_ptr(), self.n_pages)
+        self.ref = C.byref(self.c)
+
+
+class PgBatch:
+    """Where n_rows packed rows belong: sequence b has rows row_start[b] .. row_start[b + 1] - 1, length[b] cache rows in pages[b].  The int32
+    tensors are read on the device by each call and may change between calls; at: indices of the rows (None: the last ones of each
+    sequence), origin: where each sequence's mask blocks start."""
+
+    def __init__(self, ctx: PgContext, row_start: torch.Tensor, length: torch.Tensor, pages: torch.Tensor, n_rows: int,
+                 at: Optional[torch.Tensor] = None, origin: Optional[torch.Tensor] = None):
+        batch, cols = pages.shape
+        self.device, self.n_rows, self.keep = ctx.device, int(n_rows), (row_start, length, pages, at, origin)
+        self.c = d2c_pg_batch(_checked(row_start, "row_start", torch.int32, (batch + 1,), ctx.device),
+                              _checked(length, "length", torch.int32, (batch,), ctx.device),
+                              _checked(pages, "pages", torch.int32, (batch, cols), ctx.device),
+                              _checked(at, "at", torch.int32, (self.n_rows,), ctx.device),
+                              _checked(origin, "origin", torch.int32, (batch,), ctx.device), batch, self.n_rows, cols)
+        self.ref = C.byref(self.c)

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libd2c.so")
 SOURCES = ["gemm.hip", "rowwise.hip", "attention.hip", "attention_tiled.hip", "select.hip", "api.hip",
-           "q8_cache.hip", "q8_attention.hip", "q8_linear.hip", "q8_api.hip"]
+           "q8_cache.hip", "q8_attention.hip", "q8_linear.hip", "q8_api.hip", "pg_rows.hip", "pg_attention.hip", "pg_api.hip"]
 # packed FP32 instructions are switched off for every device compile
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-Wno-unused-command-line-argument"]

@@ -1,0 +1,656 @@
+// Attention of the packed rows of a batch over their sequences' pages (see include/d2c_pg.h).
+//
+// For each kv head the m rows of a sequence and the G = H / Hkv heads that share it make R = m G queries, taken 32 at a time.  A wave forms
+// S^T[32 keys x 32 queries] = K Q^T and O^T[D x 32 queries] += V^T P^T with 32 x 32 matrix instructions.  An accumulator of S^T holds, for one query,
+// the keys in just the order in which V lies in its pages, so the probabilities never leave registers; and both K's and V's operands lie
+// there as 16 bytes a lane, so a unit of 32 rows is loaded in whole lines, whatever page it is in.
+//   softmax in base 2 with a reference per query that is raised only when a score passes it by 2^8 (the result is the same softmax); sums in
+//   fp32 before probabilities are rounded to T for the second product.
+//   masks: query r sees the keys lo_r <= j < hi_r.  Keys outside some query's range are looked at again (scores set to -inf, V zeroed where no
+//   query sees it); elsewhere there is no mask.  If such a unit's V holds an infinity or NaN (0 times it would be NaN), its product is done once
+//   for each query, with the V rows that this query sees.
+// The keys of a tile are split over workgroups where tiles alone would not fill the chip; each split leaves its reference, sum and
+// unnormalised O, and a second launch joins them in order.  Which workgroup does what is computed on the device from the row starts and lengths, by every
+// workgroup for itself (plan), so that a captured call follows them.
+#include <algorithm>
+#include <cmath>
+
+#include "internal.h"
+#include "pg.h"
+
+namespace d2c {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr float kFloor = -3.0e38f;      // a reference that no score has raised: finite, so that differences with it are no NaN
+constexpr float kRaise = 8.f;
+
+struct AttendArgs {
+  PgBatch batch;
+  PgPages pages;
+  const void* q;
+  void* out;
+  int64_t q_ld, out_ld;
+  int H, Hkv, page_log2, block, window;
+  float c2;                      // scale * log2(e)
+  int max_splits, part_first, part_limit;      // partial tiles of this launch
+  float* part_o;                 // [part][32][D]
+  float2* part_ml;               // [part][32]: reference, sum
+  float2* row_ml;                // [row][H]: reference, 1 / sum (where the average is wanted), or null
+  int2* info;                    // [sequence]: splits, first part
+};
+
+// ------------------------------------------------------------------ the plan
+
+struct PlanSeq { int row0, m, length, unit0; };     // unit0: first unit that a row of the sequence can see
+struct Plan {
+  PlanSeq* seq;                  // [batch]
+  int* first;                    // [batch + 1] first item
+  int* split;                    // [batch] splits << 24 | first partial tile
+  int chunk, items;              // units of a split
+};
+inline size_t plan_bytes(int batch) { return (size_t)batch * (sizeof(PlanSeq) + 8) + 16; }
+
+__device__ __forceinline__ int wave_sum_int(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+  return v;
+}
+
+// An item is (tile of TILES * 32 queries, split, kv head) of a sequence; kv heads run fastest, so that tiles that read the same keys are a
+// multiple of Hkv workgroups apart (on one XCD where that is a multiple of 8).  The number of splits: of 1 .. 64 for the longest sequence, each lane
+// of a wave takes one and estimates the time as rounds of workgroups times (units of a split + what an item costs besides).
+template <int TILES, int THREADS>
+__device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* lds, float item_cost) {
+  constexpr int kWaves = THREADS / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, batch = a.batch.batch, G = a.H / a.Hkv;
+  Plan p;
+  p.seq = reinterpret_cast<PlanSeq*>(lds);
+  p.first = reinterpret_cast<int*>(lds + (size_t)batch * sizeof(PlanSeq));
+  p.split = p.first + batch + 1;
+  __shared__ float load[kWaves][64];
+  __shared__ int most[kWaves], rows_of[kWaves], result[2];
+  int units = 0, rows = 0;
+  for (int b = tid; b < batch; b += THREADS) {
+    const int lo = a.batch.row_start[b], hi = a.batch.row_start[b + 1], len = a.batch.length[b];
+    PlanSeq s;
+    s.row0 = max(0, min(lo, a.batch.n_rows));
+    s.m = max(0, min(hi, a.batch.n_rows) - s.row0);
+    s.length = max(0, min(len, a.batch.page_cols << a.page_log2));
+    s.unit0 = a.window > 0 && !a.batch.at ? max(0, s.length - s.m - a.window + 1) / kPgUnit : 0;
+    p.seq[b] = s;
+    if (s.m > 0) units = max(units, (s.length + kPgUnit - 1) / kPgUnit - s.unit0);
+    rows = min(rows + s.m, 1 << 22);             // (starts that are not ascending: the sum tells; n_rows is 2^20 at most)
+  }
+  for (int o = 32; o > 0; o >>= 1) {
+    units = max(units, __shfl_xor(units, o, kWave));
+    rows = min(rows + __shfl_xor(rows, o, kWave), 1 << 22);
+  }
+  if (lane == 0) { most[wave] = units; rows_of[wave] = rows; }
+  __syncthreads();
+  units = 1;
+  rows = 0;
+  for (int w = 0; w < kWaves; ++w) { units = max(units, most[w]); rows = min(rows + rows_of[w], 1 << 22); }
+  const bool sane = rows <= a.batch.n_rows;
+  const int chunk = (units + lane) / (lane + 1);          // of lane + 1 splits
+  const float inv = 1.f / (float)chunk;
+  float items = 0.f;
+  for (int b = wave; b < batch; b += kWaves) {
+    const PlanSeq s = p.seq[b];
+    const int tiles = (s.m * G + 32 * TILES - 1) / (32 * TILES), n = (s.length + kPgUnit - 1) / kPgUnit - s.unit0;
+    items += (float)tiles * fmaxf(1.f, ceilf((float)n * inv - 1e-3f));
+  }
+  load[wave][lane] = items * (float)a.Hkv;
+  __syncthreads();
+  float cost = 0.f;
+  for (int w = 0; w < kWaves; ++w) cost += load[w][lane];
+  cost = ceilf(cost / (float)gridDim.x) * ((float)chunk + item_cost);
+  if (lane >= a.max_splits) cost = 3e38f;
+  // the cheapest, of equal ones the fewest splits
+  float best = cost;
+  for (int o = 32; o > 0; o >>= 1) best = fminf(best, __shfl_xor(best, o, kWave));
+  p.chunk = __shfl(chunk, (int)__builtin_ctzll(__ballot(cost == best)), kWave);
+  if (wave == 0) {
+    int item = 0, part = a.part_first;
+    for (int b0 = 0; b0 < batch; b0 += 64) {
+      const int b = b0 + lane;
+      int n_items = 0, n_parts = 0, splits = 1;
+      if (b < batch && sane) {
+        const PlanSeq s = p.seq[b];
+        const int tiles = (s.m * G + 32 * TILES - 1) / (32 * TILES), n = (s.length + kPgUnit - 1) / kPgUnit - s.unit0;
+        splits = max(1, (n + p.chunk - 1) / p.chunk);
+        const int64_t parts = (int64_t)((s.m * G + 31) / 32) * a.Hkv * splits;
+        n_parts = splits > 1 ? (int)min(parts, (int64_t)1 << 24) : 0;
+        n_items = tiles * a.Hkv;
+      }
+      int at_part = n_parts;
+      for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(at_part, o, kWave);
+        if (lane >= o) at_part += v;
+      }
+      // a sequence whose parts have no room is not split
+      const bool fits = part + at_part <= a.part_limit;
+      if (!fits) splits = 1;
+      n_items *= splits;
+      int at_item = n_items;
+      for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(at_item, o, kWave);
+        if (lane >= o) at_item += v;
+      }
+      if (b < batch) {
+        p.first[b] = item + at_item - n_items;
+        p.split[b] = splits << 24 | (splits > 1 ? part + at_part - n_parts : 0);
+      }
+      item += __shfl(at_item, 63, kWave);
+      part = min(part + __shfl(at_part, 63, kWave), 1 << 28);
+    }
+    if (lane == 0) { p.first[batch] = item; result[0] = item; }
+  }
+  __syncthreads();
+  p.items = result[0];
+  // what the join and the average read
+  if (blockIdx.x == 0)
+    for (int b = tid; b < batch; b += THREADS) a.info[b] = make_int2(p.split[b] >> 24, p.split[b] & 0xffffff);
+  return p;
+}
+// the sequence of an item: as many as end at or before it
+__device__ __forceinline__ int seq_of(const Plan& p, int batch, int item) {
+  const int lane = threadIdx.x & 63;
+  int n = 0;
+  for (int b0 = 0; b0 < batch; b0 += 64) n += __popcll(__ballot(b0 + lane < batch && p.first[b0 + min(lane, batch - 1 - b0) + 1] <= item));
+  return n;
+}
+
+// Keys that a row of index i sees: lo <= j < hi, lo > hi - 1 where there are none
+__device__ __forceinline__ void visible(const AttendArgs& a, int i, int origin, int length, int& lo, int& hi) {
+  lo = 0;
+  hi = length;
+  if (a.block > 0) {
+    const int64_t end = i < origin ? origin : origin + ((int64_t)(i - origin) / a.block + 1) * a.block;
+    hi = (int)min((int64_t)length, end);
+  }
+  if (a.window > 0) {
+    lo = (int)max((int64_t)0, (int64_t)i - a.window + 1);
+    if (a.block == 0) hi = (int)min((int64_t)length, (int64_t)i + a.window);
+  }
+  if (i < 0 && (a.batch.at || a.block > 0 || a.window > 0)) hi = 0;
+  if (lo >= hi) { lo = 0x7fffffff; hi = 0; }
+}
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
+// acc += A B^T over a pair of 16-byte pieces per lane: 16 (float: 8) along the contraction
+template <typename T> __device__ __forceinline__ f32x16 mm(const u32x4& a, const u32x4& b, f32x16 acc);
+template <> __device__ __forceinline__ f32x16 mm<bf16>(const u32x4& a, const u32x4& b, f32x16 acc) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x16 mm<float>(const u32x4& a, const u32x4& b, f32x16 acc) {
+  const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], y[j], acc, 0, 0, 0);
+  return acc;
+}
+// key of accumulator element i, within a unit
+template <typename T> __device__ __forceinline__ int key_of(int i, int g) { return sizeof(T) == 2 ? 16 * (i >> 3) + 8 * g + (i & 7) : 8 * (i >> 2) + 4 * g + (i & 3); }
+// probabilities as operands: pieces s = 0 .. 16 / E - 1
+template <typename T> __device__ __forceinline__ u32x4 p_piece(const float (&x)[16], int s);
+template <> __device__ __forceinline__ u32x4 p_piece<bf16>(const float (&x)[16], int s) {
+  return u32x4{pack2(x[8 * s], x[8 * s + 1]), pack2(x[8 * s + 2], x[8 * s + 3]), pack2(x[8 * s + 4], x[8 * s + 5]), pack2(x[8 * s + 6], x[8 * s + 7])};
+}
+template <> __device__ __forceinline__ u32x4 p_piece<float>(const float (&x)[16], int s) {
+  return __builtin_bit_cast(u32x4, f32x4{x[4 * s], x[4 * s + 1], x[4 * s + 2], x[4 * s + 3]});
+}
+// a piece of V with the elements of keys outside [lo, hi) zeroed; key: of its first element
+template <typename T> __device__ __forceinline__ u32x4 keep_keys(u32x4 v, int key, int lo, int hi) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const int k = key + 2 * w;
+      v[w] &= (k >= lo && k < hi ? 0xffffu : 0u) | (k + 1 >= lo && k + 1 < hi ? 0xffff0000u : 0u);
+    }
+  } else {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) v[w] = key + w >= lo && key + w < hi ? v[w] : 0u;
+  }
+  return v;
+}
+template <typename T> __device__ __forceinline__ bool not_finite(const u32x4& v) {
+  bool bad = false;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if constexpr (sizeof(T) == 2) bad = bad || (v[w] & 0x7f80u) == 0x7f80u || (v[w] & 0x7f800000u) == 0x7f800000u;
+    else bad = bad || (v[w] & 0x7f800000u) == 0x7f800000u;
+  }
+  return bad;
+}
+
+// The 32 queries of a tile, one per lane and half: where they are, what they see
+struct Queries {
+  int row, head, lo, hi;          // lo, hi: this lane's query
+  bool valid;
+  int all_lo, all_hi;             // what any of them sees lies within
+  int both_lo, both_hi;           // what all of them see
+};
+__device__ __forceinline__ Queries queries_of(const AttendArgs& a, const PlanSeq& s, int b, int hk, int first, int r32) {
+  const int G = a.H / a.Hkv, R = s.m * G;
+  Queries q;
+  const int r = first + r32;
+  q.valid = r < R;                        // past the last: the tile's first query again, not stored
+  const int use = q.valid ? r : first;
+  q.row = use / G;
+  q.head = hk * G + (use - q.row * G);
+  q.row += s.row0;
+  const int i = a.batch.at ? a.batch.at[q.row] : s.length - s.m + (q.row - s.row0);
+  visible(a, i, a.batch.origin ? max(0, a.batch.origin[b]) : 0, s.length, q.lo, q.hi);
+  q.all_lo = q.both_lo = q.lo;
+  q.all_hi = q.both_hi = q.hi;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    q.all_lo = min(q.all_lo, __shfl_xor(q.all_lo, o, kWave));
+    q.both_lo = max(q.both_lo, __shfl_xor(q.both_lo, o, kWave));
+    q.all_hi = max(q.all_hi, __shfl_xor(q.all_hi, o, kWave));
+    q.both_hi = min(q.both_hi, __shfl_xor(q.both_hi, o, kWave));
+  }
+  q.all_lo = __builtin_amdgcn_readfirstlane(q.all_lo);
+  q.both_lo = __builtin_amdgcn_readfirstlane(q.both_lo);
+  q.all_hi = __builtin_amdgcn_readfirstlane(q.all_hi);
+  q.both_hi = __builtin_amdgcn_readfirstlane(q.both_hi);
+  return q;
+}
+
+// Scores of a unit -> probabilities; o and l are relative to 2^ref, which is raised only where a score passes it by more than kRaise
+template <typename T, int DT>
+__device__ __forceinline__ void softmax_unit(const f32x16& s, bool edge, int key0, const Queries& q, float c2, float& ref, float& l, f32x16 (&o)[DT],
+                                             float (&x)[16]) {
+  const int g = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = s[i];
+  if (edge) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int key = key0 + key_of<T>(i, g);
+      x[i] = key >= q.lo && key < q.hi ? x[i] : -INFINITY;
+    }
+  }
+  float top = x[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+  if (__ballot(top * c2 > ref + kRaise) != 0) {
+    top = fmaxf(top, __shfl_xor(top, 32, kWave)) * c2;
+    const float to = top > ref + kRaise ? top : ref, alpha = exp2_hw(ref - to);
+    ref = to;
+    l *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    x[i] = exp2_hw(fmaf(x[i], c2, -ref));
+    sum += x[i];
+  }
+  l += sum;
+}
+
+// O^T += V^T P^T of one unit whose V pieces are in registers
+template <typename T, int DT>
+__device__ __forceinline__ void values_unit(u32x4 (&v)[kPgUnit / (32 / (int)sizeof(T))][DT], const float (&x)[16], bool edge, int key0, const Queries& q,
+                                            f32x16 (&o)[DT]) {
+  constexpr int E = 16 / sizeof(T), NS = kPgUnit / (2 * E);
+  const int lane = threadIdx.x & 63, g = lane >> 5, r32 = lane & 31;
+  u32x4 p[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) p[s] = p_piece<T>(x, s);
+  bool bad = false;
+  if (edge) {
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        v[s][dt] = keep_keys<T>(v[s][dt], key0 + (2 * s + g) * E, q.all_lo, q.all_hi);
+        bad = bad || not_finite<T>(v[s][dt]);
+      }
+    bad = __ballot(bad) != 0;
+  }
+  if (!bad) {
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt] = mm<T>(v[s][dt], p[s], o[dt]);
+  } else {
+    for (int n = 0; n < 32; ++n) {
+      const int lo = __builtin_amdgcn_readlane(q.lo, n), hi = __builtin_amdgcn_readlane(q.hi, n);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        f32x16 own = {};
+#pragma unroll
+        for (int s = 0; s < NS; ++s) own = mm<T>(keep_keys<T>(v[s][dt], key0 + (2 * s + g) * E, lo, hi), p[s], own);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] = r32 == n ? o[dt][i] + own[i] : o[dt][i];
+      }
+    }
+  }
+}
+
+template <typename T> __device__ __forceinline__ void store2(T* p, float a, float b);
+template <> __device__ __forceinline__ void store2<bf16>(bf16* p, float a, float b) { *reinterpret_cast<uint32_t*>(p) = pack2(a, b); }
+template <> __device__ __forceinline__ void store2<float>(float* p, float a, float b) { *reinterpret_cast<float2*>(p) = make_float2(a, b); }
+
+// ------------------------------------------------------------------ few queries: operands straight from the pages
+
+constexpr int kWaves = 8;
+constexpr int kFewThreads = 64 * kWaves;
+
+// One tile of 32 queries per workgroup: its waves take the units of a split in turn and are merged through LDS.
+template <typename T, int D>
+__global__ __launch_bounds__(kFewThreads) void pg_few_kernel(const AttendArgs a) {
+  constexpr int E = 16 / sizeof(T), DT = D / 32, NF = D / (2 * E), NS = kPgUnit / (2 * E);
+  extern __shared__ __attribute__((aligned(16))) unsigned char plan_lds[];
+  __shared__ float merge[kWaves][DT * 16][64];
+  __shared__ float wref[kWaves][32], wl[kWaves][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
+  const Plan plan = make_plan<1, kFewThreads>(a, plan_lds, 16.f);
+  const int G = a.H / a.Hkv;
+  const size_t head_pitch = (size_t)D << a.page_log2;           // elements
+  for (int item = blockIdx.x; item < plan.items; item += gridDim.x) {
+    const int b = seq_of(plan, a.batch.batch, item);
+    const PlanSeq s = plan.seq[b];
+    const int splits = plan.split[b] >> 24, local = item - plan.first[b];
+    const int hk = local % a.Hkv, split = local / a.Hkv % splits, tile = local / a.Hkv / splits;
+    const Queries q = queries_of(a, s, b, hk, tile * 32, r32);
+    // units of this split that a query sees; none: [0, 0)
+    int u0 = s.unit0 + split * plan.chunk, u1 = splits == 1 ? 0x7fffffff : u0 + plan.chunk;
+    if (splits == 1) u0 = 0;
+    if (q.all_hi > 0) {
+      u0 = max(u0, q.all_lo / kPgUnit);
+      u1 = min(u1, (q.all_hi + kPgUnit - 1) / kPgUnit);
+    } else u1 = u0;
+    const int n_units = max(0, u1 - u0), n_mine = (n_units - wave + kWaves - 1) / kWaves;
+
+    u32x4 qf[NF];
+    const T* qrow = (const T*)a.q + (int64_t)q.row * a.q_ld + q.head * D + g * E;
+#pragma unroll
+    for (int f = 0; f < NF; ++f) qf[f] = ld16(qrow + f * 2 * E);
+
+    f32x16 o[DT] = {};
+    float ref = kFloor, l = 0.f;
+    const int32_t* pages = a.batch.pages + (int64_t)b * a.batch.page_cols;
+    int ids = 0;                              // page numbers of this wave's next 64 units
+    auto page_of = [&](int k) {
+      if ((k & 63) == 0) {
+        const int u = min(u0 + wave + (k + lane) * kWaves, u1 - 1);
+        ids = pages[u >> (a.page_log2 - 5)];
+      }
+      return __builtin_amdgcn_readlane(ids, k & 63);
+    };
+    u32x4 kr[NF], vr[NS][DT];
+    auto load_k = [&](const T* base) {
+#pragma unroll
+      for (int f = 0; f < NF; ++f) kr[f] = ld16(base + ((2 * f + g) * kPgUnit + r32) * E);
+    };
+    auto load_v = [&](const T* base) {
+#pragma unroll
+      for (int st = 0; st < NS; ++st)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vr[st][dt] = ld16(base + ((2 * st + g) * D + 32 * dt + r32) * E);
+    };
+    auto unit_at = [&](int page, int u) {
+      const int in = u & ((1 << (a.page_log2 - 5)) - 1);
+      const int safe = (unsigned)page < (unsigned)a.pages.n_pages ? page : 0;
+      return ((size_t)safe * a.Hkv + hk) * head_pitch + (size_t)in * kPgUnit * D;
+    };
+    for (int k = 0; k < n_mine; ++k) {
+      const int u = u0 + wave + k * kWaves, page = page_of(k);
+      if ((unsigned)page >= (unsigned)a.pages.n_pages) continue;
+      const size_t at = unit_at(page, u);
+      load_k((const T*)a.pages.k + at);
+      load_v((const T*)a.pages.v + at);
+      const int key0 = u * kPgUnit;
+      const bool edge = key0 < q.both_lo || key0 + kPgUnit > q.both_hi;
+      f32x16 acc = {};
+#pragma unroll
+      for (int f = 0; f < NF; ++f) acc = mm<T>(kr[f], qf[f], acc);
+      float x[16];
+      softmax_unit<T, DT>(acc, edge, key0, q, a.c2, ref, l, o, x);
+      values_unit<T, DT>(vr, x, edge, key0, q, o);
+    }
+    l += __shfl_xor(l, 32, kWave);
+
+    // merge the waves that had a unit: each adds up an eighth of every accumulator, two neighbouring dimensions of a query
+    const int n_waves = min(kWaves, n_units);
+    if (wave < n_waves) {
+      if (g == 0) { wref[wave][r32] = ref; wl[wave][r32] = l; }
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) merge[wave][dt * 16 + i][lane] = o[dt][i];
+    }
+    __syncthreads();
+    float top = kFloor, sum = 0.f;
+    for (int w = 0; w < n_waves; ++w) top = fmaxf(top, wref[w][r32]);
+    float y[2][DT] = {};
+    for (int w = 0; w < n_waves; ++w) {
+      const float weight = exp2_hw(wref[w][r32] - top);
+      sum += wl[w][r32] * weight;
+      // a wave that saw nothing of a query has zeros there
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) y[j][dt] = fmaf(merge[w][dt * 16 + 2 * wave + j][lane], weight, y[j][dt]);
+    }
+    const int d0 = 8 * (wave / 2) + 4 * g + wave % 2 * 2;
+    if (q.valid) {
+      if (splits == 1) {
+        const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+        T* to = (T*)a.out + (int64_t)q.row * a.out_ld + q.head * D + d0;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) store2<T>(to + 32 * dt, y[0][dt] * inv, y[1][dt] * inv);
+        if (a.row_ml && wave == 0 && g == 0) a.row_ml[(size_t)q.row * a.H + q.head] = make_float2(top, inv);
+      } else {
+        const int sub = tile, n_sub = (s.m * G + 31) / 32;
+        const size_t part = (size_t)(plan.split[b] & 0xffffff) + ((size_t)hk * n_sub + sub) * splits + split;
+        float* to = a.part_o + (part * 32 + r32) * D + d0;
+        if (n_units > 0) {
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<float2*>(to + 32 * dt) = make_float2(y[0][dt], y[1][dt]);
+        }
+        if (wave == 0 && g == 0) a.part_ml[part * 32 + r32] = make_float2(top, sum);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------ splits joined
+
+// A wave for each query that was split, in the order of the splits.  A split that saw nothing of it (sum 0) is not read.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void pg_join_kernel(const AttendArgs a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, G = a.H / a.Hkv;
+  const int64_t n = (int64_t)a.batch.n_rows * a.H;
+  for (int64_t id = (int64_t)blockIdx.x * 4 + wave; id < n; id += (int64_t)gridDim.x * 4) {
+    const int r = (int)(id / a.H), head = (int)(id % a.H);
+    const PgRowAt row = pg_row_at(a.batch, r, a.page_log2);
+    if (row.seq < 0) continue;
+    const int2 info = a.info[row.seq];
+    if (info.x <= 1) continue;
+    const int row0 = a.batch.row_start[row.seq], m = a.batch.row_start[row.seq + 1] - row0;
+    const int pair = (r - row0) * G + head % G, n_sub = (m * G + 31) / 32;
+    const size_t part = (size_t)info.y + ((size_t)(head / G) * n_sub + pair / 32) * info.x;
+    const float2 ml = lane < info.x ? a.part_ml[(part + lane) * 32 + pair % 32] : make_float2(kFloor, 0.f);
+    const float top = wave_max(ml.x), weight = exp2_hw(ml.x - top);
+    const float sum = wave_sum(ml.y * weight);
+    float2 y = make_float2(0.f, 0.f);
+    for (int s = 0; s < info.x; ++s) {
+      const float w = __shfl(weight, s, kWave);
+      if (__shfl(ml.y, s, kWave) == 0.f) continue;
+      const float* from = a.part_o + ((part + s) * 32 + pair % 32) * D;
+      if constexpr (D == 128) {
+        const float2 v = *reinterpret_cast<const float2*>(from + 2 * lane);
+        y.x = fmaf(v.x, w, y.x);
+        y.y = fmaf(v.y, w, y.y);
+      } else y.x = fmaf(from[lane], w, y.x);
+    }
+    const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+    T* to = (T*)a.out + (int64_t)r * a.out_ld + head * D;
+    if constexpr (D == 128) store2<T>(to + 2 * lane, y.x * inv, y.y * inv);
+    else to[lane] = from_f32<T>(y.x * inv);
+    if (a.row_ml && lane == 0) a.row_ml[id] = make_float2(top, inv);
+  }
+}
+
+// ------------------------------------------------------------------ the head average
+
+// A workgroup takes 32 rows of a sequence and 32 of its keys at a time; its waves take the heads in turn, scores computed again, and the waves'
+// sums are added in order.  blockIdx.y: tiles of 32 rows, sequence after sequence; blockIdx.x: ranges of units.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void pg_average_kernel(const AttendArgs a, float* avg, int64_t avg_ld) {
+  constexpr int E = 16 / sizeof(T), NF = D / (2 * E), kW = 4;
+  __shared__ float sums[kW][32][33];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
+  // the sequence of this tile of rows
+  int b = -1, tile = 0, before = 0;
+  for (int b0 = 0; b0 < a.batch.batch && b < 0; b0 += 64) {
+    const int s = b0 + lane;
+    int n = 0;
+    if (s < a.batch.batch) {
+      const int lo = max(0, min(a.batch.row_start[s], a.batch.n_rows)), hi = min(a.batch.row_start[s + 1], a.batch.n_rows);
+      n = (max(0, hi - lo) + 31) / 32;
+    }
+    int end = n;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(end, o, kWave);
+      if (lane >= o) end += v;
+    }
+    const uint64_t past = __ballot(before + end > (int)blockIdx.y);
+    if (past) {
+      const int at = (int)__builtin_ctzll(past);
+      b = b0 + at;
+      tile = (int)blockIdx.y - (before + __shfl(end - n, at, kWave));
+    } else before += __shfl(end, 63, kWave);
+  }
+  if (b < 0) return;
+  const int row0 = max(0, min(a.batch.row_start[b], a.batch.n_rows)), m = min(a.batch.row_start[b + 1], a.batch.n_rows) - row0;
+  const int length = max(0, min(a.batch.length[b], a.batch.page_cols << a.page_log2));
+  const int cols = (int)min((int64_t)length, avg_ld), G = a.H / a.Hkv;
+  const bool valid = tile * 32 + r32 < m;
+  const int row = row0 + (valid ? tile * 32 + r32 : tile * 32);
+  int lo, hi;
+  visible(a, a.batch.at ? a.batch.at[row] : length - m + (row - row0), a.batch.origin ? max(0, a.batch.origin[b]) : 0, length, lo, hi);
+  const int32_t* pages = a.batch.pages + (int64_t)b * a.batch.page_cols;
+  const size_t head_pitch = (size_t)D << a.page_log2;
+  const float share = 1.f / (float)a.H;
+  for (int u = blockIdx.x; u * kPgUnit < cols; u += gridDim.x) {
+    const int page = pages[u >> (a.page_log2 - 5)], key0 = u * kPgUnit;
+    const bool there = (unsigned)page < (unsigned)a.pages.n_pages;
+    float total[16] = {};
+    if (there) {
+      const size_t at = (size_t)page * a.Hkv * head_pitch + (size_t)(u & ((1 << (a.page_log2 - 5)) - 1)) * kPgUnit * D;
+      for (int head = wave; head < a.H; head += kW) {
+        const T* base = (const T*)a.pages.k + at + (head / G) * head_pitch;
+        const T* qrow = (const T*)a.q + (int64_t)row * a.q_ld + head * D + g * E;
+        const float2 ml = a.row_ml[(size_t)row * a.H + head];
+        f32x16 acc = {};
+#pragma unroll
+        for (int f = 0; f < NF; ++f) acc = mm<T>(ld16(base + ((2 * f + g) * kPgUnit + r32) * E), ld16(qrow + f * 2 * E), acc);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = key0 + key_of<T>(i, g);
+          const float p = exp2_hw(fmaf(acc[i], a.c2, -ml.x)) * ml.y;
+          total[i] += key >= lo && key < hi ? p : 0.f;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sums[wave][r32][key_of<T>(i, g)] = total[i];
+    __syncthreads();
+    for (int c = threadIdx.x; c < 32 * 32; c += 256) {
+      const int rr = c / 32, key = c % 32;
+      float y = 0.f;
+#pragma unroll
+      for (int w = 0; w < kW; ++w) y += sums[w][rr][key];
+      if (tile * 32 + rr < m && key0 + key < cols) avg[(int64_t)(row0 + tile * 32 + rr) * avg_ld + key0 + key] = y * share;
+    }
+    __syncthreads();
+  }
+}
+
+}  // namespace
+
+PgWorkspace pg_workspace(const PgShape& s, int max_rows, int max_batch) {
+  PgWorkspace w{};
+  if (max_rows <= 0) return w;
+  const int64_t G = s.H / s.Hkv;
+  w.parts = (int)std::min<int64_t>(4096, (max_rows * G / 32 + std::min(max_rows, max_batch)) * s.Hkv * kPgMaxSplits);
+  auto take = [&](size_t bytes) {
+    const size_t at = w.bytes;
+    w.bytes += (bytes + 255) & ~(size_t)255;
+    return at;
+  };
+  w.part_o = take((size_t)w.parts * 32 * s.D * 4);
+  w.part_ml = take((size_t)w.parts * 32 * 8);
+  w.row_ml = take((size_t)max_rows * s.H * 8);
+  w.info = take((size_t)max_batch * 8);
+  return w;
+}
+
+template <typename T, int D>
+static hipError_t attention_d(const PgShape& s, AttendArgs a, const PgAttend& call, int cus, hipStream_t st) {
+  const PgBatch& b = a.batch;
+  // units of the longest cache that the page table can name
+  const int64_t units = (int64_t)b.page_cols << (s.page_log2 - 5);
+  a.max_splits = (int)std::min<int64_t>(kPgMaxSplits, std::max<int64_t>(1, units / kWaves));
+  hipError_t e;
+  const size_t lds = plan_bytes(b.batch);
+  hipLaunchKernelGGL((pg_few_kernel<T, D>), dim3(cus), dim3(kFewThreads), lds, st, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (a.max_splits > 1) {
+    const int64_t waves = (int64_t)b.n_rows * s.H;
+    hipLaunchKernelGGL((pg_join_kernel<T, D>), dim3((unsigned)std::min<int64_t>(2048, (waves + 3) / 4)), dim3(256), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (call.avg) {
+    const int64_t tiles = (int64_t)b.n_rows / 32 + std::min(b.n_rows, b.batch);
+    const int64_t cols = std::min<int64_t>(call.avg_ld, (int64_t)b.page_cols << s.page_log2);
+    const int64_t wide = std::max<int64_t>(1, std::min<int64_t>((cols + 31) / 32, 65536));
+    hipLaunchKernelGGL((pg_average_kernel<T, D>), dim3((unsigned)wide, (unsigned)tiles), dim3(256), 0, st, a, call.avg, call.avg_ld);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+hipError_t launch_pg_attention(const PgShape& s, const PgPages& pages, const PgBatch& batch, const PgAttend& call, const PgWorkspace& w, void* ws,
+                               int cus, hipStream_t st) {
+  AttendArgs a{};
+  a.batch = batch;
+  a.pages = pages;
+  a.q = call.q;
+  a.out = call.out;
+  a.q_ld = call.q_ld;
+  a.out_ld = call.out_ld;
+  a.H = s.H;
+  a.Hkv = s.Hkv;
+  a.page_log2 = s.page_log2;
+  a.block = call.block;
+  a.window = call.window;
+  a.c2 = call.scale * 1.44269504088896341f;
+  a.part_first = 0;
+  a.part_limit = w.parts;
+  char* at = (char*)ws;
+  a.part_o = (float*)(at + w.part_o);
+  a.part_ml = (float2*)(at + w.part_ml);
+  a.row_ml = call.avg ? (float2*)(at + w.row_ml) : nullptr;
+  a.info = (int2*)(at + w.info);
+  if (s.dtype == kF32) return s.D == 64 ? attention_d<float, 64>(s, a, call, cus, st) : attention_d<float, 128>(s, a, call, cus, st);
+  return s.D == 64 ? attention_d<bf16, 64>(s, a, call, cus, st) : attention_d<bf16, 128>(s, a, call, cus, st);
+}
+
+}  // namespace d2c
