@@ -61,6 +61,7 @@ template <> __device__ __forceinline__ int pg_slot<bf16>(int t) { return (t & 19
 // The sequence of packed row r and what it says of the row; the whole wave asks for one row.  Starts and lengths arrive in one round of loads.
 struct PgRowAt {
   int seq, index, length;                // seq -1: the row belongs to none
+  int first, count;                      // rows of the sequence
 };
 __device__ __forceinline__ PgRowAt pg_row_at(const PgBatch& b, int r, int page_log2) {
   const int lane = threadIdx.x & 63;
@@ -78,9 +79,11 @@ __device__ __forceinline__ PgRowAt pg_row_at(const PgBatch& b, int r, int page_l
       break;
     }
   }
-  PgRowAt a{-1, 0, 0};
+  PgRowAt a{-1, 0, 0, 0, 0};
   if (seq >= b.batch || r < first || r >= next || first < 0 || next > b.n_rows) return a;
   a.seq = seq;
+  a.first = first;
+  a.count = next - first;
   a.length = max(0, min(len, b.page_cols << page_log2));
   a.index = b.at ? b.at[r] : a.length - (next - first) + (r - first);
   return a;

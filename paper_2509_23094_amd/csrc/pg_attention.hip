@@ -7,8 +7,8 @@
 //   softmax in base 2 with a reference per query that is raised only when a score passes it by 2^8 (the result is the same softmax); sums in
 //   fp32 before probabilities are rounded to T for the second product.
 //   masks: query r sees the keys lo_r <= j < hi_r.  Keys outside some query's range are looked at again (scores set to -inf, V zeroed where no
-//   query sees it); elsewhere there is no mask.  If such a unit's V holds an infinity or NaN (0 times it would be NaN), its product is done once
-//   for each query, with the V rows that this query sees.
+//   query sees it); elsewhere there is no mask.  What is not finite in such a unit's V (0 times it would be NaN) is left out of the product and
+//   added by itself where a query sees it.
 // The keys of a tile are split over workgroups where tiles alone would not fill the chip; each split leaves its reference, sum and
 // unnormalised O, and a second launch joins them in order.  Which workgroup does what is computed on the device from the row starts and lengths, by every
 // workgroup for itself (plan), so that a captured call follows them.
@@ -52,11 +52,22 @@ struct Plan {
 };
 inline size_t plan_bytes(int batch) { return (size_t)batch * (sizeof(PlanSeq) + 8) + 16; }
 
-__device__ __forceinline__ int wave_sum_int(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+// Reductions and scans over the wave by data-parallel moves within it (a shuffle through LDS takes ten times as long, and a plan is all
+// latency).  Inclusive scan: lane 63 ends with the whole.
+template <int CTRL, int ROWS> __device__ __forceinline__ int moved(int v, int none) { return __builtin_amdgcn_update_dpp(none, v, CTRL, ROWS, 0xf, false); }
+template <typename F> __device__ __forceinline__ int scan(int v, int none, F f) {
+  v = f(v, moved<0x111, 0xf>(v, none));        // row_shr 1, 2, 4, 8: within 16 lanes
+  v = f(v, moved<0x112, 0xf>(v, none));
+  v = f(v, moved<0x114, 0xf>(v, none));
+  v = f(v, moved<0x118, 0xf>(v, none));
+  v = f(v, moved<0x142, 0xa>(v, none));        // lane 15 of a row to the next row, lane 31 to the upper half
+  v = f(v, moved<0x143, 0xc>(v, none));
   return v;
 }
+__device__ __forceinline__ int scan_sum(int v) { return scan(v, 0, [](int a, int b) { return a + b; }); }
+__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
+__device__ __forceinline__ int reduce_max(int v) { return last_lane(scan(v, INT32_MIN, [](int a, int b) { return max(a, b); })); }
+__device__ __forceinline__ int reduce_min(int v) { return last_lane(scan(v, INT32_MAX, [](int a, int b) { return min(a, b); })); }
 
 // An item is (tile of TILES * 32 queries, split, kv head) of a sequence; kv heads run fastest, so that tiles that read the same keys are a
 // multiple of Hkv workgroups apart (on one XCD where that is a multiple of 8).  The number of splits: of 1 .. 64 for the longest sequence, each lane
@@ -83,10 +94,8 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
     if (s.m > 0) units = max(units, (s.length + kPgUnit - 1) / kPgUnit - s.unit0);
     rows = min(rows + s.m, 1 << 22);             // (starts that are not ascending: the sum tells; n_rows is 2^20 at most)
   }
-  for (int o = 32; o > 0; o >>= 1) {
-    units = max(units, __shfl_xor(units, o, kWave));
-    rows = min(rows + __shfl_xor(rows, o, kWave), 1 << 22);
-  }
+  units = reduce_max(units);
+  rows = last_lane(scan_sum(rows));
   if (lane == 0) { most[wave] = units; rows_of[wave] = rows; }
   __syncthreads();
   units = 1;
@@ -106,11 +115,10 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
   float cost = 0.f;
   for (int w = 0; w < kWaves; ++w) cost += load[w][lane];
   cost = ceilf(cost / (float)gridDim.x) * ((float)chunk + item_cost);
-  if (lane >= a.max_splits) cost = 3e38f;
-  // the cheapest, of equal ones the fewest splits
-  float best = cost;
-  for (int o = 32; o > 0; o >>= 1) best = fminf(best, __shfl_xor(best, o, kWave));
-  p.chunk = __shfl(chunk, (int)__builtin_ctzll(__ballot(cost == best)), kWave);
+  // the cheapest, of equal ones the fewest splits (a positive float's bits are in its order)
+  const int bits = lane < a.max_splits ? __builtin_bit_cast(int, cost) : INT32_MAX;
+  const int best = reduce_min(bits);
+  p.chunk = __builtin_amdgcn_readlane(chunk, (int)__builtin_ctzll(__ballot(bits == best)));
   if (wave == 0) {
     int item = 0, part = a.part_first;
     for (int b0 = 0; b0 < batch; b0 += 64) {
@@ -124,26 +132,18 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
         n_parts = splits > 1 ? (int)min(parts, (int64_t)1 << 24) : 0;
         n_items = tiles * a.Hkv;
       }
-      int at_part = n_parts;
-      for (int o = 1; o < 64; o <<= 1) {
-        const int v = __shfl_up(at_part, o, kWave);
-        if (lane >= o) at_part += v;
-      }
+      const int at_part = scan_sum(n_parts);
       // a sequence whose parts have no room is not split
       const bool fits = part + at_part <= a.part_limit;
       if (!fits) splits = 1;
       n_items *= splits;
-      int at_item = n_items;
-      for (int o = 1; o < 64; o <<= 1) {
-        const int v = __shfl_up(at_item, o, kWave);
-        if (lane >= o) at_item += v;
-      }
+      const int at_item = scan_sum(n_items);
       if (b < batch) {
         p.first[b] = item + at_item - n_items;
         p.split[b] = splits << 24 | (splits > 1 ? part + at_part - n_parts : 0);
       }
-      item += __shfl(at_item, 63, kWave);
-      part = min(part + __shfl(at_part, 63, kWave), 1 << 28);
+      item += last_lane(at_item);
+      part = min(part + last_lane(at_part), 1 << 28);
     }
     if (lane == 0) { p.first[batch] = item; result[0] = item; }
   }
@@ -220,14 +220,22 @@ template <typename T> __device__ __forceinline__ u32x4 keep_keys(u32x4 v, int ke
   }
   return v;
 }
-template <typename T> __device__ __forceinline__ bool not_finite(const u32x4& v) {
-  bool bad = false;
+// zeroes what is not finite; true if there was something
+template <typename T> __device__ __forceinline__ bool drop_not_finite(u32x4& v) {
+  bool any = false;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    if constexpr (sizeof(T) == 2) bad = bad || (v[w] & 0x7f80u) == 0x7f80u || (v[w] & 0x7f800000u) == 0x7f800000u;
-    else bad = bad || (v[w] & 0x7f800000u) == 0x7f800000u;
+    if constexpr (sizeof(T) == 2) {
+      const bool lo = (v[w] & 0x7f80u) == 0x7f80u, hi = (v[w] & 0x7f800000u) == 0x7f800000u;
+      any = any || lo || hi;
+      v[w] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+    } else {
+      const bool bad = (v[w] & 0x7f800000u) == 0x7f800000u;
+      any = any || bad;
+      v[w] = bad ? 0u : v[w];
+    }
   }
-  return bad;
+  return any;
 }
 
 // The 32 queries of a tile, one per lane and half: where they are, what they see
@@ -248,19 +256,10 @@ __device__ __forceinline__ Queries queries_of(const AttendArgs& a, const PlanSeq
   q.row += s.row0;
   const int i = a.batch.at ? a.batch.at[q.row] : s.length - s.m + (q.row - s.row0);
   visible(a, i, a.batch.origin ? max(0, a.batch.origin[b]) : 0, s.length, q.lo, q.hi);
-  q.all_lo = q.both_lo = q.lo;
-  q.all_hi = q.both_hi = q.hi;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    q.all_lo = min(q.all_lo, __shfl_xor(q.all_lo, o, kWave));
-    q.both_lo = max(q.both_lo, __shfl_xor(q.both_lo, o, kWave));
-    q.all_hi = max(q.all_hi, __shfl_xor(q.all_hi, o, kWave));
-    q.both_hi = min(q.both_hi, __shfl_xor(q.both_hi, o, kWave));
-  }
-  q.all_lo = __builtin_amdgcn_readfirstlane(q.all_lo);
-  q.both_lo = __builtin_amdgcn_readfirstlane(q.both_lo);
-  q.all_hi = __builtin_amdgcn_readfirstlane(q.all_hi);
-  q.both_hi = __builtin_amdgcn_readfirstlane(q.both_hi);
+  q.all_lo = reduce_min(q.lo);
+  q.both_lo = reduce_max(q.lo);
+  q.all_hi = reduce_max(q.hi);
+  q.both_hi = reduce_min(q.hi);
   return q;
 }
 
@@ -300,61 +299,68 @@ __device__ __forceinline__ void softmax_unit(const f32x16& s, bool edge, int key
   l += sum;
 }
 
-// O^T += V^T P^T of one unit whose V pieces are in registers
+// O^T += V^T P^T of one unit whose V pieces are in registers.  In an edge unit V is zeroed where no query sees it, and where it is not finite (0
+// times it would be NaN for the queries that do not see the row): what was dropped is then added for the queries that do.  unit: V in memory.
 template <typename T, int DT>
 __device__ __forceinline__ void values_unit(u32x4 (&v)[kPgUnit / (32 / (int)sizeof(T))][DT], const float (&x)[16], bool edge, int key0, const Queries& q,
-                                            f32x16 (&o)[DT]) {
+                                            const T* unit, f32x16 (&o)[DT]) {
   constexpr int E = 16 / sizeof(T), NS = kPgUnit / (2 * E);
-  const int lane = threadIdx.x & 63, g = lane >> 5, r32 = lane & 31;
-  u32x4 p[NS];
-#pragma unroll
-  for (int s = 0; s < NS; ++s) p[s] = p_piece<T>(x, s);
-  bool bad = false;
+  const int g = (threadIdx.x & 63) >> 5;
+  bool dropped = false;
   if (edge) {
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         v[s][dt] = keep_keys<T>(v[s][dt], key0 + (2 * s + g) * E, q.all_lo, q.all_hi);
-        bad = bad || not_finite<T>(v[s][dt]);
+        dropped = drop_not_finite<T>(v[s][dt]) || dropped;
       }
-    bad = __ballot(bad) != 0;
+    dropped = __ballot(dropped) != 0;
   }
-  if (!bad) {
 #pragma unroll
-    for (int s = 0; s < NS; ++s)
+  for (int s = 0; s < NS; ++s) {
+    const u32x4 p = p_piece<T>(x, s);
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[dt] = mm<T>(v[s][dt], p[s], o[dt]);
-  } else {
-    for (int n = 0; n < 32; ++n) {
-      const int lo = __builtin_amdgcn_readlane(q.lo, n), hi = __builtin_amdgcn_readlane(q.hi, n);
+    for (int dt = 0; dt < DT; ++dt) o[dt] = mm<T>(v[s][dt], p, o[dt]);
+  }
+  if (__builtin_expect(dropped, 0)) {
+#pragma unroll 1
+    for (int j = 0; j < kPgUnit; ++j) {
+      const int key = key0 + j;
+      if (key < q.all_lo || key >= q.all_hi) continue;
+      const bool sees = key >= q.lo && key < q.hi;
+      const T* row = unit + (j / E) * (32 * DT * E) + 4 * g * E + j % E;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        f32x16 own = {};
 #pragma unroll
-        for (int s = 0; s < NS; ++s) own = mm<T>(keep_keys<T>(v[s][dt], key0 + (2 * s + g) * E, lo, hi), p[s], own);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[dt][i] = r32 == n ? o[dt][i] + own[i] : o[dt][i];
+        for (int i = 0; i < 16; ++i) {
+          const float y = to_f32(row[(32 * dt + 8 * (i >> 2) + (i & 3)) * E]);
+          o[dt][i] += sees && !(fabsf(y) <= 3.402823466e38f) ? y : 0.f;
+        }
+        __builtin_amdgcn_sched_barrier(0);       // a tile at a time: this rare path must not cost the loop registers
       }
     }
   }
 }
 
-template <typename T> __device__ __forceinline__ void store2(T* p, float a, float b);
-template <> __device__ __forceinline__ void store2<bf16>(bf16* p, float a, float b) { *reinterpret_cast<uint32_t*>(p) = pack2(a, b); }
-template <> __device__ __forceinline__ void store2<float>(float* p, float a, float b) { *reinterpret_cast<float2*>(p) = make_float2(a, b); }
+template <typename T> __device__ __forceinline__ void store4(T* p, const f32x4& v);
+template <> __device__ __forceinline__ void store4<bf16>(bf16* p, const f32x4& v) { *reinterpret_cast<u32x2*>(p) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])}; }
+template <> __device__ __forceinline__ void store4<float>(float* p, const f32x4& v) { *reinterpret_cast<f32x4*>(p) = v; }
+// of a sum of exponentials: 0 where a row saw nothing, NaN stays
+__device__ __forceinline__ float inverse_of(float sum) { return sum > 0.f ? 1.f / sum : sum; }
 
 // ------------------------------------------------------------------ few queries: operands straight from the pages
 
-constexpr int kWaves = 8;
+constexpr int kWaves = 4;
 constexpr int kFewThreads = 64 * kWaves;
 
 // One tile of 32 queries per workgroup: its waves take the units of a split in turn and are merged through LDS.
 template <typename T, int D>
-__global__ __launch_bounds__(kFewThreads) void pg_few_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs a) {
   constexpr int E = 16 / sizeof(T), DT = D / 32, NF = D / (2 * E), NS = kPgUnit / (2 * E);
   extern __shared__ __attribute__((aligned(16))) unsigned char plan_lds[];
-  __shared__ float merge[kWaves][DT * 16][64];
+  __shared__ __attribute__((aligned(16))) float merge[kWaves][DT * 16][64];       // before: the queries
+  u32x4 (*q_lds)[64] = reinterpret_cast<u32x4 (*)[64]>(&merge[0][0][0]);
   __shared__ float wref[kWaves][32], wl[kWaves][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
   const Plan plan = make_plan<1, kFewThreads>(a, plan_lds, 16.f);
@@ -375,10 +381,13 @@ __global__ __launch_bounds__(kFewThreads) void pg_few_kernel(const AttendArgs a)
     } else u1 = u0;
     const int n_units = max(0, u1 - u0), n_mine = (n_units - wave + kWaves - 1) / kWaves;
 
-    u32x4 qf[NF];
-    const T* qrow = (const T*)a.q + (int64_t)q.row * a.q_ld + q.head * D + g * E;
+    // the queries as operands, for all waves
+    {
+      const T* qrow = (const T*)a.q + (int64_t)q.row * a.q_ld + q.head * D + g * E;
 #pragma unroll
-    for (int f = 0; f < NF; ++f) qf[f] = ld16(qrow + f * 2 * E);
+      for (int f = wave; f < NF; f += kWaves) q_lds[f][lane] = ld16(qrow + f * 2 * E);
+    }
+    __syncthreads();
 
     f32x16 o[DT] = {};
     float ref = kFloor, l = 0.f;
@@ -392,40 +401,68 @@ __global__ __launch_bounds__(kFewThreads) void pg_few_kernel(const AttendArgs a)
       return __builtin_amdgcn_readlane(ids, k & 63);
     };
     u32x4 kr[NF], vr[NS][DT];
-    auto load_k = [&](const T* base) {
-#pragma unroll
-      for (int f = 0; f < NF; ++f) kr[f] = ld16(base + ((2 * f + g) * kPgUnit + r32) * E);
-    };
-    auto load_v = [&](const T* base) {
-#pragma unroll
-      for (int st = 0; st < NS; ++st)
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) vr[st][dt] = ld16(base + ((2 * st + g) * D + 32 * dt + r32) * E);
-    };
-    auto unit_at = [&](int page, int u) {
+    auto unit_at = [&](int page, int u) __attribute__((always_inline)) {
       const int in = u & ((1 << (a.page_log2 - 5)) - 1);
       const int safe = (unsigned)page < (unsigned)a.pages.n_pages ? page : 0;
       return ((size_t)safe * a.Hkv + hk) * head_pitch + (size_t)in * kPgUnit * D;
     };
-    for (int k = 0; k < n_mine; ++k) {
-      const int u = u0 + wave + k * kWaves, page = page_of(k);
-      if ((unsigned)page >= (unsigned)a.pages.n_pages) continue;
-      const size_t at = unit_at(page, u);
-      load_k((const T*)a.pages.k + at);
-      load_v((const T*)a.pages.v + at);
-      const int key0 = u * kPgUnit;
-      const bool edge = key0 < q.both_lo || key0 + kPgUnit > q.both_hi;
-      f32x16 acc = {};
+    const int k_lane = (g * kPgUnit + r32) * 16, v_lane = (g * D + r32) * 16;
+    constexpr int kUnitBytes = kPgUnit * D * (int)sizeof(T);
+    auto load_k = [&](size_t at) __attribute__((always_inline)) {
+      const __amdgpu_buffer_rsrc_t src = __builtin_amdgcn_make_buffer_rsrc((T*)a.pages.k + at, 0, kUnitBytes, 0x00020000);
 #pragma unroll
-      for (int f = 0; f < NF; ++f) acc = mm<T>(kr[f], qf[f], acc);
-      float x[16];
-      softmax_unit<T, DT>(acc, edge, key0, q, a.c2, ref, l, o, x);
-      values_unit<T, DT>(vr, x, edge, key0, q, o);
+      for (int f = 0; f < NF; ++f) kr[f] = __builtin_amdgcn_raw_buffer_load_b128(src, k_lane, f * (2 * kPgUnit * 16), 0);
+    };
+    auto load_v = [&](size_t at) __attribute__((always_inline)) {
+      const __amdgpu_buffer_rsrc_t src = __builtin_amdgcn_make_buffer_rsrc((T*)a.pages.v + at, 0, kUnitBytes, 0x00020000);
+#pragma unroll
+      for (int st = 0; st < NS; ++st)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vr[st][dt] = __builtin_amdgcn_raw_buffer_load_b128(src, v_lane, (2 * st * D + 32 * dt) * 16, 0);
+    };
+    // The next unit's K is requested as soon as this one's is used, V likewise.  Float heads of 128 have no registers for that: K when it is
+    // needed, V behind the scores.
+    constexpr bool kAhead = sizeof(T) == 2 || D == 64;
+    int page = 0, next = 0;
+    size_t at = 0, at_next = 0;
+    if (n_mine > 0) {
+      page = page_of(0);
+      at = unit_at(page, u0 + wave);
+      if (kAhead) {
+        load_k(at);
+        load_v(at);
+      }
+    }
+    for (int k = 0; k < n_mine; ++k) {
+      const int u = u0 + wave + k * kWaves, key0 = u * kPgUnit;
+      const bool more = k + 1 < n_mine, there = (unsigned)page < (unsigned)a.pages.n_pages;
+      if (more) {
+        next = page_of(k + 1);
+        at_next = unit_at(next, u + kWaves);
+      }
+      if (there) {
+        const bool edge = key0 < q.both_lo || key0 + kPgUnit > q.both_hi;
+        if (!kAhead) load_k(at);
+        f32x16 acc = {};
+#pragma unroll
+        for (int f = 0; f < NF; ++f) acc = mm<T>(kr[f], q_lds[f][lane], acc);
+        if (!kAhead) {
+          __builtin_amdgcn_sched_barrier(0);
+          load_v(at);
+        } else if (more) load_k(at_next);
+        float x[16];
+        softmax_unit<T, DT>(acc, edge, key0, q, a.c2, ref, l, o, x);
+        values_unit<T, DT>(vr, x, edge, key0, q, (const T*)a.pages.v + at, o);
+      } else if (kAhead && more) load_k(at_next);
+      if (kAhead && more) load_v(at_next);
+      page = next;
+      at = at_next;
     }
     l += __shfl_xor(l, 32, kWave);
 
     // merge the waves that had a unit: each adds up an eighth of every accumulator, two neighbouring dimensions of a query
     const int n_waves = min(kWaves, n_units);
+    __syncthreads();
     if (wave < n_waves) {
       if (g == 0) { wref[wave][r32] = ref; wl[wave][r32] = l; }
 #pragma unroll
@@ -436,31 +473,30 @@ __global__ __launch_bounds__(kFewThreads) void pg_few_kernel(const AttendArgs a)
     __syncthreads();
     float top = kFloor, sum = 0.f;
     for (int w = 0; w < n_waves; ++w) top = fmaxf(top, wref[w][r32]);
-    float y[2][DT] = {};
+    constexpr int kMine = 16 / kWaves;            // accumulators of each tile of dimensions: neighbours
+    float y[DT][kMine] = {};
     for (int w = 0; w < n_waves; ++w) {
       const float weight = exp2_hw(wref[w][r32] - top);
       sum += wl[w][r32] * weight;
-      // a wave that saw nothing of a query has zeros there
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) y[j][dt] = fmaf(merge[w][dt * 16 + 2 * wave + j][lane], weight, y[j][dt]);
+        for (int j = 0; j < kMine; ++j) y[dt][j] = fmaf(merge[w][dt * 16 + kMine * wave + j][lane], weight, y[dt][j]);
     }
-    const int d0 = 8 * (wave / 2) + 4 * g + wave % 2 * 2;
+    const int d0 = 8 * wave + 4 * g;
     if (q.valid) {
       if (splits == 1) {
-        const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+        const float inv = inverse_of(sum);
         T* to = (T*)a.out + (int64_t)q.row * a.out_ld + q.head * D + d0;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) store2<T>(to + 32 * dt, y[0][dt] * inv, y[1][dt] * inv);
+        for (int dt = 0; dt < DT; ++dt) store4<T>(to + 32 * dt, f32x4{y[dt][0] * inv, y[dt][1] * inv, y[dt][2] * inv, y[dt][3] * inv});
         if (a.row_ml && wave == 0 && g == 0) a.row_ml[(size_t)q.row * a.H + q.head] = make_float2(top, inv);
       } else {
-        const int sub = tile, n_sub = (s.m * G + 31) / 32;
-        const size_t part = (size_t)(plan.split[b] & 0xffffff) + ((size_t)hk * n_sub + sub) * splits + split;
+        const size_t part = (size_t)(plan.split[b] & 0xffffff) + ((size_t)hk * ((s.m * G + 31) / 32) + tile) * splits + split;
         float* to = a.part_o + (part * 32 + r32) * D + d0;
         if (n_units > 0) {
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<float2*>(to + 32 * dt) = make_float2(y[0][dt], y[1][dt]);
+          for (int dt = 0; dt < DT; ++dt) store4<float>(to + 32 * dt, f32x4{y[dt][0], y[dt][1], y[dt][2], y[dt][3]});
         }
         if (wave == 0 && g == 0) a.part_ml[part * 32 + r32] = make_float2(top, sum);
       }
@@ -471,10 +507,12 @@ __global__ __launch_bounds__(kFewThreads) void pg_few_kernel(const AttendArgs a)
 
 // ------------------------------------------------------------------ splits joined
 
-// A wave for each query that was split, in the order of the splits.  A split that saw nothing of it (sum 0) is not read.
+// A wave for each query that was split: its groups of D / 4 lanes take the splits in turn, eight loads at a time, and are added in order.  A split
+// that saw nothing of the query (sum 0) is not read.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void pg_join_kernel(const AttendArgs a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, G = a.H / a.Hkv;
+  constexpr int kLanes = D / 4, kGroups = 64 / kLanes;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, G = a.H / a.Hkv, group = lane / kLanes, d = lane % kLanes * 4;
   const int64_t n = (int64_t)a.batch.n_rows * a.H;
   for (int64_t id = (int64_t)blockIdx.x * 4 + wave; id < n; id += (int64_t)gridDim.x * 4) {
     const int r = (int)(id / a.H), head = (int)(id % a.H);
@@ -482,27 +520,36 @@ __global__ __launch_bounds__(256) void pg_join_kernel(const AttendArgs a) {
     if (row.seq < 0) continue;
     const int2 info = a.info[row.seq];
     if (info.x <= 1) continue;
-    const int row0 = a.batch.row_start[row.seq], m = a.batch.row_start[row.seq + 1] - row0;
-    const int pair = (r - row0) * G + head % G, n_sub = (m * G + 31) / 32;
+    const int pair = (r - row.first) * G + head % G, n_sub = (row.count * G + 31) / 32;
     const size_t part = (size_t)info.y + ((size_t)(head / G) * n_sub + pair / 32) * info.x;
     const float2 ml = lane < info.x ? a.part_ml[(part + lane) * 32 + pair % 32] : make_float2(kFloor, 0.f);
     const float top = wave_max(ml.x), weight = exp2_hw(ml.x - top);
     const float sum = wave_sum(ml.y * weight);
-    float2 y = make_float2(0.f, 0.f);
-    for (int s = 0; s < info.x; ++s) {
-      const float w = __shfl(weight, s, kWave);
-      if (__shfl(ml.y, s, kWave) == 0.f) continue;
-      const float* from = a.part_o + ((part + s) * 32 + pair % 32) * D;
-      if constexpr (D == 128) {
-        const float2 v = *reinterpret_cast<const float2*>(from + 2 * lane);
-        y.x = fmaf(v.x, w, y.x);
-        y.y = fmaf(v.y, w, y.y);
-      } else y.x = fmaf(from[lane], w, y.x);
+    const float* from = a.part_o + (part * 32 + pair % 32) * D + d;
+    f32x4 y = {};
+#pragma unroll 1
+    for (int s0 = 0; s0 < info.x; s0 += 8 * kGroups) {
+      f32x4 v[8];
+      float w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int s = s0 + j * kGroups + group;
+        w[j] = __shfl(weight, min(s, 63), kWave);
+        const float saw = __shfl(ml.y, min(s, 63), kWave);          // (all lanes take part)
+        const bool there = s < info.x && saw != 0.f;
+        v[j] = there ? *reinterpret_cast<const f32x4*>(from + (size_t)s * 32 * D) : f32x4{};
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = fmaf(v[j][i], w[j], y[i]);
     }
-    const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
-    T* to = (T*)a.out + (int64_t)r * a.out_ld + head * D;
-    if constexpr (D == 128) store2<T>(to + 2 * lane, y.x * inv, y.y * inv);
-    else to[lane] = from_f32<T>(y.x * inv);
+#pragma unroll
+    for (int o = kLanes; o < 64; o <<= 1)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] += __shfl_xor(y[i], o, kWave);
+    const float inv = inverse_of(sum);
+    if (group == 0) store4<T>((T*)a.out + (int64_t)r * a.out_ld + head * D + d, y * inv);
     if (a.row_ml && lane == 0) a.row_ml[id] = make_float2(top, inv);
   }
 }
@@ -525,17 +572,13 @@ __global__ __launch_bounds__(256) void pg_average_kernel(const AttendArgs a, flo
       const int lo = max(0, min(a.batch.row_start[s], a.batch.n_rows)), hi = min(a.batch.row_start[s + 1], a.batch.n_rows);
       n = (max(0, hi - lo) + 31) / 32;
     }
-    int end = n;
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(end, o, kWave);
-      if (lane >= o) end += v;
-    }
+    const int end = scan_sum(n);
     const uint64_t past = __ballot(before + end > (int)blockIdx.y);
     if (past) {
       const int at = (int)__builtin_ctzll(past);
       b = b0 + at;
       tile = (int)blockIdx.y - (before + __shfl(end - n, at, kWave));
-    } else before += __shfl(end, 63, kWave);
+    } else before += last_lane(end);
   }
   if (b < 0) return;
   const int row0 = max(0, min(a.batch.row_start[b], a.batch.n_rows)), m = min(a.batch.row_start[b + 1], a.batch.n_rows) - row0;
@@ -610,7 +653,7 @@ static hipError_t attention_d(const PgShape& s, AttendArgs a, const PgAttend& ca
   a.max_splits = (int)std::min<int64_t>(kPgMaxSplits, std::max<int64_t>(1, units / kWaves));
   hipError_t e;
   const size_t lds = plan_bytes(b.batch);
-  hipLaunchKernelGGL((pg_few_kernel<T, D>), dim3(cus), dim3(kFewThreads), lds, st, a);
+  hipLaunchKernelGGL((pg_few_kernel<T, D>), dim3(2 * cus), dim3(kFewThreads), lds, st, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (a.max_splits > 1) {
     const int64_t waves = (int64_t)b.n_rows * s.H;

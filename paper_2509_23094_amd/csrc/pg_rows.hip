@@ -88,7 +88,7 @@ __global__ __launch_bounds__(kThreads) void pg_rows_kernel(const RowsArgs a) {
   const int64_t id = (int64_t)blockIdx.x * (kThreads / 64) + wave;
   const int r = (int)(id / a.parts), part = (int)(id % a.parts);
   if (r >= a.n) return;
-  PgRowAt row{0, 0, 0};
+  PgRowAt row{0, 0, 0, 0, 0};
   if (a.batch.batch > 0) {
     row = pg_row_at(a.batch, r, a.page_log2);
     if (row.seq < 0) return;
