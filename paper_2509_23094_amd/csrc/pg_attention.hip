@@ -14,6 +14,7 @@
 // workgroup for itself (plan), so that a captured call follows them.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "internal.h"
 #include "pg.h"
@@ -34,11 +35,12 @@ struct AttendArgs {
   int64_t q_ld, out_ld;
   int H, Hkv, page_log2, block, window;
   float c2;                      // scale * log2(e)
+  int more_than, up_to;          // queries of a kv head that a sequence has to be this launch's
   int max_splits, part_first, part_limit;      // partial tiles of this launch
   float* part_o;                 // [part][32][D]
   float2* part_ml;               // [part][32]: reference, sum
   float2* row_ml;                // [row][H]: reference, 1 / sum (where the average is wanted), or null
-  int2* info;                    // [sequence]: splits, first part
+  int4* info;                    // [sequence]: splits, first part, tiles of 32 queries that are split
 };
 
 // ------------------------------------------------------------------ the plan
@@ -48,9 +50,10 @@ struct Plan {
   PlanSeq* seq;                  // [batch]
   int* first;                    // [batch + 1] first item
   int* split;                    // [batch] splits << 24 | first partial tile
+  int* whole;                    // [batch] tiles that are not split: the last ones, which come first
   int chunk, items;              // units of a split
 };
-inline size_t plan_bytes(int batch) { return (size_t)batch * (sizeof(PlanSeq) + 8) + 16; }
+inline size_t plan_bytes(int batch) { return (size_t)batch * (sizeof(PlanSeq) + 12) + 16; }
 
 // Reductions and scans over the wave by data-parallel moves within it (a shuffle through LDS takes ten times as long, and a plan is all
 // latency).  Inclusive scan: lane 63 ends with the whole.
@@ -70,8 +73,27 @@ __device__ __forceinline__ int reduce_max(int v) { return last_lane(scan(v, INT3
 __device__ __forceinline__ int reduce_min(int v) { return last_lane(scan(v, INT32_MAX, [](int a, int b) { return min(a, b); })); }
 
 // An item is (tile of TILES * 32 queries, split, kv head) of a sequence; kv heads run fastest, so that tiles that read the same keys are a
-// multiple of Hkv workgroups apart (on one XCD where that is a multiple of 8).  The number of splits: of 1 .. 64 for the longest sequence, each lane
-// of a wave takes one and estimates the time as rounds of workgroups times (units of a split + what an item costs besides).
+// multiple of Hkv workgroups apart (on one XCD where that is a multiple of 8).  As many tiles as fill whole rounds of workgroups are not split (a
+// sequence's last ones, which a mask leaves the most keys, come first); the rest is, in splits of equal length for all sequences: of 1 .. 64 for the
+// longest sequence, each lane of a wave takes one and estimates the time as rounds of workgroups times (units of a split + what an item costs besides).
+template <int TILES> __device__ __forceinline__ int tiles_in(int queries) { return (queries + 32 * TILES - 1) / (32 * TILES); }
+// tiles of 32 queries of a sequence that are split: the first ones
+template <int TILES> __device__ __forceinline__ int split_tiles(const Plan& p, int b, int G) {
+  const int m = p.seq[b].m * G;
+  return min((m + 31) / 32, (tiles_in<TILES>(m) - p.whole[b]) * TILES);
+}
+// Where an item of a sequence is: tile, split, kv head
+struct Place { int tile, hk, split, splits; };
+template <int TILES> __device__ __forceinline__ Place place_of(const Plan& p, int b, int item, int Hkv, int G) {
+  const int local = item - p.first[b], whole = p.whole[b], tiles = tiles_in<TILES>(p.seq[b].m * G), splits = p.split[b] >> 24;
+  const int at = local / Hkv;
+  Place w;
+  w.hk = local - at * Hkv;
+  w.splits = at < whole ? 1 : splits;
+  w.split = at < whole ? 0 : (at - whole) % splits;
+  w.tile = tiles - 1 - (at < whole ? at : whole + (at - whole) / splits);
+  return w;
+}
 template <int TILES, int THREADS>
 __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* lds, float item_cost) {
   constexpr int kWaves = THREADS / 64;
@@ -80,35 +102,46 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
   p.seq = reinterpret_cast<PlanSeq*>(lds);
   p.first = reinterpret_cast<int*>(lds + (size_t)batch * sizeof(PlanSeq));
   p.split = p.first + batch + 1;
+  p.whole = p.split + batch;
   __shared__ float load[kWaves][64];
-  __shared__ int most[kWaves], rows_of[kWaves], result[2];
-  int units = 0, rows = 0;
+  __shared__ int most[kWaves], rows_of[kWaves], tiles_of[kWaves], result[2];
+  int units = 0, rows = 0, tiles = 0;
   for (int b = tid; b < batch; b += THREADS) {
     const int lo = a.batch.row_start[b], hi = a.batch.row_start[b + 1], len = a.batch.length[b];
     PlanSeq s;
     s.row0 = max(0, min(lo, a.batch.n_rows));
     s.m = max(0, min(hi, a.batch.n_rows) - s.row0);
     s.length = max(0, min(len, a.batch.page_cols << a.page_log2));
+    rows = min(rows + s.m, 1 << 22);             // (starts that are not ascending: the sum tells; n_rows is 2^20 at most)
+    if (s.m * G <= a.more_than || s.m * G > a.up_to) s.m = 0;
+    tiles = min(tiles + tiles_in<TILES>(s.m * G), 1 << 25);
     s.unit0 = a.window > 0 && !a.batch.at ? max(0, s.length - s.m - a.window + 1) / kPgUnit : 0;
     p.seq[b] = s;
     if (s.m > 0) units = max(units, (s.length + kPgUnit - 1) / kPgUnit - s.unit0);
-    rows = min(rows + s.m, 1 << 22);             // (starts that are not ascending: the sum tells; n_rows is 2^20 at most)
   }
   units = reduce_max(units);
   rows = last_lane(scan_sum(rows));
-  if (lane == 0) { most[wave] = units; rows_of[wave] = rows; }
+  tiles = last_lane(scan_sum(tiles));
+  if (lane == 0) { most[wave] = units; rows_of[wave] = rows; tiles_of[wave] = tiles; }
   __syncthreads();
   units = 1;
   rows = 0;
-  for (int w = 0; w < kWaves; ++w) { units = max(units, most[w]); rows = min(rows + rows_of[w], 1 << 22); }
+  int all = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    units = max(units, most[w]);
+    rows = min(rows + rows_of[w], 1 << 22);
+    all += tiles_of[w];
+  }
   const bool sane = rows <= a.batch.n_rows;
+  all *= a.Hkv;
+  const float share = all < (int)gridDim.x ? 0.f : (float)(all / (int)gridDim.x * (int)gridDim.x) / (float)all + 1e-6f;      // of tiles that stay whole
   const int chunk = (units + lane) / (lane + 1);          // of lane + 1 splits
   const float inv = 1.f / (float)chunk;
   float items = 0.f;
   for (int b = wave; b < batch; b += kWaves) {
     const PlanSeq s = p.seq[b];
-    const int tiles = (s.m * G + 32 * TILES - 1) / (32 * TILES), n = (s.length + kPgUnit - 1) / kPgUnit - s.unit0;
-    items += (float)tiles * fmaxf(1.f, ceilf((float)n * inv - 1e-3f));
+    const int tiles = tiles_in<TILES>(s.m * G), n = (s.length + kPgUnit - 1) / kPgUnit - s.unit0;
+    items += (float)(tiles - (int)((float)tiles * share)) * fmaxf(1.f, ceilf((float)n * inv - 1e-3f));
   }
   load[wave][lane] = items * (float)a.Hkv;
   __syncthreads();
@@ -123,23 +156,26 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
     int item = 0, part = a.part_first;
     for (int b0 = 0; b0 < batch; b0 += 64) {
       const int b = b0 + lane;
-      int n_items = 0, n_parts = 0, splits = 1;
+      int n_tiles = 0, n_parts = 0, splits = 1, n_whole = 0;
       if (b < batch && sane) {
         const PlanSeq s = p.seq[b];
-        const int tiles = (s.m * G + 32 * TILES - 1) / (32 * TILES), n = (s.length + kPgUnit - 1) / kPgUnit - s.unit0;
+        n_tiles = tiles_in<TILES>(s.m * G);
+        n_whole = (int)((float)n_tiles * share);
+        const int n = (s.length + kPgUnit - 1) / kPgUnit - s.unit0;
         splits = max(1, (n + p.chunk - 1) / p.chunk);
-        const int64_t parts = (int64_t)((s.m * G + 31) / 32) * a.Hkv * splits;
+        const int64_t parts = (int64_t)min((s.m * G + 31) / 32, (n_tiles - n_whole) * TILES) * a.Hkv * splits;
         n_parts = splits > 1 ? (int)min(parts, (int64_t)1 << 24) : 0;
-        n_items = tiles * a.Hkv;
       }
       const int at_part = scan_sum(n_parts);
       // a sequence whose parts have no room is not split
       const bool fits = part + at_part <= a.part_limit;
       if (!fits) splits = 1;
-      n_items *= splits;
+      if (splits == 1) n_whole = n_tiles;
+      const int n_items = (n_whole + (n_tiles - n_whole) * splits) * a.Hkv;
       const int at_item = scan_sum(n_items);
       if (b < batch) {
         p.first[b] = item + at_item - n_items;
+        p.whole[b] = n_whole;
         p.split[b] = splits << 24 | (splits > 1 ? part + at_part - n_parts : 0);
       }
       item += last_lane(at_item);
@@ -151,7 +187,8 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
   p.items = result[0];
   // what the join and the average read
   if (blockIdx.x == 0)
-    for (int b = tid; b < batch; b += THREADS) a.info[b] = make_int2(p.split[b] >> 24, p.split[b] & 0xffffff);
+    for (int b = tid; b < batch; b += THREADS)
+      if (p.seq[b].m > 0) a.info[b] = make_int4(p.split[b] >> 24, p.split[b] & 0xffffff, split_tiles<TILES>(p, b, G), 0);
   return p;
 }
 // the sequence of an item: as many as end at or before it
@@ -263,13 +300,9 @@ __device__ __forceinline__ Queries queries_of(const AttendArgs& a, const PlanSeq
   return q;
 }
 
-// Scores of a unit -> probabilities; o and l are relative to 2^ref, which is raised only where a score passes it by more than kRaise
-template <typename T, int DT>
-__device__ __forceinline__ void softmax_unit(const f32x16& s, bool edge, int key0, const Queries& q, float c2, float& ref, float& l, f32x16 (&o)[DT],
-                                             float (&x)[16]) {
+// A unit's scores, -inf where the query does not see the key
+template <typename T> __device__ __forceinline__ void mask_unit(f32x16& x, bool edge, int key0, const Queries& q) {
   const int g = (threadIdx.x & 63) >> 5;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] = s[i];
   if (edge) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -277,33 +310,65 @@ __device__ __forceinline__ void softmax_unit(const f32x16& s, bool edge, int key
       x[i] = key >= q.lo && key < q.hi ? x[i] : -INFINITY;
     }
   }
+}
+__device__ __forceinline__ float top_of(const f32x16& x) {
   float top = x[0];
 #pragma unroll
   for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-  if (__ballot(top * c2 > ref + kRaise) != 0) {
-    top = fmaxf(top, __shfl_xor(top, 32, kWave)) * c2;
-    const float to = top > ref + kRaise ? top : ref, alpha = exp2_hw(ref - to);
-    ref = to;
-    l *= alpha;
+  return top;
+}
+// o and l are relative to 2^ref, which is raised only where a score (top: this lane's largest) passes it by more than kRaise
+template <int DT> __device__ __forceinline__ void raise(float top, float c2, float& ref, float& l, f32x16 (&o)[DT]) {
+  if (__ballot(top * c2 > ref + kRaise) == 0) return;
+  top = fmaxf(top, __shfl_xor(top, 32, kWave)) * c2;
+  const float to = top > ref + kRaise ? top : ref, alpha = exp2_hw(ref - to);
+  ref = to;
+  l *= alpha;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+  for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
-  }
-  float sum = 0.f;
+    for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
+}
+// masked scores -> probabilities against the reference, as operands; their sum goes to l
+template <typename T> __device__ __forceinline__ void exps_unit(const f32x16& s, float c2, float ref, float& l, u32x4 (&p)[kPgUnit / (32 / (int)sizeof(T))]) {
+  float x[16], sum = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    x[i] = exp2_hw(fmaf(x[i], c2, -ref));
+    x[i] = exp2_hw(fmaf(s[i], c2, -ref));
     sum += x[i];
   }
   l += sum;
+#pragma unroll
+  for (int i = 0; i < kPgUnit / (32 / (int)sizeof(T)); ++i) p[i] = p_piece<T>(x, i);
 }
 
-// O^T += V^T P^T of one unit whose V pieces are in registers.  In an edge unit V is zeroed where no query sees it, and where it is not finite (0
-// times it would be NaN for the queries that do not see the row): what was dropped is then added for the queries that do.  unit: V in memory.
+// What is not finite in the rows of V that some of the queries see, for those that do: 0 times it would be NaN for the others, so products leave it out
+// (V zeroed).  unit: V in memory.
+template <typename T, int DT> __device__ __forceinline__ void add_not_finite(const T* unit, int key0, const Queries& q, f32x16 (&o)[DT]) {
+  constexpr int E = 16 / sizeof(T);
+  const int g = (threadIdx.x & 63) >> 5;
+#pragma unroll 1
+  for (int j = 0; j < kPgUnit; ++j) {
+    const int key = key0 + j;
+    if (key < q.all_lo || key >= q.all_hi) continue;
+    const bool sees = key >= q.lo && key < q.hi;
+    const T* row = unit + (j / E) * (32 * DT * E) + 4 * g * E + j % E;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float y = to_f32(row[(32 * dt + 8 * (i >> 2) + (i & 3)) * E]);
+        o[dt][i] += sees && !(fabsf(y) <= 3.402823466e38f) ? y : 0.f;
+      }
+      __builtin_amdgcn_sched_barrier(0);       // a tile at a time: this rare path must not cost registers
+    }
+  }
+}
+
+// O^T += V^T P^T of one unit whose V pieces are in registers.  In an edge unit V is zeroed where no query sees it, and where it is not finite.
 template <typename T, int DT>
-__device__ __forceinline__ void values_unit(u32x4 (&v)[kPgUnit / (32 / (int)sizeof(T))][DT], const float (&x)[16], bool edge, int key0, const Queries& q,
-                                            const T* unit, f32x16 (&o)[DT]) {
+__device__ __forceinline__ void values_unit(u32x4 (&v)[kPgUnit / (32 / (int)sizeof(T))][DT], const u32x4 (&p)[kPgUnit / (32 / (int)sizeof(T))], bool edge, int key0,
+                                            const Queries& q, const T* unit, f32x16 (&o)[DT]) {
   constexpr int E = 16 / sizeof(T), NS = kPgUnit / (2 * E);
   const int g = (threadIdx.x & 63) >> 5;
   bool dropped = false;
@@ -318,29 +383,10 @@ __device__ __forceinline__ void values_unit(u32x4 (&v)[kPgUnit / (32 / (int)size
     dropped = __ballot(dropped) != 0;
   }
 #pragma unroll
-  for (int s = 0; s < NS; ++s) {
-    const u32x4 p = p_piece<T>(x, s);
+  for (int s = 0; s < NS; ++s)
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[dt] = mm<T>(v[s][dt], p, o[dt]);
-  }
-  if (__builtin_expect(dropped, 0)) {
-#pragma unroll 1
-    for (int j = 0; j < kPgUnit; ++j) {
-      const int key = key0 + j;
-      if (key < q.all_lo || key >= q.all_hi) continue;
-      const bool sees = key >= q.lo && key < q.hi;
-      const T* row = unit + (j / E) * (32 * DT * E) + 4 * g * E + j % E;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float y = to_f32(row[(32 * dt + 8 * (i >> 2) + (i & 3)) * E]);
-          o[dt][i] += sees && !(fabsf(y) <= 3.402823466e38f) ? y : 0.f;
-        }
-        __builtin_amdgcn_sched_barrier(0);       // a tile at a time: this rare path must not cost the loop registers
-      }
-    }
-  }
+    for (int dt = 0; dt < DT; ++dt) o[dt] = mm<T>(v[s][dt], p[s], o[dt]);
+  if (__builtin_expect(dropped, 0)) add_not_finite<T, DT>(unit, key0, q, o);
 }
 
 template <typename T> __device__ __forceinline__ void store4(T* p, const f32x4& v);
@@ -350,6 +396,9 @@ template <> __device__ __forceinline__ void store4<float>(float* p, const f32x4&
 __device__ __forceinline__ float inverse_of(float sum) { return sum > 0.f ? 1.f / sum : sum; }
 
 // ------------------------------------------------------------------ few queries: operands straight from the pages
+
+constexpr int kFewQueries = 512;        // of a sequence and kv head
+constexpr int kManyWaves = 8;
 
 constexpr int kWaves = 4;
 constexpr int kFewThreads = 64 * kWaves;
@@ -369,8 +418,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
   for (int item = blockIdx.x; item < plan.items; item += gridDim.x) {
     const int b = seq_of(plan, a.batch.batch, item);
     const PlanSeq s = plan.seq[b];
-    const int splits = plan.split[b] >> 24, local = item - plan.first[b];
-    const int hk = local % a.Hkv, split = local / a.Hkv % splits, tile = local / a.Hkv / splits;
+    const Place at_item = place_of<1>(plan, b, item, a.Hkv, G);
+    const int hk = at_item.hk, split = at_item.split, tile = at_item.tile, splits = at_item.splits;
     const Queries q = queries_of(a, s, b, hk, tile * 32, r32);
     // units of this split that a query sees; none: [0, 0)
     int u0 = s.unit0 + split * plan.chunk, u1 = splits == 1 ? 0x7fffffff : u0 + plan.chunk;
@@ -450,9 +499,11 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
           __builtin_amdgcn_sched_barrier(0);
           load_v(at);
         } else if (more) load_k(at_next);
-        float x[16];
-        softmax_unit<T, DT>(acc, edge, key0, q, a.c2, ref, l, o, x);
-        values_unit<T, DT>(vr, x, edge, key0, q, (const T*)a.pages.v + at, o);
+        u32x4 p[NS];
+        mask_unit<T>(acc, edge, key0, q);
+        raise<DT>(top_of(acc), a.c2, ref, l, o);
+        exps_unit<T>(acc, a.c2, ref, l, p);
+        values_unit<T, DT>(vr, p, edge, key0, q, (const T*)a.pages.v + at, o);
       } else if (kAhead && more) load_k(at_next);
       if (kAhead && more) load_v(at_next);
       page = next;
@@ -492,7 +543,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
         for (int dt = 0; dt < DT; ++dt) store4<T>(to + 32 * dt, f32x4{y[dt][0] * inv, y[dt][1] * inv, y[dt][2] * inv, y[dt][3] * inv});
         if (a.row_ml && wave == 0 && g == 0) a.row_ml[(size_t)q.row * a.H + q.head] = make_float2(top, inv);
       } else {
-        const size_t part = (size_t)(plan.split[b] & 0xffffff) + ((size_t)hk * ((s.m * G + 31) / 32) + tile) * splits + split;
+        const size_t part = (size_t)(plan.split[b] & 0xffffff) + ((size_t)hk * split_tiles<1>(plan, b, G) + tile) * splits + split;
         float* to = a.part_o + (part * 32 + r32) * D + d0;
         if (n_units > 0) {
 #pragma unroll
@@ -505,52 +556,348 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
   }
 }
 
+// ------------------------------------------------------------------ many queries: K and V shared through LDS
+
+// The descriptor of a buffer of `bytes` from p on, and 64 pieces of 16 bytes from it (this lane's: at voffset + soffset) into LDS from `to` on.  As
+// builtins the compiler waits for all of them in front of any read of LDS; here the kernel waits by itself, once a block.  Nothing is
+// written but LDS, and the wait (for everything that is out) stands before the barrier behind which it is read.
+__device__ __forceinline__ u32x4 buffer_of(const void* p, uint32_t bytes) {
+  const uint64_t at = (uint64_t)p;
+  return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, bytes, 0x00020000u};
+}
+__device__ __forceinline__ void load_to_lds(const unsigned char* to, const u32x4& from, int voffset, int soffset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               :
+               : "s"(lds_address(to)), "v"(voffset), "s"(from), "s"(soffset)
+               : "memory", "m0");
+}
+
+// Eight tiles of 32 queries per workgroup, one a wave.  K and V of 64 keys (float: 32) at a time go from the pages straight into LDS, where they lie as in
+// memory, so that every operand is 16 neighbouring bytes a lane.
+// The two waves of a SIMD take turns: while one is at its matrix instructions (P V of the last block, Q K of this one) the other is at its exponentials.
+// Time goes in half steps, each ended by a barrier: waves 0 - 3 have the products of block k in half step 2k and its softmax in 2k + 1, waves 4 - 7 one
+// half step later.  K of block k + 1 and V of block k are requested at the start of half step 2k (whoever read their places before
+// has passed a barrier since) and have to be there at the end of 2k + 1.
+template <typename T, int D>
+__global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
+  constexpr int E = 16 / sizeof(T), DT = D / 32, NF = D / (2 * E), NS = kPgUnit / (2 * E), kUnits = sizeof(T) == 2 ? 2 : 1;
+  constexpr int kUnitBytes = kPgUnit * D * (int)sizeof(T), kOperand = kUnits * kUnitBytes, kPieces = kUnitBytes / 1024;
+  constexpr int kRing = 4, kPerMm = sizeof(T) == 2 ? 1 : 4, kAll = (1 << kUnits) - 1;
+  extern __shared__ __attribute__((aligned(16))) unsigned char plan_lds[];
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * 2 * kOperand];      // K, K, V, V
+  __shared__ int range[kManyWaves][4], dropped_at[2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
+  const int v_lane = (g * D + r32) * 16;
+  const bool second = wave >= kManyWaves / 2;
+  const Plan plan = make_plan<kManyWaves, 64 * kManyWaves>(a, plan_lds, 8.f);
+  const int G = a.H / a.Hkv;
+  const size_t head_pitch = (size_t)D << a.page_log2;           // elements
+  for (int round = 0; (int64_t)round * gridDim.x < plan.items; ++round) {
+    // every other round backwards (by eights, which stay on their XCD): the tiles of a masked prompt get shorter from item to item
+    const int at_wg = round & 1 ? (int)((gridDim.x / 8 - 1 - blockIdx.x / 8) * 8 + blockIdx.x % 8) : (int)blockIdx.x;
+    const int item = round * gridDim.x + at_wg;
+    if (item >= plan.items) continue;
+    const int b = seq_of(plan, a.batch.batch, item);
+    const PlanSeq s = plan.seq[b];
+    const Place at_item = place_of<kManyWaves>(plan, b, item, a.Hkv, G);
+    const int hk = at_item.hk, split = at_item.split, tile = at_item.tile, splits = at_item.splits, R = s.m * G, sub = tile * kManyWaves + wave;
+    const bool active = sub * 32 < R;
+    const Queries q = queries_of(a, s, b, hk, active ? sub * 32 : tile * kManyWaves * 32, r32);
+    u32x4 qf[NF];
+    const T* qrow = (const T*)a.q + (int64_t)q.row * a.q_ld + q.head * D + g * E;
+#pragma unroll
+    for (int f = 0; f < NF; ++f) qf[f] = ld16(qrow + f * 2 * E);
+    // keys that any wave sees, and that all of them see
+    if (lane == 0) { range[wave][0] = q.all_lo; range[wave][1] = q.all_hi; range[wave][2] = q.both_lo; range[wave][3] = q.both_hi; }
+    if (threadIdx.x < 2) dropped_at[threadIdx.x] = -1;
+    __syncthreads();
+    int lo = range[0][0], hi = range[0][1], in_lo = range[0][2], in_hi = range[0][3];
+#pragma unroll
+    for (int w = 1; w < kManyWaves; ++w) {
+      lo = min(lo, range[w][0]);
+      hi = max(hi, range[w][1]);
+      in_lo = max(in_lo, range[w][2]);
+      in_hi = min(in_hi, range[w][3]);
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    in_lo = __builtin_amdgcn_readfirstlane(in_lo);
+    in_hi = __builtin_amdgcn_readfirstlane(in_hi);
+    int u0 = splits == 1 ? 0 : s.unit0 + split * plan.chunk, u1 = splits == 1 ? 0x7fffffff : u0 + plan.chunk;
+    if (hi > 0) {
+      u0 = max(u0, lo / kPgUnit);
+      u1 = min(u1, (hi + kPgUnit - 1) / kPgUnit);
+    } else u1 = u0;
+    const int n_units = max(0, u1 - u0), n_blocks = (n_units + kUnits - 1) / kUnits;
+
+    const int32_t* pages = a.batch.pages + (int64_t)b * a.batch.page_cols;
+    int ids = 0;                              // page numbers of 64 units
+    uint32_t flags = 0;                       // which units of the blocks k - 1 .. k + 2 are there: kUnits bits at 2 (k % 16)
+    size_t v_at[kUnits] = {};                 // where the block whose V is requested next lies
+    int v_there = 0;
+    auto there = [&](int k) __attribute__((always_inline)) { return (int)(flags >> (2 * (k & 15))) & kAll; };
+    auto piece_loop = [&](unsigned char* to, const T* from) __attribute__((always_inline)) {
+      const u32x4 src = buffer_of(from, kUnitBytes);
+#pragma unroll
+      for (int j = 0; j < (kPieces + kManyWaves - 1) / kManyWaves; ++j) {
+        const int piece = j * kManyWaves + wave;
+        if (kPieces % kManyWaves == 0 || piece < kPieces) load_to_lds(to + piece * 1024, src, lane * 16, piece * 1024);
+      }
+    };
+    // V of block k (found when its K was) and K of block k + 1 into their places
+    auto stage = [&](int k) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u)
+        if (v_there >> u & 1) piece_loop(lds + (2 + (k & 1)) * kOperand + u * kUnitBytes, (const T*)a.pages.v + v_at[u]);
+      v_there = 0;
+      ++k;
+      if (k >= n_blocks) return;
+      if (k * kUnits % 64 == 0) ids = pages[min(u0 + k * kUnits + lane, u1 - 1) >> (a.page_log2 - 5)];
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) {
+        const int unit = k * kUnits + u, page = __builtin_amdgcn_readlane(ids, unit & 63);
+        if (unit < n_units && (unsigned)page < (unsigned)a.pages.n_pages) {
+          v_there |= 1 << u;
+          v_at[u] = ((size_t)page * a.Hkv + hk) * head_pitch + (size_t)((u0 + unit) & ((1 << (a.page_log2 - 5)) - 1)) * kPgUnit * D;
+          piece_loop(lds + (k & 1) * kOperand + u * kUnitBytes, (const T*)a.pages.k + v_at[u]);
+        }
+      }
+      flags = (flags & ~(3u << (2 * (k & 15)))) | (uint32_t)v_there << (2 * (k & 15));
+    };
+    auto requested = [&]() __attribute__((always_inline)) {       // everything this wave has requested is there (vmcnt(0))
+      __builtin_amdgcn_s_waitcnt(0x70 | 0xf00);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto barrier = [&]() __attribute__((always_inline)) {
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
+
+    // V of a block of which a query of the workgroup does not see a key, once it is there: zeroed where none does, and where it is not
+    // finite, so that the products need not look.  All waves; a barrier more.
+    auto inside = [&](int k) __attribute__((always_inline)) {
+      const int key0 = (u0 + k * kUnits) * kPgUnit;
+      return there(k) == kAll && key0 >= in_lo && key0 + kUnits * kPgUnit <= in_hi;
+    };
+    auto clean = [&](int k) __attribute__((always_inline)) {
+      if (inside(k)) return;
+      const int key0 = (u0 + k * kUnits) * kPgUnit;
+      u32x4* v = reinterpret_cast<u32x4*>(lds + (2 + (k & 1)) * kOperand);
+      bool dropped = false;
+      for (int i = threadIdx.x; i < kOperand / 16; i += 64 * kManyWaves) {
+        const int u = i / (kUnitBytes / 16), key = key0 + u * kPgUnit + i % (kUnitBytes / 16) / D * E;
+        u32x4 x = there(k) >> u & 1 ? keep_keys<T>(v[i], key, lo, hi) : u32x4{};
+        dropped = drop_not_finite<T>(x) || dropped;
+        v[i] = x;
+      }
+      if (dropped) dropped_at[k & 1] = k;
+      __syncthreads();
+    };
+
+    f32x16 o[DT] = {}, acc[kUnits];
+    u32x4 p[kUnits][NS];
+    float ref = kFloor, l = 0.f;
+    // One block's P V (the last block's) and Q K as a row of matrix instructions, operands through a ring of registers, the next ones requested right
+    // behind the instruction that uses the last ones (the scheduler is told to keep that order).
+    auto products = [&](auto with_pv, auto with_qk, int k) __attribute__((always_inline)) {
+      constexpr int NV = with_pv ? kUnits * NS * DT : 0, N = NV + (with_qk ? kUnits * NF : 0);
+      const unsigned char *kb = lds + (k & 1) * kOperand + lane * 16, *vb = lds + (2 + (~k & 1)) * kOperand + v_lane;
+      u32x4 ring[kRing];
+      auto read = [&](int i) __attribute__((always_inline)) {
+        return *reinterpret_cast<const u32x4*>(i < NV ? vb + i / (NS * DT) * kUnitBytes + i / DT % NS * (2 * D * 16) + i % DT * 512
+                                                      : kb + (i - NV) / NF * kUnitBytes + (i - NV) % NF * 1024);
+      };
+#pragma unroll
+      for (int i = 0; i < kRing; ++i) ring[i] = read(i);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (i < NV) o[i % DT] = mm<T>(ring[i % kRing], p[i / (NS * DT)][i / DT % NS], o[i % DT]);
+        else {
+          const int u = (i - NV) / NF, f = (i - NV) % NF;
+          acc[u] = mm<T>(ring[i % kRing], qf[f], f == 0 ? f32x16{} : acc[u]);
+        }
+        if (i + kRing < N) ring[i % kRing] = read(i + kRing);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x100, kRing, 0);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, kPerMm, 0);
+        if (i + kRing < N) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (with_pv && !inside(k - 1) && __builtin_expect(__builtin_amdgcn_readfirstlane(dropped_at[~k & 1]) == k - 1, 0)) {
+#pragma unroll 1
+        for (int u = 0; u < kUnits; ++u) {
+          const int unit = u0 + (k - 1) * kUnits + u;
+          if (!(there(k - 1) >> u & 1)) continue;
+          const size_t page = (size_t)pages[unit >> (a.page_log2 - 5)];
+          add_not_finite<T, DT>((const T*)a.pages.v + (page * a.Hkv + hk) * head_pitch + (size_t)(unit & ((1 << (a.page_log2 - 5)) - 1)) * kPgUnit * D,
+                                unit * kPgUnit, q, o);
+        }
+      }
+    };
+    auto softmax = [&](int k) __attribute__((always_inline)) {
+      const int key0 = (u0 + k * kUnits) * kPgUnit;
+      if (!(there(k) == kAll && key0 >= q.both_lo && key0 + kUnits * kPgUnit <= q.both_hi)) {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+          const bool is = there(k) >> u & 1;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = key0 + u * kPgUnit + key_of<T>(i, g);
+            acc[u][i] = is && key >= q.lo && key < q.hi ? acc[u][i] : -INFINITY;
+          }
+        }
+      }
+      float top = top_of(acc[0]);
+#pragma unroll
+      for (int u = 1; u < kUnits; ++u) top = fmaxf(top, top_of(acc[u]));
+      raise<DT>(top, a.c2, ref, l, o);
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) exps_unit<T>(acc[u], a.c2, ref, l, p[u]);
+    };
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+    // the end of half step 2k or 2k + 1
+    auto half = [&]() __attribute__((always_inline)) { barrier(); };
+    auto full = [&](int k) __attribute__((always_inline)) {
+      requested();
+      barrier();
+      clean(k);
+    };
+
+    stage(-1);
+    requested();
+    barrier();
+    if (n_blocks > 0) {
+      if (!second) {
+        stage(0);
+        if (active) products(no, yes, 0);
+        half();
+        if (active) softmax(0);
+        full(0);
+        for (int k = 1; k < n_blocks; ++k) {
+          stage(k);
+          if (active) products(yes, yes, k);
+          half();
+          if (active) softmax(k);
+          full(k);
+        }
+        if (active) products(yes, no, n_blocks);
+        half();
+      } else {
+        stage(0);
+        half();
+        if (active) products(no, yes, 0);
+        full(0);
+        stage(1);
+        if (active) softmax(0);
+        half();
+        for (int k = 1; k < n_blocks; ++k) {
+          if (active) products(yes, yes, k);
+          full(k);
+          stage(k + 1);
+          if (active) softmax(k);
+          half();
+        }
+        if (active) products(yes, no, n_blocks);
+      }
+    }
+
+    l += __shfl_xor(l, 32, kWave);
+    if (active && q.valid) {
+      if (splits == 1) {
+        const float inv = inverse_of(l);
+        T* to = (T*)a.out + (int64_t)q.row * a.out_ld + q.head * D + 4 * g;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 16; i += 4)
+            store4<T>(to + 32 * dt + 2 * i, f32x4{o[dt][i] * inv, o[dt][i + 1] * inv, o[dt][i + 2] * inv, o[dt][i + 3] * inv});
+        if (a.row_ml && g == 0) a.row_ml[(size_t)q.row * a.H + q.head] = make_float2(ref, inv);
+      } else {
+        const size_t part = (size_t)(plan.split[b] & 0xffffff) + ((size_t)hk * split_tiles<kManyWaves>(plan, b, G) + sub) * splits + split;
+        float* to = a.part_o + (part * 32 + r32) * D + 4 * g;
+        if (n_units > 0) {
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) store4<float>(to + 32 * dt + 2 * i, f32x4{o[dt][i], o[dt][i + 1], o[dt][i + 2], o[dt][i + 3]});
+        }
+        if (g == 0) a.part_ml[part * 32 + r32] = make_float2(ref, l);
+      }
+    }
+    __syncthreads();
+  }
+}
+
 // ------------------------------------------------------------------ splits joined
 
-// A wave for each query that was split: its groups of D / 4 lanes take the splits in turn, eight loads at a time, and are added in order.  A split
-// that saw nothing of the query (sum 0) is not read.
+// A workgroup for 8 queries of a tile that was split, two a wave: its groups of D / 4 lanes take the splits in turn, eight loads at a time, and are added
+// in order.  A split that saw nothing of the query (sum 0) is not read.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void pg_join_kernel(const AttendArgs a) {
   constexpr int kLanes = D / 4, kGroups = 64 / kLanes;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, G = a.H / a.Hkv, group = lane / kLanes, d = lane % kLanes * 4;
-  const int64_t n = (int64_t)a.batch.n_rows * a.H;
-  for (int64_t id = (int64_t)blockIdx.x * 4 + wave; id < n; id += (int64_t)gridDim.x * 4) {
-    const int r = (int)(id / a.H), head = (int)(id % a.H);
-    const PgRowAt row = pg_row_at(a.batch, r, a.page_log2);
-    if (row.seq < 0) continue;
-    const int2 info = a.info[row.seq];
-    if (info.x <= 1) continue;
-    const int pair = (r - row.first) * G + head % G, n_sub = (row.count * G + 31) / 32;
-    const size_t part = (size_t)info.y + ((size_t)(head / G) * n_sub + pair / 32) * info.x;
-    const float2 ml = lane < info.x ? a.part_ml[(part + lane) * 32 + pair % 32] : make_float2(kFloor, 0.f);
-    const float top = wave_max(ml.x), weight = exp2_hw(ml.x - top);
-    const float sum = wave_sum(ml.y * weight);
-    const float* from = a.part_o + (part * 32 + pair % 32) * D + d;
-    f32x4 y = {};
-#pragma unroll 1
-    for (int s0 = 0; s0 < info.x; s0 += 8 * kGroups) {
-      f32x4 v[8];
-      float w[8];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = a.H / a.Hkv, group = lane / kLanes, d = lane % kLanes * 4;
+  for (int job = blockIdx.x;; job += gridDim.x) {
+    // the sequence of this job: those that are split have Hkv * (split tiles) * 4 jobs each
+    int b = -1, before = 0, local = 0;
+    int4 info = make_int4(0, 0, 0, 0);
+    for (int b0 = 0; b0 < a.batch.batch && b < 0; b0 += 64) {
+      const int s = b0 + lane;
+      int4 mine = make_int4(1, 0, 0, 0);
+      if (s < a.batch.batch && a.batch.row_start[s + 1] > a.batch.row_start[s]) mine = a.info[s];
+      const int n = mine.x > 1 ? a.Hkv * mine.z * 4 : 0, end = scan_sum(n);
+      const uint64_t past = __ballot(before + end > job);
+      if (past) {
+        const int at = (int)__builtin_ctzll(past);
+        b = b0 + at;
+        local = job - (before + __builtin_amdgcn_readlane(end - n, at));
+        info = make_int4(__builtin_amdgcn_readlane(mine.x, at), __builtin_amdgcn_readlane(mine.y, at), __builtin_amdgcn_readlane(mine.z, at), 0);
+      } else before += last_lane(end);
+    }
+    if (b < 0) return;
+    const int row0 = max(0, min(a.batch.row_start[b], a.batch.n_rows)), m = min(a.batch.row_start[b + 1], a.batch.n_rows) - row0;
+    const int hk = local / (4 * info.z), sub = local / 4 % info.z;
+    const size_t part = (size_t)info.y + ((size_t)hk * info.z + sub) * info.x;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int s = s0 + j * kGroups + group;
-        w[j] = __shfl(weight, min(s, 63), kWave);
-        const float saw = __shfl(ml.y, min(s, 63), kWave);          // (all lanes take part)
-        const bool there = s < info.x && saw != 0.f;
-        v[j] = there ? *reinterpret_cast<const f32x4*>(from + (size_t)s * 32 * D) : f32x4{};
+    for (int j = 0; j < 2; ++j) {
+      const int at = local % 4 * 8 + wave * 2 + j, pair = sub * 32 + at;
+      if (pair >= m * G) continue;
+      const int r = row0 + pair / G, head = hk * G + pair % G;
+      const float2 ml = lane < info.x ? a.part_ml[(part + lane) * 32 + at] : make_float2(kFloor, 0.f);
+      const float top = wave_max(ml.x), weight = exp2_hw(ml.x - top);
+      const float sum = wave_sum(ml.y * weight);
+      const float* from = a.part_o + (part * 32 + at) * D + d;
+      f32x4 y = {};
+#pragma unroll 1
+      for (int s0 = 0; s0 < info.x; s0 += 8 * kGroups) {
+        f32x4 v[8];
+        float w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int s = s0 + i * kGroups + group;
+          w[i] = __shfl(weight, min(s, 63), kWave);
+          const float saw = __shfl(ml.y, min(s, 63), kWave);          // (all lanes take part)
+          const bool there = s < info.x && saw != 0.f;
+          v[i] = there ? *reinterpret_cast<const f32x4*>(from + (size_t)s * 32 * D) : f32x4{};
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) y[k] = fmaf(v[i][k], w[i], y[k]);
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+      for (int o = kLanes; o < 64; o <<= 1)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = fmaf(v[j][i], w[j], y[i]);
+        for (int k = 0; k < 4; ++k) y[k] += __shfl_xor(y[k], o, kWave);
+      const float inv = inverse_of(sum);
+      if (group == 0) store4<T>((T*)a.out + (int64_t)r * a.out_ld + head * D + d, y * inv);
+      if (a.row_ml && lane == 0) a.row_ml[(size_t)r * a.H + head] = make_float2(top, inv);
     }
-#pragma unroll
-    for (int o = kLanes; o < 64; o <<= 1)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] += __shfl_xor(y[i], o, kWave);
-    const float inv = inverse_of(sum);
-    if (group == 0) store4<T>((T*)a.out + (int64_t)r * a.out_ld + head * D + d, y * inv);
-    if (a.row_ml && lane == 0) a.row_ml[id] = make_float2(top, inv);
   }
 }
 
@@ -628,11 +975,13 @@ __global__ __launch_bounds__(256) void pg_average_kernel(const AttendArgs a, flo
 
 }  // namespace
 
+constexpr int kMaxParts = 12288;       // 16.6 KB each with heads of 128
+
 PgWorkspace pg_workspace(const PgShape& s, int max_rows, int max_batch) {
   PgWorkspace w{};
   if (max_rows <= 0) return w;
   const int64_t G = s.H / s.Hkv;
-  w.parts = (int)std::min<int64_t>(4096, (max_rows * G / 32 + std::min(max_rows, max_batch)) * s.Hkv * kPgMaxSplits);
+  w.parts = (int)std::min<int64_t>(kMaxParts, (max_rows * G / 32 + std::min(max_rows, max_batch)) * s.Hkv * kPgMaxSplits);
   auto take = [&](size_t bytes) {
     const size_t at = w.bytes;
     w.bytes += (bytes + 255) & ~(size_t)255;
@@ -641,7 +990,7 @@ PgWorkspace pg_workspace(const PgShape& s, int max_rows, int max_batch) {
   w.part_o = take((size_t)w.parts * 32 * s.D * 4);
   w.part_ml = take((size_t)w.parts * 32 * 8);
   w.row_ml = take((size_t)max_rows * s.H * 8);
-  w.info = take((size_t)max_batch * 8);
+  w.info = take((size_t)max_batch * 16);
   return w;
 }
 
@@ -651,13 +1000,32 @@ static hipError_t attention_d(const PgShape& s, AttendArgs a, const PgAttend& ca
   // units of the longest cache that the page table can name
   const int64_t units = (int64_t)b.page_cols << (s.page_log2 - 5);
   a.max_splits = (int)std::min<int64_t>(kPgMaxSplits, std::max<int64_t>(1, units / kWaves));
-  hipError_t e;
+  hipError_t e = hipSuccess;
   const size_t lds = plan_bytes(b.batch);
-  hipLaunchKernelGGL((pg_few_kernel<T, D>), dim3(2 * cus), dim3(kFewThreads), lds, st, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
+  // Few queries or many: each sequence goes by its own number, which only the device knows.  What the host knows: all of them are few; or there is
+  // one sequence; or as many rows as sequences, single tokens (if they are not, the kernel for few queries takes them tile by tile).
+  const int64_t queries = (int64_t)b.n_rows * (s.H / s.Hkv);
+  const bool few_only = queries <= kFewQueries || b.n_rows <= b.batch, many_only = !few_only && b.batch == 1;
+  const int parts = a.part_limit;
+  if (!many_only) {
+    a.more_than = 0;
+    a.up_to = few_only ? 0x7fffffff : kFewQueries;
+    a.part_limit = few_only ? parts : parts / 4;
+    hipLaunchKernelGGL((pg_few_kernel<T, D>), dim3(2 * cus), dim3(kFewThreads), lds, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (!few_only) {
+    a.more_than = many_only ? 0 : kFewQueries;
+    a.up_to = 0x7fffffff;
+    a.part_first = many_only ? 0 : parts / 4;
+    a.part_limit = parts;
+    hipLaunchKernelGGL((pg_many_kernel<T, D>), dim3(cus), dim3(64 * kManyWaves), lds, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
   if (a.max_splits > 1) {
-    const int64_t waves = (int64_t)b.n_rows * s.H;
-    hipLaunchKernelGGL((pg_join_kernel<T, D>), dim3((unsigned)std::min<int64_t>(2048, (waves + 3) / 4)), dim3(256), 0, st, a);
+    // no more jobs than tiles of 8 queries (a last tile of 32 counts whole), and no more workgroups than fill the chip
+    const int64_t jobs = s.Hkv * 4 * ((queries + 31) / 32 + std::min(b.n_rows, b.batch));
+    hipLaunchKernelGGL((pg_join_kernel<T, D>), dim3((unsigned)std::min<int64_t>(8 * cus, jobs)), dim3(256), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (call.avg) {
@@ -691,7 +1059,7 @@ hipError_t launch_pg_attention(const PgShape& s, const PgPages& pages, const PgB
   a.part_o = (float*)(at + w.part_o);
   a.part_ml = (float2*)(at + w.part_ml);
   a.row_ml = call.avg ? (float2*)(at + w.row_ml) : nullptr;
-  a.info = (int2*)(at + w.info);
+  a.info = (int4*)(at + w.info);
   if (s.dtype == kF32) return s.D == 64 ? attention_d<float, 64>(s, a, call, cus, st) : attention_d<float, 128>(s, a, call, cus, st);
   return s.D == 64 ? attention_d<bf16, 64>(s, a, call, cus, st) : attention_d<bf16, 128>(s, a, call, cus, st);
 }
