@@ -610,15 +610,13 @@ class Q8Batch:
 
 # ---------------------------------------------------------------------- the paged cache (include/d2c_pg.h)
 
-def _rows(t: torch.Tensor, what: str, dtypes, n: int, width: Optional[int], device: int):
+def _rows(t: torch.Tensor, what: str, dtype: torch.dtype, n: int, width: int, device: int):
     """(pointer, pitch in elements) of rows [n, width] whose elements lie together; the rows may lie apart."""
-    if t.dtype not in dtypes or t.dim() != 2 or t.shape[0] != n or (width is not None and t.shape[1] != width) or \
-            (t.shape[1] > 1 and t.stride(1) != 1) or t.get_device() != device:
-        raise D2CError(D2C_EINVAL, "%s: rows of %s, %s x %s on device %d expected, got %s %s strides %s on %s"
-                       % (what, " or ".join(map(str, dtypes)), n, width, device, t.dtype, tuple(t.shape), t.stride(), t.device))
-    if n <= 1:
-        return t.data_ptr(), t.shape[1]              # (a single row's stride can be anything)
-    return t.data_ptr(), t.stride(0)
+    pitch = t.stride()
+    if t.dtype is not dtype or t.shape != (n, width) or t.get_device() != device or pitch[1] != 1:
+        raise D2CError(D2C_EINVAL, "%s: rows of %s, %d x %d on device %d expected, got %s %s strides %s on %s"
+                       % (what, dtype, n, width, device, t.dtype, tuple(t.shape), t.stride(), t.device))
+    return t.data_ptr(), pitch[0] if n > 1 else width              # (a single row's stride can be anything)
 
 
 class Rotary:
@@ -685,12 +683,14 @@ class PgContext:
         return int(_lib.d2c_pg_workspace_bytes(self.handle))
 
     def _source(self, t: torch.Tensor, what: str):
-        if t.dtype not in (torch.float32, self.torch_dtype):
+        if t.dtype is torch.float32:
+            return D2C_F32
+        if t.dtype is not self.torch_dtype:
             raise D2CError(D2C_EINVAL, "%s: float32 or %s expected, got %s" % (what, self.torch_dtype, t.dtype))
-        return D2C_F32 if t.dtype is torch.float32 else D2C_BF16
+        return D2C_BF16
 
     def _pos(self, pos: Optional[torch.Tensor], n: int) -> Optional[int]:
-        return _checked(pos, "pos", torch.int32, (self.n_axes, n), self.device)
+        return None if pos is None else _checked(pos, "pos", torch.int32, (self.n_axes, n), self.device)
 
     def _match(self, cache: "PgCache", batch: "PgBatch") -> None:
         if cache.geo != self.geo or batch.device != self.device:
@@ -700,12 +700,12 @@ class PgContext:
     # ------------------------------------------------------------------ C ABI calls
     def d2c_pg_rotate(self, x: torch.Tensor, pos: torch.Tensor, out: torch.Tensor, inverse: bool = False) -> None:
         """x [n, heads * head_dim] (float32 or the storage type) turned by pos [n_axes, n] into out (storage type; may be x)."""
-        n, width = x.shape
         kind = self._source(x, "x")
-        if width % self.head_dim:
-            raise D2CError(D2C_EINVAL, "x: whole heads expected")
-        xp, x_ld = _rows(x, "x", (x.dtype,), n, width, self.device)
-        op, o_ld = _rows(out, "out", (self.torch_dtype,), n, width, self.device)
+        if x.dim() != 2 or x.shape[1] == 0 or x.shape[1] % self.head_dim:
+            raise D2CError(D2C_EINVAL, "x: rows of whole heads expected, got %s" % (tuple(x.shape),))
+        n, width = x.shape
+        xp, x_ld = _rows(x, "x", x.dtype, n, width, self.device)
+        op, o_ld = _rows(out, "out", self.torch_dtype, n, width, self.device)
         self._check(_lib.d2c_pg_rotate(self.handle, xp, x_ld, kind, n, width // self.head_dim, self._pos(pos, n), int(inverse), op, o_ld,
                                        _stream()))
 
@@ -713,28 +713,28 @@ class PgContext:
                       q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> None:
         """Rows k, v [n_rows, d_kv] into the pages, k turned by pos [n_axes, n_rows] (None: the rows' indices); q likewise into q_out."""
         self._match(cache, batch)
-        n, t = batch.n_rows, (k.dtype,)
+        n, t = batch.n_rows, k.dtype
         a = d2c_pg_new(dtype=self._source(k, "k"), pos=self._pos(pos, n))
         a.k, a.k_ld = _rows(k, "k", t, n, self.d_kv, self.device)
         a.v, a.v_ld = _rows(v, "v", t, n, self.d_kv, self.device)
         if q is not None:
             a.q, a.q_ld = _rows(q, "q", t, n, self.d_q, self.device)
         if q_out is not None:
-            a.q_out, a.q_out_ld = _rows(q_out, "q_out", (self.torch_dtype,), n, self.d_q, self.device)
+            a.q_out, a.q_out_ld = _rows(q_out, "q_out", self.torch_dtype, n, self.d_q, self.device)
         self._check(_lib.d2c_pg_append(self.handle, cache.ref, batch.ref, C.byref(a), _stream()))
 
     def d2c_pg_read(self, cache: "PgCache", batch: "PgBatch", out_k: Optional[torch.Tensor], out_v: Optional[torch.Tensor]) -> None:
         """Values of the cache rows that the batch's rows stand for."""
         self._match(cache, batch)
-        kp, k_ld = _rows(out_k, "out_k", (self.torch_dtype,), batch.n_rows, self.d_kv, self.device) if out_k is not None else (None, 0)
-        vp, v_ld = _rows(out_v, "out_v", (self.torch_dtype,), batch.n_rows, self.d_kv, self.device) if out_v is not None else (None, 0)
+        kp, k_ld = _rows(out_k, "out_k", self.torch_dtype, batch.n_rows, self.d_kv, self.device) if out_k is not None else (None, 0)
+        vp, v_ld = _rows(out_v, "out_v", self.torch_dtype, batch.n_rows, self.d_kv, self.device) if out_v is not None else (None, 0)
         self._check(_lib.d2c_pg_read(self.handle, cache.ref, batch.ref, kp, k_ld, vp, v_ld, _stream()))
 
     def d2c_pg_attention(self, cache: "PgCache", batch: "PgBatch", q: torch.Tensor, out: torch.Tensor, block: int = 0, window: int = 0,
                          scale: Optional[float] = None, attn_avg: Optional[torch.Tensor] = None) -> None:
         """Rows of q [n_rows, d_q] against their sequences' pages: block 0 no mask, 1 causal, more: blocks that see each other in whole."""
         self._match(cache, batch)
-        n, t = batch.n_rows, (self.torch_dtype,)
+        n, t = batch.n_rows, self.torch_dtype
         if scale is not None and not scale > 0:
             raise D2CError(D2C_EINVAL, "scale must be positive")
         a = d2c_pg_attend(block=block, window=window, scale=0.0 if scale is None else scale)

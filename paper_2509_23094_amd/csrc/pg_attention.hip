@@ -40,7 +40,7 @@ struct AttendArgs {
   float* part_o;                 // [part][32][D]
   float2* part_ml;               // [part][32]: reference, sum
   float2* row_ml;                // [row][H]: reference, 1 / sum (where the average is wanted), or null
-  int4* info;                    // [sequence]: splits, first part, tiles of 32 queries that are split
+  int4* info;                    // [sequence]: splits | first part << 8, tiles of 32 queries that are split, first row, rows
 };
 
 // ------------------------------------------------------------------ the plan
@@ -188,7 +188,8 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
   // what the join and the average read
   if (blockIdx.x == 0)
     for (int b = tid; b < batch; b += THREADS)
-      if (p.seq[b].m > 0) a.info[b] = make_int4(p.split[b] >> 24, p.split[b] & 0xffffff, split_tiles<TILES>(p, b, G), 0);
+      if (p.seq[b].m > 0 || a.batch.row_start[b + 1] <= a.batch.row_start[b])      // (empty ones: by every launch)
+        a.info[b] = make_int4(p.split[b] >> 24 | (p.split[b] & 0xffffff) << 8, split_tiles<TILES>(p, b, G), p.seq[b].row0, p.seq[b].m);
   return p;
 }
 // the sequence of an item: as many as end at or before it
@@ -836,67 +837,85 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
 
 // ------------------------------------------------------------------ splits joined
 
-// A workgroup for 8 queries of a tile that was split, two a wave: its groups of D / 4 lanes take the splits in turn, eight loads at a time, and are added
-// in order.  A split that saw nothing of the query (sum 0) is not read.
+// Groups of D / 4 lanes. Up to 8 splits: a group for each query, all of its splits requested at once; more: a workgroup for each query, its groups take
+// the splits in turn, and their sums are added in order.  What a split that saw nothing of the query (sum 0) left is not used.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void pg_join_kernel(const AttendArgs a) {
-  constexpr int kLanes = D / 4, kGroups = 64 / kLanes;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = a.H / a.Hkv, group = lane / kLanes, d = lane % kLanes * 4;
+  constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kFew = 8, kEach = kPgMaxSplits / kGroups;
+  __shared__ f32x4 sums[kGroups][kLanes];
+  const int lane = threadIdx.x & 63, G = a.H / a.Hkv, group = threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
   for (int job = blockIdx.x;; job += gridDim.x) {
-    // the sequence of this job: those that are split have Hkv * (split tiles) * 4 jobs each
     int b = -1, before = 0, local = 0;
     int4 info = make_int4(0, 0, 0, 0);
     for (int b0 = 0; b0 < a.batch.batch && b < 0; b0 += 64) {
-      const int s = b0 + lane;
-      int4 mine = make_int4(1, 0, 0, 0);
-      if (s < a.batch.batch && a.batch.row_start[s + 1] > a.batch.row_start[s]) mine = a.info[s];
-      const int n = mine.x > 1 ? a.Hkv * mine.z * 4 : 0, end = scan_sum(n);
+      const int4 mine = b0 + lane < a.batch.batch ? a.info[b0 + lane] : make_int4(1, 0, 0, 0);
+      const int splits = mine.x & 255, n = splits > 1 ? a.Hkv * mine.y * (splits > kFew ? 32 : 32 / kGroups) : 0, end = scan_sum(n);
       const uint64_t past = __ballot(before + end > job);
       if (past) {
         const int at = (int)__builtin_ctzll(past);
         b = b0 + at;
         local = job - (before + __builtin_amdgcn_readlane(end - n, at));
-        info = make_int4(__builtin_amdgcn_readlane(mine.x, at), __builtin_amdgcn_readlane(mine.y, at), __builtin_amdgcn_readlane(mine.z, at), 0);
+        info = make_int4(__builtin_amdgcn_readlane(mine.x, at), __builtin_amdgcn_readlane(mine.y, at), __builtin_amdgcn_readlane(mine.z, at),
+                         __builtin_amdgcn_readlane(mine.w, at));
       } else before += last_lane(end);
     }
     if (b < 0) return;
-    const int row0 = max(0, min(a.batch.row_start[b], a.batch.n_rows)), m = min(a.batch.row_start[b + 1], a.batch.n_rows) - row0;
-    const int hk = local / (4 * info.z), sub = local / 4 % info.z;
-    const size_t part = (size_t)info.y + ((size_t)hk * info.z + sub) * info.x;
+    const int splits = info.x & 255, per = splits > kFew ? 32 : 32 / kGroups;       // jobs of a tile
+    const int hk = local / (per * info.y), sub = local / per % info.y;
+    const size_t part = (size_t)(info.x >> 8) + ((size_t)hk * info.y + sub) * splits;
+    const int at = splits > kFew ? local % 32 : local % per * kGroups + group, pair = sub * 32 + at;
+    const bool valid = pair < info.w * G;
+    const float2* ml = a.part_ml + part * 32 + (valid ? at : 0);
+    const float* from = a.part_o + (part * 32 + (valid ? at : 0)) * D + d;
+    float top = kFloor, sum = 0.f;
+    f32x4 y = {};
+    if (splits <= kFew) {
+      f32x4 v[kFew];
+      float2 m[kFew];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int at = local % 4 * 8 + wave * 2 + j, pair = sub * 32 + at;
-      if (pair >= m * G) continue;
-      const int r = row0 + pair / G, head = hk * G + pair % G;
-      const float2 ml = lane < info.x ? a.part_ml[(part + lane) * 32 + at] : make_float2(kFloor, 0.f);
-      const float top = wave_max(ml.x), weight = exp2_hw(ml.x - top);
-      const float sum = wave_sum(ml.y * weight);
-      const float* from = a.part_o + (part * 32 + at) * D + d;
-      f32x4 y = {};
-#pragma unroll 1
-      for (int s0 = 0; s0 < info.x; s0 += 8 * kGroups) {
-        f32x4 v[8];
-        float w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int s = s0 + i * kGroups + group;
-          w[i] = __shfl(weight, min(s, 63), kWave);
-          const float saw = __shfl(ml.y, min(s, 63), kWave);          // (all lanes take part)
-          const bool there = s < info.x && saw != 0.f;
-          v[i] = there ? *reinterpret_cast<const f32x4*>(from + (size_t)s * 32 * D) : f32x4{};
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) y[k] = fmaf(v[i][k], w[i], y[k]);
+      for (int i = 0; i < kFew; ++i) {
+        m[i] = i < splits ? ml[i * 32] : make_float2(kFloor, 0.f);
+        v[i] = i < splits ? *reinterpret_cast<const f32x4*>(from + (size_t)i * 32 * D) : f32x4{};
       }
 #pragma unroll
-      for (int o = kLanes; o < 64; o <<= 1)
+      for (int i = 0; i < kFew; ++i) top = fmaxf(top, m[i].x);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) y[k] += __shfl_xor(y[k], o, kWave);
+      for (int i = 0; i < kFew; ++i) {
+        const float w = exp2_hw(m[i].x - top);
+        sum += m[i].y * w;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] += m[i].y == 0.f ? 0.f : v[i][k] * w;
+      }
+    } else {
+      f32x4 v[kEach];
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int s = i * kGroups + group;
+        v[i] = s < splits ? *reinterpret_cast<const f32x4*>(from + (size_t)s * 32 * D) : f32x4{};
+      }
+      const float2 m = lane < splits ? ml[lane * 32] : make_float2(kFloor, 0.f);
+      top = wave_max(m.x);
+      const float weight = exp2_hw(m.x - top);
+      sum = wave_sum(m.y * weight);
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int s = i * kGroups + group;
+        const float w = __shfl(weight, s, kWave), saw = __shfl(m.y, s, kWave);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] += saw == 0.f ? 0.f : v[i][k] * w;
+      }
+      __syncthreads();                       // (the sums of the job before have been read)
+      sums[group][d / 4] = y;
+      __syncthreads();
+      y = sums[0][d / 4];
+#pragma unroll
+      for (int i = 1; i < kGroups; ++i) y += sums[i][d / 4];
+    }
+    if (valid && (splits <= kFew || group == 0)) {
       const float inv = inverse_of(sum);
-      if (group == 0) store4<T>((T*)a.out + (int64_t)r * a.out_ld + head * D + d, y * inv);
-      if (a.row_ml && lane == 0) a.row_ml[(size_t)r * a.H + head] = make_float2(top, inv);
+      const int r = info.z + pair / G, head = hk * G + pair % G;
+      store4<T>((T*)a.out + (int64_t)r * a.out_ld + head * D + d, y * inv);
+      if (a.row_ml && d == 0) a.row_ml[(size_t)r * a.H + head] = make_float2(top, inv);
     }
   }
 }
@@ -1023,8 +1042,8 @@ static hipError_t attention_d(const PgShape& s, AttendArgs a, const PgAttend& ca
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (a.max_splits > 1) {
-    // no more jobs than tiles of 8 queries (a last tile of 32 counts whole), and no more workgroups than fill the chip
-    const int64_t jobs = s.Hkv * 4 * ((queries + 31) / 32 + std::min(b.n_rows, b.batch));
+    // no more workgroups than jobs (a sequence's last tile counts whole), or than fill the chip
+    const int64_t jobs = s.Hkv * (a.max_splits > 8 ? 32 : 4) * ((queries + 31) / 32 + std::min(b.n_rows, b.batch));
     hipLaunchKernelGGL((pg_join_kernel<T, D>), dim3((unsigned)std::min<int64_t>(8 * cus, jobs)), dim3(256), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
