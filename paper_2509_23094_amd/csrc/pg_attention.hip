@@ -27,13 +27,24 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kFloor = -3.0e38f;      // a reference that no score has raised: finite, so that differences with it are no NaN
 constexpr float kRaise = 8.f;
 
+// n / d for n below 2^30 without a division (one takes a wave a quarter of a microsecond): m = ceil(2^(32 + s) / d) is less than d / 2^(32 + s) above
+// the quotient, which n d < 2^(32 + s) 2^30 / 2^31 does not notice; powers of two (m = 0) are shifts.
+struct Div { uint32_t m; int s; };
+inline Div div_by(uint32_t d) {
+  int s = 0;
+  while ((uint64_t)2 << s <= d) ++s;
+  return Div{(d & (d - 1)) == 0 ? 0u : (uint32_t)((((uint64_t)1 << (32 + s)) + d - 1) / d), s};
+}
+__device__ __forceinline__ int operator/(int n, const Div& d) { return (int)((d.m ? __umulhi((uint32_t)n, d.m) : (uint32_t)n) >> d.s); }
+
 struct AttendArgs {
   PgBatch batch;
   PgPages pages;
   const void* q;
   void* out;
   int64_t q_ld, out_ld;
-  int H, Hkv, page_log2, block, window;
+  int H, Hkv, G, page_log2, block, window;
+  Div by_hkv, by_g;
   float c2;                      // scale * log2(e)
   int more_than, up_to;          // queries of a kv head that a sequence has to be this launch's
   int max_splits, part_first, part_limit;      // partial tiles of this launch
@@ -84,20 +95,33 @@ template <int TILES> __device__ __forceinline__ int split_tiles(const Plan& p, i
 }
 // Where an item of a sequence is: tile, split, kv head
 struct Place { int tile, hk, split, splits; };
-template <int TILES> __device__ __forceinline__ Place place_of(const Plan& p, int b, int item, int Hkv, int G) {
-  const int local = item - p.first[b], whole = p.whole[b], tiles = tiles_in<TILES>(p.seq[b].m * G), splits = p.split[b] >> 24;
-  const int at = local / Hkv;
+template <int TILES> __device__ __forceinline__ Place place_of(const AttendArgs& a, const Plan& p, int b, int item) {
+  const int local = item - p.first[b], whole = p.whole[b], tiles = tiles_in<TILES>(p.seq[b].m * a.G), splits = p.split[b] >> 24;
+  const int at = local / a.by_hkv;
   Place w;
-  w.hk = local - at * Hkv;
-  w.splits = at < whole ? 1 : splits;
-  w.split = at < whole ? 0 : (at - whole) % splits;
-  w.tile = tiles - 1 - (at < whole ? at : whole + (at - whole) / splits);
+  w.hk = local - at * a.Hkv;
+  w.splits = 1;
+  w.split = 0;
+  w.tile = tiles - 1 - at;
+  if (at >= whole) {                     // below 2^14 (there are no more partial tiles): the quotient in fp32 is off by one at the most
+    const int n = at - whole;
+    int t = (int)((float)n * __builtin_amdgcn_rcpf((float)splits));
+    t -= n < t * splits;
+    t += n >= (t + 1) * splits;
+    w.splits = splits;
+    w.split = n - t * splits;
+    w.tile = tiles - 1 - whole - t;
+  }
+  w.hk = __builtin_amdgcn_readfirstlane(w.hk);
+  w.splits = __builtin_amdgcn_readfirstlane(w.splits);
+  w.split = __builtin_amdgcn_readfirstlane(w.split);
+  w.tile = __builtin_amdgcn_readfirstlane(w.tile);
   return w;
 }
 template <int TILES, int THREADS>
 __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* lds, float item_cost) {
   constexpr int kWaves = THREADS / 64;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, batch = a.batch.batch, G = a.H / a.Hkv;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, batch = a.batch.batch, G = a.G;
   Plan p;
   p.seq = reinterpret_cast<PlanSeq*>(lds);
   p.first = reinterpret_cast<int*>(lds + (size_t)batch * sizeof(PlanSeq));
@@ -284,12 +308,12 @@ struct Queries {
   int both_lo, both_hi;           // what all of them see
 };
 __device__ __forceinline__ Queries queries_of(const AttendArgs& a, const PlanSeq& s, int b, int hk, int first, int r32) {
-  const int G = a.H / a.Hkv, R = s.m * G;
+  const int G = a.G, R = s.m * G;
   Queries q;
   const int r = first + r32;
   q.valid = r < R;                        // past the last: the tile's first query again, not stored
   const int use = q.valid ? r : first;
-  q.row = use / G;
+  q.row = use / a.by_g;
   q.head = hk * G + (use - q.row * G);
   q.row += s.row0;
   const int i = a.batch.at ? a.batch.at[q.row] : s.length - s.m + (q.row - s.row0);
@@ -414,12 +438,12 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
   __shared__ float wref[kWaves][32], wl[kWaves][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
   const Plan plan = make_plan<1, kFewThreads>(a, plan_lds, 16.f);
-  const int G = a.H / a.Hkv;
+  const int G = a.G;
   const size_t head_pitch = (size_t)D << a.page_log2;           // elements
   for (int item = blockIdx.x; item < plan.items; item += gridDim.x) {
     const int b = seq_of(plan, a.batch.batch, item);
     const PlanSeq s = plan.seq[b];
-    const Place at_item = place_of<1>(plan, b, item, a.Hkv, G);
+    const Place at_item = place_of<1>(a, plan, b, item);
     const int hk = at_item.hk, split = at_item.split, tile = at_item.tile, splits = at_item.splits;
     const Queries q = queries_of(a, s, b, hk, tile * 32, r32);
     // units of this split that a query sees; none: [0, 0)
@@ -431,16 +455,6 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
     } else u1 = u0;
     const int n_units = max(0, u1 - u0), n_mine = (n_units - wave + kWaves - 1) / kWaves;
 
-    // the queries as operands, for all waves
-    {
-      const T* qrow = (const T*)a.q + (int64_t)q.row * a.q_ld + q.head * D + g * E;
-#pragma unroll
-      for (int f = wave; f < NF; f += kWaves) q_lds[f][lane] = ld16(qrow + f * 2 * E);
-    }
-    __syncthreads();
-
-    f32x16 o[DT] = {};
-    float ref = kFloor, l = 0.f;
     const int32_t* pages = a.batch.pages + (int64_t)b * a.batch.page_cols;
     int ids = 0;                              // page numbers of this wave's next 64 units
     auto page_of = [&](int k) {
@@ -483,6 +497,16 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
         load_v(at);
       }
     }
+    // the queries as operands, for all waves (their way to LDS is behind the first unit's requests)
+    {
+      const T* qrow = (const T*)a.q + (int64_t)q.row * a.q_ld + q.head * D + g * E;
+#pragma unroll
+      for (int f = wave; f < NF; f += kWaves) q_lds[f][lane] = ld16(qrow + f * 2 * E);
+    }
+    __syncthreads();
+
+    f32x16 o[DT] = {};
+    float ref = kFloor, l = 0.f;
     for (int k = 0; k < n_mine; ++k) {
       const int u = u0 + wave + k * kWaves, key0 = u * kPgUnit;
       const bool more = k + 1 < n_mine, there = (unsigned)page < (unsigned)a.pages.n_pages;
@@ -591,7 +615,7 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
   const int v_lane = (g * D + r32) * 16;
   const bool second = wave >= kManyWaves / 2;
   const Plan plan = make_plan<kManyWaves, 64 * kManyWaves>(a, plan_lds, 8.f);
-  const int G = a.H / a.Hkv;
+  const int G = a.G;
   const size_t head_pitch = (size_t)D << a.page_log2;           // elements
   for (int round = 0; (int64_t)round * gridDim.x < plan.items; ++round) {
     // every other round backwards (by eights, which stay on their XCD): the tiles of a masked prompt get shorter from item to item
@@ -600,7 +624,7 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
     if (item >= plan.items) continue;
     const int b = seq_of(plan, a.batch.batch, item);
     const PlanSeq s = plan.seq[b];
-    const Place at_item = place_of<kManyWaves>(plan, b, item, a.Hkv, G);
+    const Place at_item = place_of<kManyWaves>(a, plan, b, item);
     const int hk = at_item.hk, split = at_item.split, tile = at_item.tile, splits = at_item.splits, R = s.m * G, sub = tile * kManyWaves + wave;
     const bool active = sub * 32 < R;
     const Queries q = queries_of(a, s, b, hk, active ? sub * 32 : tile * kManyWaves * 32, r32);
@@ -1068,6 +1092,9 @@ hipError_t launch_pg_attention(const PgShape& s, const PgPages& pages, const PgB
   a.out_ld = call.out_ld;
   a.H = s.H;
   a.Hkv = s.Hkv;
+  a.G = s.H / s.Hkv;
+  a.by_hkv = div_by(s.Hkv);
+  a.by_g = div_by(a.G);
   a.page_log2 = s.page_log2;
   a.block = call.block;
   a.window = call.window;
