@@ -60,12 +60,84 @@ template <typename T> __device__ __forceinline__ T* v_place(T* unit, int D, int 
   return unit + (t / E) * (D * E) + d * E + t % E;
 }
 
+// What 32 neighbouring packed rows are, a row a lane (both halves of the wave the same): see pg_row_at.
+__device__ __forceinline__ PgRowAt rows_at(const PgBatch& b, int r0, int page_log2) {
+  const int lane = threadIdx.x & 63, r = r0 + (lane & 31);
+  int seq = 0, first = 0, next = 0, len = 0;
+  bool found = false;
+  for (int s0 = 0; s0 < b.batch && !__all(found); s0 += 64) {
+    const int s = min(s0 + lane, b.batch - 1);
+    const int lo = b.row_start[s], hi = b.row_start[s + 1], n = b.length[s];
+    int mine = 0;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      const int behind = __popcll(__ballot(s0 + lane < b.batch && hi <= r0 + j));
+      mine = (lane & 31) == j ? behind : mine;
+    }
+    const int f = __shfl(lo, min(mine, 63), 64), e = __shfl(hi, min(mine, 63), 64), l = __shfl(n, min(mine, 63), 64);
+    if (!found) {
+      seq += mine;
+      found = mine < 64;
+      first = f;
+      next = e;
+      len = l;
+    }
+  }
+  PgRowAt a{-1, 0, 0, 0, 0};
+  if (!found || seq >= b.batch || r >= b.n_rows || r < first || r >= next || first < 0 || next > b.n_rows) return a;
+  a.seq = seq;
+  a.first = first;
+  a.count = next - first;
+  a.length = max(0, min(len, b.page_cols << page_log2));
+  a.index = b.at ? b.at[r] : a.length - a.count + (r - first);
+  return a;
+}
+
+// 32 packed rows and their places in V, for tiles that turn rows into V's pieces (E rows of a dimension) and back through LDS: rows E of
+// which fill a piece move as 16 bytes, the others value by value (2 bytes, which for a whole prompt of 2500 rows x 4096 took 58 us of 80).
+struct ValueRows {
+  size_t at;                     // of dimension 0, this lane's row
+  uint32_t in, there, lead, rest;      // rows of a sequence; that have a place; first rows of whole pieces; that are in none of those
+};
+template <typename T, int D>
+__device__ __forceinline__ ValueRows value_rows(const PgBatch& batch, int n_pages, int Hkv, int r0, int page_log2) {
+  constexpr int E = 16 / sizeof(T);
+  const int lane = threadIdx.x & 63;
+  const PgRowAt row = rows_at(batch, r0, page_log2);
+  ValueRows v;
+  int page = -1;
+  if (row.seq >= 0 && row.index >= 0 && row.index < row.length) page = batch.pages[(int64_t)row.seq * batch.page_cols + (row.index >> page_log2)];
+  const bool there = (unsigned)page < (unsigned)n_pages;
+  const int in = row.index & ((1 << page_log2) - 1), t = in & (kPgUnit - 1);
+  v.at = there ? (((size_t)page * Hkv) << page_log2) * D + (size_t)(in & ~(kPgUnit - 1)) * D + (t / E) * (D * E) + t % E : 0;
+  v.in = (uint32_t)__ballot(row.seq >= 0);
+  v.there = (uint32_t)__ballot(there);
+  const int lo = (int)(uint32_t)v.at, hi = (int)(uint32_t)(v.at >> 32);
+  bool lead = there && t % E == 0 && (lane & 31) + E <= 32;
+#pragma unroll
+  for (int k = 1; k < E; ++k) {
+    const int l = __shfl(lo, (lane + k) & 63, 64), h = __shfl(hi, (lane + k) & 63, 64);
+    lead = lead && (v.there >> ((lane + k) & 31) & 1) && h == hi && l == lo + k;
+  }
+  v.lead = (uint32_t)__ballot(lead);
+  uint32_t whole = 0;
+#pragma unroll
+  for (int k = 0; k < E; ++k) whole |= v.lead << k;
+  v.rest = v.there & ~whole;
+  return v;
+}
+__device__ __forceinline__ size_t value_at(const ValueRows& v, int j) {
+  return (size_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v.at, j) | (size_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v.at >> 32), j) << 32;
+}
+template <typename T, int D> constexpr int kTileBytes = 32 * (D + 16 / (int)sizeof(T)) * (int)sizeof(T);
+
 struct RowsArgs {
   PgRotation rot;
   PgBatch batch;
   PgRows rows;
   PgPages pages;
   int n, parts, H, Hkv, page_log2;
+  int v_tiles, v_heads;                  // workgroups in front that bring V in tiles (0: with the rows), kv heads of each
 };
 
 // Where dimension octets of chunk `sub` (16 dimensions of a head) lie, and its first pair (-1: not turned)
@@ -81,11 +153,53 @@ template <bool kNeighbours> __device__ __forceinline__ void chunk_of(int sub, in
   }
 }
 
+// 32 rows of V into their pages, v_heads kv heads of them
+template <typename TS, typename T, int D> __device__ __forceinline__ void put_values(const RowsArgs& a, T* tile) {
+  constexpr int E = 16 / sizeof(T), kPitch = D + E;
+  const int groups = (a.n + 31) / 32, r0 = (int)blockIdx.x % groups * 32, h0 = (int)blockIdx.x / groups * a.v_heads;
+  const ValueRows v = value_rows<T, D>(a.batch, a.pages.n_pages, a.Hkv, r0, a.page_log2);
+  if (v.there == 0) return;
+  const int d = threadIdx.x % D;
+  for (int h = h0; h < min(a.Hkv, h0 + a.v_heads); ++h) {
+    T* out = (T*)a.pages.v + (((size_t)h * D) << a.page_log2) + (size_t)d * E;
+    for (int c = threadIdx.x; c < 32 * (D / 8); c += kThreads) {
+      const int j = c / (D / 8), at = c % (D / 8) * 8;
+      if (v.there >> j & 1) {
+        float x[8];
+        load8((const TS*)a.rows.v + (int64_t)(r0 + j) * a.rows.v_ld + h * D + at, x);
+        store8(tile + j * kPitch + at, x);
+      }
+    }
+    __syncthreads();
+    int i = threadIdx.x / D;                   // (whole waves: D is 64 or 128)
+    for (uint32_t m = v.lead; m; m &= m - 1, --i) {
+      if (i % (kThreads / D)) continue;
+      const int j = __builtin_ctz(m);
+      union { T x[E]; u32x4 raw; } w;
+#pragma unroll
+      for (int k = 0; k < E; ++k) w.x[k] = tile[(j + k) * kPitch + d];
+      *reinterpret_cast<u32x4*>(out + value_at(v, j)) = w.raw;
+    }
+    i = threadIdx.x / D;
+    for (uint32_t m = v.rest; m; m &= m - 1, --i) {
+      if (i % (kThreads / D)) continue;
+      const int j = __builtin_ctz(m);
+      out[value_at(v, j)] = tile[j * kPitch + d];
+    }
+    __syncthreads();
+  }
+}
+
 template <typename TS, typename T, int D, bool kNeighbours>
 __global__ __launch_bounds__(kThreads) void pg_rows_kernel(const RowsArgs a) {
   __shared__ float2 table[kThreads / 64][64];
+  __shared__ __attribute__((aligned(16))) unsigned char tile_lds[kTileBytes<T, D>];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t id = (int64_t)blockIdx.x * (kThreads / 64) + wave;
+  if ((int)blockIdx.x < a.v_tiles) {
+    put_values<TS, T, D>(a, reinterpret_cast<T*>(tile_lds));
+    return;
+  }
+  const int64_t id = (int64_t)(blockIdx.x - a.v_tiles) * (kThreads / 64) + wave;
   const int r = (int)(id / a.parts), part = (int)(id % a.parts);
   if (r >= a.n) return;
   PgRowAt row{0, 0, 0, 0, 0};
@@ -122,7 +236,7 @@ __global__ __launch_bounds__(kThreads) void pg_rows_kernel(const RowsArgs a) {
   __builtin_amdgcn_wave_barrier();
 
   constexpr int kSub = D / 16;
-  const int nq = a.rows.q ? a.rows.q_heads * kSub : 0, nk = a.rows.k ? a.Hkv * kSub : 0, total = nq + 2 * nk;
+  const int nq = a.rows.q ? a.rows.q_heads * kSub : 0, nk = a.rows.k ? a.Hkv * kSub : 0, total = nq + (a.v_tiles ? nk : 2 * nk);
   const int per = ((total + 63) / 64 + a.parts - 1) / a.parts * 64;
   const int end = min(total, (part + 1) * per);
   for (int c = part * per + lane; c < end; c += 64) {
@@ -182,12 +296,55 @@ struct ReadArgs {
   void *out_k, *out_v;
   int64_t k_ld, v_ld;
   int parts, Hkv, page_log2;
+  int v_tiles, v_heads;                  // as above
 };
+
+// 32 rows of V from their pages
+template <typename T, int D> __device__ __forceinline__ void get_values(const ReadArgs& a, T* tile) {
+  constexpr int E = 16 / sizeof(T), kPitch = D + E;
+  const int groups = (a.batch.n_rows + 31) / 32, r0 = (int)blockIdx.x % groups * 32, h0 = (int)blockIdx.x / groups * a.v_heads;
+  const ValueRows v = value_rows<T, D>(a.batch, a.pages.n_pages, a.Hkv, r0, a.page_log2);
+  if (v.in == 0) return;
+  const int d = threadIdx.x % D;
+  for (int h = h0; h < min(a.Hkv, h0 + a.v_heads); ++h) {
+    const T* from = (const T*)a.pages.v + (((size_t)h * D) << a.page_log2) + (size_t)d * E;
+    int i = threadIdx.x / D;
+    for (uint32_t m = v.lead; m; m &= m - 1, --i) {
+      if (i % (kThreads / D)) continue;
+      const int j = __builtin_ctz(m);
+      union { T x[E]; u32x4 raw; } w;
+      w.raw = ld16(from + value_at(v, j));
+#pragma unroll
+      for (int k = 0; k < E; ++k) tile[(j + k) * kPitch + d] = w.x[k];
+    }
+    i = threadIdx.x / D;
+    for (uint32_t m = v.rest; m; m &= m - 1, --i) {
+      if (i % (kThreads / D)) continue;
+      const int j = __builtin_ctz(m);
+      tile[j * kPitch + d] = from[value_at(v, j)];
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 32 * (D / 8); c += kThreads) {
+      const int j = c / (D / 8), at = c % (D / 8) * 8;
+      if (v.in >> j & 1) {
+        float x[8] = {};
+        if (v.there >> j & 1) load8(tile + j * kPitch + at, x);
+        store8((T*)a.out_v + (int64_t)(r0 + j) * a.v_ld + h * D + at, x);
+      }
+    }
+    __syncthreads();
+  }
+}
 
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void pg_read_kernel(const ReadArgs a) {
+  __shared__ __attribute__((aligned(16))) unsigned char tile_lds[kTileBytes<T, D>];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t id = (int64_t)blockIdx.x * (kThreads / 64) + wave;
+  if ((int)blockIdx.x < a.v_tiles) {
+    get_values<T, D>(a, reinterpret_cast<T*>(tile_lds));
+    return;
+  }
+  const int64_t id = (int64_t)(blockIdx.x - a.v_tiles) * (kThreads / 64) + wave;
   const int r = (int)(id / a.parts), part = (int)(id % a.parts);
   if (r >= a.batch.n_rows) return;
   const PgRowAt row = pg_row_at(a.batch, r, a.page_log2);
@@ -199,7 +356,7 @@ __global__ __launch_bounds__(kThreads) void pg_read_kernel(const ReadArgs a) {
   const size_t at = there ? (((size_t)page * a.Hkv) << a.page_log2) * D + (size_t)(in & ~(kPgUnit - 1)) * D : 0;
   const size_t head_pitch = (size_t)D << a.page_log2;
   constexpr int kOct = D / 8, E = 16 / sizeof(T);
-  const int nk = a.out_k ? a.Hkv * kOct : 0, total = nk + (a.out_v ? a.Hkv * kOct : 0);
+  const int nk = a.out_k ? a.Hkv * kOct : 0, total = nk + (a.out_v && !a.v_tiles ? a.Hkv * kOct : 0);
   const int per = ((total + 63) / 64 + a.parts - 1) / a.parts * 64;
   const int end = min(total, (part + 1) * per);
   for (int c = part * per + lane; c < end; c += 64) {
@@ -220,10 +377,19 @@ __global__ __launch_bounds__(kThreads) void pg_read_kernel(const ReadArgs a) {
 
 // A wave for each row, several where there are few: 2048 waves give each SIMD of the chip two
 int parts_for(int n, int chunks) { return std::max(1, std::min((chunks + 63) / 64, (2048 + n - 1) / n)); }
+// V in tiles of 32 rows and v_heads kv heads, from kTileRows rows on: workgroups
+constexpr int kTileRows = 256;
+int value_tiles(int n, int Hkv, int& v_heads) {
+  v_heads = 1;
+  if (n < kTileRows) return 0;
+  const int64_t groups = (n + 31) / 32;
+  v_heads = (int)std::max<int64_t>(1, std::min<int64_t>(Hkv, groups * Hkv / 4096));
+  return (int)(groups * ((Hkv + v_heads - 1) / v_heads));
+}
 
 template <typename TS, typename T, int D>
 hipError_t rows_d(const RowsArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)(((int64_t)a.n * a.parts + kThreads / 64 - 1) / (kThreads / 64)));
+  const dim3 grid((unsigned)(a.v_tiles + ((int64_t)a.n * a.parts + kThreads / 64 - 1) / (kThreads / 64)));
   if (a.rot.pairing) hipLaunchKernelGGL((pg_rows_kernel<TS, T, D, true>), grid, dim3(kThreads), 0, st, a);
   else hipLaunchKernelGGL((pg_rows_kernel<TS, T, D, false>), grid, dim3(kThreads), 0, st, a);
   return hipGetLastError();
@@ -246,7 +412,8 @@ hipError_t launch_pg_rows(const PgShape& s, const PgRotation& rot, const PgPages
   a.H = s.H;
   a.Hkv = s.Hkv;
   a.page_log2 = s.page_log2;
-  a.parts = parts_for(n, ((rows.q ? rows.q_heads : 0) + (rows.k ? 2 * s.Hkv : 0)) * (s.D / 16));
+  a.v_tiles = rows.v ? value_tiles(n, s.Hkv, a.v_heads) : 0;
+  a.parts = parts_for(n, ((rows.q ? rows.q_heads : 0) + (rows.k ? s.Hkv : 0) + (rows.v && !a.v_tiles ? s.Hkv : 0)) * (s.D / 16));
   const bool from_f32 = rows.src_dtype == kF32;
   if (s.dtype == kF32) return rows_t<float, float>(s.D, a, st);
   return from_f32 ? rows_t<float, bf16>(s.D, a, st) : rows_t<bf16, bf16>(s.D, a, st);
@@ -254,9 +421,11 @@ hipError_t launch_pg_rows(const PgShape& s, const PgRotation& rot, const PgPages
 
 hipError_t launch_pg_read(const PgShape& s, const PgPages& pages, const PgBatch& batch, void* out_k, int64_t k_ld, void* out_v, int64_t v_ld,
                           hipStream_t st) {
-  ReadArgs a{batch, pages, out_k, out_v, k_ld, v_ld, 1, s.Hkv, s.page_log2};
-  a.parts = parts_for(batch.n_rows, ((out_k != nullptr) + (out_v != nullptr)) * s.Hkv * (s.D / 8));
-  const dim3 grid((unsigned)(((int64_t)batch.n_rows * a.parts + kThreads / 64 - 1) / (kThreads / 64)));
+  ReadArgs a{batch, pages, out_k, out_v, k_ld, v_ld, 1, s.Hkv, s.page_log2, 0, 1};
+  if (out_v) a.v_tiles = value_tiles(batch.n_rows, s.Hkv, a.v_heads);
+  const int n_rest = (out_k != nullptr) + (out_v != nullptr && !a.v_tiles);
+  a.parts = parts_for(batch.n_rows, n_rest * s.Hkv * (s.D / 8));
+  const dim3 grid((unsigned)(a.v_tiles + (n_rest ? ((int64_t)batch.n_rows * a.parts + kThreads / 64 - 1) / (kThreads / 64) : 0)));
   if (s.dtype == kF32) {
     if (s.D == 64) hipLaunchKernelGGL((pg_read_kernel<float, 64>), grid, dim3(kThreads), 0, st, a);
     else hipLaunchKernelGGL((pg_read_kernel<float, 128>), grid, dim3(kThreads), 0, st, a);
