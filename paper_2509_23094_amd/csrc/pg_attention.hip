@@ -867,7 +867,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(256) void pg_join_kernel(const AttendArgs a) {
   constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kFew = 8, kEach = kPgMaxSplits / kGroups;
   __shared__ f32x4 sums[kGroups][kLanes];
-  const int lane = threadIdx.x & 63, G = a.H / a.Hkv, group = threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
+  const int lane = threadIdx.x & 63, G = a.G, group = threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
   for (int job = blockIdx.x;; job += gridDim.x) {
     int b = -1, before = 0, local = 0;
     int4 info = make_int4(0, 0, 0, 0);
@@ -946,13 +946,16 @@ __global__ __launch_bounds__(256) void pg_join_kernel(const AttendArgs a) {
 
 // ------------------------------------------------------------------ the head average
 
-// A workgroup takes 32 rows of a sequence and 32 of its keys at a time; its waves take the heads in turn, scores computed again, and the waves'
-// sums are added in order.  blockIdx.y: tiles of 32 rows, sequence after sequence; blockIdx.x: ranges of units.
+// A workgroup takes 32 rows of a sequence and one or two units of its keys; its eight waves take the heads in turn, scores computed again, and the waves'
+// sums are added in order.  Tiles of rows that read the same keys are neighbours on one XCD: blockIdx.x = (group of units / 8 * tiles + tile) * 8 +
+// group % 8, tiles of 32 rows sequence after sequence.
+template <typename T, int D> constexpr int kAvgUnits = D * (int)sizeof(T) > 256 ? 1 : 2;      // (float heads of 128 have registers for one)
 template <typename T, int D>
-__global__ __launch_bounds__(256) void pg_average_kernel(const AttendArgs a, float* avg, int64_t avg_ld) {
-  constexpr int E = 16 / sizeof(T), NF = D / (2 * E), kW = 4;
+__global__ __launch_bounds__(512, 2) void pg_average_kernel(const AttendArgs a, float* avg, int64_t avg_ld, int tiles, int wide) {
+  constexpr int E = 16 / sizeof(T), NF = D / (2 * E), kW = 8, U = kAvgUnits<T, D>;
   __shared__ float sums[kW][32][33];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
+  const int at_tile = (int)(blockIdx.x / 8) % tiles, at_group = (int)(blockIdx.x / 8) / tiles * 8 + (int)(blockIdx.x % 8);
   // the sequence of this tile of rows
   int b = -1, tile = 0, before = 0;
   for (int b0 = 0; b0 < a.batch.batch && b < 0; b0 += 64) {
@@ -963,56 +966,99 @@ __global__ __launch_bounds__(256) void pg_average_kernel(const AttendArgs a, flo
       n = (max(0, hi - lo) + 31) / 32;
     }
     const int end = scan_sum(n);
-    const uint64_t past = __ballot(before + end > (int)blockIdx.y);
+    const uint64_t past = __ballot(before + end > at_tile);
     if (past) {
       const int at = (int)__builtin_ctzll(past);
       b = b0 + at;
-      tile = (int)blockIdx.y - (before + __shfl(end - n, at, kWave));
+      tile = at_tile - (before + __shfl(end - n, at, kWave));
     } else before += last_lane(end);
   }
   if (b < 0) return;
   const int row0 = max(0, min(a.batch.row_start[b], a.batch.n_rows)), m = min(a.batch.row_start[b + 1], a.batch.n_rows) - row0;
   const int length = max(0, min(a.batch.length[b], a.batch.page_cols << a.page_log2));
-  const int cols = (int)min((int64_t)length, avg_ld), G = a.H / a.Hkv;
+  const int cols = (int)min((int64_t)length, avg_ld);
   const bool valid = tile * 32 + r32 < m;
   const int row = row0 + (valid ? tile * 32 + r32 : tile * 32);
   int lo, hi;
   visible(a, a.batch.at ? a.batch.at[row] : length - m + (row - row0), a.batch.origin ? max(0, a.batch.origin[b]) : 0, length, lo, hi);
+  const int all_lo = reduce_min(lo), all_hi = reduce_max(hi), both_lo = reduce_max(lo), both_hi = reduce_min(hi);
   const int32_t* pages = a.batch.pages + (int64_t)b * a.batch.page_cols;
   const size_t head_pitch = (size_t)D << a.page_log2;
   const float share = 1.f / (float)a.H;
-  for (int u = blockIdx.x; u * kPgUnit < cols; u += gridDim.x) {
-    const int page = pages[u >> (a.page_log2 - 5)], key0 = u * kPgUnit;
-    const bool there = (unsigned)page < (unsigned)a.pages.n_pages;
-    float total[16] = {};
-    if (there) {
-      const size_t at = (size_t)page * a.Hkv * head_pitch + (size_t)(u & ((1 << (a.page_log2 - 5)) - 1)) * kPgUnit * D;
-      for (int head = wave; head < a.H; head += kW) {
-        const T* base = (const T*)a.pages.k + at + (head / G) * head_pitch;
-        const T* qrow = (const T*)a.q + (int64_t)row * a.q_ld + head * D + g * E;
-        const float2 ml = a.row_ml[(size_t)row * a.H + head];
-        f32x16 acc = {};
+  for (int64_t u0 = (int64_t)at_group * U; u0 * kPgUnit < cols; u0 += (int64_t)wide * U) {
+    size_t at[U];
+    bool any[U];                         // a unit that is there, and that some row of the tile sees; others: zeros
+    float total[U][16] = {};
 #pragma unroll
-        for (int f = 0; f < NF; ++f) acc = mm<T>(ld16(base + ((2 * f + g) * kPgUnit + r32) * E), ld16(qrow + f * 2 * E), acc);
+    for (int u = 0; u < U; ++u) {
+      const int unit = (int)u0 + u, key0 = unit * kPgUnit;
+      at[u] = 0;
+      any[u] = key0 < cols && key0 < all_hi && key0 + kPgUnit > all_lo;
+      if (any[u]) {
+        const int page = pages[unit >> (a.page_log2 - 5)];
+        any[u] = (unsigned)page < (unsigned)a.pages.n_pages;
+        if (any[u]) at[u] = (size_t)page * a.Hkv * head_pitch + (size_t)(unit & ((1 << (a.page_log2 - 5)) - 1)) * kPgUnit * D;
+      }
+    }
+    // the next head's operands are requested behind the products of this one
+    u32x4 kr[U][NF], qr[NF];
+    float2 ml;
+    auto load = [&](int head) __attribute__((always_inline)) {
+      const T* qrow = (const T*)a.q + (int64_t)row * a.q_ld + head * D + g * E;
+      ml = a.row_ml[(size_t)row * a.H + head];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = key0 + key_of<T>(i, g);
-          const float p = exp2_hw(fmaf(acc[i], a.c2, -ml.x)) * ml.y;
-          total[i] += key >= lo && key < hi ? p : 0.f;
+      for (int f = 0; f < NF; ++f) qr[f] = ld16(qrow + f * 2 * E);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const T* base = (const T*)a.pages.k + at[u] + (head / a.by_g) * head_pitch + (g * kPgUnit + r32) * E;
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+          if (any[u]) kr[u][f] = ld16(base + 2 * f * kPgUnit * E);
+      }
+    };
+    if (wave < a.H) load(wave);
+    for (int head = wave; head < a.H; head += kW) {
+      f32x16 acc[U] = {};
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (any[u])
+#pragma unroll
+          for (int f = 0; f < NF; ++f) acc[u] = mm<T>(kr[u][f], qr[f], acc[u]);
+      const float2 now = ml;
+      if (head + kW < a.H) load(head + kW);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (!any[u]) continue;
+        const int key0 = ((int)u0 + u) * kPgUnit;
+        if (key0 >= both_lo && key0 + kPgUnit <= both_hi) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) total[u][i] = fmaf(exp2_hw(fmaf(acc[u][i], a.c2, -now.x)), now.y, total[u][i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = key0 + key_of<T>(i, g);
+            const float p = exp2_hw(fmaf(acc[u][i], a.c2, -now.x)) * now.y;
+            total[u][i] += key >= lo && key < hi ? p : 0.f;
+          }
         }
       }
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sums[wave][r32][key_of<T>(i, g)] = total[i];
-    __syncthreads();
-    for (int c = threadIdx.x; c < 32 * 32; c += 256) {
-      const int rr = c / 32, key = c % 32;
-      float y = 0.f;
+    for (int u = 0; u < U; ++u) {
+      const int key0 = ((int)u0 + u) * kPgUnit;
+      if (key0 >= cols) break;
 #pragma unroll
-      for (int w = 0; w < kW; ++w) y += sums[w][rr][key];
-      if (tile * 32 + rr < m && key0 + key < cols) avg[(int64_t)(row0 + tile * 32 + rr) * avg_ld + key0 + key] = y * share;
+      for (int i = 0; i < 16; ++i) sums[wave][r32][key_of<T>(i, g)] = total[u][i];
+      __syncthreads();
+      for (int c = threadIdx.x; c < 32 * 32; c += 64 * kW) {
+        const int rr = c / 32, key = c % 32;
+        float y = 0.f;
+#pragma unroll
+        for (int w = 0; w < kW; ++w) y += sums[w][rr][key];
+        if (tile * 32 + rr < m && key0 + key < cols) avg[(int64_t)(row0 + tile * 32 + rr) * avg_ld + key0 + key] = y * share;
+      }
+      __syncthreads();
     }
-    __syncthreads();
   }
 }
 
@@ -1072,10 +1118,11 @@ static hipError_t attention_d(const PgShape& s, AttendArgs a, const PgAttend& ca
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (call.avg) {
-    const int64_t tiles = (int64_t)b.n_rows / 32 + std::min(b.n_rows, b.batch);
-    const int64_t cols = std::min<int64_t>(call.avg_ld, (int64_t)b.page_cols << s.page_log2);
-    const int64_t wide = std::max<int64_t>(1, std::min<int64_t>((cols + 31) / 32, 65536));
-    hipLaunchKernelGGL((pg_average_kernel<T, D>), dim3((unsigned)wide, (unsigned)tiles), dim3(256), 0, st, a, call.avg, call.avg_ld);
+    // groups of units: a multiple of 8, and no more than leave 2^22 workgroups in all
+    const int64_t tiles = (int64_t)b.n_rows / 32 + std::min(b.n_rows, b.batch), cols = std::min<int64_t>(call.avg_ld, (int64_t)b.page_cols << s.page_log2);
+    const int64_t groups = (cols + 32 * kAvgUnits<T, D> - 1) / (32 * kAvgUnits<T, D>);
+    const int64_t wide = std::max<int64_t>(1, std::min((groups + 7) / 8, (1 << 22) / 8 / tiles)) * 8;
+    hipLaunchKernelGGL((pg_average_kernel<T, D>), dim3((unsigned)(wide * tiles)), dim3(512), 0, st, a, call.avg, call.avg_ld, (int)tiles, (int)wide);
     e = hipGetLastError();
   }
   return e;

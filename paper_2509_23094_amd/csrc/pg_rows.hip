@@ -377,11 +377,13 @@ __global__ __launch_bounds__(kThreads) void pg_read_kernel(const ReadArgs a) {
 
 // A wave for each row, several where there are few: 2048 waves give each SIMD of the chip two
 int parts_for(int n, int chunks) { return std::max(1, std::min((chunks + 63) / 64, (2048 + n - 1) / n)); }
-// V in tiles of 32 rows and v_heads kv heads, from kTileRows rows on: workgroups
-constexpr int kTileRows = 256;
-int value_tiles(int n, int Hkv, int& v_heads) {
+// V in tiles of 32 rows and v_heads kv heads: how many workgroups, 0 where rows bring their V themselves.  Tiles pay where sequences have several rows
+// (whole pieces), and from 2^18 values on.  Append and read, us, by rows and by tiles: one sequence, 32 kv heads of 128: 64 rows 12.0 and 11.1,
+// 256 rows 24.5 and 15.3, 2048 rows 95 and 54; 4 kv heads: 256 rows 9.3 and 10.8, 512 rows 11.6 and 11.5, 1024 rows 15.6 and 13.5; 64 sequences
+// of one row, 32 kv heads: 13.6 and 16.5, 1000 of them 73 and 87.
+int value_tiles(int n, int batch, int Hkv, int D, int& v_heads) {
   v_heads = 1;
-  if (n < kTileRows) return 0;
+  if (n / 8 < batch || (int64_t)n * Hkv * D < 1 << 18) return 0;
   const int64_t groups = (n + 31) / 32;
   v_heads = (int)std::max<int64_t>(1, std::min<int64_t>(Hkv, groups * Hkv / 4096));
   return (int)(groups * ((Hkv + v_heads - 1) / v_heads));
@@ -412,7 +414,7 @@ hipError_t launch_pg_rows(const PgShape& s, const PgRotation& rot, const PgPages
   a.H = s.H;
   a.Hkv = s.Hkv;
   a.page_log2 = s.page_log2;
-  a.v_tiles = rows.v ? value_tiles(n, s.Hkv, a.v_heads) : 0;
+  a.v_tiles = rows.v ? value_tiles(n, batch->batch, s.Hkv, s.D, a.v_heads) : 0;
   a.parts = parts_for(n, ((rows.q ? rows.q_heads : 0) + (rows.k ? s.Hkv : 0) + (rows.v && !a.v_tiles ? s.Hkv : 0)) * (s.D / 16));
   const bool from_f32 = rows.src_dtype == kF32;
   if (s.dtype == kF32) return rows_t<float, float>(s.D, a, st);
@@ -422,7 +424,7 @@ hipError_t launch_pg_rows(const PgShape& s, const PgRotation& rot, const PgPages
 hipError_t launch_pg_read(const PgShape& s, const PgPages& pages, const PgBatch& batch, void* out_k, int64_t k_ld, void* out_v, int64_t v_ld,
                           hipStream_t st) {
   ReadArgs a{batch, pages, out_k, out_v, k_ld, v_ld, 1, s.Hkv, s.page_log2, 0, 1};
-  if (out_v) a.v_tiles = value_tiles(batch.n_rows, s.Hkv, a.v_heads);
+  if (out_v) a.v_tiles = value_tiles(batch.n_rows, batch.batch, s.Hkv, s.D, a.v_heads);
   const int n_rest = (out_k != nullptr) + (out_v != nullptr && !a.v_tiles);
   a.parts = parts_for(batch.n_rows, n_rest * s.Hkv * (s.D / 8));
   const dim3 grid((unsigned)(a.v_tiles + (n_rest ? ((int64_t)batch.n_rows * a.parts + kThreads / 64 - 1) / (kThreads / 64) : 0)));
