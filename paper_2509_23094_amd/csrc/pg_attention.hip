@@ -46,7 +46,7 @@ struct AttendArgs {
   int H, Hkv, G, page_log2, block, window;
   Div by_hkv, by_g;
   float c2;                      // scale * log2(e)
-  int more_than, up_to;          // queries of a kv head that a sequence has to be this launch's
+  float more_than, up_to;        // work (see work_of) that a sequence has to be this launch's
   int max_splits, part_first, part_limit;      // partial tiles of this launch
   float* part_o;                 // [part][32][D]
   float2* part_ml;               // [part][32]: reference, sum
@@ -88,6 +88,13 @@ __device__ __forceinline__ int reduce_min(int v) { return last_lane(scan(v, INT3
 // sequence's last ones, which a mask leaves the most keys, come first); the rest is, in splits of equal length for all sequences: of 1 .. 64 for the
 // longest sequence, each lane of a wave takes one and estimates the time as rounds of workgroups times (units of a split + what an item costs besides).
 template <int TILES> __device__ __forceinline__ int tiles_in(int queries) { return (queries + 32 * TILES - 1) / (32 * TILES); }
+// About how many (query, key) pairs a sequence has
+__device__ __forceinline__ float work_of(const AttendArgs& a, int m, int length) {
+  float keys = (float)length;
+  if (a.block > 0 && !a.batch.at) keys = fmaxf(keys - 0.5f * (float)m, 0.5f * keys);
+  if (a.window > 0) keys = fminf(keys, (float)a.window * (a.block > 0 ? 1.f : 2.f));
+  return (float)m * (float)a.H * keys;
+}
 // tiles of 32 queries of a sequence that are split: the first ones
 template <int TILES> __device__ __forceinline__ int split_tiles(const Plan& p, int b, int G) {
   const int m = p.seq[b].m * G;
@@ -137,7 +144,8 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
     s.m = max(0, min(hi, a.batch.n_rows) - s.row0);
     s.length = max(0, min(len, a.batch.page_cols << a.page_log2));
     rows = min(rows + s.m, 1 << 22);             // (starts that are not ascending: the sum tells; n_rows is 2^20 at most)
-    if (s.m * G <= a.more_than || s.m * G > a.up_to) s.m = 0;
+    const float work = work_of(a, s.m, s.length);
+    if (work <= a.more_than || work > a.up_to) s.m = 0;
     tiles = min(tiles + tiles_in<TILES>(s.m * G), 1 << 25);
     s.unit0 = a.window > 0 && !a.batch.at ? max(0, s.length - s.m - a.window + 1) / kPgUnit : 0;
     p.seq[b] = s;
@@ -422,7 +430,10 @@ __device__ __forceinline__ float inverse_of(float sum) { return sum > 0.f ? 1.f 
 
 // ------------------------------------------------------------------ few queries: operands straight from the pages
 
-constexpr int kFewQueries = 512;        // of a sequence and kv head
+// (query, key) pairs, all heads, from which on a sequence goes to the kernel for many queries.  us by the one for few and by it: bf16, 32 heads of 128, 8000
+// keys: 256 rows (66e6) 66 and 58, 128 rows 43 and 47; 28 on 4, 4000 keys: 1024 rows (115e6) 105 and 90, 512 rows 57 and 59; 12 heads of 64 on 2, 16000 keys: 1024
+// rows (197e6) 104 and 88, 512 rows 61 and 67; float, where both wait for the matrix cores, 32 heads, 2048 keys, 2000 rows, no mask 646 and 531, causal 376 and 533.
+template <typename T, int D> constexpr float kMuch = sizeof(T) == 4 ? 256e6f : D == 64 ? 128e6f : 64e6f;
 constexpr int kManyWaves = 8;
 
 constexpr int kWaves = 4;
@@ -437,7 +448,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
   u32x4 (*q_lds)[64] = reinterpret_cast<u32x4 (*)[64]>(&merge[0][0][0]);
   __shared__ float wref[kWaves][32], wl[kWaves][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
-  const Plan plan = make_plan<1, kFewThreads>(a, plan_lds, 16.f);
+  const Plan plan = make_plan<1, kFewThreads>(a, plan_lds, 32.f);
   const int G = a.G;
   const size_t head_pitch = (size_t)D << a.page_log2;           // elements
   for (int item = blockIdx.x; item < plan.items; item += gridDim.x) {
@@ -1091,22 +1102,21 @@ static hipError_t attention_d(const PgShape& s, AttendArgs a, const PgAttend& ca
   a.max_splits = (int)std::min<int64_t>(kPgMaxSplits, std::max<int64_t>(1, units / kWaves));
   hipError_t e = hipSuccess;
   const size_t lds = plan_bytes(b.batch);
-  // Few queries or many: each sequence goes by its own number, which only the device knows.  What the host knows: all of them are few; or there is
-  // one sequence; or as many rows as sequences, single tokens (if they are not, the kernel for few queries takes them tile by tile).
+  // Few products or many: each sequence goes by its own work, which only the device knows.  What the host knows: all together cannot have that much
+  // work; or as many rows as sequences, single tokens (if they are not, the kernel for few queries takes them all).
   const int64_t queries = (int64_t)b.n_rows * (s.H / s.Hkv);
-  const bool few_only = queries <= kFewQueries || b.n_rows <= b.batch, many_only = !few_only && b.batch == 1;
+  const double most = (double)b.n_rows * s.H * std::min((double)((int64_t)b.page_cols << s.page_log2), a.window > 0 ? 2.0 * a.window : 1e30);
+  const bool few_only = most <= kMuch<T, D> || b.n_rows <= b.batch;
   const int parts = a.part_limit;
-  if (!many_only) {
-    a.more_than = 0;
-    a.up_to = few_only ? 0x7fffffff : kFewQueries;
-    a.part_limit = few_only ? parts : parts / 4;
-    hipLaunchKernelGGL((pg_few_kernel<T, D>), dim3(2 * cus), dim3(kFewThreads), lds, st, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
+  a.more_than = -1.f;
+  a.up_to = few_only ? 3e38f : kMuch<T, D>;
+  a.part_limit = few_only ? parts : parts / 4;
+  hipLaunchKernelGGL((pg_few_kernel<T, D>), dim3(2 * cus), dim3(kFewThreads), lds, st, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
   if (!few_only) {
-    a.more_than = many_only ? 0 : kFewQueries;
-    a.up_to = 0x7fffffff;
-    a.part_first = many_only ? 0 : parts / 4;
+    a.more_than = kMuch<T, D>;
+    a.up_to = 3e38f;
+    a.part_first = parts / 4;
     a.part_limit = parts;
     hipLaunchKernelGGL((pg_many_kernel<T, D>), dim3(cus), dim3(64 * kManyWaves), lds, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
