@@ -135,9 +135,11 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
   p.split = p.first + batch + 1;
   p.whole = p.split + batch;
   __shared__ float load[kWaves][64];
-  __shared__ int most[kWaves], rows_of[kWaves], tiles_of[kWaves], result[2];
+  __shared__ int most[kWaves], rows_of[kWaves], tiles_of[kWaves];
+  // a few sequences: each wave does it all by itself (they write the same values), without a barrier
+  const bool solo = batch <= 16;
   int units = 0, rows = 0, tiles = 0;
-  for (int b = tid; b < batch; b += THREADS) {
+  for (int b = solo ? lane : tid; b < batch; b += THREADS) {
     const int lo = a.batch.row_start[b], hi = a.batch.row_start[b + 1], len = a.batch.length[b];
     PlanSeq s;
     s.row0 = max(0, min(lo, a.batch.n_rows));
@@ -151,18 +153,18 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
     p.seq[b] = s;
     if (s.m > 0) units = max(units, (s.length + kPgUnit - 1) / kPgUnit - s.unit0);
   }
-  units = reduce_max(units);
+  units = max(1, reduce_max(units));
   rows = last_lane(scan_sum(rows));
-  tiles = last_lane(scan_sum(tiles));
-  if (lane == 0) { most[wave] = units; rows_of[wave] = rows; tiles_of[wave] = tiles; }
-  __syncthreads();
-  units = 1;
-  rows = 0;
-  int all = 0;
-  for (int w = 0; w < kWaves; ++w) {
-    units = max(units, most[w]);
-    rows = min(rows + rows_of[w], 1 << 22);
-    all += tiles_of[w];
+  int all = last_lane(scan_sum(tiles));
+  if (!solo) {
+    if (lane == 0) { most[wave] = units; rows_of[wave] = rows; tiles_of[wave] = all; }
+    __syncthreads();
+    rows = all = 0;
+    for (int w = 0; w < kWaves; ++w) {
+      units = max(units, most[w]);
+      rows = min(rows + rows_of[w], 1 << 22);
+      all = min(all + tiles_of[w], 1 << 25);
+    }
   }
   const bool sane = rows <= a.batch.n_rows;
   all *= a.Hkv;
@@ -170,21 +172,24 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
   const int chunk = (units + lane) / (lane + 1);          // of lane + 1 splits
   const float inv = 1.f / (float)chunk;
   float items = 0.f;
-  for (int b = wave; b < batch; b += kWaves) {
+  for (int b = solo ? 0 : wave; b < batch; b += solo ? 1 : kWaves) {
     const PlanSeq s = p.seq[b];
     const int tiles = tiles_in<TILES>(s.m * G), n = (s.length + kPgUnit - 1) / kPgUnit - s.unit0;
     items += (float)(tiles - (int)((float)tiles * share)) * fmaxf(1.f, ceilf((float)n * inv - 1e-3f));
   }
-  load[wave][lane] = items * (float)a.Hkv;
-  __syncthreads();
-  float cost = 0.f;
-  for (int w = 0; w < kWaves; ++w) cost += load[w][lane];
+  float cost = items * (float)a.Hkv;
+  if (!solo) {
+    load[wave][lane] = cost;
+    __syncthreads();
+    cost = 0.f;
+    for (int w = 0; w < kWaves; ++w) cost += load[w][lane];
+  }
   cost = ceilf(cost / (float)gridDim.x) * ((float)chunk + item_cost);
   // the cheapest, of equal ones the fewest splits (a positive float's bits are in its order)
   const int bits = lane < a.max_splits ? __builtin_bit_cast(int, cost) : INT32_MAX;
   const int best = reduce_min(bits);
   p.chunk = __builtin_amdgcn_readlane(chunk, (int)__builtin_ctzll(__ballot(bits == best)));
-  if (wave == 0) {
+  if (solo || wave == 0) {
     int item = 0, part = a.part_first;
     for (int b0 = 0; b0 < batch; b0 += 64) {
       const int b = b0 + lane;
@@ -213,10 +218,11 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
       item += last_lane(at_item);
       part = min(part + last_lane(at_part), 1 << 28);
     }
-    if (lane == 0) { p.first[batch] = item; result[0] = item; }
+    if (lane == 0) p.first[batch] = item;
   }
-  __syncthreads();
-  p.items = result[0];
+  if (solo) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  else __syncthreads();
+  p.items = p.first[batch];
   // what the join and the average read
   if (blockIdx.x == 0)
     for (int b = tid; b < batch; b += THREADS)
@@ -1099,7 +1105,8 @@ static hipError_t attention_d(const PgShape& s, AttendArgs a, const PgAttend& ca
   const PgBatch& b = a.batch;
   // units of the longest cache that the page table can name
   const int64_t units = (int64_t)b.page_cols << (s.page_log2 - 5);
-  a.max_splits = (int)std::min<int64_t>(kPgMaxSplits, std::max<int64_t>(1, units / kWaves));
+  // short ones are not split: a second launch costs more than it saves (one token, 28 heads on 4: 200 rows 10.9 us, split 12.8; 600 rows 13.9 and 13.0)
+  a.max_splits = units <= (sizeof(T) == 4 ? 2 : 3) * kWaves ? 1 : (int)std::min<int64_t>(kPgMaxSplits, units / kWaves);
   hipError_t e = hipSuccess;
   const size_t lds = plan_bytes(b.batch);
   // Few products or many: each sequence goes by its own work, which only the device knows.  What the host knows: all together cannot have that much
