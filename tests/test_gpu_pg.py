@@ -10,7 +10,8 @@ from gpu_util import say
 pytestmark = pytest.mark.gpu
 
 HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}          # rounding to T
-GEOS = {"mha": (4, 4, 64), "gqa": (8, 2, 64), "dream": (28, 4, 128), "odd": (5, 1, 128), "llada": (32, 32, 128), "three": (6, 2, 128)}
+GEOS = {"mha": (4, 4, 64), "gqa": (8, 2, 64), "dream": (28, 4, 128), "odd": (5, 1, 128), "llada": (32, 32, 128), "three": (6, 2, 128), "thirds": (9, 3, 64),
+        "wide": (48, 1, 64)}
 
 
 def B():
@@ -366,7 +367,7 @@ MASKS = [dict(), dict(block=1), dict(block=32), dict(block=1, window=40), dict(w
 @pytest.mark.parametrize("geo,page_rows,lengths,counts", [
     ("mha", 32, [1], [1]), ("dream", 64, [1023], [1]), ("gqa", 32, [257, 33, 32, 31, 1, 0, 300], [1, 2, 0, 31, 1, 3, 40]),
     ("odd", 128, [400, 129, 128], [7, 129, 1]), ("three", 256, [513, 64], [200, 64]), ("mha", 64, [389], [389]),
-    ("llada", 64, [130, 97], [70, 97])])
+    ("llada", 64, [130, 97], [70, 97]), ("thirds", 32, [333, 70], [33, 1]), ("wide", 64, [200, 65], [3, 65])])
 def test_attention(geo, page_rows, lengths, counts, dtype, mask):
     say("attention %s %s pages of %d, %s rows on %s, %s" % (geo, dtype, page_rows, counts, lengths, mask))
     p = Pool(geo, dtype, page_rows, lengths, seed=len(lengths)).fill()
@@ -585,6 +586,136 @@ def test_streams():
                 p.ctx.d2c_pg_attention(p.cache, b, q[0], o, block=1)
     torch.cuda.synchronize()
     assert all(torch.equal(o, w[3]) for o, w in zip(outs, work))
+
+
+# ------------------------------------------------------------------ sequences with many products (the kernel for many queries)
+
+def expect_big(p, q, out, avg, block=0, window=0):
+    """Pool.expect with the plain form in 64 bits on the GPU: the same bounds."""
+    seq, idx, _ = p.where
+    numbered = p.at is not None or block > 0 or window > 0
+    got, G = out.double().view(p.n_rows, p.H, p.D), p.H // p.Hkv
+    assert bool((out[torch.from_numpy(seq < 0).cuda()] == 7.0).all())
+    for b in range(len(p.lengths)):
+        rows = np.flatnonzero(seq == b)
+        if len(rows) == 0:
+            continue
+        k, v, there = p.keys(b)
+        n, origin = len(there), 0 if p.origin is None else int(p.origin[b])
+        if n == 0:                           # nothing to see
+            assert not bool(got[torch.from_numpy(rows).cuda()].any()) and (avg is None or bool((avg[torch.from_numpy(rows).cuda()] == 7.0).all()))
+            continue
+        ok = torch.from_numpy(np.array([R.seen(idx[r], n, block, window, origin, numbered) & there for r in rows]).reshape(len(rows), n)).cuda()
+        k, v = (torch.from_numpy(np.ascontiguousarray(np.where(there[:, None, None], x, 0.0))).cuda() for x in (k, v))
+        sees, where, total = ok.any(1), torch.from_numpy(rows).cuda(), torch.zeros(ok.shape, dtype=torch.float64, device="cuda")
+        worst = torch.zeros(len(rows), dtype=torch.float64, device="cuda")
+        for h in range(p.H):
+            kk, vv, qq = k[:, h // G].contiguous(), v[:, h // G].contiguous(), q[where, h * p.D:(h + 1) * p.D].double()
+            s = (qq @ kk.t()) * p.scale
+            score = (p.D + 8) * 2.0 ** -24 * ((qq.abs() @ kk.abs().t()) * p.scale).amax(1)
+            w = torch.softmax(s.masked_fill(~ok, -float("inf")), 1)
+            w[~sees] = 0
+            o, mag = w @ vv, w @ vv.abs()
+            rel = 2 * score[:, None] + (n / 16 + 160) * 2.0 ** -24 + 2.0 ** -20 + (HALF["bf16"] if p.dtype == "bf16" else 0)
+            off = (got[where, h] - o).abs()
+            assert bool((off <= HALF[p.dtype] * o.abs() + rel * mag + 1e-30).all()), (b, h, float(off.max()))
+            total += w / p.H
+            worst = torch.maximum(worst, score)
+        if avg is not None:
+            tol = (2 * worst[:, None] + 2.0 ** -19 + (n / 16 + p.H + 160) * 2.0 ** -24) * total + 1e-30
+            assert bool(((avg[where, :n].double() - total).abs() <= tol).all()) and bool((avg[where, n:] == 7.0).all())
+            assert bool((avg[where, :n][~ok] == 0).all())
+
+
+def attend_big(p, batch, average=False, **mask):
+    q = torch.randn((p.n_rows, p.H * p.D), device="cuda", generator=torch.Generator("cuda").manual_seed(5)).to(p.ctx.torch_dtype)
+    out = torch.full_like(q, 7.0)
+    avg = torch.full((p.n_rows, max(p.lengths)), 7.0, device="cuda") if average else None
+    p.ctx.d2c_pg_attention(p.cache, batch, q, out, attn_avg=avg, **mask)
+    torch.cuda.synchronize()
+    expect_big(p, q, out, avg, **mask)
+    return q, out
+
+
+BIG = {  # (heads, kv heads, head dimension), type, lengths, rows: the first has more than 64e6 (128e6, 256e6) products, the others fewer
+    "llada": ((32, 32, 128), "bf16", [3500, 900, 64, 0], [700, 1, 40, 2]),
+    "dream": ((28, 4, 128), "bf16", [4001, 4001], [777, 1]),
+    "d64": ((32, 8, 64), "bf16", [3333, 100], [1801, 100]),
+    "f32": ((32, 32, 128), "f32", [5003, 33], [2601, 33]),
+    "f32 d64": ((33, 3, 64), "f32", [5003], [2601]),
+}
+
+
+@pytest.mark.parametrize("mask", [dict(), dict(block=1), dict(block=48)], ids=str)
+@pytest.mark.parametrize("name", BIG)
+def test_many_products(name, mask):
+    geo, dtype, lengths, counts = BIG[name]
+    say("many products, %s, %s" % (name, mask))
+    p = Pool(geo, dtype, 64, lengths, seed=3).fill()
+    attend_big(p, p.batch(counts, lead=1, tail=2), average=name == "dream", **mask)
+
+
+def test_many_products_in_a_window():
+    p = Pool("llada", "bf16", 32, [4100, 50], seed=5).fill()
+    b = p.batch([3001, 50], origin=np.array([7, 0]))
+    attend_big(p, b, block=1, window=900)
+    attend_big(p, b, block=32, window=901)
+    attend_big(p, b, window=450)
+
+
+def test_many_products_of_selected_rows_and_missing_pages():
+    """Indices in no order, some that see nothing; pages that are not there, inside blocks and between them."""
+    p = Pool("llada", "bf16", 32, [3200, 40], seed=6).fill()
+    p.pages[0, 5], p.pages[0, 10:13], p.pages[0, 99] = -1, p.n_pages, -9
+    at = np.concatenate([p.rng.permutation(3200)[:900], [-1, -7, 5000, 3199, 0], p.rng.integers(0, 40, 20)])
+    b = p.batch([905, 20], at=at)
+    attend_big(p, b, average=True)
+    attend_big(p, b, block=1)
+
+
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+def test_many_products_do_not_see_what_they_do_not_see(what):
+    p = Pool("llada", "bf16", 32, [3300], seed=7).fill()
+    b = p.batch([1000])
+    q, clean = attend_big(p, b, block=1)
+    spot = [3299, 3100, 2700, 2450]
+    at = B().PgBatch(p.ctx, ints([0, len(spot)]), ints([3300]), ints(p.pages[:1]), len(spot), at=ints(spot))
+    t = torch.full((len(spot), p.Hkv * p.D), what, dtype=p.ctx.torch_dtype, device="cuda")
+    good = [torch.empty_like(t) for _ in range(2)]
+    p.ctx.d2c_pg_read(p.cache, at, *good)
+    p.ctx.d2c_pg_append(p.cache, at, good[0], t)                  # V alone: the probabilities stay
+    out = torch.zeros_like(clean)
+    p.ctx.d2c_pg_attention(p.cache, b, q, out, block=1)
+    seen = torch.tensor([2300 + r >= min(spot) for r in range(1000)], device="cuda")
+    assert torch.equal(out[~seen], clean[~seen])
+    if what != what:
+        assert bool(out[seen].isnan().all())
+    else:
+        assert torch.equal(out[seen], torch.full_like(out[seen], what))
+    p.ctx.d2c_pg_append(p.cache, at, t, good[1])                  # K alone
+    p.ctx.d2c_pg_attention(p.cache, b, q, out, block=1)
+    assert torch.equal(out[~seen], clean[~seen])
+
+
+def test_many_products_repeat_to_the_bit_and_follow_their_lengths():
+    p = Pool("dream", "bf16", 64, [5000, 700], seed=9).fill()
+    b = p.batch([1000, 3])
+    q, first = attend_big(p, b, block=1)
+    out = torch.zeros_like(first)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.ctx.d2c_pg_attention(p.cache, b, q, out, block=1)
+    for n in (5000, 3000, 1001, 5000):
+        b.keep[1].copy_(ints([n, 700]))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        out.zero_()
+        p.ctx.d2c_pg_attention(p.cache, b, q, out, block=1)
+        assert torch.equal(got, out)
+    assert torch.equal(out, first)
 
 
 # ------------------------------------------------------------------ together
