@@ -63,6 +63,10 @@ struct Plan {
   int* split;                    // [batch] splits << 24 | first partial tile
   int* whole;                    // [batch] tiles that are not split: the last ones, which come first
   int chunk, items;              // units of a split
+  // of a few sequences: lane b's own of the above, so that an item is found without LDS
+  bool solo;
+  PlanSeq my;
+  int my_first, my_end, my_split, my_whole;
 };
 inline size_t plan_bytes(int batch) { return (size_t)batch * (sizeof(PlanSeq) + 12) + 16; }
 
@@ -96,34 +100,8 @@ __device__ __forceinline__ float work_of(const AttendArgs& a, int m, int length)
   return (float)m * (float)a.H * keys;
 }
 // tiles of 32 queries of a sequence that are split: the first ones
-template <int TILES> __device__ __forceinline__ int split_tiles(const Plan& p, int b, int G) {
-  const int m = p.seq[b].m * G;
-  return min((m + 31) / 32, (tiles_in<TILES>(m) - p.whole[b]) * TILES);
-}
-// Where an item of a sequence is: tile, split, kv head
-struct Place { int tile, hk, split, splits; };
-template <int TILES> __device__ __forceinline__ Place place_of(const AttendArgs& a, const Plan& p, int b, int item) {
-  const int local = item - p.first[b], whole = p.whole[b], tiles = tiles_in<TILES>(p.seq[b].m * a.G), splits = p.split[b] >> 24;
-  const int at = local / a.by_hkv;
-  Place w;
-  w.hk = local - at * a.Hkv;
-  w.splits = 1;
-  w.split = 0;
-  w.tile = tiles - 1 - at;
-  if (at >= whole) {                     // below 2^14 (there are no more partial tiles): the quotient in fp32 is off by one at the most
-    const int n = at - whole;
-    int t = (int)((float)n * __builtin_amdgcn_rcpf((float)splits));
-    t -= n < t * splits;
-    t += n >= (t + 1) * splits;
-    w.splits = splits;
-    w.split = n - t * splits;
-    w.tile = tiles - 1 - whole - t;
-  }
-  w.hk = __builtin_amdgcn_readfirstlane(w.hk);
-  w.splits = __builtin_amdgcn_readfirstlane(w.splits);
-  w.split = __builtin_amdgcn_readfirstlane(w.split);
-  w.tile = __builtin_amdgcn_readfirstlane(w.tile);
-  return w;
+template <int TILES> __device__ __forceinline__ int split_tiles(int queries, int whole) {
+  return min((queries + 31) / 32, (tiles_in<TILES>(queries) - whole) * TILES);
 }
 template <int TILES, int THREADS>
 __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* lds, float item_cost) {
@@ -138,6 +116,8 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
   __shared__ int most[kWaves], rows_of[kWaves], tiles_of[kWaves];
   // a few sequences: each wave does it all by itself (they write the same values), without a barrier
   const bool solo = batch <= 16;
+  p.solo = solo;
+  p.my = PlanSeq{0, 0, 0, 0};
   int units = 0, rows = 0, tiles = 0;
   for (int b = solo ? lane : tid; b < batch; b += THREADS) {
     const int lo = a.batch.row_start[b], hi = a.batch.row_start[b + 1], len = a.batch.length[b];
@@ -150,7 +130,7 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
     if (work <= a.more_than || work > a.up_to) s.m = 0;
     tiles = min(tiles + tiles_in<TILES>(s.m * G), 1 << 25);
     s.unit0 = a.window > 0 && !a.batch.at ? max(0, s.length - s.m - a.window + 1) / kPgUnit : 0;
-    p.seq[b] = s;
+    p.seq[b] = p.my = s;
     if (s.m > 0) units = max(units, (s.length + kPgUnit - 1) / kPgUnit - s.unit0);
   }
   units = max(1, reduce_max(units));
@@ -210,10 +190,14 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
       if (splits == 1) n_whole = n_tiles;
       const int n_items = (n_whole + (n_tiles - n_whole) * splits) * a.Hkv;
       const int at_item = scan_sum(n_items);
+      p.my_end = item + at_item;
+      p.my_first = p.my_end - n_items;
+      p.my_whole = n_whole;
+      p.my_split = splits << 24 | (splits > 1 ? part + at_part - n_parts : 0);
       if (b < batch) {
-        p.first[b] = item + at_item - n_items;
+        p.first[b] = p.my_first;
         p.whole[b] = n_whole;
-        p.split[b] = splits << 24 | (splits > 1 ? part + at_part - n_parts : 0);
+        p.split[b] = p.my_split;
       }
       item += last_lane(at_item);
       part = min(part + last_lane(at_part), 1 << 28);
@@ -222,20 +206,61 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
   }
   if (solo) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   else __syncthreads();
-  p.items = p.first[batch];
+  p.items = solo ? last_lane(p.my_end) : p.first[batch];
   // what the join and the average read
   if (blockIdx.x == 0)
     for (int b = tid; b < batch; b += THREADS)
       if (p.seq[b].m > 0 || a.batch.row_start[b + 1] <= a.batch.row_start[b])      // (empty ones: by every launch)
-        a.info[b] = make_int4(p.split[b] >> 24 | (p.split[b] & 0xffffff) << 8, split_tiles<TILES>(p, b, G), p.seq[b].row0, p.seq[b].m);
+        a.info[b] = make_int4(p.split[b] >> 24 | (p.split[b] & 0xffffff) << 8, split_tiles<TILES>(p.seq[b].m * G, p.whole[b]), p.seq[b].row0, p.seq[b].m);
   return p;
 }
-// the sequence of an item: as many as end at or before it
-__device__ __forceinline__ int seq_of(const Plan& p, int batch, int item) {
+// Of the sequence that an item belongs to (as many as end at or before it): all that the item's work needs
+struct Found { int b, first, split, whole; PlanSeq seq; };
+__device__ __forceinline__ Found find(const Plan& p, int batch, int item) {
   const int lane = threadIdx.x & 63;
-  int n = 0;
-  for (int b0 = 0; b0 < batch; b0 += 64) n += __popcll(__ballot(b0 + lane < batch && p.first[b0 + min(lane, batch - 1 - b0) + 1] <= item));
-  return n;
+  Found f;
+  if (p.solo) {
+    f.b = __popcll(__ballot(lane < batch && p.my_end <= item));
+    auto of = [&](int mine) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(mine, f.b); };
+    f.first = of(p.my_first);
+    f.split = of(p.my_split);
+    f.whole = of(p.my_whole);
+    f.seq = PlanSeq{of(p.my.row0), of(p.my.m), of(p.my.length), of(p.my.unit0)};
+    return f;
+  }
+  f.b = 0;
+  for (int b0 = 0; b0 < batch; b0 += 64) f.b += __popcll(__ballot(b0 + lane < batch && p.first[b0 + min(lane, batch - 1 - b0) + 1] <= item));
+  f.first = p.first[f.b];
+  f.split = p.split[f.b];
+  f.whole = p.whole[f.b];
+  f.seq = p.seq[f.b];
+  return f;
+}
+
+// Where an item of a sequence is: tile, split, kv head
+struct Place { int tile, hk, split, splits; };
+template <int TILES> __device__ __forceinline__ Place place_of(const AttendArgs& a, const Found& f, int item) {
+  const int local = item - f.first, whole = f.whole, tiles = tiles_in<TILES>(f.seq.m * a.G), splits = f.split >> 24;
+  const int at = local / a.by_hkv;
+  Place w;
+  w.hk = local - at * a.Hkv;
+  w.splits = 1;
+  w.split = 0;
+  w.tile = tiles - 1 - at;
+  if (at >= whole) {                     // below 2^14 (there are no more partial tiles): the quotient in fp32 is off by one at the most
+    const int n = at - whole;
+    int t = (int)((float)n * __builtin_amdgcn_rcpf((float)splits));
+    t -= n < t * splits;
+    t += n >= (t + 1) * splits;
+    w.splits = splits;
+    w.split = n - t * splits;
+    w.tile = tiles - 1 - whole - t;
+  }
+  w.hk = __builtin_amdgcn_readfirstlane(w.hk);
+  w.splits = __builtin_amdgcn_readfirstlane(w.splits);
+  w.split = __builtin_amdgcn_readfirstlane(w.split);
+  w.tile = __builtin_amdgcn_readfirstlane(w.tile);
+  return w;
 }
 
 // Keys that a row of index i sees: lo <= j < hi, lo > hi - 1 where there are none
@@ -450,7 +475,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs a) {
   constexpr int E = 16 / sizeof(T), DT = D / 32, NF = D / (2 * E), NS = kPgUnit / (2 * E);
   extern __shared__ __attribute__((aligned(16))) unsigned char plan_lds[];
-  __shared__ __attribute__((aligned(16))) float merge[kWaves][DT * 16][64];       // before: the queries
+  __shared__ f32x4 merge[kWaves][DT * 4][64];       // before: the queries
   u32x4 (*q_lds)[64] = reinterpret_cast<u32x4 (*)[64]>(&merge[0][0][0]);
   __shared__ float wref[kWaves][32], wl[kWaves][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
@@ -458,9 +483,10 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
   const int G = a.G;
   const size_t head_pitch = (size_t)D << a.page_log2;           // elements
   for (int item = blockIdx.x; item < plan.items; item += gridDim.x) {
-    const int b = seq_of(plan, a.batch.batch, item);
-    const PlanSeq s = plan.seq[b];
-    const Place at_item = place_of<1>(a, plan, b, item);
+    const Found found = find(plan, a.batch.batch, item);
+    const int b = found.b;
+    const PlanSeq s = found.seq;
+    const Place at_item = place_of<1>(a, found, item);
     const int hk = at_item.hk, split = at_item.split, tile = at_item.tile, splits = at_item.splits;
     const Queries q = queries_of(a, s, b, hk, tile * 32, r32);
     // units of this split that a query sees; none: [0, 0)
@@ -471,6 +497,13 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
       u1 = min(u1, (q.all_hi + kPgUnit - 1) / kPgUnit);
     } else u1 = u0;
     const int n_units = max(0, u1 - u0), n_mine = (n_units - wave + kWaves - 1) / kWaves;
+
+    // the queries as operands, a wave's share, to LDS once the first unit is requested too
+    constexpr int kMyQ = (NF + kWaves - 1) / kWaves;
+    u32x4 my_q[kMyQ];
+    const T* qrow = (const T*)a.q + (int64_t)q.row * a.q_ld + q.head * D + g * E;
+#pragma unroll
+    for (int i = 0; i < kMyQ; ++i) my_q[i] = ld16(qrow + min(wave + i * kWaves, NF - 1) * 2 * E);
 
     const int32_t* pages = a.batch.pages + (int64_t)b * a.batch.page_cols;
     int ids = 0;                              // page numbers of this wave's next 64 units
@@ -514,12 +547,9 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
         load_v(at);
       }
     }
-    // the queries as operands, for all waves (their way to LDS is behind the first unit's requests)
-    {
-      const T* qrow = (const T*)a.q + (int64_t)q.row * a.q_ld + q.head * D + g * E;
 #pragma unroll
-      for (int f = wave; f < NF; f += kWaves) q_lds[f][lane] = ld16(qrow + f * 2 * E);
-    }
+    for (int i = 0; i < kMyQ; ++i)
+      if (NF % kWaves == 0 || wave + i * kWaves < NF) q_lds[wave + i * kWaves][lane] = my_q[i];
     __syncthreads();
 
     f32x16 o[DT] = {};
@@ -553,7 +583,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
     }
     l += __shfl_xor(l, 32, kWave);
 
-    // merge the waves that had a unit: each adds up an eighth of every accumulator, two neighbouring dimensions of a query
+    // merge the waves that had a unit: each adds up a quarter of every tile of dimensions, four neighbours of a query
+    static_assert(kWaves == 4, "a wave's share of a tile of dimensions is one f32x4");
     const int n_waves = min(kWaves, n_units);
     __syncthreads();
     if (wave < n_waves) {
@@ -561,20 +592,27 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) merge[wave][dt * 16 + i][lane] = o[dt][i];
+        for (int i = 0; i < 4; ++i) merge[wave][dt * 4 + i][lane] = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
     }
     __syncthreads();
-    float top = kFloor, sum = 0.f;
-    for (int w = 0; w < n_waves; ++w) top = fmaxf(top, wref[w][r32]);
-    constexpr int kMine = 16 / kWaves;            // accumulators of each tile of dimensions: neighbours
-    float y[DT][kMine] = {};
-    for (int w = 0; w < n_waves; ++w) {
-      const float weight = exp2_hw(wref[w][r32] - top);
-      sum += wl[w][r32] * weight;
+    float top = kFloor, sum = 0.f, weight[kWaves];
+    f32x4 y[DT] = {}, part_of[kWaves][DT];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      weight[w] = w < n_waves ? wref[w][r32] : kFloor;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) part_of[w][dt] = w < n_waves ? merge[w][dt * 4 + wave][lane] : f32x4{};
+    }
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, weight[w]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      weight[w] = exp2_hw(weight[w] - top);
+      sum += w < n_waves ? wl[w][r32] * weight[w] : 0.f;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int j = 0; j < kMine; ++j) y[dt][j] = fmaf(merge[w][dt * 16 + kMine * wave + j][lane], weight, y[dt][j]);
+        for (int j = 0; j < 4; ++j) y[dt][j] = fmaf(part_of[w][dt][j], weight[w], y[dt][j]);
     }
     const int d0 = 8 * wave + 4 * g;
     if (q.valid) {
@@ -582,14 +620,14 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
         const float inv = inverse_of(sum);
         T* to = (T*)a.out + (int64_t)q.row * a.out_ld + q.head * D + d0;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) store4<T>(to + 32 * dt, f32x4{y[dt][0] * inv, y[dt][1] * inv, y[dt][2] * inv, y[dt][3] * inv});
+        for (int dt = 0; dt < DT; ++dt) store4<T>(to + 32 * dt, y[dt] * inv);
         if (a.row_ml && wave == 0 && g == 0) a.row_ml[(size_t)q.row * a.H + q.head] = make_float2(top, inv);
       } else {
-        const size_t part = (size_t)(plan.split[b] & 0xffffff) + ((size_t)hk * split_tiles<1>(plan, b, G) + tile) * splits + split;
+        const size_t part = (size_t)(found.split & 0xffffff) + ((size_t)hk * split_tiles<1>(s.m * G, found.whole) + tile) * splits + split;
         float* to = a.part_o + (part * 32 + r32) * D + d0;
         if (n_units > 0) {
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt) store4<float>(to + 32 * dt, f32x4{y[dt][0], y[dt][1], y[dt][2], y[dt][3]});
+          for (int dt = 0; dt < DT; ++dt) store4<float>(to + 32 * dt, y[dt]);
         }
         if (wave == 0 && g == 0) a.part_ml[part * 32 + r32] = make_float2(top, sum);
       }
@@ -608,10 +646,11 @@ __device__ __forceinline__ u32x4 buffer_of(const void* p, uint32_t bytes) {
   return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, bytes, 0x00020000u};
 }
 __device__ __forceinline__ void load_to_lds(const unsigned char* to, const u32x4& from, int voffset, int soffset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-               :
+  uint32_t m0;                           // (the compiler's own is put back)
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0)
                : "s"(lds_address(to)), "v"(voffset), "s"(from), "s"(soffset)
-               : "memory", "m0");
+               : "memory");
 }
 
 // Eight tiles of 32 queries per workgroup, one a wave.  K and V of 64 keys (float: 32) at a time go from the pages straight into LDS, where they lie as in
@@ -639,9 +678,10 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
     const int at_wg = round & 1 ? (int)((gridDim.x / 8 - 1 - blockIdx.x / 8) * 8 + blockIdx.x % 8) : (int)blockIdx.x;
     const int item = round * gridDim.x + at_wg;
     if (item >= plan.items) continue;
-    const int b = seq_of(plan, a.batch.batch, item);
-    const PlanSeq s = plan.seq[b];
-    const Place at_item = place_of<kManyWaves>(a, plan, b, item);
+    const Found found = find(plan, a.batch.batch, item);
+    const int b = found.b;
+    const PlanSeq s = found.seq;
+    const Place at_item = place_of<kManyWaves>(a, found, item);
     const int hk = at_item.hk, split = at_item.split, tile = at_item.tile, splits = at_item.splits, R = s.m * G, sub = tile * kManyWaves + wave;
     const bool active = sub * 32 < R;
     const Queries q = queries_of(a, s, b, hk, active ? sub * 32 : tile * kManyWaves * 32, r32);
@@ -861,7 +901,7 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
             store4<T>(to + 32 * dt + 2 * i, f32x4{o[dt][i] * inv, o[dt][i + 1] * inv, o[dt][i + 2] * inv, o[dt][i + 3] * inv});
         if (a.row_ml && g == 0) a.row_ml[(size_t)q.row * a.H + q.head] = make_float2(ref, inv);
       } else {
-        const size_t part = (size_t)(plan.split[b] & 0xffffff) + ((size_t)hk * split_tiles<kManyWaves>(plan, b, G) + sub) * splits + split;
+        const size_t part = (size_t)(found.split & 0xffffff) + ((size_t)hk * split_tiles<kManyWaves>(R, found.whole) + sub) * splits + split;
         float* to = a.part_o + (part * 32 + r32) * D + 4 * g;
         if (n_units > 0) {
 #pragma unroll
