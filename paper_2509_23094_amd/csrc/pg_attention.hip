@@ -54,6 +54,12 @@ struct AttendArgs {
   int4* info;                    // [sequence]: splits | first part << 8, tiles of 32 queries that are split, first row, rows
 };
 
+// All cache lines of the arguments at once: as they are needed one by one, each first use of a line waits for memory.
+__device__ __forceinline__ void fetch_arguments(const AttendArgs& a) {
+  asm volatile("" ::"s"(a.batch.row_start), "s"(a.batch.page_cols), "s"(a.pages.n_pages), "s"(a.out_ld), "s"(a.H), "s"(a.window), "s"(a.by_g.s), "s"(a.c2),
+               "s"(a.part_limit), "s"(a.part_ml), "s"(a.info));
+}
+
 // ------------------------------------------------------------------ the plan
 
 struct PlanSeq { int row0, m, length, unit0; };     // unit0: first unit that a row of the sequence can see
@@ -479,6 +485,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
   u32x4 (*q_lds)[64] = reinterpret_cast<u32x4 (*)[64]>(&merge[0][0][0]);
   __shared__ float wref[kWaves][32], wl[kWaves][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
+  fetch_arguments(a);
   const Plan plan = make_plan<1, kFewThreads>(a, plan_lds, 32.f);
   const int G = a.G;
   const size_t head_pitch = (size_t)D << a.page_log2;           // elements
@@ -670,6 +677,7 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
   const int v_lane = (g * D + r32) * 16;
   const bool second = wave >= kManyWaves / 2;
+  fetch_arguments(a);
   const Plan plan = make_plan<kManyWaves, 64 * kManyWaves>(a, plan_lds, 8.f);
   const int G = a.G;
   const size_t head_pitch = (size_t)D << a.page_log2;           // elements
