@@ -664,16 +664,17 @@ __device__ __forceinline__ void load_to_lds(const unsigned char* to, const u32x4
 // memory, so that every operand is 16 neighbouring bytes a lane.
 // The two waves of a SIMD take turns: while one is at its matrix instructions (P V of the last block, Q K of this one) the other is at its exponentials.
 // Time goes in half steps, each ended by a barrier: waves 0 - 3 have the products of block k in half step 2k and its softmax in 2k + 1, waves 4 - 7 one
-// half step later.  K of block k + 1 and V of block k are requested at the start of half step 2k (whoever read their places before
-// has passed a barrier since) and have to be there at the end of 2k + 1.
+// half step later.  In half step 2k waves 0 - 3 request V of block k between their products, waves 4 - 7 K of block k + 1 between their exponentials (whoever
+// read their places before has passed a barrier since); they have to be there at the end of 2k + 1.
 template <typename T, int D>
 __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
   constexpr int E = 16 / sizeof(T), DT = D / 32, NF = D / (2 * E), NS = kPgUnit / (2 * E), kUnits = sizeof(T) == 2 ? 2 : 1;
-  constexpr int kUnitBytes = kPgUnit * D * (int)sizeof(T), kOperand = kUnits * kUnitBytes, kPieces = kUnitBytes / 1024;
+  constexpr int kUnitBytes = kPgUnit * D * (int)sizeof(T), kOperand = kUnits * kUnitBytes, kPieces = kUnitBytes / 1024, kLoads = kUnits * kPieces / 4;
   constexpr int kRing = 4, kPerMm = sizeof(T) == 2 ? 1 : 4, kAll = (1 << kUnits) - 1;
   extern __shared__ __attribute__((aligned(16))) unsigned char plan_lds[];
   __shared__ __attribute__((aligned(16))) unsigned char lds[2 * 2 * kOperand];      // K, K, V, V
-  __shared__ int range[kManyWaves][4], dropped_at[2];
+  __shared__ int range[kManyWaves][4];
+  __shared__ uint32_t dropped_in[32];                   // blocks k % 1024 of which `clean` took something out
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
   const int v_lane = (g * D + r32) * 16;
   const bool second = wave >= kManyWaves / 2;
@@ -699,7 +700,7 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
     for (int f = 0; f < NF; ++f) qf[f] = ld16(qrow + f * 2 * E);
     // keys that any wave sees, and that all of them see
     if (lane == 0) { range[wave][0] = q.all_lo; range[wave][1] = q.all_hi; range[wave][2] = q.both_lo; range[wave][3] = q.both_hi; }
-    if (threadIdx.x < 2) dropped_at[threadIdx.x] = -1;
+    if (threadIdx.x < 32) dropped_in[threadIdx.x] = 0;
     __syncthreads();
     int lo = range[0][0], hi = range[0][1], in_lo = range[0][2], in_hi = range[0][3];
 #pragma unroll
@@ -721,39 +722,31 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
     const int n_units = max(0, u1 - u0), n_blocks = (n_units + kUnits - 1) / kUnits;
 
     const int32_t* pages = a.batch.pages + (int64_t)b * a.batch.page_cols;
-    int ids = 0;                              // page numbers of 64 units
-    uint32_t flags = 0;                       // which units of the blocks k - 1 .. k + 2 are there: kUnits bits at 2 (k % 16)
-    size_t v_at[kUnits] = {};                 // where the block whose V is requested next lies
-    int v_there = 0;
+    // Of 64 units, one a lane: where it lies in the pools (bytes).  Waves 0 - 3 request V of block k, waves 4 - 7 K of block k + 1 (which they find first).
+    uint32_t at_low = 0, at_high = 0;
+    uint64_t have = 0;                        // which of them are there
+    uint32_t flags = 0;                       // which units of the last blocks are there: kUnits bits at 2 (k % 16)
     auto there = [&](int k) __attribute__((always_inline)) { return (int)(flags >> (2 * (k & 15))) & kAll; };
-    auto piece_loop = [&](unsigned char* to, const T* from) __attribute__((always_inline)) {
-      const u32x4 src = buffer_of(from, kUnitBytes);
-#pragma unroll
-      for (int j = 0; j < (kPieces + kManyWaves - 1) / kManyWaves; ++j) {
-        const int piece = j * kManyWaves + wave;
-        if (kPieces % kManyWaves == 0 || piece < kPieces) load_to_lds(to + piece * 1024, src, lane * 16, piece * 1024);
+    auto find_block = [&](int k) __attribute__((always_inline)) {
+      const int first = k * kUnits & 63;
+      if (first == 0) {
+        const int unit = min(u0 + k * kUnits + lane, u1 - 1), page = pages[unit >> (a.page_log2 - 5)];
+        const size_t at = (((size_t)page * a.Hkv + hk) * head_pitch + (size_t)(unit & ((1 << (a.page_log2 - 5)) - 1)) * kPgUnit * D) * sizeof(T);
+        at_low = (uint32_t)at;
+        at_high = (uint32_t)(at >> 32);
+        have = __ballot(k * kUnits + lane < n_units && (unsigned)page < (unsigned)a.pages.n_pages);
+        asm volatile("" : "+v"(at_low), "+v"(at_high));      // (the wait for the page numbers belongs here: behind the branch it would be one for all that is out, each time)
       }
+      flags = (flags & ~(3u << (2 * (k & 15)))) | ((uint32_t)(have >> first) & kAll) << (2 * (k & 15));
     };
-    // V of block k (found when its K was) and K of block k + 1 into their places
-    auto stage = [&](int k) __attribute__((always_inline)) {
-#pragma unroll
-      for (int u = 0; u < kUnits; ++u)
-        if (v_there >> u & 1) piece_loop(lds + (2 + (k & 1)) * kOperand + u * kUnitBytes, (const T*)a.pages.v + v_at[u]);
-      v_there = 0;
-      ++k;
-      if (k >= n_blocks) return;
-      if (k * kUnits % 64 == 0) ids = pages[min(u0 + k * kUnits + lane, u1 - 1) >> (a.page_log2 - 5)];
-#pragma unroll
-      for (int u = 0; u < kUnits; ++u) {
-        const int unit = k * kUnits + u, page = __builtin_amdgcn_readlane(ids, unit & 63);
-        if (unit < n_units && (unsigned)page < (unsigned)a.pages.n_pages) {
-          v_there |= 1 << u;
-          v_at[u] = ((size_t)page * a.Hkv + hk) * head_pitch + (size_t)((u0 + unit) & ((1 << (a.page_log2 - 5)) - 1)) * kPgUnit * D;
-          piece_loop(lds + (k & 1) * kOperand + u * kUnitBytes, (const T*)a.pages.k + v_at[u]);
-        }
-      }
-      flags = (flags & ~(3u << (2 * (k & 15)))) | (uint32_t)v_there << (2 * (k & 15));
+    // the j-th of a wave's kLoads pieces of a block; of a unit that is not there nothing is read (a buffer of no bytes)
+    auto load = [&](const void* pool, int place, int k, int j) __attribute__((always_inline)) {
+      const int u = j * 4 / kPieces, piece = j * 4 % kPieces + (wave & 3), l = (k * kUnits & 63) + u;
+      const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_high, l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)at_low, l);
+      load_to_lds(lds + (place + (k & 1)) * kOperand + u * kUnitBytes + piece * 1024,
+                  buffer_of((const char*)pool + off, there(k) >> u & 1 ? kUnitBytes : 0), lane * 16, piece * 1024);
     };
+    auto nothing = [](int) {};
     auto requested = [&]() __attribute__((always_inline)) {       // everything this wave has requested is there (vmcnt(0))
       __builtin_amdgcn_s_waitcnt(0x70 | 0xf00);
       __builtin_amdgcn_sched_barrier(0);
@@ -783,7 +776,7 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
         dropped = drop_not_finite<T>(x) || dropped;
         v[i] = x;
       }
-      if (dropped) dropped_at[k & 1] = k;
+      if (dropped) atomicOr(&dropped_in[k / 32 % 32], 1u << (k & 31));
       __syncthreads();
     };
 
@@ -792,7 +785,7 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
     float ref = kFloor, l = 0.f;
     // One block's P V (the last block's) and Q K as a row of matrix instructions, operands through a ring of registers, the next ones requested right
     // behind the instruction that uses the last ones (the scheduler is told to keep that order).
-    auto products = [&](auto with_pv, auto with_qk, int k) __attribute__((always_inline)) {
+    auto products = [&](auto with_pv, auto with_qk, int k, auto load) __attribute__((always_inline)) {
       constexpr int NV = with_pv ? kUnits * NS * DT : 0, N = NV + (with_qk ? kUnits * NF : 0);
       const unsigned char *kb = lds + (k & 1) * kOperand + lane * 16, *vb = lds + (2 + (~k & 1)) * kOperand + v_lane;
       u32x4 ring[kRing];
@@ -802,34 +795,28 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
       };
 #pragma unroll
       for (int i = 0; i < kRing; ++i) ring[i] = read(i);
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        if (i < NV) o[i % DT] = mm<T>(ring[i % kRing], p[i / (NS * DT)][i / DT % NS], o[i % DT]);
-        else {
-          const int u = (i - NV) / NF, f = (i - NV) % NF;
-          acc[u] = mm<T>(ring[i % kRing], qf[f], f == 0 ? f32x16{} : acc[u]);
-        }
-        if (i + kRing < N) ring[i % kRing] = read(i + kRing);
-      }
       __builtin_amdgcn_sched_group_barrier(0x100, kRing, 0);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, kPerMm, 0);
-        if (i + kRing < N) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      if (with_pv && !inside(k - 1) && __builtin_expect(__builtin_amdgcn_readfirstlane(dropped_at[~k & 1]) == k - 1, 0)) {
-#pragma unroll 1
-        for (int u = 0; u < kUnits; ++u) {
-          const int unit = u0 + (k - 1) * kUnits + u;
-          if (!(there(k - 1) >> u & 1)) continue;
-          const size_t page = (size_t)pages[unit >> (a.page_log2 - 5)];
-          add_not_finite<T, DT>((const T*)a.pages.v + (page * a.Hkv + hk) * head_pitch + (size_t)(unit & ((1 << (a.page_log2 - 5)) - 1)) * kPgUnit * D,
-                                unit * kPgUnit, q, o);
+      for (int j = 0; j < kLoads; ++j) {
+        load(j);
+#pragma unroll
+        for (int i = j * (N / kLoads); i < (j + 1) * (N / kLoads); ++i) {
+          if (i < NV) o[i % DT] = mm<T>(ring[i % kRing], p[i / (NS * DT)][i / DT % NS], o[i % DT]);
+          else {
+            const int u = (i - NV) / NF, f = (i - NV) % NF;
+            acc[u] = mm<T>(ring[i % kRing], qf[f], f == 0 ? f32x16{} : acc[u]);
+          }
+          if (i + kRing < N) ring[i % kRing] = read(i + kRing);
         }
+#pragma unroll
+        for (int i = j * (N / kLoads); i < (j + 1) * (N / kLoads); ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, kPerMm, 0);
+          if (i + kRing < N) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     };
-    auto softmax = [&](int k) __attribute__((always_inline)) {
+    auto softmax = [&](int k, auto load) __attribute__((always_inline)) {
       const int key0 = (u0 + k * kUnits) * kPgUnit;
       if (!(there(k) == kAll && key0 >= q.both_lo && key0 + kUnits * kPgUnit <= q.both_hi)) {
 #pragma unroll
@@ -847,7 +834,17 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
       for (int u = 1; u < kUnits; ++u) top = fmaxf(top, top_of(acc[u]));
       raise<DT>(top, a.c2, ref, l, o);
 #pragma unroll
-      for (int u = 0; u < kUnits; ++u) exps_unit<T>(acc[u], a.c2, ref, l, p[u]);
+      for (int u = 0; u < kUnits; ++u) {
+#pragma unroll
+        for (int j = u * (kLoads / kUnits); j < (u + 1) * (kLoads / kUnits); ++j) load(j);
+        exps_unit<T>(acc[u], a.c2, ref, l, p[u]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      // (here and not behind the barrier)
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+        for (int i = 0; i < NS; ++i) asm volatile("" : "+v"(p[u][i]));
     };
     constexpr std::true_type yes{};
     constexpr std::false_type no{};
@@ -859,44 +856,64 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
       clean(k);
     };
 
-    stage(-1);
-    requested();
-    barrier();
     if (n_blocks > 0) {
       if (!second) {
-        stage(0);
-        if (active) products(no, yes, 0);
-        half();
-        if (active) softmax(0);
-        full(0);
-        for (int k = 1; k < n_blocks; ++k) {
-          stage(k);
-          if (active) products(yes, yes, k);
+        auto load_v = [&](int k) { return [&, k](int j) __attribute__((always_inline)) { load(a.pages.v, 2, k, j); }; };
+        auto step = [&](auto with_pv, int k) __attribute__((always_inline)) {
+          find_block(k);
+          if (active) products(with_pv, yes, k, load_v(k));
+          else
+            for (int j = 0; j < kLoads; ++j) load_v(k)(j);
           half();
-          if (active) softmax(k);
+          if (active) softmax(k, nothing);
           full(k);
-        }
-        if (active) products(yes, no, n_blocks);
+        };
+        barrier();
+        step(no, 0);
+        for (int k = 1; k < n_blocks; ++k) step(yes, k);
+        if (active) products(yes, no, n_blocks, nothing);
         half();
       } else {
-        stage(0);
+        auto load_k = [&](int k) { return [&, k](int j) __attribute__((always_inline)) { load(a.pages.k, 0, k, j); }; };
+        auto load_all = [&](int k) __attribute__((always_inline)) {
+#pragma unroll
+          for (int j = 0; j < kLoads; ++j) load_k(k)(j);
+        };
+        find_block(0);
+        load_all(0);
+        requested();
+        barrier();
+        find_block(1);
+        load_all(1);
         half();
-        if (active) products(no, yes, 0);
+        if (active) products(no, yes, 0, nothing);
         full(0);
-        stage(1);
-        if (active) softmax(0);
+        find_block(2);
+        if (active) softmax(0, load_k(2));
+        else load_all(2);
         half();
         for (int k = 1; k < n_blocks; ++k) {
-          if (active) products(yes, yes, k);
+          if (active) products(yes, yes, k, nothing);
           full(k);
-          stage(k + 1);
-          if (active) softmax(k);
+          find_block(k + 2);
+          if (active) softmax(k, load_k(k + 2));
+          else load_all(k + 2);
           half();
         }
-        if (active) products(yes, no, n_blocks);
+        if (active) products(yes, no, n_blocks, nothing);
       }
     }
 
+    // what `clean` took out, for the queries that see it (it can come last: a sum that has met infinity or NaN stays there)
+    if (active && n_blocks > 0 && __builtin_expect(__ballot(dropped_in[lane & 31] != 0) != 0, 0)) {
+#pragma unroll 1
+      for (int k = 0; k < n_units; ++k) {
+        const int unit = u0 + k, page = pages[unit >> (a.page_log2 - 5)], block = k / kUnits;
+        if (!(dropped_in[block / 32 % 32] >> (block & 31) & 1) || (unsigned)page >= (unsigned)a.pages.n_pages) continue;
+        add_not_finite<T, DT>((const T*)a.pages.v + ((size_t)page * a.Hkv + hk) * head_pitch + (size_t)(unit & ((1 << (a.page_log2 - 5)) - 1)) * kPgUnit * D,
+                              unit * kPgUnit, q, o);
+      }
+    }
     l += __shfl_xor(l, 32, kWave);
     if (active && q.valid) {
       if (splits == 1) {
