@@ -700,10 +700,10 @@ class PgContext:
     # ------------------------------------------------------------------ C ABI calls
     def d2c_pg_rotate(self, x: torch.Tensor, pos: torch.Tensor, out: torch.Tensor, inverse: bool = False) -> None:
         """x [n, heads * head_dim] (float32 or the storage type) turned by pos [n_axes, n] into out (storage type; may be x)."""
-        kind = self._source(x, "x")
-        if x.dim() != 2 or x.shape[1] == 0 or x.shape[1] % self.head_dim:
-            raise D2CError(D2C_EINVAL, "x: rows of whole heads expected, got %s" % (tuple(x.shape),))
-        n, width = x.shape
+        kind, shape = self._source(x, "x"), x.shape
+        if len(shape) != 2 or shape[1] == 0 or shape[1] % self.head_dim:
+            raise D2CError(D2C_EINVAL, "x: rows of whole heads expected, got %s" % (tuple(shape),))
+        n, width = shape
         xp, x_ld = _rows(x, "x", x.dtype, n, width, self.device)
         op, o_ld = _rows(out, "out", self.torch_dtype, n, width, self.device)
         self._check(_lib.d2c_pg_rotate(self.handle, xp, x_ld, kind, n, width // self.head_dim, self._pos(pos, n), int(inverse), op, o_ld,
