@@ -697,6 +697,29 @@ def test_many_products_do_not_see_what_they_do_not_see(what):
     assert torch.equal(out[~seen], clean[~seen])
 
 
+@pytest.mark.parametrize("geo,dtype,length,m", [("dream", "bf16", 70003, 40), ("dream", "f32", 70003, 140), ("llada", "f32", 3300, 2500)])
+def test_many_products_meet_infinities_far_back(geo, dtype, length, m):
+    """Some rows see an infinity of V, in a block of keys of which another page is not there; more blocks of keys than are told apart when it is looked for."""
+    p = Pool(geo, dtype, 32, [length], seed=11).fill()
+    spot = length - 15
+    p.pages[0, spot // 32 - 1] = -1
+    b = p.batch([m])
+    q = torch.randn((m, p.H * p.D), device="cuda", generator=torch.Generator("cuda").manual_seed(5)).to(p.ctx.torch_dtype)
+    clean = torch.zeros_like(q)
+    p.ctx.d2c_pg_attention(p.cache, b, q, clean, block=1)
+    at = B().PgBatch(p.ctx, ints([0, 1]), ints([length]), ints(p.pages[:1]), 1, at=ints([spot]))
+    t = torch.zeros((1, p.Hkv * p.D), dtype=p.ctx.torch_dtype, device="cuda")
+    keep = [torch.empty_like(t) for _ in range(2)]
+    p.ctx.d2c_pg_read(p.cache, at, *keep)
+    t[0, ::2], t[0, 1::2] = float("inf"), keep[1][0, 1::2]       # every other dimension
+    p.ctx.d2c_pg_append(p.cache, at, keep[0], t)
+    out = torch.zeros_like(q)
+    p.ctx.d2c_pg_attention(p.cache, b, q, out, block=1)
+    seen = torch.arange(length - m, length, device="cuda") >= spot
+    assert torch.equal(out[~seen], clean[~seen]) and torch.equal(out[seen][:, 1::2], clean[seen][:, 1::2])
+    assert bool((out[seen][:, ::2] == float("inf")).all()) and bool(clean.isfinite().all())
+
+
 def test_many_products_repeat_to_the_bit_and_follow_their_lengths():
     p = Pool("dream", "bf16", 64, [5000, 700], seed=9).fill()
     b = p.batch([1000, 3])
