@@ -612,11 +612,14 @@ class Q8Batch:
 
 def _rows(t: torch.Tensor, what: str, dtype: torch.dtype, n: int, width: int, device: int):
     """(pointer, pitch in elements) of rows [n, width] whose elements lie together; the rows may lie apart."""
-    pitch = t.stride()
-    if t.dtype is not dtype or t.shape != (n, width) or t.get_device() != device or pitch[1] != 1:
-        raise D2CError(D2C_EINVAL, "%s: rows of %s, %d x %d on device %d expected, got %s %s strides %s on %s"
-                       % (what, dtype, n, width, device, t.dtype, tuple(t.shape), t.stride(), t.device))
-    return t.data_ptr(), pitch[0] if n > 1 else width              # (a single row's stride can be anything)
+    if t.dtype is dtype and t.get_device() == device and t.shape == (n, width):
+        if t.is_contiguous():
+            return t.data_ptr(), width
+        pitch = t.stride()
+        if pitch[1] == 1:
+            return t.data_ptr(), pitch[0] if n > 1 else width      # (a single row's stride can be anything)
+    raise D2CError(D2C_EINVAL, "%s: rows of %s, %d x %d on device %d expected, got %s %s strides %s on %s"
+                   % (what, dtype, n, width, device, t.dtype, tuple(t.shape), t.stride(), t.device))
 
 
 class Rotary:
@@ -713,14 +716,12 @@ class PgContext:
                       q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> None:
         """Rows k, v [n_rows, d_kv] into the pages, k turned by pos [n_axes, n_rows] (None: the rows' indices); q likewise into q_out."""
         self._match(cache, batch)
-        n, t = batch.n_rows, k.dtype
-        a = d2c_pg_new(dtype=self._source(k, "k"), pos=self._pos(pos, n))
-        a.k, a.k_ld = _rows(k, "k", t, n, self.d_kv, self.device)
-        a.v, a.v_ld = _rows(v, "v", t, n, self.d_kv, self.device)
-        if q is not None:
-            a.q, a.q_ld = _rows(q, "q", t, n, self.d_q, self.device)
-        if q_out is not None:
-            a.q_out, a.q_out_ld = _rows(q_out, "q_out", self.torch_dtype, n, self.d_q, self.device)
+        n, t, dev = batch.n_rows, k.dtype, self.device
+        kp, k_ld = _rows(k, "k", t, n, self.d_kv, dev)
+        vp, v_ld = _rows(v, "v", t, n, self.d_kv, dev)
+        qp, q_ld = _rows(q, "q", t, n, self.d_q, dev) if q is not None else (None, 0)
+        op, o_ld = _rows(q_out, "q_out", self.torch_dtype, n, self.d_q, dev) if q_out is not None else (None, 0)
+        a = d2c_pg_new(qp, kp, vp, q_ld, k_ld, v_ld, self._source(k, "k"), self._pos(pos, n), op, o_ld)
         self._check(_lib.d2c_pg_append(self.handle, cache.ref, batch.ref, C.byref(a), _stream()))
 
     def d2c_pg_read(self, cache: "PgCache", batch: "PgBatch", out_k: Optional[torch.Tensor], out_v: Optional[torch.Tensor]) -> None:
@@ -737,13 +738,14 @@ class PgContext:
         n, t = batch.n_rows, self.torch_dtype
         if scale is not None and not scale > 0:
             raise D2CError(D2C_EINVAL, "scale must be positive")
-        a = d2c_pg_attend(block=block, window=window, scale=0.0 if scale is None else scale)
-        a.q, a.q_ld = _rows(q, "q", t, n, self.d_q, self.device)
-        a.out, a.out_ld = _rows(out, "out", t, n, self.d_q, self.device)
+        qp, q_ld = _rows(q, "q", t, n, self.d_q, self.device)
+        op, o_ld = _rows(out, "out", t, n, self.d_q, self.device)
+        ap, a_ld = None, 0
         if attn_avg is not None:
             if attn_avg.dim() != 2 or attn_avg.shape[1] < 1:
                 raise D2CError(D2C_EINVAL, "attn_avg: [n_rows, columns] expected, got %s" % (tuple(attn_avg.shape),))
-            a.attn_avg, a.avg_ld = _checked(attn_avg, "attn_avg", torch.float32, (n, attn_avg.shape[-1]), self.device), attn_avg.shape[-1]
+            ap, a_ld = _checked(attn_avg, "attn_avg", torch.float32, (n, attn_avg.shape[-1]), self.device), attn_avg.shape[-1]
+        a = d2c_pg_attend(qp, q_ld, op, o_ld, ap, a_ld, block, window, 0.0 if scale is None else scale)
         self._check(_lib.d2c_pg_attention(self.handle, cache.ref, batch.ref, C.byref(a), _stream()))
 
 
