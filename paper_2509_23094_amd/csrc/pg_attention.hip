@@ -96,7 +96,8 @@ __device__ __forceinline__ int reduce_min(int v) { return last_lane(scan(v, INT3
 // An item is (tile of TILES * 32 queries, split, kv head) of a sequence; kv heads run fastest, so that tiles that read the same keys are a
 // multiple of Hkv workgroups apart (on one XCD where that is a multiple of 8).  As many tiles as fill whole rounds of workgroups are not split (a
 // sequence's last ones, which a mask leaves the most keys, come first); the rest is, in splits of equal length for all sequences: of 1 .. 64 for the
-// longest sequence, each lane of a wave takes one and estimates the time as rounds of workgroups times (units of a split + what an item costs besides).
+// longest sequence, each lane of a wave takes one and estimates the time as rounds of workgroups times (units of a split + what an item costs besides:
+// as much as 32 units of the kernel for few, 8 of the one for many; with 8 for few, 200 tokens on 1500 keys each took 92 us, with 32 they take 81).
 template <int TILES> __device__ __forceinline__ int tiles_in(int queries) { return (queries + 32 * TILES - 1) / (32 * TILES); }
 // About how many (query, key) pairs a sequence has
 __device__ __forceinline__ float work_of(const AttendArgs& a, int m, int length) {
@@ -476,7 +477,10 @@ constexpr int kManyWaves = 8;
 constexpr int kWaves = 4;
 constexpr int kFewThreads = 64 * kWaves;
 
-// One tile of 32 queries per workgroup: its waves take the units of a split in turn and are merged through LDS.
+// One tile of 32 queries per workgroup: its waves take the units of a split in turn and are merged through LDS.  K and V are used once, so nothing is staged:
+// two workgroups a compute unit, each wave with the next unit's K or V on its way while it works on what has come.  Bound by memory where caches are long
+// (64 tokens, 28 heads on 4, 279000 keys in all: 118 us, 4.8 TB/s, what a large copy reaches; one token, 60001 keys: 24 us, 5.0 TB/s, matrix cores 8 % and
+// vector units 16 % busy), by its chain of dependent steps where they are short (1023 keys: 7 - 9 us, of which the plan 1.7).
 template <typename T, int D>
 __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs a) {
   constexpr int E = 16 / sizeof(T), DT = D / 32, NF = D / (2 * E), NS = kPgUnit / (2 * E);
@@ -660,6 +664,9 @@ __device__ __forceinline__ void load_to_lds(const unsigned char* to, const u32x4
                : "memory");
 }
 
+// 2500 causal queries on 7000 keys, 32 heads of 128: 268 - 285 us, 0.83 - 0.88 PFLOP/s of what the masks leave (a product of 8192^3 by the library: 1.23);
+// matrix cores busy 51 %, vector units 49 % of the time, and the clock falls with both: a block of 64 keys went from 6100 clocks to 4200 as requests were
+// spread between instructions, and from 2.76 us to 2.3 only.
 // Eight tiles of 32 queries per workgroup, one a wave.  K and V of 64 keys (float: 32) at a time go from the pages straight into LDS, where they lie as in
 // memory, so that every operand is 16 neighbouring bytes a lane.
 // The two waves of a SIMD take turns: while one is at its matrix instructions (P V of the last block, Q K of this one) the other is at its exponentials.
@@ -944,7 +951,8 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
 // ------------------------------------------------------------------ splits joined
 
 // Groups of D / 4 lanes. Up to 8 splits: a group for each query, all of its splits requested at once; more: a workgroup for each query, its groups take
-// the splits in turn, and their sums are added in order.  What a split that saw nothing of the query (sum 0) left is not used.
+// the splits in turn, and their sums are added in order.  What a split that saw nothing of the query (sum 0) left is not used.  A launch of its own:
+// 2.7 - 4 us for a token, 13 for the 57 MB that 22 tiles of 256 queries x 4 kv heads in 5 splits leave.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void pg_join_kernel(const AttendArgs a) {
   constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kFew = 8, kEach = kPgMaxSplits / kGroups;
@@ -1028,9 +1036,10 @@ __global__ __launch_bounds__(256) void pg_join_kernel(const AttendArgs a) {
 
 // ------------------------------------------------------------------ the head average
 
-// A workgroup takes 32 rows of a sequence and one or two units of its keys; its eight waves take the heads in turn, scores computed again, and the waves'
-// sums are added in order.  Tiles of rows that read the same keys are neighbours on one XCD: blockIdx.x = (group of units / 8 * tiles + tile) * 8 +
-// group % 8, tiles of 32 rows sequence after sequence.
+// A workgroup takes 32 rows of a sequence and one or two units of its keys; its eight waves take the heads in turn and the waves' sums are added in order.
+// Scores are computed again: kept ones would be H times the average's bytes, out and in.  Tiles of rows that read the same keys are neighbours on
+// one XCD: blockIdx.x = (group of units / 8 * tiles + tile) * 8 + group % 8, tiles of 32 rows sequence after sequence.  4 sequences of 38 - 45 rows on 1823
+// keys, 32 heads: 19 us (one round of workgroups: each wave's chain Q, K -> scores -> exponentials, four heads long; without the order by XCD 28).
 template <typename T, int D> constexpr int kAvgUnits = D * (int)sizeof(T) > 256 ? 1 : 2;      // (float heads of 128 have registers for one)
 template <typename T, int D>
 __global__ __launch_bounds__(512, 2) void pg_average_kernel(const AttendArgs a, float* avg, int64_t avg_ld, int tiles, int wide) {

@@ -3,6 +3,8 @@
 // A wave takes (a part of) one row.  Its lanes form the row's angles, a pair each, in 64 bits: positions may be any 32-bit number, and of a product
 // in 32 bits nothing would be left behind the revolutions.  Only the fraction of a revolution goes on, in two floats: the first through
 // sincospi, the second as a first-order correction.  Then each lane turns 16 dimensions of a head at a time, in fp32, rounded once.
+// All of it is bound by memory, or by one launch's chain (position -> angle -> row) where rows are few: 6075 rows of 4096, float in, bf16 out, 31.5 us (4.7 TB/s);
+// a prompt of 2500 rows with q, k and v of 4096 each into its pages and k, v back 53.7 us (3.8 TB/s); one row 2.7 us; 64 rows of 64 sequences 3.4 and 2.6 us.
 #include <algorithm>
 
 #include "internal.h"
@@ -190,6 +192,13 @@ template <typename TS, typename T, int D> __device__ __forceinline__ void put_va
   }
 }
 
+// Workgroup wg of `count`, every 256 of them in another order: workgroups go round the 8 XCDs, and those of one XCD take neighbouring rows, because 8 rows'
+// pieces of K share a line that should go through one L2 (a prompt of 2500 rows into its pages and back 72 us without, 66 with it in the append, 60 in both).
+__device__ __forceinline__ int by_xcd(int wg, int count) {
+  const int j = wg & 255;
+  return wg - j + 256 <= count ? wg - j + (j & 7) * 32 + (j >> 3) : wg;
+}
+
 template <typename TS, typename T, int D, bool kNeighbours>
 __global__ __launch_bounds__(kThreads) void pg_rows_kernel(const RowsArgs a) {
   __shared__ float2 table[kThreads / 64][64];
@@ -199,7 +208,8 @@ __global__ __launch_bounds__(kThreads) void pg_rows_kernel(const RowsArgs a) {
     put_values<TS, T, D>(a, reinterpret_cast<T*>(tile_lds));
     return;
   }
-  const int64_t id = (int64_t)(blockIdx.x - a.v_tiles) * (kThreads / 64) + wave;
+  const int wg = (int)blockIdx.x - a.v_tiles;
+  const int64_t id = (int64_t)(a.rows.k ? by_xcd(wg, (int)gridDim.x - a.v_tiles) : wg) * (kThreads / 64) + wave;
   const int r = (int)(id / a.parts), part = (int)(id % a.parts);
   if (r >= a.n) return;
   PgRowAt row{0, 0, 0, 0, 0};
@@ -344,7 +354,7 @@ __global__ __launch_bounds__(kThreads) void pg_read_kernel(const ReadArgs a) {
     get_values<T, D>(a, reinterpret_cast<T*>(tile_lds));
     return;
   }
-  const int64_t id = (int64_t)(blockIdx.x - a.v_tiles) * (kThreads / 64) + wave;
+  const int64_t id = (int64_t)by_xcd((int)blockIdx.x - a.v_tiles, (int)gridDim.x - a.v_tiles) * (kThreads / 64) + wave;
   const int r = (int)(id / a.parts), part = (int)(id % a.parts);
   if (r >= a.batch.n_rows) return;
   const PgRowAt row = pg_row_at(a.batch, r, a.page_log2);
@@ -375,17 +385,19 @@ __global__ __launch_bounds__(kThreads) void pg_read_kernel(const ReadArgs a) {
   }
 }
 
-// A wave for each row, several where there are few: 2048 waves give each SIMD of the chip two
-int parts_for(int n, int chunks) { return std::max(1, std::min((chunks + 63) / 64, (2048 + n - 1) / n)); }
+// Waves for each row, so that there are 8192 in all: eight a SIMD, for a load that is out has to cover 2 us of latency (6075 rows of 4096 32 us, with 2048 34; a
+// prompt of 2500 rows into its pages and back 62 us, with 2048 70, with 16384 68, each before V's workgroups took four heads)
+int parts_for(int n, int chunks) { return std::max(1, std::min((chunks + 63) / 64, (8192 + n - 1) / n)); }
 // V in tiles of 32 rows and v_heads kv heads: how many workgroups, 0 where rows bring their V themselves.  Tiles pay where sequences have several rows
 // (whole pieces), and from 2^18 values on.  Append and read, us, by rows and by tiles: one sequence, 32 kv heads of 128: 64 rows 12.0 and 11.1,
 // 256 rows 24.5 and 15.3, 2048 rows 95 and 54; 4 kv heads: 256 rows 9.3 and 10.8, 512 rows 11.6 and 11.5, 1024 rows 15.6 and 13.5; 64 sequences
-// of one row, 32 kv heads: 13.6 and 16.5, 1000 of them 73 and 87.
+// of one row, 32 kv heads: 13.6 and 16.5, 1000 of them 73 and 87.  Up to four heads a workgroup, so that a row is read 1 KB at a time: 60 -> 54 us for 2500 rows
+// (two 56.5, six 53.5; 8 sequences of 300 rows 54, with two 51).
 int value_tiles(int n, int batch, int Hkv, int D, int& v_heads) {
   v_heads = 1;
   if (n / 8 < batch || (int64_t)n * Hkv * D < 1 << 18) return 0;
   const int64_t groups = (n + 31) / 32;
-  v_heads = (int)std::max<int64_t>(1, std::min<int64_t>(Hkv, groups * Hkv / 4096));
+  v_heads = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(Hkv, 4), groups * Hkv / 512));
   return (int)(groups * ((Hkv + v_heads - 1) / v_heads));
 }
 
