@@ -97,7 +97,8 @@ __device__ __forceinline__ int reduce_min(int v) { return last_lane(scan(v, INT3
 // multiple of Hkv workgroups apart (on one XCD where that is a multiple of 8).  As many tiles as fill whole rounds of workgroups are not split (a
 // sequence's last ones, which a mask leaves the most keys, come first); the rest is, in splits of equal length for all sequences: of 1 .. 64 for the
 // longest sequence, each lane of a wave takes one and estimates the time as rounds of workgroups times (units of a split + what an item costs besides:
-// as much as 32 units of the kernel for few, 8 of the one for many; with 8 for few, 200 tokens on 1500 keys each took 92 us, with 32 they take 81).
+// as much as 32 units of the kernel for few, 8 of the one for many; with 8 for few, 200 tokens on 1500 keys each took 92 us, with 32 they take 81), and what the partial
+// results cost, 128 KB out and in for an item of the kernel for many (0.06 units: 1024 rows of 28 heads on 16000 keys 318 -> 247 us, 1500 of 32 on 8000 235 -> 216).
 template <int TILES> __device__ __forceinline__ int tiles_in(int queries) { return (queries + 32 * TILES - 1) / (32 * TILES); }
 // About how many (query, key) pairs a sequence has
 __device__ __forceinline__ float work_of(const AttendArgs& a, int m, int length) {
@@ -111,7 +112,7 @@ template <int TILES> __device__ __forceinline__ int split_tiles(int queries, int
   return min((queries + 31) / 32, (tiles_in<TILES>(queries) - whole) * TILES);
 }
 template <int TILES, int THREADS>
-__device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* lds, float item_cost) {
+__device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* lds, float item_cost, float part_cost) {
   constexpr int kWaves = THREADS / 64;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, batch = a.batch.batch, G = a.G;
   Plan p;
@@ -171,7 +172,7 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
     cost = 0.f;
     for (int w = 0; w < kWaves; ++w) cost += load[w][lane];
   }
-  cost = ceilf(cost / (float)gridDim.x) * ((float)chunk + item_cost);
+  cost = ceilf(cost / (float)gridDim.x) * ((float)chunk + item_cost) + (lane > 0 ? part_cost * cost : 0.f);
   // the cheapest, of equal ones the fewest splits (a positive float's bits are in its order)
   const int bits = lane < a.max_splits ? __builtin_bit_cast(int, cost) : INT32_MAX;
   const int best = reduce_min(bits);
@@ -490,7 +491,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
   __shared__ float wref[kWaves][32], wl[kWaves][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
   fetch_arguments(a);
-  const Plan plan = make_plan<1, kFewThreads>(a, plan_lds, 32.f);
+  const Plan plan = make_plan<1, kFewThreads>(a, plan_lds, 32.f, 0.f);
   const int G = a.G;
   const size_t head_pitch = (size_t)D << a.page_log2;           // elements
   for (int item = blockIdx.x; item < plan.items; item += gridDim.x) {
@@ -686,7 +687,7 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
   const int v_lane = (g * D + r32) * 16;
   const bool second = wave >= kManyWaves / 2;
   fetch_arguments(a);
-  const Plan plan = make_plan<kManyWaves, 64 * kManyWaves>(a, plan_lds, 8.f);
+  const Plan plan = make_plan<kManyWaves, 64 * kManyWaves>(a, plan_lds, 8.f, 0.06f);
   const int G = a.G;
   const size_t head_pitch = (size_t)D << a.page_log2;           // elements
   for (int round = 0; (int64_t)round * gridDim.x < plan.items; ++round) {
