@@ -650,18 +650,18 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
 
 // ------------------------------------------------------------------ many queries: K and V shared through LDS
 
-// The descriptor of a buffer of `bytes` from p on, and 64 pieces of 16 bytes from it (this lane's: at voffset + soffset) into LDS from `to` on.  As
+// The descriptor of a buffer of `bytes` from p on, and 64 pieces of 16 bytes from it (this lane's: at voffset) into LDS from `to` on.  As
 // builtins the compiler waits for all of them in front of any read of LDS; here the kernel waits by itself, once a block.  Nothing is
 // written but LDS, and the wait (for everything that is out) stands before the barrier behind which it is read.
 __device__ __forceinline__ u32x4 buffer_of(const void* p, uint32_t bytes) {
   const uint64_t at = (uint64_t)p;
   return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, bytes, 0x00020000u};
 }
-__device__ __forceinline__ void load_to_lds(const unsigned char* to, const u32x4& from, int voffset, int soffset) {
+__device__ __forceinline__ void load_to_lds(const unsigned char* to, const u32x4& from, int voffset) {
   uint32_t m0;                           // (the compiler's own is put back)
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
                : "=&s"(m0)
-               : "s"(lds_address(to)), "v"(voffset), "s"(from), "s"(soffset)
+               : "s"(lds_address(to)), "v"(voffset), "s"(from)
                : "memory");
 }
 
@@ -750,9 +750,10 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
     // the j-th of a wave's kLoads pieces of a block; of a unit that is not there nothing is read (a buffer of no bytes)
     auto load = [&](const void* pool, int place, int k, int j) __attribute__((always_inline)) {
       const int u = j * 4 / kPieces, piece = j * 4 % kPieces + (wave & 3), l = (k * kUnits & 63) + u;
+      const bool is = there(k) >> u & 1;
       const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_high, l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)at_low, l);
-      load_to_lds(lds + (place + (k & 1)) * kOperand + u * kUnitBytes + piece * 1024,
-                  buffer_of((const char*)pool + off, there(k) >> u & 1 ? kUnitBytes : 0), lane * 16, piece * 1024);
+      load_to_lds(lds + (place + (k & 1)) * kOperand + u * kUnitBytes + piece * 1024, buffer_of((const char*)pool + (is ? off : 0) + piece * 1024, is ? 1024 : 0),
+                  lane * 16);
     };
     auto nothing = [](int) {};
     auto requested = [&]() __attribute__((always_inline)) {       // everything this wave has requested is there (vmcnt(0))
