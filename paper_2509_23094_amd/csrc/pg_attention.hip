@@ -473,17 +473,16 @@ __device__ __forceinline__ float inverse_of(float sum) { return sum > 0.f ? 1.f 
 // keys: 256 rows (66e6) 66 and 58, 128 rows 43 and 47; 28 on 4, 4000 keys: 1024 rows (115e6) 105 and 90, 512 rows 57 and 59; 12 heads of 64 on 2, 16000 keys: 1024
 // rows (197e6) 104 and 88, 512 rows 61 and 67; float, where both wait for the matrix cores, 32 heads, 2048 keys, 2000 rows, no mask 646 and 531, causal 376 and 533.
 template <typename T, int D> constexpr float kMuch = sizeof(T) == 4 ? 256e6f : D == 64 ? 128e6f : 64e6f;
-constexpr int kManyWaves = 8;
+constexpr int kManyWaves = 8, kFewWaves = 4;
 
-constexpr int kWaves = 4;
-constexpr int kFewThreads = 64 * kWaves;
 
 // One tile of 32 queries per workgroup: its waves take the units of a split in turn and are merged through LDS.  K and V are used once, so nothing is staged:
 // two workgroups a compute unit, each wave with the next unit's K or V on its way while it works on what has come.  Bound by memory where caches are long
 // (64 tokens, 28 heads on 4, 279000 keys in all: 118 us, 4.8 TB/s, what a large copy reaches; one token, 60001 keys: 24 us, 5.0 TB/s, matrix cores 8 % and
-// vector units 16 % busy), by its chain of dependent steps where they are short (1023 keys: 7 - 9 us, of which the plan 1.7).
-template <typename T, int D>
-__global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs a) {
+// vector units 16 % busy), by its chain of dependent steps where they are short (1023 keys: 7 - 9 us, of which the plan 1.7).  The host takes eight waves instead
+// of four where that saves the second launch.
+template <typename T, int D, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 2) void pg_few_kernel(const AttendArgs a) {
   constexpr int E = 16 / sizeof(T), DT = D / 32, NF = D / (2 * E), NS = kPgUnit / (2 * E);
   extern __shared__ __attribute__((aligned(16))) unsigned char plan_lds[];
   __shared__ f32x4 merge[kWaves][DT * 4][64];       // before: the queries
@@ -491,7 +490,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
   __shared__ float wref[kWaves][32], wl[kWaves][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, r32 = lane & 31;
   fetch_arguments(a);
-  const Plan plan = make_plan<1, kFewThreads>(a, plan_lds, 32.f, 0.f);
+  const Plan plan = make_plan<1, 64 * kWaves>(a, plan_lds, 32.f, 0.f);
   const int G = a.G;
   const size_t head_pitch = (size_t)D << a.page_log2;           // elements
   for (int item = blockIdx.x; item < plan.items; item += gridDim.x) {
@@ -595,8 +594,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
     }
     l += __shfl_xor(l, 32, kWave);
 
-    // merge the waves that had a unit: each adds up a quarter of every tile of dimensions, four neighbours of a query
-    static_assert(kWaves == 4, "a wave's share of a tile of dimensions is one f32x4");
+    // merge the waves that had a unit: each adds up some fours of neighbouring dimensions, 8 n + 4 g on with n = wave, wave + kWaves ..
+    constexpr int kFours = DT * 4 / kWaves;
     const int n_waves = min(kWaves, n_units);
     __syncthreads();
     if (wave < n_waves) {
@@ -608,12 +607,12 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
     }
     __syncthreads();
     float top = kFloor, sum = 0.f, weight[kWaves];
-    f32x4 y[DT] = {}, part_of[kWaves][DT];
+    f32x4 y[kFours] = {}, part_of[kWaves][kFours];
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       weight[w] = w < n_waves ? wref[w][r32] : kFloor;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) part_of[w][dt] = w < n_waves ? merge[w][dt * 4 + wave][lane] : f32x4{};
+      for (int n = 0; n < kFours; ++n) part_of[w][n] = w < n_waves ? merge[w][n * kWaves + wave][lane] : f32x4{};
     }
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) top = fmaxf(top, weight[w]);
@@ -622,9 +621,9 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
       weight[w] = exp2_hw(weight[w] - top);
       sum += w < n_waves ? wl[w][r32] * weight[w] : 0.f;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
+      for (int n = 0; n < kFours; ++n)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) y[dt][j] = fmaf(part_of[w][dt][j], weight[w], y[dt][j]);
+        for (int j = 0; j < 4; ++j) y[n][j] = fmaf(part_of[w][n][j], weight[w], y[n][j]);
     }
     const int d0 = 8 * wave + 4 * g;
     if (q.valid) {
@@ -632,14 +631,14 @@ __global__ __launch_bounds__(kFewThreads, 2) void pg_few_kernel(const AttendArgs
         const float inv = inverse_of(sum);
         T* to = (T*)a.out + (int64_t)q.row * a.out_ld + q.head * D + d0;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) store4<T>(to + 32 * dt, y[dt] * inv);
+        for (int n = 0; n < kFours; ++n) store4<T>(to + 8 * kWaves * n, y[n] * inv);
         if (a.row_ml && wave == 0 && g == 0) a.row_ml[(size_t)q.row * a.H + q.head] = make_float2(top, inv);
       } else {
         const size_t part = (size_t)(found.split & 0xffffff) + ((size_t)hk * split_tiles<1>(s.m * G, found.whole) + tile) * splits + split;
         float* to = a.part_o + (part * 32 + r32) * D + d0;
         if (n_units > 0) {
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt) store4<float>(to + 32 * dt, y[dt]);
+          for (int n = 0; n < kFours; ++n) store4<float>(to + 8 * kWaves * n, y[n]);
         }
         if (wave == 0 && g == 0) a.part_ml[part * 32 + r32] = make_float2(top, sum);
       }
@@ -1181,20 +1180,28 @@ static hipError_t attention_d(const PgShape& s, AttendArgs a, const PgAttend& ca
   const PgBatch& b = a.batch;
   // units of the longest cache that the page table can name
   const int64_t units = (int64_t)b.page_cols << (s.page_log2 - 5);
-  // short ones are not split: a second launch costs more than it saves (one token, 28 heads on 4: 200 rows 10.9 us, split 12.8; 600 rows 13.9 and 13.0)
-  a.max_splits = units <= (sizeof(T) == 4 ? 2 : 3) * kWaves ? 1 : (int)std::min<int64_t>(kPgMaxSplits, units / kWaves);
+  // Short caches are not split: a second launch costs more than it saves (us, one token, 28 heads on 4: 200 keys 10.9, split 12.8; 600 keys 13.9 and 13.0).
+  // Longer ones of bf16 neither, if workgroups of eight waves, one a compute unit, take all tiles at once: up to 768 keys, or 1536 where there are too many tiles
+  // for many splits (one token, 28 heads on 4: 450 keys 11.6, split 12.1, 800 keys 12.0 and 12.0, 1023 keys 13.7 and 12.4; 100 rows, 32 heads: 600 keys 13.2
+  // and 18.7, 1536 keys 18.0 and 22.2, 2040 keys 21.9 and 22.8; 200 rows, 12 heads of 64 on 2: 700 keys 10.5 and 13.2; float 4 heads of 64, 389 keys 17 and 16).
+  const int64_t queries = (int64_t)b.n_rows * (s.H / s.Hkv), tiles = ((queries + 31) / 32 + std::min(b.n_rows, b.batch)) * s.Hkv;
+  const bool small = units <= (sizeof(T) == 4 ? 2 : 3) * kFewWaves;
+  const bool wide = !small && sizeof(T) == 2 && tiles <= cus && units <= (tiles > 64 ? 48 : 24) && b.batch <= 256;      // (there is LDS for the plan of 256)
+  a.max_splits = small || wide ? 1 : (int)std::min<int64_t>(kPgMaxSplits, units / kFewWaves);
   hipError_t e = hipSuccess;
   const size_t lds = plan_bytes(b.batch);
   // Few products or many: each sequence goes by its own work, which only the device knows.  What the host knows: all together cannot have that much
   // work; or as many rows as sequences, single tokens (if they are not, the kernel for few queries takes them all).
-  const int64_t queries = (int64_t)b.n_rows * (s.H / s.Hkv);
   const double most = (double)b.n_rows * s.H * std::min((double)((int64_t)b.page_cols << s.page_log2), a.window > 0 ? 2.0 * a.window : 1e30);
   const bool few_only = most <= kMuch<T, D> || b.n_rows <= b.batch;
   const int parts = a.part_limit;
   a.more_than = -1.f;
   a.up_to = few_only ? 3e38f : kMuch<T, D>;
   a.part_limit = few_only ? parts : parts / 4;
-  hipLaunchKernelGGL((pg_few_kernel<T, D>), dim3(2 * cus), dim3(kFewThreads), lds, st, a);
+  if constexpr (sizeof(T) == 2) {
+    if (wide) hipLaunchKernelGGL((pg_few_kernel<T, D, 2 * kFewWaves>), dim3((unsigned)tiles), dim3(128 * kFewWaves), lds, st, a);
+  }
+  if (!wide) hipLaunchKernelGGL((pg_few_kernel<T, D, kFewWaves>), dim3(2 * cus), dim3(64 * kFewWaves), lds, st, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (!few_only) {
     a.more_than = kMuch<T, D>;

@@ -588,6 +588,33 @@ def test_streams():
     assert all(torch.equal(o, w[3]) for o, w in zip(outs, work))
 
 
+# ------------------------------------------------------------------ caches of middle length (one launch of wider workgroups)
+
+@pytest.mark.parametrize("mask", [dict(), dict(block=1), dict(block=32, window=300)], ids=str)
+@pytest.mark.parametrize("geo,page_rows,lengths,counts", [
+    ("dream", 32, [760, 33, 0, 449], [1, 1, 2, 1]),       # each wave several units, one, none
+    ("llada", 64, [1500, 64, 1], [70, 1, 1]),             # more than 64 tiles
+    ((12, 2, 64), 256, [1400], [200]),
+    ("gqa", 32, [500, 700], [3, 40]),
+])
+def test_middle_caches(geo, page_rows, lengths, counts, mask):
+    say("%s %s %s" % (geo, lengths, mask))
+    p = Pool(geo, "bf16", page_rows, lengths, seed=4).fill()
+    p.attend(p.batch(counts, lead=1, tail=2), average=True, **mask)
+
+
+def test_middle_caches_of_many_sequences():
+    lengths = [(37 * i) % 701 for i in range(60)]
+    p = Pool("dream", "bf16", 64, lengths, seed=4).fill()
+    p.attend(p.batch([1 if n else 0 for n in lengths]), block=1)
+
+
+@pytest.mark.parametrize("what", [float("nan"), float("inf")])
+@pytest.mark.parametrize("counts,length", [([3], 700), ([100], 600)])
+def test_middle_caches_do_not_show_what_is_not_seen(what, counts, length):
+    test_what_a_row_does_not_see_does_not_change_it("bf16", what, counts, length)
+
+
 # ------------------------------------------------------------------ sequences with many products (the kernel for many queries)
 
 def expect_big(p, q, out, avg, block=0, window=0):
