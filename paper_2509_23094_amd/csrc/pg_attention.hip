@@ -46,7 +46,7 @@ struct AttendArgs {
   int H, Hkv, G, page_log2, block, window;
   Div by_hkv, by_g;
   float c2;                      // scale * log2(e)
-  float more_than, up_to;        // work (see work_of) that a sequence has to be this launch's
+  float much, together;          // work (see work_of) from which on a sequence is for the kernel for many queries: its own, that of all that fill tiles
   int max_splits, part_first, part_limit;      // partial tiles of this launch
   float* part_o;                 // [part][32][D]
   float2* part_ml;               // [part][32]: reference, sum
@@ -111,6 +111,18 @@ __device__ __forceinline__ float work_of(const AttendArgs& a, int m, int length)
 template <int TILES> __device__ __forceinline__ int split_tiles(int queries, int whole) {
   return min((queries + 31) / 32, (tiles_in<TILES>(queries) - whole) * TILES);
 }
+// A sequence goes to the kernel for many queries by its own work; or together with at least three others that fill their tiles there, by the work of all of
+// them (a sum of whole numbers, counted above it: both kernels have to come to the same).
+constexpr float kWorkUnit = 65536.f;
+constexpr int kOne = 1 << 21;
+__device__ __forceinline__ int share_of_work(const AttendArgs& a, int m, int length) {
+  const int R = m * a.G, tiles = (R + 255) / 256;
+  const int n = (int64_t)10 * R >= (int64_t)7 * 256 * tiles ? (int)fminf(work_of(a, m, length) / kWorkUnit, 1024.f) : 0;
+  return n > 0 ? n + kOne : 0;
+}
+__device__ __forceinline__ bool has_much(const AttendArgs& a, int m, int length, bool together) {
+  return work_of(a, m, length) > a.much || (together && (float)(share_of_work(a, m, length) % kOne) * kWorkUnit > a.together / 64.f);
+}
 template <int TILES, int THREADS>
 __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* lds, float item_cost, float part_cost) {
   constexpr int kWaves = THREADS / 64;
@@ -126,6 +138,23 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
   const bool solo = batch <= 16;
   p.solo = solo;
   p.my = PlanSeq{0, 0, 0, 0};
+  bool together = false;
+  if (a.together < 3e38f) {
+    uint32_t sum = 0;                  // (1024 sequences: 2^31)
+    for (int b = solo ? lane : tid; b < batch; b += THREADS) {
+      const int row0 = max(0, min(a.batch.row_start[b], a.batch.n_rows)), m = max(0, min(a.batch.row_start[b + 1], a.batch.n_rows) - row0);
+      sum += (uint32_t)share_of_work(a, m, max(0, min(a.batch.length[b], a.batch.page_cols << a.page_log2)));
+    }
+    sum = (uint32_t)last_lane(scan_sum((int)sum));
+    if (!solo) {
+      if (lane == 0) most[wave] = (int)sum;
+      __syncthreads();
+      sum = 0;
+      for (int w = 0; w < kWaves; ++w) sum += (uint32_t)most[w];
+      __syncthreads();
+    }
+    together = sum / kOne >= 4 && (float)(sum % kOne) * kWorkUnit > a.together;
+  }
   int units = 0, rows = 0, tiles = 0;
   for (int b = solo ? lane : tid; b < batch; b += THREADS) {
     const int lo = a.batch.row_start[b], hi = a.batch.row_start[b + 1], len = a.batch.length[b];
@@ -134,8 +163,7 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
     s.m = max(0, min(hi, a.batch.n_rows) - s.row0);
     s.length = max(0, min(len, a.batch.page_cols << a.page_log2));
     rows = min(rows + s.m, 1 << 22);             // (starts that are not ascending: the sum tells; n_rows is 2^20 at most)
-    const float work = work_of(a, s.m, s.length);
-    if (work <= a.more_than || work > a.up_to) s.m = 0;
+    if (has_much(a, s.m, s.length, together) != (TILES > 1)) s.m = 0;
     tiles = min(tiles + tiles_in<TILES>(s.m * G), 1 << 25);
     s.unit0 = a.window > 0 && !a.batch.at ? max(0, s.length - s.m - a.window + 1) / kPgUnit : 0;
     p.seq[b] = p.my = s;
@@ -472,6 +500,9 @@ __device__ __forceinline__ float inverse_of(float sum) { return sum > 0.f ? 1.f 
 // (query, key) pairs, all heads, from which on a sequence goes to the kernel for many queries.  us by the one for few and by it: bf16, 32 heads of 128, 8000
 // keys: 256 rows (66e6) 66 and 58, 128 rows 43 and 47; 28 on 4, 4000 keys: 1024 rows (115e6) 105 and 90, 512 rows 57 and 59; 12 heads of 64 on 2, 16000 keys: 1024
 // rows (197e6) 104 and 88, 512 rows 61 and 67; float, where both wait for the matrix cores, 32 heads, 2048 keys, 2000 rows, no mask 646 and 531, causal 376 and 533.
+// Several sequences of bf16 heads of 128 together, from half of it on, but for those with less than a 64th of that (others: no gain).  Lengths falling evenly to a
+// 20th, 28 heads on 4: 24 of 300 rows on 600 keys 104 and 87, 8 of 100 on 4000 82 and 66, 4 of 500 on 2000 83 and 71, but 12 of 400 on 1500 124 and 134; 32
+// heads: 16 of 256 on 600 83 and 64, 6 of 700 on 2000 155 and 123; two of 512 on 2000, which stay where they are, 55 and 69.
 template <typename T, int D> constexpr float kMuch = sizeof(T) == 4 ? 256e6f : D == 64 ? 128e6f : 64e6f;
 constexpr int kManyWaves = 8, kFewWaves = 4;
 
@@ -1195,8 +1226,8 @@ static hipError_t attention_d(const PgShape& s, AttendArgs a, const PgAttend& ca
   const double most = (double)b.n_rows * s.H * std::min((double)((int64_t)b.page_cols << s.page_log2), a.window > 0 ? 2.0 * a.window : 1e30);
   const bool few_only = most <= kMuch<T, D> || b.n_rows <= b.batch;
   const int parts = a.part_limit;
-  a.more_than = -1.f;
-  a.up_to = few_only ? 3e38f : kMuch<T, D>;
+  a.much = few_only ? 3e38f : kMuch<T, D>;
+  a.together = few_only || sizeof(T) == 4 || D == 64 ? 3e38f : 0.5f * kMuch<T, D>;
   a.part_limit = few_only ? parts : parts / 4;
   if constexpr (sizeof(T) == 2) {
     if (wide) hipLaunchKernelGGL((pg_few_kernel<T, D, 2 * kFewWaves>), dim3((unsigned)tiles), dim3(128 * kFewWaves), lds, st, a);
@@ -1204,8 +1235,6 @@ static hipError_t attention_d(const PgShape& s, AttendArgs a, const PgAttend& ca
   if (!wide) hipLaunchKernelGGL((pg_few_kernel<T, D, kFewWaves>), dim3(2 * cus), dim3(64 * kFewWaves), lds, st, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (!few_only) {
-    a.more_than = kMuch<T, D>;
-    a.up_to = 3e38f;
     a.part_first = parts / 4;
     a.part_limit = parts;
     hipLaunchKernelGGL((pg_many_kernel<T, D>), dim3(cus), dim3(64 * kManyWaves), lds, st, a);

@@ -682,6 +682,18 @@ def test_many_products(name, mask):
     attend_big(p, p.batch(counts, lead=1, tail=2), average=name == "dream", **mask)
 
 
+@pytest.mark.parametrize("geo,counts,lengths", [
+    ("llada", [512, 1, 287, 250, 512, 0, 512], [1500, 1500, 1400, 1300, 1450, 9, 700]),      # together; two do not fill their tiles
+    ("dream", [110] * 17 + [30, 2], [1000] * 17 + [900, 64]),                                # more than 16 sequences
+])
+def test_many_products_together(geo, counts, lengths):
+    """None of the sequences has many products by itself."""
+    p = Pool(geo, "bf16", 64, lengths, seed=13, max_rows=4096).fill()
+    b = p.batch(counts, lead=1, tail=2)
+    attend_big(p, b, block=1)
+    attend_big(p, b, average=True)
+
+
 def test_many_products_in_a_window():
     p = Pool("llada", "bf16", 32, [4100, 50], seed=5).fill()
     b = p.batch([3001, 50], origin=np.array([7, 0]))
