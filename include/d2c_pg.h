@@ -125,6 +125,7 @@ int d2c_pg_read(d2c_pg* ctx, const d2c_pg_cache* cache, const d2c_pg_batch* batc
  * What a row does not see (NaN and infinities among it) does not change its result.
  * Scores are q k^T * scale (0: 1 / sqrt(D)); scores, softmax and sums are fp32; scores are meant to stay below 2^100 in magnitude.
  * bfloat16: probabilities are rounded to bfloat16 for the product with V, their sum is not.
+ * The same call gives the same bits; with other sequences beside it, a sequence's sums can be split otherwise.
  * attn_avg float [n_rows, avg_ld], or NULL: columns below the sequence's length (and avg_ld) get the mean over the heads of the
  * softmax rows, 0 where the row sees nothing; columns behind are left as they are. */
 typedef struct {
