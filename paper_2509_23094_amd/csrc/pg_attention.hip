@@ -243,10 +243,11 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
   if (solo) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   else __syncthreads();
   p.items = solo ? last_lane(p.my_end) : p.first[batch];
-  // what the join and the average read
+  // what the join reads, of every sequence anew: by the launch that has its rows, of one without rows (none within the batch's: p.seq alone
+  // does not tell) by each launch, with no tiles.  A record that stays would be an earlier call's, with rows that this one may not have.
   if (blockIdx.x == 0)
     for (int b = tid; b < batch; b += THREADS)
-      if (p.seq[b].m > 0 || a.batch.row_start[b + 1] <= a.batch.row_start[b])      // (empty ones: by every launch)
+      if (p.seq[b].m > 0 || min(a.batch.row_start[b + 1], a.batch.n_rows) <= max(0, min(a.batch.row_start[b], a.batch.n_rows)))
         a.info[b] = make_int4(p.split[b] >> 24 | (p.split[b] & 0xffffff) << 8, split_tiles<TILES>(p.seq[b].m * G, p.whole[b]), p.seq[b].row0, p.seq[b].m);
   return p;
 }

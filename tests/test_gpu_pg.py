@@ -921,3 +921,28 @@ def test_row_starts_that_are_no_row_starts_harm_nothing_else():
         p.ctx.d2c_pg_append(p.cache, b, k, k, q=q, q_out=guard[20:40])
         torch.cuda.synchronize()
         assert (guard[:20] == 7).all() and (guard[40:] == 7).all()
+
+
+def split_pool(counts, seed=0):
+    """Three sequences whose caches are long enough that their tiles are split and joined, with a valid batch of `counts` rows."""
+    p = Pool("gqa", "bf16", 32, [2000, 1900, 1801], seed=seed).fill()
+    batch = p.batch(counts)
+    return p, batch, p.values(sum(counts), p.H)[0]
+
+
+@pytest.mark.parametrize("starts", [[0, 20, 25, 30], [0, 1, 30, 31], [20, 21, 22, 23], [-9, -5, -1, 20], [30, 40, 50, 60], [-5, -4, -3, -2], [0, 20, 20, 20]])
+def test_nothing_is_joined_from_the_call_before(starts):
+    """A call whose sequences are empty once their starts are taken into the batch, behind one of more rows that was split: nothing of the earlier
+    call's splits is joined into this one's output, or behind it."""
+    say("records, starts %s" % starts)
+    p, whole, q = split_pool([40, 40, 40])
+    want = torch.empty_like(q)
+    p.ctx.d2c_pg_attention(p.cache, whole, q, want, block=1)
+    guard = torch.full((400, 512), 7.0, dtype=torch.bfloat16, device="cuda")
+    bad = B().PgBatch(p.ctx, ints(starts), ints(p.lengths), ints(p.pages), 20)
+    p.ctx.d2c_pg_attention(p.cache, bad, q[:20], guard[200:220], block=1)
+    torch.cuda.synchronize()
+    assert (guard[:200] == 7).all() and (guard[220:] == 7).all()
+    again = torch.empty_like(want)
+    p.ctx.d2c_pg_attention(p.cache, whole, q, again, block=1)
+    assert torch.equal(again, want)
