@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include "common.h"
+#include "pg_plan.h"
 
 namespace d2c {
 

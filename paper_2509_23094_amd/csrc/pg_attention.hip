@@ -142,7 +142,7 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
   if (a.together < 3e38f) {
     uint32_t sum = 0;                  // (1024 sequences: 2^31)
     for (int b = solo ? lane : tid; b < batch; b += THREADS) {
-      const int row0 = max(0, min(a.batch.row_start[b], a.batch.n_rows)), m = max(0, min(a.batch.row_start[b + 1], a.batch.n_rows) - row0);
+      const int m = pg_span(a.batch.row_start[b], a.batch.row_start[b + 1], a.batch.n_rows).m;
       sum += (uint32_t)share_of_work(a, m, max(0, min(a.batch.length[b], a.batch.page_cols << a.page_log2)));
     }
     sum = (uint32_t)last_lane(scan_sum((int)sum));
@@ -159,8 +159,9 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
   for (int b = solo ? lane : tid; b < batch; b += THREADS) {
     const int lo = a.batch.row_start[b], hi = a.batch.row_start[b + 1], len = a.batch.length[b];
     PlanSeq s;
-    s.row0 = max(0, min(lo, a.batch.n_rows));
-    s.m = max(0, min(hi, a.batch.n_rows) - s.row0);
+    const PgSpan span = pg_span(lo, hi, a.batch.n_rows);
+    s.row0 = span.row0;
+    s.m = span.m;
     s.length = max(0, min(len, a.batch.page_cols << a.page_log2));
     rows = min(rows + s.m, 1 << 22);             // (starts that are not ascending: the sum tells; n_rows is 2^20 at most)
     if (has_much(a, s.m, s.length, together) != (TILES > 1)) s.m = 0;
@@ -247,7 +248,7 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
   // does not tell) by each launch, with no tiles.  A record that stays would be an earlier call's, with rows that this one may not have.
   if (blockIdx.x == 0)
     for (int b = tid; b < batch; b += THREADS)
-      if (p.seq[b].m > 0 || min(a.batch.row_start[b + 1], a.batch.n_rows) <= max(0, min(a.batch.row_start[b], a.batch.n_rows)))
+      if (p.seq[b].m > 0 || pg_span(a.batch.row_start[b], a.batch.row_start[b + 1], a.batch.n_rows).m == 0)
         a.info[b] = make_int4(p.split[b] >> 24 | (p.split[b] & 0xffffff) << 8, split_tiles<TILES>(p.seq[b].m * G, p.whole[b]), p.seq[b].row0, p.seq[b].m);
   return p;
 }
@@ -1085,10 +1086,7 @@ __global__ __launch_bounds__(512, 2) void pg_average_kernel(const AttendArgs a, 
   for (int b0 = 0; b0 < a.batch.batch && b < 0; b0 += 64) {
     const int s = b0 + lane;
     int n = 0;
-    if (s < a.batch.batch) {
-      const int lo = max(0, min(a.batch.row_start[s], a.batch.n_rows)), hi = min(a.batch.row_start[s + 1], a.batch.n_rows);
-      n = (max(0, hi - lo) + 31) / 32;
-    }
+    if (s < a.batch.batch) n = (pg_span(a.batch.row_start[s], a.batch.row_start[s + 1], a.batch.n_rows).m + 31) / 32;
     const int end = scan_sum(n);
     const uint64_t past = __ballot(before + end > at_tile);
     if (past) {
@@ -1098,7 +1096,8 @@ __global__ __launch_bounds__(512, 2) void pg_average_kernel(const AttendArgs a, 
     } else before += last_lane(end);
   }
   if (b < 0) return;
-  const int row0 = max(0, min(a.batch.row_start[b], a.batch.n_rows)), m = min(a.batch.row_start[b + 1], a.batch.n_rows) - row0;
+  const PgSpan span = pg_span(a.batch.row_start[b], a.batch.row_start[b + 1], a.batch.n_rows);
+  const int row0 = span.row0, m = span.m;
   const int length = max(0, min(a.batch.length[b], a.batch.page_cols << a.page_log2));
   const int cols = (int)min((int64_t)length, avg_ld);
   const bool valid = tile * 32 + r32 < m;

@@ -1,0 +1,15 @@
+// Whole-number arithmetic of the paged attention's plans, for host and device alike (constexpr functions; no HIP in this file).
+#pragma once
+#include <stdint.h>
+
+namespace d2c {
+
+struct PgSpan { int row0, m; };
+// The rows of the batch between two row starts, whatever these hold: each is taken into [0, n_rows] before the difference, which a start of -2^31 would
+// otherwise carry past 32 bits; none where they do not ascend.
+constexpr PgSpan pg_span(int lo, int hi, int n_rows) {
+  const int first = lo < 0 ? 0 : lo < n_rows ? lo : n_rows, end = hi < 0 ? 0 : hi < n_rows ? hi : n_rows;
+  return PgSpan{first, end > first ? end - first : 0};
+}
+
+}  // namespace d2c

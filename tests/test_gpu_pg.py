@@ -946,3 +946,22 @@ def test_nothing_is_joined_from_the_call_before(starts):
     again = torch.empty_like(want)
     p.ctx.d2c_pg_attention(p.cache, whole, q, again, block=1)
     assert torch.equal(again, want)
+
+
+@pytest.mark.parametrize("starts", [[40, -(1 << 31), 5, 20], [0, 20, -(1 << 31), (1 << 31) - 1], [(1 << 31) - 1, -(1 << 31), (1 << 31) - 1, 0], [19, -(1 << 31), 18, 20],
+                                    [5, 20, 3, 20], [20, 0, 20, 0]])
+def test_extreme_row_starts_stay_within_the_rows(starts):
+    """Starts whose differences leave 32 bits, with the head average, on caches that are split: only the call's own rows are written."""
+    say("extreme starts %s" % starts)
+    p, whole, q = split_pool([40, 40, 40], seed=1)
+    want, mean = torch.empty_like(q), torch.full((120, 2000), 7.0, device="cuda")
+    p.ctx.d2c_pg_attention(p.cache, whole, q, want, block=1, attn_avg=mean)
+    guard, beside = torch.full((400, 512), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((400, 2000), 7.0, device="cuda")
+    bad = B().PgBatch(p.ctx, ints(starts), ints(p.lengths), ints(p.pages), 20)
+    p.ctx.d2c_pg_attention(p.cache, bad, q[:20], guard[200:220], block=1, attn_avg=beside[200:220])
+    torch.cuda.synchronize()
+    for g in (guard, beside):
+        assert (g[:200] == 7).all() and (g[220:] == 7).all()
+    again, once = torch.empty_like(want), torch.full_like(mean, 7.0)
+    p.ctx.d2c_pg_attention(p.cache, whole, q, again, block=1, attn_avg=once)
+    assert torch.equal(again, want) and torch.equal(once, mean)

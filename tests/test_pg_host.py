@@ -1,8 +1,11 @@
 """CPU-side checks of the paged cache: the header against the library and the binding, refusals that need no GPU, and what the plain 64-bit
 forms (which the GPU tests compare with) promise."""
 import ctypes
+import itertools
 import os
 import re
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -140,3 +143,31 @@ def test_plain_places():
     assert seq.tolist() == [-1, 0, 0, 2, 2, -1] and idx[1:5].tolist() == [2, 3, 62, 63] and ln[3] == 64
     page, row = R.place(seq, idx, ln, np.array([[5, -1], [0, 0], [7, 9]]), 32, 9)
     assert page.tolist() == [-1, 5, 5, -1, -1, -1] and row[1:3].tolist() == [2, 3]
+
+
+# ------------------------------------------------------------------ the plans' whole numbers
+
+PLAN = """
+#include "%s"
+extern "C" void span(int lo, int hi, int n, int* out) { const d2c::PgSpan s = d2c::pg_span(lo, hi, n); out[0] = s.row0; out[1] = s.m; }
+"""
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    """csrc/pg_plan.h, which the kernels use, compiled for the host; overflows of whole numbers end the program."""
+    if shutil.which("g++") is None:
+        pytest.skip("no g++")
+    at = tmp_path_factory.mktemp("plan")
+    (at / "plan.cpp").write_text(PLAN % os.path.join(ROOT, "paper_2509_23094_amd", "csrc", "pg_plan.h"))
+    subprocess.run(["g++", "-std=c++17", "-O1", "-ftrapv", "-shared", "-fPIC", "-o", str(at / "plan.so"), str(at / "plan.cpp")], check=True)
+    return ctypes.CDLL(str(at / "plan.so"))
+
+
+def test_rows_between_any_two_starts(plan):
+    edges = sorted({0, 1, 5, 19, 20, 21, 40, 1 << 20, (1 << 20) + 1, 1 << 30, (1 << 31) - 2, (1 << 31) - 1} | {-1, -5, -(1 << 30), 1 - (1 << 31), -(1 << 31)})
+    out = (ctypes.c_int * 2)()
+    for n, lo, hi in itertools.product((1, 20, 120, 1 << 20), edges, edges):
+        plan.span(lo, hi, n, out)
+        row0, end = min(max(lo, 0), n), min(max(hi, 0), n)
+        assert list(out) == [row0, max(0, end - row0)], (lo, hi, n)
