@@ -192,7 +192,7 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
   for (int b = solo ? 0 : wave; b < batch; b += solo ? 1 : kWaves) {
     const PlanSeq s = p.seq[b];
     const int tiles = tiles_in<TILES>(s.m * G), n = (s.length + kPgUnit - 1) / kPgUnit - s.unit0;
-    items += (float)(tiles - (int)((float)tiles * share)) * fmaxf(1.f, ceilf((float)n * inv - 1e-3f));
+    items += (float)(tiles - pg_whole(tiles, share)) * fmaxf(1.f, ceilf((float)n * inv - 1e-3f));
   }
   float cost = items * (float)a.Hkv;
   if (!solo) {
@@ -214,7 +214,7 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs& a, unsigned char* ld
       if (b < batch && sane) {
         const PlanSeq s = p.seq[b];
         n_tiles = tiles_in<TILES>(s.m * G);
-        n_whole = (int)((float)n_tiles * share);
+        n_whole = pg_whole(n_tiles, share);
         const int n = (s.length + kPgUnit - 1) / kPgUnit - s.unit0;
         splits = max(1, (n + p.chunk - 1) / p.chunk);
         const int64_t parts = (int64_t)min((s.m * G + 31) / 32, (n_tiles - n_whole) * TILES) * a.Hkv * splits;

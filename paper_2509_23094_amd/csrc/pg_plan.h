@@ -12,4 +12,10 @@ constexpr PgSpan pg_span(int lo, int hi, int n_rows) {
   return PgSpan{first, end > first ? end - first : 0};
 }
 
+// How many of `tiles` stay whole: a share that is a little above 1 where all do (see make_plan), so that from 2^20 tiles on the product would pass them.
+constexpr int pg_whole(int tiles, float share) {
+  const int n = (int)((float)tiles * share);
+  return n < tiles ? n : tiles;
+}
+
 }  // namespace d2c

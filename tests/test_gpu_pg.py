@@ -965,3 +965,17 @@ def test_extreme_row_starts_stay_within_the_rows(starts):
     again, once = torch.empty_like(want), torch.full_like(mean, 7.0)
     p.ctx.d2c_pg_attention(p.cache, whole, q, again, block=1, attn_avg=once)
     assert torch.equal(again, want) and torch.equal(once, mean)
+
+
+def test_a_million_tiles():
+    """2^20 rows of 32 heads on one: as many tiles as fill whole rounds of workgroups, more than fp32 counts one by one.  Every row sees itself alone,
+    those before the cache nothing."""
+    n = 1 << 20
+    say("%d rows" % n)
+    p = Pool((32, 1, 64), "bf16", 32, [512], max_rows=n).fill()
+    b = B().PgBatch(p.ctx, ints([0, n]), ints([512]), ints(p.pages), n)
+    q, out = torch.ones((n, 2048), dtype=torch.bfloat16, device="cuda"), torch.full((n, 2048), 7.0, dtype=torch.bfloat16, device="cuda")
+    p.ctx.d2c_pg_attention(p.cache, b, q, out, block=1, window=1)
+    assert torch.equal(out[n - 512:].view(512, 32, 64), tensor(p.keys(0)[1], "bf16").expand(512, 32, 64))
+    rest = out[:n - 512].view(torch.int32)
+    assert not rest.any(), rest.any(1).nonzero()[:4].tolist()

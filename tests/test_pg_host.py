@@ -150,6 +150,7 @@ def test_plain_places():
 PLAN = """
 #include "%s"
 extern "C" void span(int lo, int hi, int n, int* out) { const d2c::PgSpan s = d2c::pg_span(lo, hi, n); out[0] = s.row0; out[1] = s.m; }
+extern "C" int whole(int tiles, float share) { return d2c::pg_whole(tiles, share); }
 """
 
 
@@ -171,3 +172,16 @@ def test_rows_between_any_two_starts(plan):
         plan.span(lo, hi, n, out)
         row0, end = min(max(lo, 0), n), min(max(hi, 0), n)
         assert list(out) == [row0, max(0, end - row0)], (lo, hi, n)
+
+
+def test_no_more_tiles_stay_whole_than_there_are(plan):
+    """Tiles of kernels for few and many queries that fill whole rounds exactly: the share as make_plan forms it, in fp32."""
+    for workgroups, rounds in itertools.product((256, 512), (1, 2, 3, 2047, 2048, 2049, 4096, 40000, 65536)):
+        tiles = workgroups * rounds
+        share = np.float32(np.float32(tiles) / np.float32(tiles) + np.float32(1e-6))
+        assert plan.whole(tiles, ctypes.c_float(share)) == tiles
+        if rounds <= 2048:           # (from there on a part of a round is less than a millionth of all)
+            less = tiles + workgroups // 2
+            share = np.float32(np.float32(tiles) / np.float32(less) + np.float32(1e-6))
+            assert tiles <= plan.whole(less, ctypes.c_float(share)) <= tiles + 2
+    assert plan.whole(0, ctypes.c_float(1.000001)) == 0
