@@ -723,8 +723,8 @@ __global__ __launch_bounds__(512, 2) void pg_many_kernel(const AttendArgs a) {
   const int G = a.G;
   const size_t head_pitch = (size_t)D << a.page_log2;           // elements
   for (int round = 0; (int64_t)round * gridDim.x < plan.items; ++round) {
-    // every other round backwards (by eights, which stay on their XCD): the tiles of a masked prompt get shorter from item to item
-    const int at_wg = round & 1 ? (int)((gridDim.x / 8 - 1 - blockIdx.x / 8) * 8 + blockIdx.x % 8) : (int)blockIdx.x;
+    // every other round backwards: the tiles of a masked prompt get shorter from item to item
+    const int at_wg = round & 1 ? pg_backwards((int)blockIdx.x, (int)gridDim.x) : (int)blockIdx.x;
     const int item = round * gridDim.x + at_wg;
     if (item >= plan.items) continue;
     const Found found = find(plan, a.batch.batch, item);

@@ -18,4 +18,7 @@ constexpr int pg_whole(int tiles, float share) {
   return n < tiles ? n : tiles;
 }
 
+// Workgroup wg of `count` in a round that goes backwards: by eights, which stay on their XCD; those that fill no eight keep their place.
+constexpr int pg_backwards(int wg, int count) { return wg < count / 8 * 8 ? (count / 8 - 1 - wg / 8) * 8 + wg % 8 : wg; }
+
 }  // namespace d2c

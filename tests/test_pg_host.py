@@ -151,6 +151,7 @@ PLAN = """
 #include "%s"
 extern "C" void span(int lo, int hi, int n, int* out) { const d2c::PgSpan s = d2c::pg_span(lo, hi, n); out[0] = s.row0; out[1] = s.m; }
 extern "C" int whole(int tiles, float share) { return d2c::pg_whole(tiles, share); }
+extern "C" int backwards(int wg, int count) { return d2c::pg_backwards(wg, count); }
 """
 
 
@@ -185,3 +186,12 @@ def test_no_more_tiles_stay_whole_than_there_are(plan):
             share = np.float32(np.float32(tiles) / np.float32(less) + np.float32(1e-6))
             assert tiles <= plan.whole(less, ctypes.c_float(share)) <= tiles + 2
     assert plan.whole(0, ctypes.c_float(1.000001)) == 0
+
+
+@pytest.mark.parametrize("count", [1, 7, 8, 9, 15, 31, 32, 64, 100, 128, 250, 255, 256, 257, 304])
+def test_a_round_that_goes_backwards_leaves_out_no_workgroup(plan, count):
+    order = [plan.backwards(wg, count) for wg in range(count)]
+    assert sorted(order) == list(range(count))
+    assert all(at % 8 == wg % 8 for wg, at in enumerate(order))                  # on its XCD
+    if count % 8 == 0:
+        assert order[:8] == list(range(count - 8, count))
