@@ -610,6 +610,13 @@ class Q8Batch:
 
 # ---------------------------------------------------------------------- the paged cache (include/d2c_pg.h)
 
+def _int32(x: int, what: str) -> int:
+    """A whole number that the C interface takes in 32 bits: ctypes would keep the low ones of any."""
+    if not -(1 << 31) <= x < 1 << 31:
+        raise D2CError(D2C_EINVAL, "%s: %s does not fit 32 bits" % (what, x))
+    return x
+
+
 def _rows(t: torch.Tensor, what: str, dtype: torch.dtype, n: int, width: int, device: int):
     """(pointer, pitch in elements) of rows [n, width] whose elements lie together; the rows may lie apart."""
     if t.dtype is dtype and t.get_device() == device and t.shape == (n, width):
@@ -651,6 +658,9 @@ class PgContext:
     def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, dtype: str, page_rows: int = 64, max_rows: int = 0, max_batch: int = 1,
                  rotary: Optional[Rotary] = None):
         self.handle = C.c_void_p()
+        for what, x in (("n_heads", n_heads), ("n_kv_heads", n_kv_heads), ("head_dim", head_dim), ("page_rows", page_rows), ("max_rows", max_rows),
+                        ("max_batch", max_batch)):
+            _int32(x, what)
         self.n_heads, self.n_kv_heads, self.head_dim, self.dtype = int(n_heads), int(n_kv_heads), int(head_dim), dtype
         self.page_rows, self.rotary = int(page_rows), rotary
         self.torch_dtype = torch_dtype(dtype)
@@ -734,6 +744,7 @@ class PgContext:
     def d2c_pg_attention(self, cache: "PgCache", batch: "PgBatch", q: torch.Tensor, out: torch.Tensor, block: int = 0, window: int = 0,
                          scale: Optional[float] = None, attn_avg: Optional[torch.Tensor] = None) -> None:
         """Rows of q [n_rows, d_q] against their sequences' pages: block 0 no mask, 1 causal, more: blocks that see each other in whole."""
+        _int32(block, "block"), _int32(window, "window")
         self._match(cache, batch)
         n, t = batch.n_rows, self.torch_dtype
         if scale is not None and not scale > 0:
@@ -773,6 +784,7 @@ class PgBatch:
     def __init__(self, ctx: PgContext, row_start: torch.Tensor, length: torch.Tensor, pages: torch.Tensor, n_rows: int,
                  at: Optional[torch.Tensor] = None, origin: Optional[torch.Tensor] = None):
         batch, cols = pages.shape
+        _int32(n_rows, "n_rows"), _int32(cols, "page_cols")
         self.device, self.n_rows, self.keep = ctx.device, int(n_rows), (row_start, length, pages, at, origin)
         self.c = d2c_pg_batch(_checked(row_start, "row_start", torch.int32, (batch + 1,), ctx.device),
                               _checked(length, "length", torch.int32, (batch,), ctx.device),

@@ -95,6 +95,27 @@ def test_rotary_ladders():
             B.Rotary(**bad)
 
 
+@built
+@pytest.mark.parametrize("value", [(1 << 32) + 64, 1 << 32, 1 << 31, -(1 << 31) - 1, (1 << 64) + 1])
+def test_binding_refuses_what_32_bits_do_not_hold(value):
+    """Nothing goes on with the low 32 bits of a larger number (2^32 + 1 as a block would be causal)."""
+    import torch
+    from paper_2509_23094_amd import binding as B
+    sizes = dict(n_heads=4, n_kv_heads=2, head_dim=64, page_rows=64, max_rows=16, max_batch=4)
+    for name in sizes:
+        with pytest.raises(B.D2CError, match=name) as e:
+            B.PgContext(dtype="bf16", **{**sizes, name: value})
+        assert e.value.code == B.D2C_EINVAL
+    ctx = object.__new__(B.PgContext)
+    ctx.handle, ctx.device = None, 0
+    for name in ("block", "window"):
+        with pytest.raises(B.D2CError, match=name):
+            ctx.d2c_pg_attention(None, None, None, None, **{name: value})
+    none = torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(B.D2CError, match="n_rows"):
+        B.PgBatch(ctx, none, none, none.view(1, 1), value)
+
+
 # ------------------------------------------------------------------ the plain forms
 
 def test_plain_rotation():
