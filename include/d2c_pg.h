@@ -136,7 +136,7 @@ typedef struct {
   float* attn_avg;
   int64_t avg_ld;                 /* at most 2^30 */
   int32_t block, window;          /* 0 = none; up to 2^30 */
-  float scale;                    /* positive and finite; 0 = 1 / sqrt(D) */
+  float scale;                    /* positive, at most 2^127; 0 = 1 / sqrt(D) */
 } d2c_pg_attend;
 int d2c_pg_attention(d2c_pg* ctx, const d2c_pg_cache* cache, const d2c_pg_batch* batch, const d2c_pg_attend* args, void* stream);
 

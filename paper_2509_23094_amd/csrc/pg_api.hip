@@ -267,7 +267,8 @@ int d2c_pg_attention(d2c_pg* c, const d2c_pg_cache* cache, const d2c_pg_batch* b
   if (!args) return fail(c, D2C_EINVAL, "null args");
   if (batch->n_rows > c->dims.max_rows) return fail(c, D2C_ESHAPE, "n_rows exceeds max_rows of the handle");
   if (args->block < 0 || args->window < 0 || args->block > 1 << 30 || args->window > 1 << 30) return fail(c, D2C_EINVAL, "block and window must be in 0 .. 2^30");
-  if (!(args->scale >= 0.f) || !(args->scale <= 3.4e38f)) return fail(c, D2C_EINVAL, "scale must be positive and finite, or 0");
+  // (above it the product with log2(e) is no float, and a score of 0 times that no number)
+  if (!(args->scale >= 0.f) || !(args->scale <= 0x1p127f)) return fail(c, D2C_EINVAL, "scale must be positive and at most 2^127, or 0");
   if (none) return D2C_OK;
   const int64_t n = batch->n_rows, d_q = (int64_t)c->dims.n_heads * c->dims.head_dim;
   if ((rc = check_rows(c, args->q, n, d_q, args->q_ld, c->dims.dtype, false))) return rc;

@@ -979,3 +979,26 @@ def test_a_million_tiles():
     assert torch.equal(out[n - 512:].view(512, 32, 64), tensor(p.keys(0)[1], "bf16").expand(512, 32, 64))
     rest = out[:n - 512].view(torch.int32)
     assert not rest.any(), rest.any(1).nonzero()[:4].tolist()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [1e-44, 2.0 ** -126, 2.0 ** 127])
+def test_scales_at_the_ends_of_their_range(dtype, scale):
+    """Scores of 0 times any scale, behind a mask: every row is the mean of the keys it sees (queries of zeros; a scale that 32 bits hold only as a
+    subnormal, and the largest)."""
+    p = Pool("gqa", dtype, 32, [70, 33], max_rows=64).fill()
+    b = p.batch([40, 3])
+    q = (tensor(np.zeros((43, 512)), dtype), np.zeros((43, 8, 64)))
+    p.attend(b, block=1, scale=scale, average=True, q=q)
+    p.attend(b, block=32, window=40, scale=scale, q=q)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 127 * (1 + 2.0 ** -23), 3e38, float("inf")])
+def test_scales_above_their_range_are_refused(scale):
+    """From there on the product with log2(e) is no number of 32 bits (0 times infinity would be NaN)."""
+    p = Pool("gqa", "bf16", 32, [70], max_rows=64).fill()
+    b, t = p.batch([3]), torch.full((3, 512), 7.0, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(B().D2CError, match="scale"):
+        p.ctx.d2c_pg_attention(p.cache, b, torch.zeros_like(t), t, scale=scale)
+    torch.cuda.synchronize()
+    assert (t == 7).all()
