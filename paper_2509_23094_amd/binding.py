@@ -745,10 +745,10 @@ class PgContext:
                          scale: Optional[float] = None, attn_avg: Optional[torch.Tensor] = None) -> None:
         """Rows of q [n_rows, d_q] against their sequences' pages: block 0 no mask, 1 causal, more: blocks that see each other in whole."""
         _int32(block, "block"), _int32(window, "window")
+        if scale is not None and not C.c_float(scale).value > 0:      # (as 0 in 32 bits it would be the default)
+            raise D2CError(D2C_EINVAL, "scale must be positive in 32 bits")
         self._match(cache, batch)
         n, t = batch.n_rows, self.torch_dtype
-        if scale is not None and not scale > 0:
-            raise D2CError(D2C_EINVAL, "scale must be positive")
         qp, q_ld = _rows(q, "q", t, n, self.d_q, self.device)
         op, o_ld = _rows(out, "out", t, n, self.d_q, self.device)
         ap, a_ld = None, 0

@@ -116,6 +116,18 @@ def test_binding_refuses_what_32_bits_do_not_hold(value):
         B.PgBatch(ctx, none, none, none.view(1, 1), value)
 
 
+@built
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-46, 1e-50, 5e-324, -1e-50, -1.0, float("nan"), float("-inf")])
+def test_binding_refuses_scales_that_are_not_positive_in_32_bits(scale):
+    """A positive number that 32 bits round to 0 does not become the default 1 / sqrt(D)."""
+    from paper_2509_23094_amd import binding as B
+    ctx = object.__new__(B.PgContext)
+    ctx.handle = None
+    with pytest.raises(B.D2CError, match="scale") as e:
+        ctx.d2c_pg_attention(None, None, None, None, scale=scale)
+    assert e.value.code == B.D2C_EINVAL
+
+
 # ------------------------------------------------------------------ the plain forms
 
 def test_plain_rotation():
