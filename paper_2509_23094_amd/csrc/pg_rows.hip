@@ -138,7 +138,7 @@ struct RowsArgs {
   PgBatch batch;
   PgRows rows;
   PgPages pages;
-  int n, parts, H, Hkv, page_log2;
+  int n, parts, Hkv, page_log2;
   int v_tiles, v_heads;                  // workgroups in front that bring V in tiles (0: with the rows), kv heads of each
 };
 
@@ -423,7 +423,6 @@ hipError_t launch_pg_rows(const PgShape& s, const PgRotation& rot, const PgPages
   a.rows = rows;
   a.pages = pages;
   a.n = n;
-  a.H = s.H;
   a.Hkv = s.Hkv;
   a.page_log2 = s.page_log2;
   a.v_tiles = rows.v ? value_tiles(n, batch->batch, s.Hkv, s.D, a.v_heads) : 0;
