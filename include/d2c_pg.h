@@ -30,8 +30,11 @@
  * On the device, where no error can be returned:
  *   - a length counts as at least 0 and at most page_cols * page_rows;
  *   - a page number outside [0, n_pages) is a page that is not there: its rows are not written, and not seen;
+ *   - a negative origin counts as 0;
  *   - rows before row_start[0] and from row_start[batch] on belong to no sequence and are left as they are; row starts
  *     outside [0, n_rows] or not ascending leave all outputs and the caches undefined, and nothing else.
+ * What d2c_pg_attention launches goes by the host's numbers, page_cols * page_rows among them, as lengths are known on the device only: where
+ * sequences are short beside their table, a narrower one can save a launch or two (a call takes its own page_cols; rows of pages [batch, page_cols]).
  */
 #ifndef D2C_PG_H
 #define D2C_PG_H

@@ -337,7 +337,9 @@ template <> __device__ __forceinline__ f32x16 mm<float>(const u32x4& a, const u3
 }
 // key of accumulator element i, within a unit
 template <typename T> __device__ __forceinline__ int key_of(int i, int g) { return sizeof(T) == 2 ? 16 * (i >> 3) + 8 * g + (i & 7) : 8 * (i >> 2) + 4 * g + (i & 3); }
-// probabilities as operands: pieces s = 0 .. 16 / E - 1
+// Probabilities as operands: pieces s = 0 .. 16 / E - 1.  bf16: rounded to it (half a step, 2^-8 of each), because the matrix instruction takes both operands in one type
+// and the other is V; their sum, the references and O stay in fp32.  Outputs of the timed cases are off by 1.6 - 2.0e-3 (norm) against 64 bits, where fp32
+// probabilities and the output's own rounding leave 1.6 - 1.7e-3; a second piece for what the rounding leaves would be half as many products again.
 template <typename T> __device__ __forceinline__ u32x4 p_piece(const float (&x)[16], int s);
 template <> __device__ __forceinline__ u32x4 p_piece<bf16>(const float (&x)[16], int s) {
   return u32x4{pack2(x[8 * s], x[8 * s + 1]), pack2(x[8 * s + 2], x[8 * s + 3]), pack2(x[8 * s + 4], x[8 * s + 5]), pack2(x[8 * s + 6], x[8 * s + 7])};
@@ -502,9 +504,13 @@ __device__ __forceinline__ float inverse_of(float sum) { return sum > 0.f ? 1.f 
 // (query, key) pairs, all heads, from which on a sequence goes to the kernel for many queries.  us by the one for few and by it: bf16, 32 heads of 128, 8000
 // keys: 256 rows (66e6) 66 and 58, 128 rows 43 and 47; 28 on 4, 4000 keys: 1024 rows (115e6) 105 and 90, 512 rows 57 and 59; 12 heads of 64 on 2, 16000 keys: 1024
 // rows (197e6) 104 and 88, 512 rows 61 and 67; float, where both wait for the matrix cores, 32 heads, 2048 keys, 2000 rows, no mask 646 and 531, causal 376 and 533.
+// Float has one threshold for what a mask does differently to the two: it keeps both of those calls in the kernel for few, which the causal one gains more by (157)
+// than the other loses (115).
 // Several sequences of bf16 heads of 128 together, from half of it on, but for those with less than a 64th of that (others: no gain).  Lengths falling evenly to a
-// 20th, 28 heads on 4: 24 of 300 rows on 600 keys 104 and 87, 8 of 100 on 4000 82 and 66, 4 of 500 on 2000 83 and 71, but 12 of 400 on 1500 124 and 134; 32
-// heads: 16 of 256 on 600 83 and 64, 6 of 700 on 2000 155 and 123; two of 512 on 2000, which stay where they are, 55 and 69.
+// 20th, 28 heads on 4: 24 of 300 rows on 600 keys 104 and 87, 8 of 100 on 4000 82 and 66, 4 of 500 on 2000 83 and 71, but 12 of 400 on 1500, which nothing
+// here tells apart from them, 124 and 134; 32 heads: 16 of 256 on 600 83 and 64, 6 of 700 on 2000 155 and 123; two of 512 on 2000, which stay where they are, 55
+// and 69.  The host leaves the second launch out wherever rows times the page table's keys stay below the whole of it, so sequences that fill their tables and
+// have between half of it and all of it together stay in the kernel for few.
 template <typename T, int D> constexpr float kMuch = sizeof(T) == 4 ? 256e6f : D == 64 ? 128e6f : 64e6f;
 constexpr int kManyWaves = 8, kFewWaves = 4;
 
@@ -697,7 +703,7 @@ __device__ __forceinline__ void load_to_lds(const unsigned char* to, const u32x4
                : "memory");
 }
 
-// 2500 causal queries on 7000 keys, 32 heads of 128: 268 - 285 us, 0.83 - 0.88 PFLOP/s of what the masks leave (a product of 8192^3 by the library: 1.23);
+// 2500 causal queries on 7000 keys, 32 heads of 128: 266 - 302 us by card and clock, 0.78 - 0.89 PFLOP/s of what the masks leave (a product of 8192^3 by the library: 1.23);
 // matrix cores busy 51 %, vector units 49 % of the time, and the clock falls with both: a block of 64 keys went from 6100 clocks to 4200 as requests were
 // spread between instructions, and from 2.76 us to 2.3 only.
 // Eight tiles of 32 queries per workgroup, one a wave.  K and V of 64 keys (float: 32) at a time go from the pages straight into LDS, where they lie as in
